@@ -264,6 +264,114 @@ accept_status accept_mbq_compress(const accept_mbq_params* p, const float* d_x, 
 accept_status accept_mbq_decompress(const accept_mbq_params* p, const void* d_stream, size_t stream_bytes,
                                     float* d_xhat, void* d_ws, size_t ws_bytes, void* cuda_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators beside the codec: what the stage that receives a boundary tensor runs on it first.
+ * Layer norm forward and backward, quantisation to 8-bit floating point with one power-of-two scale
+ * for each block of 128 values, and the matrix product of operands in that form (the linear layer's
+ * forward product and both of its gradients).  They follow the rules of the entry points above:
+ * asynchronous on the stream, nothing allocated, buffers and workspace owned by the caller.  The
+ * paper has no counterpart of them.
+ */
+typedef enum { ACCEPT_DTYPE_F32 = 0, ACCEPT_DTYPE_BF16 = 1, ACCEPT_DTYPE_F16 = 2 } accept_dtype;
+/* 8-bit formats: E4M3 without infinities (largest value 448) and E5M2 (largest finite value 57344). */
+typedef enum { ACCEPT_FORMAT_E4M3 = 0, ACCEPT_FORMAT_E5M2 = 1 } accept_format;
+/* Values that share a scale: 128 neighbours of a row, or 128 x 128. */
+typedef enum { ACCEPT_BLOCK_ROW = 0, ACCEPT_BLOCK_SQUARE = 1 } accept_block;
+
+/*
+ * Layer norm over the rows of a rows x cols matrix.
+ *   forward   mean = sum x / cols,  var = sum (x - mean)^2 / cols,  rstd = 1 / sqrt(var + eps),
+ *             y = (x - mean) rstd gamma + beta
+ *   backward  xhat = (x - mean) rstd,  h = dy gamma,
+ *             dx = rstd (h - mean(h) - xhat mean(h xhat)),  dgamma = sum_rows dy xhat,  dbeta = sum_rows dy
+ *   rows, cols  rows >= 0 (no rows: the forward pass does nothing, the backward pass writes zero dgamma and
+ *               dbeta), 1 <= cols < 2^31.
+ *   ld_x, ld_y  values between the starts of two rows (>= cols) of x and dx, and of y and dy.
+ *   dtype_x     type of x and dx;  dtype_y: of y and dy;  dtype_w: of gamma and beta.  Statistics and the
+ *               gradients of gamma and beta are fp32, as is everything computed on the way.
+ * Pointers need the alignment of their values; rows that start on 16-byte boundaries are read in 16-byte
+ * pieces.  A row that holds a NaN or an infinity comes out as NaN; other rows do not notice.
+ */
+typedef struct {
+  uint64_t rows, cols;
+  uint64_t ld_x, ld_y;
+  float eps;       /* >= 0 */
+  int32_t dtype_x; /* accept_dtype */
+  int32_t dtype_y;
+  int32_t dtype_w;
+} accept_layer_norm_params;
+
+accept_status accept_layer_norm_check_params(const accept_layer_norm_params* p);
+size_t accept_layer_norm_workspace_size(const accept_layer_norm_params* p); /* of the backward pass; 0 if p is invalid */
+/* gamma and beta may each be NULL (1 and 0); mean and rstd (rows values each) may be NULL where no backward pass follows. */
+accept_status accept_layer_norm_forward(const accept_layer_norm_params* p, const void* d_x, const void* d_gamma,
+                                        const void* d_beta, void* d_y, float* d_mean, float* d_rstd, void* cuda_stream);
+/* d_gamma may be NULL (1).  dx, or dgamma and dbeta, may be NULL: then they are not written.  dgamma and dbeta are
+ * summed in an order that depends on the sizes alone: the same call gives the same bits.  d_ws: 16-byte aligned. */
+accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, const void* d_dy, const void* d_x,
+                                         const void* d_gamma, const float* d_mean, const float* d_rstd, void* d_dx,
+                                         float* d_dgamma, float* d_dbeta, void* d_ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * Quantisation to 8-bit floating point in blocks of 128.
+ *   block  ROW: 128 consecutive values of a row (the last block of a row may be shorter);  SQUARE: 128 x 128
+ *   scale  a = the largest finite |x| of the block; e = the least integer with a 2^-e <= F (the format's largest
+ *          value), held to [-127, 127]; 0 where a = 0.  Scale byte e + 127.
+ *   code   x 2^-e (exact) rounded to the format, ties to even.  NaN and infinities become the format's NaN, and
+ *          ACCEPT_DEV_NONFINITE is set in the status word.
+ * One read of x gives either or both of
+ *   rows     q (rows x cols): blocks run along the columns;
+ *   columns  q_t (cols x rows): the transpose, blocks run along the rows.
+ * A square block has the same scale in both.  Layout of a coded R x C matrix (R = rows or cols):
+ *   codes    R rows of C bytes, each row padded with zero bytes to a multiple of 16
+ *            (accept_block_data_size bytes, 16-byte aligned);
+ *   scales   the order in which the tensor cores read them: 512 bytes for 128 rows and four blocks; the byte of row r
+ *            and block b is at ((b / 4) ceil(R / 128) + r / 128) 512 + (r % 32) 16 + (r / 32 % 4) 4 + b % 4
+ *            (accept_block_scale_size bytes, 16-byte aligned; rows and blocks of the padding hold 127).
+ *            Square blocks repeat their byte for each row.
+ *   rows, cols  >= 0, below 2^31;  ld: values between the starts of two rows of x (>= cols)
+ */
+typedef struct {
+  uint64_t rows, cols;
+  uint64_t ld;
+  int32_t dtype;  /* accept_dtype of x */
+  int32_t format; /* accept_format */
+  int32_t block;  /* accept_block */
+  int32_t reserved; /* 0 */
+} accept_quantize_params;
+
+accept_status accept_block_check_params(const accept_quantize_params* p);
+/* Bytes of the codes and of the scales, of q (transposed = 0) or q_t (1); 0 if p is invalid. */
+size_t accept_block_data_size(const accept_quantize_params* p, int transposed);
+size_t accept_block_scale_size(const accept_quantize_params* p, int transposed);
+size_t accept_block_workspace_size(const accept_quantize_params* p);
+/* q and its scales, or q_t and its scales, may be NULL; not both. */
+accept_status accept_block_quantize(const accept_quantize_params* p, const void* d_x, void* d_q, void* d_scale, void* d_qt,
+                                    void* d_scale_t, void* d_ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * d = a b^T (+ bias) (+ d):  d[i][j] = sum_k a[i][k] 2^(ea - 127) b[j][k] 2^(eb - 127) + bias[j] + (accumulate) d[i][j]
+ * for a (m x k) and b (n x k) as accept_block_quantize writes them, scale bytes 0 to 254.  Products are exact, sums are
+ * fp32 in an order that depends on the sizes alone, d is rounded once.
+ *   linear layer y = x W^T + b:   forward  a = x by rows, b = W by rows;  gradient of x: a = dy by rows, b = W by columns;
+ *   gradient of W: a = dy by columns, b = x by columns, accumulate into fp32.
+ *   m, n, k >= 0, below 2^31 (k = 0: the sum is empty);  ldd: values between the starts of two rows of d (>= n)
+ */
+typedef struct {
+  uint64_t m, n, k;
+  uint64_t ldd;
+  int32_t format_a, format_b; /* accept_format */
+  int32_t dtype_d;            /* accept_dtype */
+  int32_t accumulate;         /* 0 or 1: add to what d holds */
+} accept_matmul_params;
+
+accept_status accept_matmul_check_params(const accept_matmul_params* p);
+size_t accept_matmul_workspace_size(const accept_matmul_params* p);
+/* bias: n fp32 values, or NULL.  The status word gets ACCEPT_DEV_COPY_TIMEOUT if a wait inside the kernel ran out. */
+accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b,
+                                  const void* d_b_scale, const float* d_bias, void* d_d, void* d_ws, size_t ws_bytes,
+                                  void* cuda_stream);
+
 /*
  * Synchronises cuda_stream, copies the status word to the host and returns it in *status_bits
  * (ACCEPT_DEV_* bits).  Returns ACCEPT_ERR_CUDA if the stream reports an error.

@@ -10,4 +10,8 @@ from .binding import (  # noqa: F401
     accept_last_device_status, accept_launch_count, accept_launch_null, accept_parse_header, accept_payload_offset,
     accept_workspace_size, new_stream_buffer, new_workspace, accept_mbq_check_params, accept_mbq_compress,
     accept_mbq_compressed_size, accept_mbq_decompress, accept_mbq_payload_offset, accept_mbq_workspace_size,
+    BLOCK_ROW, BLOCK_SQUARE, DTYPE_BF16, DTYPE_F16, DTYPE_F32, FORMAT_E4M3, FORMAT_E5M2, LayerNormParams, MatmulParams,
+    QuantizeParams, accept_block_check_params, accept_block_data_size, accept_block_matmul, accept_block_quantize,
+    accept_block_scale_size, accept_block_workspace_size, accept_layer_norm_backward, accept_layer_norm_check_params,
+    accept_layer_norm_forward, accept_layer_norm_workspace_size, accept_matmul_check_params, accept_matmul_workspace_size,
 )

@@ -16,6 +16,9 @@ LIB_PATH = os.path.join(_HERE, "libaccept.so")
 RANGE_ABSMAX, RANGE_MINMAX = 0, 1
 ROUND_NEAREST, ROUND_STOCHASTIC = 0, 1
 LAYOUT_INTERLEAVED, LAYOUT_BITPLANE = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
+FORMAT_E4M3, FORMAT_E5M2 = 0, 1
+BLOCK_ROW, BLOCK_SQUARE = 0, 1
 HEADER_BYTES = 32
 
 OK = 0
@@ -35,6 +38,10 @@ EXPORTS = [
     "accept_compress_static", "accept_bounds_check_report", "accept_launch_null",
     "accept_mbq_check_params", "accept_mbq_compressed_size", "accept_mbq_payload_offset", "accept_mbq_workspace_size",
     "accept_mbq_compress", "accept_mbq_decompress",
+    "accept_layer_norm_check_params", "accept_layer_norm_workspace_size", "accept_layer_norm_forward",
+    "accept_layer_norm_backward", "accept_block_check_params", "accept_block_data_size", "accept_block_scale_size",
+    "accept_block_workspace_size", "accept_block_quantize", "accept_matmul_check_params", "accept_matmul_workspace_size",
+    "accept_block_matmul",
 ]
 
 
@@ -88,6 +95,79 @@ class MbqParams:
         return CMbqParams(self.n_elems, self.k, self.batch_index, 1 if self.init else 0, 0)
 
 
+class CLayerNormParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("ld_x", ctypes.c_uint64), ("ld_y", ctypes.c_uint64),
+                ("eps", ctypes.c_float), ("dtype_x", ctypes.c_int32), ("dtype_y", ctypes.c_int32), ("dtype_w", ctypes.c_int32)]
+
+
+class CQuantizeParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("ld", ctypes.c_uint64), ("dtype", ctypes.c_int32),
+                ("format", ctypes.c_int32), ("block", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class CMatmulParams(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_uint64), ("n", ctypes.c_uint64), ("k", ctypes.c_uint64), ("ldd", ctypes.c_uint64),
+                ("format_a", ctypes.c_int32), ("format_b", ctypes.c_int32), ("dtype_d", ctypes.c_int32),
+                ("accumulate", ctypes.c_int32)]
+
+
+@dataclass(frozen=True)
+class LayerNormParams:
+    """Layer norm over the rows of a rows x cols matrix; ld_x / ld_y 0: rows are cols values apart."""
+    rows: int
+    cols: int
+    eps: float = 1e-5
+    dtype_x: int = DTYPE_F32
+    dtype_y: int = DTYPE_F32
+    dtype_w: int = DTYPE_F32
+    ld_x: int = 0
+    ld_y: int = 0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", CLayerNormParams(self.rows, self.cols, self.ld_x or self.cols, self.ld_y or self.cols,
+                                                        self.eps, self.dtype_x, self.dtype_y, self.dtype_w))
+
+    def c(self) -> CLayerNormParams:
+        return self._c
+
+
+@dataclass(frozen=True)
+class QuantizeParams:
+    """Quantisation of a rows x cols matrix in blocks of 128; ld 0: rows are cols values apart."""
+    rows: int
+    cols: int
+    dtype: int = DTYPE_F32
+    format: int = FORMAT_E4M3
+    block: int = BLOCK_ROW
+    ld: int = 0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", CQuantizeParams(self.rows, self.cols, self.ld or self.cols, self.dtype, self.format, self.block, 0))
+
+    def c(self) -> CQuantizeParams:
+        return self._c
+
+
+@dataclass(frozen=True)
+class MatmulParams:
+    """d (m x n) = a (m x k) b (n x k)^T of coded operands; ldd 0: rows of d are n values apart."""
+    m: int
+    n: int
+    k: int
+    format_a: int = FORMAT_E4M3
+    format_b: int = FORMAT_E4M3
+    dtype_d: int = DTYPE_BF16
+    accumulate: bool = False
+    ldd: int = 0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", CMatmulParams(self.m, self.n, self.k, self.ldd or self.n, self.format_a, self.format_b,
+                                                     self.dtype_d, int(self.accumulate)))
+
+    def c(self) -> CMatmulParams:
+        return self._c
+
+
 _lib = None
 
 
@@ -138,6 +218,23 @@ def load(path: str) -> ctypes.CDLL:
     L.accept_mbq_compress.argtypes = [MP, vp, vp, vp, vp, sz, vp, sz, vp]
     L.accept_mbq_decompress.restype = ctypes.c_int
     L.accept_mbq_decompress.argtypes = [MP, vp, sz, vp, vp, sz, vp]
+    NP, QP, TP = ctypes.POINTER(CLayerNormParams), ctypes.POINTER(CQuantizeParams), ctypes.POINTER(CMatmulParams)
+    for name, params in (("accept_layer_norm", NP), ("accept_block", QP), ("accept_matmul", TP)):
+        getattr(L, name + "_check_params").restype = ctypes.c_int
+        getattr(L, name + "_check_params").argtypes = [params]
+        getattr(L, name + "_workspace_size").restype = sz
+        getattr(L, name + "_workspace_size").argtypes = [params]
+    for name in ("accept_block_data_size", "accept_block_scale_size"):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = [QP, ctypes.c_int]
+    L.accept_layer_norm_forward.restype = ctypes.c_int
+    L.accept_layer_norm_forward.argtypes = [NP, vp, vp, vp, vp, vp, vp, vp]
+    L.accept_layer_norm_backward.restype = ctypes.c_int
+    L.accept_layer_norm_backward.argtypes = [NP, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.accept_block_quantize.restype = ctypes.c_int
+    L.accept_block_quantize.argtypes = [QP, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.accept_block_matmul.restype = ctypes.c_int
+    L.accept_block_matmul.argtypes = [TP, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.accept_launch_count.restype = u64
     L.accept_launch_count.argtypes = []
     L.accept_launch_null.restype = ctypes.c_int
@@ -284,6 +381,75 @@ def accept_mbq_decompress(p: MbqParams, d_stream, d_xhat, d_ws, stream=None) -> 
                                        _stream_handle(stream)), "accept_mbq_decompress")
 
 
+# ---- operators beside the codec: layer norm, block quantisation, matrix product --------------------
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _nbytes(t) -> int:
+    return t.numel() * t.element_size()
+
+
+def accept_layer_norm_check_params(p: LayerNormParams) -> int:
+    return int(lib().accept_layer_norm_check_params(ctypes.byref(p.c())))
+
+
+def accept_layer_norm_workspace_size(p: LayerNormParams) -> int:
+    return int(lib().accept_layer_norm_workspace_size(ctypes.byref(p.c())))
+
+
+def accept_layer_norm_forward(p: LayerNormParams, d_x, d_gamma, d_beta, d_y, d_mean=None, d_rstd=None, stream=None) -> None:
+    """d_gamma / d_beta may be None; d_mean / d_rstd: float32 CUDA tensors of p.rows elements, kept for the backward pass."""
+    _check(lib().accept_layer_norm_forward(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_gamma), _ptr(d_beta), d_y.data_ptr(),
+                                           _ptr(d_mean), _ptr(d_rstd), _stream_handle(stream)), "accept_layer_norm_forward")
+
+
+def accept_layer_norm_backward(p: LayerNormParams, d_dy, d_x, d_gamma, d_mean, d_rstd, d_dx, d_dgamma, d_dbeta, d_ws, stream=None) -> None:
+    """d_gamma may be None; d_dx, or d_dgamma and d_dbeta (float32, p.cols elements), may be None: not computed."""
+    _check(lib().accept_layer_norm_backward(ctypes.byref(p.c()), d_dy.data_ptr(), d_x.data_ptr(), _ptr(d_gamma), d_mean.data_ptr(),
+                                            d_rstd.data_ptr(), _ptr(d_dx), _ptr(d_dgamma), _ptr(d_dbeta), d_ws.data_ptr(),
+                                            _nbytes(d_ws), _stream_handle(stream)), "accept_layer_norm_backward")
+
+
+def accept_block_check_params(p: QuantizeParams) -> int:
+    return int(lib().accept_block_check_params(ctypes.byref(p.c())))
+
+
+def accept_block_data_size(p: QuantizeParams, transposed: bool = False) -> int:
+    return int(lib().accept_block_data_size(ctypes.byref(p.c()), int(transposed)))
+
+
+def accept_block_scale_size(p: QuantizeParams, transposed: bool = False) -> int:
+    return int(lib().accept_block_scale_size(ctypes.byref(p.c()), int(transposed)))
+
+
+def accept_block_workspace_size(p: QuantizeParams) -> int:
+    return int(lib().accept_block_workspace_size(ctypes.byref(p.c())))
+
+
+def accept_block_quantize(p: QuantizeParams, d_x, d_q, d_scale, d_qt, d_scale_t, d_ws, stream=None) -> None:
+    """d_q / d_scale (codes along the columns) or d_qt / d_scale_t (the transpose, codes along the rows) may be None:
+    uint8 CUDA tensors of accept_block_data_size and accept_block_scale_size bytes."""
+    _check(lib().accept_block_quantize(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_q), _ptr(d_scale), _ptr(d_qt), _ptr(d_scale_t),
+                                       d_ws.data_ptr(), _nbytes(d_ws), _stream_handle(stream)), "accept_block_quantize")
+
+
+def accept_matmul_check_params(p: MatmulParams) -> int:
+    return int(lib().accept_matmul_check_params(ctypes.byref(p.c())))
+
+
+def accept_matmul_workspace_size(p: MatmulParams) -> int:
+    return int(lib().accept_matmul_workspace_size(ctypes.byref(p.c())))
+
+
+def accept_block_matmul(p: MatmulParams, d_a, d_a_scale, d_b, d_b_scale, d_bias, d_d, d_ws, stream=None) -> None:
+    """d_bias: float32 CUDA tensor of p.n elements, or None."""
+    _check(lib().accept_block_matmul(ctypes.byref(p.c()), d_a.data_ptr(), d_a_scale.data_ptr(), d_b.data_ptr(), d_b_scale.data_ptr(),
+                                     _ptr(d_bias), d_d.data_ptr(), d_ws.data_ptr(), _nbytes(d_ws), _stream_handle(stream)),
+           "accept_block_matmul")
+
+
 # ---- small conveniences for callers (allocation only) -----------------------------------------
 
 def new_stream_buffer(p, device="cuda"):
@@ -294,5 +460,7 @@ def new_stream_buffer(p, device="cuda"):
 
 def new_workspace(p, device="cuda"):
     import torch
-    size = accept_mbq_workspace_size(p) if isinstance(p, MbqParams) else accept_workspace_size(p)
+    query = {MbqParams: accept_mbq_workspace_size, LayerNormParams: accept_layer_norm_workspace_size,
+             QuantizeParams: accept_block_workspace_size, MatmulParams: accept_matmul_workspace_size}
+    size = query.get(type(p), accept_workspace_size)(p)
     return torch.zeros((size + 3) // 4, dtype=torch.int32, device=device)

@@ -3,24 +3,25 @@
 // accept_last_device_status.
 #include "../../include/accept.h"
 
-#include <atomic>
-#include <cstdlib>
 #include <cstring>
 #include <mutex>
-#include <utility>
 
+#include "accept_host.cuh"
 #include "accept_kernels.cuh"
 #include "accept_wide.cuh"
 #include "accept_mbq.cuh"
 #include "accept_strided.cuh"
 
+namespace accept {
+std::atomic<uint64_t> g_launches{0};
+}
+
 namespace {
 
 using accept::CodecArgs;
-
-std::atomic<uint64_t> g_launches{0};
-
-bool is_aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+using accept::is_aligned;
+using accept::launch_overlapped;
+using accept::launch_overlapped_shared;
 
 uint64_t n_chunks_of(const accept_params* p) { return (p->n_elems + p->chunk_elems - 1) / p->chunk_elems; }
 
@@ -67,74 +68,6 @@ CodecArgs make_args(const accept_params* p, void* d_stream, void* d_ws) {
   a.group_stride = p->group_stride;
   return a;
 }
-
-// Launch with programmatic stream serialization: every kernel of this library starts with
-// grid_dependency_handshake(), so it may be scheduled while its predecessor in the stream drains.
-template <typename... Params, typename... Args>
-cudaError_t launch_overlapped_shared(void (*fn)(Params...), dim3 grid, unsigned block, size_t shared_bytes, cudaStream_t s,
-                                     Args&&... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(block, 1, 1);
-  cfg.dynamicSmemBytes = shared_bytes;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, fn, std::forward<Args>(args)...);
-}
-
-template <typename... Params, typename... Args>
-cudaError_t launch_overlapped(void (*fn)(Params...), dim3 grid, unsigned block, cudaStream_t s, Args&&... args) {
-  return launch_overlapped_shared(fn, grid, block, 0, s, std::forward<Args>(args)...);
-}
-
-// A launch (or any runtime call) that fails ends the entry point at once: later launches of the same call
-// are not issued, and only launches that were issued are counted.  The result is the call's own return
-// value; cudaGetLastError() is never consulted, so an error left behind by the caller's earlier work is
-// neither reported as ours nor cleared.
-#define ACCEPT_LAUNCH(call)                                         \
-  do {                                                              \
-    if ((call) != cudaSuccess) return ACCEPT_ERR_CUDA;              \
-    g_launches.fetch_add(1, std::memory_order_relaxed);             \
-  } while (0)
-
-// ---- tests-only build: byte ranges the kernels of a call may touch ------------------------------------
-#ifdef ACCEPT_BOUNDS_CHECK
-// ACCEPT_BOUNDS_TEST_SHRINK=<bytes> in the environment cuts that many bytes off the end of every writable
-// range: the test of the checker itself, which shows that the last stores of a call are then counted and
-// skipped (nothing is written there, nothing faults).
-size_t bounds_test_shrink() {
-  const char* text = std::getenv("ACCEPT_BOUNDS_TEST_SHRINK");
-  return text ? (size_t)std::strtoull(text, nullptr, 10) : 0;
-}
-
-struct BoundsList {
-  accept::BoundsTable table{};
-  void add(const void* p, size_t bytes, bool writable) {
-    if (!p || table.n >= accept::kMaxBoundsRanges) return;
-    if (writable) bytes -= bounds_test_shrink() < bytes ? bounds_test_shrink() : bytes;
-    table.lo[table.n] = (unsigned long long)p;
-    table.hi[table.n] = (unsigned long long)p + bytes;
-    table.writable[table.n] = writable ? 1u : 0u;
-    ++table.n;
-  }
-  // ordered with the call's kernels on its stream (the source is pageable host memory: staged before return)
-  cudaError_t install(cudaStream_t s) const {
-    return cudaMemcpyToSymbolAsync(accept::g_bounds, &table, sizeof(table), 0, cudaMemcpyHostToDevice, s);
-  }
-};
-#define ACCEPT_BOUNDS(stream, ...)                                              \
-  do {                                                                          \
-    BoundsList bounds_list;                                                     \
-    __VA_ARGS__;                                                                \
-    if (bounds_list.install(stream) != cudaSuccess) return ACCEPT_ERR_CUDA;     \
-  } while (0)
-#else
-#define ACCEPT_BOUNDS(stream, ...) do { } while (0)
-#endif
 
 // ---- kernel tables -------------------------------------------------------------------------
 
@@ -770,7 +703,7 @@ accept_status accept_mbq_decompress(const accept_mbq_params* p, const void* d_st
   return ACCEPT_OK;
 }
 
-uint64_t accept_launch_count(void) { return g_launches.load(std::memory_order_relaxed); }
+uint64_t accept_launch_count(void) { return accept::g_launches.load(std::memory_order_relaxed); }
 
 accept_status accept_launch_null(uint32_t blocks, uint32_t threads, void* cuda_stream) {
   if (blocks == 0 || blocks > 0x7fffffffu || threads < 32 || threads > 1024) return ACCEPT_ERR_BAD_SIZE;
@@ -788,13 +721,12 @@ accept_status accept_bounds_check_report(void* cuda_stream, uint32_t* violations
   if (first_size_and_kind) *first_size_and_kind = 0;
   return ACCEPT_ERR_UNCHECKED_BUILD;
 #else
-  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   unsigned long long first[2] = {0, 0};
-  const unsigned int zero = 0;
-  if (cudaStreamSynchronize(s) != cudaSuccess) return ACCEPT_ERR_CUDA;
-  if (cudaMemcpyFromSymbol(violations, accept::g_bounds_violations, sizeof(uint32_t)) != cudaSuccess) return ACCEPT_ERR_CUDA;
-  if (cudaMemcpyFromSymbol(first, accept::g_bounds_first, sizeof(first)) != cudaSuccess) return ACCEPT_ERR_CUDA;
-  if (cudaMemcpyToSymbol(accept::g_bounds_violations, &zero, sizeof(zero)) != cudaSuccess) return ACCEPT_ERR_CUDA;
+  *violations = 0;
+  if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return ACCEPT_ERR_CUDA;
+  if (!accept::collect_bounds(violations, first) || !accept::collect_norm_bounds(violations, first) ||
+      !accept::collect_block_bounds(violations, first) || !accept::collect_matmul_bounds(violations, first))
+    return ACCEPT_ERR_CUDA;
   if (first_address) *first_address = first[0];
   if (first_size_and_kind) *first_size_and_kind = first[1];
   return ACCEPT_OK;

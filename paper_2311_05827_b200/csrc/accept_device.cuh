@@ -21,6 +21,15 @@ constexpr uint32_t kDevNonFinite = 1u, kDevBadHeader = 2u, kDevCopyTimeout = 4u;
 constexpr float kMagic = 12582912.0f;
 constexpr uint32_t kMagicBits = 0x4B400000u;
 
+// Programmatic dependent launch: a kernel launched with the stream-serialization attribute may be
+// scheduled while the kernel before it in the stream is still draining.  Every kernel here waits
+// for that predecessor (and the visibility of its writes) before it touches memory, and lets its
+// own successor be scheduled right away: what overlaps is launch latency and the tail of the grid.
+__device__ __forceinline__ void grid_dependency_handshake() {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
 // ----------------------------------------------------------------------------- memory access
 
 // Every access of the data path to caller memory (input, output, stream, workspace records) goes through
@@ -30,17 +39,18 @@ constexpr uint32_t kMagicBits = 0x4B400000u;
 // the call: one that falls outside, or a write into a read-only range, is COUNTED AND SKIPPED (a load
 // returns zeros), never trapped, so the context stays usable and the host can read the tally.
 #ifdef ACCEPT_BOUNDS_CHECK
-constexpr int kMaxBoundsRanges = 8;
+constexpr int kMaxBoundsRanges = 12;
 struct BoundsTable {
   unsigned long long lo[kMaxBoundsRanges], hi[kMaxBoundsRanges];  // [lo, hi) in bytes
   unsigned int writable[kMaxBoundsRanges];
   unsigned int n;
 };
-__device__ BoundsTable g_bounds;
-__device__ unsigned int g_bounds_violations;      // accesses skipped since the last report
-__device__ unsigned long long g_bounds_first[2];  // the first of them: address, size | write << 32
+// one table and tally for each source file that is compiled (accept_bounds_check_report adds them up)
+static __device__ BoundsTable g_bounds;
+static __device__ unsigned int g_bounds_violations;      // accesses skipped since the last report
+static __device__ unsigned long long g_bounds_first[2];  // the first of them: address, size | write << 32
 
-__device__ __noinline__ bool bounds_ok(const void* p, size_t bytes, bool write) {
+static __device__ __noinline__ bool bounds_ok(const void* p, size_t bytes, bool write) {
   const unsigned long long a = (unsigned long long)p;
   for (unsigned int i = 0; i < g_bounds.n; ++i)
     if (a >= g_bounds.lo[i] && a + bytes <= g_bounds.hi[i] && (!write || g_bounds.writable[i])) return true;

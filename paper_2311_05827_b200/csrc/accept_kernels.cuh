@@ -42,15 +42,6 @@ __device__ __forceinline__ uint32_t header_word(const CodecArgs& a, int i) {
   }
 }
 
-// Programmatic dependent launch: a kernel launched with the stream-serialization attribute may be
-// scheduled while the kernel before it in the stream is still draining.  Every kernel here waits
-// for that predecessor (and the visibility of its writes) before it touches memory, and lets its
-// own successor be scheduled right away: what overlaps is launch latency and the tail of the grid.
-__device__ __forceinline__ void grid_dependency_handshake() {
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-}
-
 // Nothing but the handshake every kernel starts with: what a launch of this library costs (accept_launch_null).
 __global__ void null_kernel() { grid_dependency_handshake(); }
 

@@ -1,0 +1,139 @@
+// Host side of the block-scaled matrix product (accept_block_matmul): argument checks, tensor maps, launches.
+#include "accept_host.cuh"
+#include "accept_matmul.cuh"
+
+namespace {
+
+using accept::is_aligned;
+using accept::launch_overlapped;
+using accept::MatmulArgs;
+
+constexpr unsigned kSms = 148;
+
+size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
+uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
+
+// The driver's encoder of tensor maps, asked for once: the library does not link the driver.
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn tensor_map_encoder() {
+  static std::atomic<EncodeFn> found{nullptr};
+  EncodeFn fn = found.load(std::memory_order_acquire);
+  if (fn) return fn;
+  void* p = nullptr;
+  cudaDriverEntryPointQueryResult result;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &result) != cudaSuccess ||
+      result != cudaDriverEntryPointSuccess)
+    return nullptr;
+  fn = reinterpret_cast<EncodeFn>(p);
+  found.store(fn, std::memory_order_release);
+  return fn;
+}
+
+// Boxes of 128 values of k by `box_rows` rows of a coded matrix, 128-byte swizzle, zeros outside.
+bool operand_map(CUtensorMap* map, const void* codes, uint64_t rows, uint64_t k, uint32_t box_rows) {
+  const EncodeFn encode = tensor_map_encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {k, rows}, strides[1] = {up(k, 16)};
+  const cuuint32_t box[2] = {128, box_rows}, steps[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(codes), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NT, bool TURNED>
+cudaError_t launch_matmul(const CUtensorMap& map_a, const CUtensorMap& map_b, const MatmulArgs& a, unsigned tiles, unsigned parts, cudaStream_t s) {
+  auto fn = accept::matmul_kernel<NT, TURNED>;
+  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::matmul_shared_bytes(NT));
+  if (err != cudaSuccess) return err;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(tiles, 1, parts);
+  cfg.blockDim = dim3(accept::kMatmulThreads, 1, 1);
+  cfg.dynamicSmemBytes = accept::matmul_shared_bytes(NT);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 1;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = parts;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, fn, map_a, map_b, a);
+}
+
+}  // namespace
+
+#ifdef ACCEPT_BOUNDS_CHECK
+bool accept::collect_matmul_bounds(uint32_t* violations, unsigned long long (&first)[2]) { return collect_bounds(violations, first); }
+#endif
+
+extern "C" {
+
+accept_status accept_matmul_check_params(const accept_matmul_params* p) {
+  if (!p) return ACCEPT_ERR_NULL;
+  if (p->m > 0x7fffffffull || p->n > 0x7fffffffull || p->k > 0x7fffffffull || p->ldd < p->n || p->ldd > (1ull << 40)) return ACCEPT_ERR_BAD_SIZE;
+  if ((up(p->m, 128) / 128) * (up(p->n, 128) / 128) > 0x7fffffffull || p->m * p->n / 256 > 0x7ffffff0ull) return ACCEPT_ERR_BAD_SIZE;
+  for (int32_t f : {p->format_a, p->format_b})
+    if (f != ACCEPT_FORMAT_E4M3 && f != ACCEPT_FORMAT_E5M2) return ACCEPT_ERR_BAD_ENUM;
+  if (p->dtype_d != ACCEPT_DTYPE_F32 && p->dtype_d != ACCEPT_DTYPE_BF16 && p->dtype_d != ACCEPT_DTYPE_F16) return ACCEPT_ERR_BAD_ENUM;
+  if (p->accumulate != 0 && p->accumulate != 1) return ACCEPT_ERR_BAD_ENUM;
+  return ACCEPT_OK;
+}
+
+size_t accept_matmul_workspace_size(const accept_matmul_params* p) { return accept_matmul_check_params(p) == ACCEPT_OK ? 16 : 0; }
+
+accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b,
+                                  const void* d_b_scale, const float* d_bias, void* d_d, void* d_ws, size_t ws_bytes,
+                                  void* cuda_stream) {
+  if (!p || !d_ws) return ACCEPT_ERR_NULL;
+  const accept_status st = accept_matmul_check_params(p);
+  if (st != ACCEPT_OK) return st;
+  if (ws_bytes < 16) return ACCEPT_ERR_TOO_SMALL;
+  if (p->m == 0 || p->n == 0) return ACCEPT_OK;
+  if (!d_d || (p->k != 0 && (!d_a || !d_a_scale || !d_b || !d_b_scale))) return ACCEPT_ERR_NULL;
+  if (!is_aligned(d_a, 16) || !is_aligned(d_a_scale, 16) || !is_aligned(d_b, 16) || !is_aligned(d_b_scale, 16) || !is_aligned(d_bias, 4) ||
+      !is_aligned(d_d, value_size(p->dtype_d)) || !is_aligned(d_ws, 4))
+    return ACCEPT_ERR_MISALIGNED;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  MatmulArgs a{};
+  a.bias = d_bias;
+  a.d = d_d;
+  a.status = static_cast<uint32_t*>(d_ws);
+  a.ldd = p->ldd;
+  a.dtype_d = p->dtype_d;
+  a.accumulate = p->accumulate;
+  ACCEPT_BOUNDS(s, bounds_list.add(d_bias, 4 * p->n, false); bounds_list.add(d_d, ((p->m - 1) * p->ldd + p->n) * value_size(p->dtype_d), true));
+  if (p->k == 0) {
+    a.rows_a = (uint32_t)p->m;
+    a.rows_b = (uint32_t)p->n;
+    ACCEPT_LAUNCH(launch_overlapped(accept::matmul_empty_kernel, dim3((unsigned)((p->m * p->n + 255) / 256)), 256, s, a));
+    return ACCEPT_OK;
+  }
+
+  const bool turned = p->m <= 128;  // few rows of a: b's rows take the 128 lanes
+  const uint64_t rows_a = turned ? p->n : p->m, rows_b = turned ? p->m : p->n;
+  const unsigned nt = !turned ? 128 : p->m <= 16 ? 16 : p->m <= 32 ? 32 : p->m <= 64 ? 64 : 128;
+  a.scale_a = static_cast<const uint8_t*>(turned ? d_b_scale : d_a_scale);
+  a.scale_b = static_cast<const uint8_t*>(turned ? d_a_scale : d_b_scale);
+  a.rows_a = (uint32_t)rows_a;
+  a.rows_b = (uint32_t)rows_b;
+  a.blocks = (uint32_t)(up(p->k, 128) / 128);
+  a.atoms_a = (uint32_t)(up(rows_a, 128) / 128);
+  a.atoms_b = (uint32_t)(up(rows_b, 128) / 128);
+  a.tiles_a = a.atoms_a;
+  a.instruction = accept::scaled_instruction((uint32_t)(turned ? p->format_b : p->format_a), (uint32_t)(turned ? p->format_a : p->format_b), 128, nt);
+  CUtensorMap map_a, map_b;
+  if (!operand_map(&map_a, turned ? d_b : d_a, rows_a, p->k, 128) || !operand_map(&map_b, turned ? d_a : d_b, rows_b, p->k, nt)) return ACCEPT_ERR_CUDA;
+  const uint64_t tiles = (uint64_t)a.tiles_a * (up(rows_b, nt) / nt);
+  unsigned parts = 1;
+  while (parts < 8 && tiles * parts * 2 <= kSms && a.blocks >= parts * 4) parts *= 2;
+  if (!turned) ACCEPT_LAUNCH((launch_matmul<128, false>(map_a, map_b, a, (unsigned)tiles, parts, s)));
+  else if (nt == 16) ACCEPT_LAUNCH((launch_matmul<16, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
+  else if (nt == 32) ACCEPT_LAUNCH((launch_matmul<32, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
+  else if (nt == 64) ACCEPT_LAUNCH((launch_matmul<64, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
+  else ACCEPT_LAUNCH((launch_matmul<128, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
+  return ACCEPT_OK;
+}
+
+}  // extern "C"
