@@ -40,6 +40,66 @@ bool operand_map(CUtensorMap* map, const void* codes, uint64_t rows, uint64_t k,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// The scales of a coded matrix as rows of 512 bytes (128 rows and four blocks of it each), `box_rows` at a time.
+bool scale_map(CUtensorMap* map, const void* scales, uint64_t atoms, uint32_t box_rows) {
+  const EncodeFn encode = tensor_map_encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {128, atoms}, strides[1] = {512};
+  const cuuint32_t box[2] = {128, box_rows}, steps[2] = {1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(scales), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Pieces of 32 x 32 values of d, each row a swizzle span (64 bytes for 16-bit types, 128 for fp32).
+bool result_map(CUtensorMap* map, void* d, int32_t dtype, uint64_t m, uint64_t n, uint64_t ldd) {
+  const EncodeFn encode = tensor_map_encoder();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {n, m}, strides[1] = {ldd * value_size(dtype)};
+  const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+  const CUtensorMapDataType type = dtype == ACCEPT_DTYPE_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : dtype == ACCEPT_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                                : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  return encode(map, type, 2, d, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                dtype == ACCEPT_DTYPE_F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Products of at least this many tiles of 256 x 256 go to the pairs of SMs.
+constexpr uint64_t kPairTilesLeast = 60;
+
+accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b, const void* d_b_scale,
+                           const MatmulArgs& base, cudaStream_t s) {
+  accept::PairArgs a{};
+  a.bias = base.bias;
+  a.d = base.d;
+  a.status = base.status;
+  a.ldd = base.ldd;
+  a.dtype_d = base.dtype_d;
+  a.accumulate = base.accumulate;
+  a.m = (uint32_t)p->m;
+  a.n = (uint32_t)p->n;
+  a.blocks = (uint32_t)(up(p->k, 128) / 128);
+  a.atoms_a = (uint32_t)(up(p->m, 128) / 128);
+  a.atoms_b = (uint32_t)(up(p->n, 128) / 128);
+  a.tiles_m = (uint32_t)(up(p->m, 256) / 256);
+  a.tiles_n = (uint32_t)(up(p->n, 256) / 256);
+  a.instruction = accept::scaled_instruction((uint32_t)p->format_a, (uint32_t)p->format_b, 256, 256);
+  const bool single = p->dtype_d == ACCEPT_DTYPE_F32;
+  a.tile_stores = is_aligned(a.d, 16) && a.ldd * value_size(p->dtype_d) % 16 == 0 && (single || !a.accumulate);
+  const uint64_t groups = (a.blocks + 3) / 4;
+  CUtensorMap map_a, map_b, map_sa, map_sb, map_d{};
+  if (!operand_map(&map_a, d_a, p->m, p->k, 128) || !operand_map(&map_b, d_b, p->n, p->k, 128) ||
+      !scale_map(&map_sa, d_a_scale, groups * a.atoms_a, 1) || !scale_map(&map_sb, d_b_scale, groups * a.atoms_b, 2) ||
+      (a.tile_stores && !result_map(&map_d, a.d, p->dtype_d, p->m, p->n, a.ldd)))
+    return ACCEPT_ERR_CUDA;
+  const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n;
+  const unsigned pairs = (unsigned)(tiles < kSms / 2 ? tiles : kSms / 2);
+  auto fn = single ? accept::matmul_pair_kernel<true> : accept::matmul_pair_kernel<false>;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::kPairSharedBytes) != cudaSuccess) return ACCEPT_ERR_CUDA;
+  ACCEPT_LAUNCH(accept::launch_overlapped_shared(fn, dim3(2 * pairs), accept::kMatmulThreads, accept::kPairSharedBytes, s, map_a, map_b, map_sa, map_sb, map_d, a));
+  return ACCEPT_OK;
+}
+
 template <int NT, bool TURNED>
 cudaError_t launch_matmul(const CUtensorMap& map_a, const CUtensorMap& map_b, const MatmulArgs& a, unsigned tiles, unsigned parts, cudaStream_t s) {
   auto fn = accept::matmul_kernel<NT, TURNED>;
@@ -110,6 +170,8 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
     ACCEPT_LAUNCH(launch_overlapped(accept::matmul_empty_kernel, dim3((unsigned)((p->m * p->n + 255) / 256)), 256, s, a));
     return ACCEPT_OK;
   }
+
+  if ((up(p->m, 256) / 256) * (up(p->n, 256) / 256) >= kPairTilesLeast) return launch_pairs(p, d_a, d_a_scale, d_b, d_b_scale, a, s);
 
   const bool turned = p->m <= 128;  // few rows of a: b's rows take the 128 lanes
   const uint64_t rows_a = turned ? p->n : p->m, rows_b = turned ? p->m : p->n;

@@ -188,6 +188,220 @@ __global__ void __launch_bounds__(kMatmulThreads) matmul_kernel(const __grid_con
   if (parts > 1) cluster_sync();  // the other blocks may still be reading this one's tile
 }
 
+// ---- large products: pairs of SMs, tiles of 256 x 256, persistent -----------------------------------------------------
+//
+// Bound by the tensor cores.  A pair of blocks holds one tile (128 rows of it in each block's tensor memory); each
+// block loads its own 128 rows of a and half of b, so an operand byte in shared memory feeds twice the products it would
+// feed for one SM alone.  Each block keeps taking tiles; the sums of the next tile are formed while the last tile's are
+// read.  Two tiles of sums (2 x 256 columns) and the scales do not fit 512 columns side by side, so the two overlap by 72
+// columns: those are read first, and the next tile's products start once they are.
+constexpr int kPairTile = 256;
+constexpr int kPairStages = 6;
+constexpr int kPairStageBytes = 2 * 128 * 128;            // 128 rows of a and 128 of b, 128 bytes each
+constexpr int kPairScaleBytes = 512 + 1024;               // scales of 128 rows of a, of 256 of b, four blocks of k
+constexpr int kPairStaging = 4 * 4096;                    // a piece of the result for each of four warps: 32 rows of 128 bytes
+constexpr int kPairSharedBytes = 1024 + kPairStages * (kPairStageBytes + kPairScaleBytes) + kPairStaging + 4 * kPairTile;
+constexpr uint32_t kPairScaleColumn = 512 - 12 * kPairStages;  // a stage's scales in tensor memory: 4 columns of a, 8 of b
+constexpr uint32_t kPairSecond = kPairScaleColumn - kPairTile; // where the second tile of sums starts
+
+struct PairArgs {
+  const float* bias;
+  void* d;
+  uint32_t* status;
+  uint64_t ldd;
+  uint32_t m, n, blocks;
+  uint32_t atoms_a, atoms_b;
+  uint32_t tiles_m, tiles_n;
+  uint32_t instruction;
+  int dtype_d, accumulate;
+  int tile_stores;   // d is stored through its tensor map (16-byte aligned rows, nothing to add but in fp32)
+};
+
+// Tiles in the order in which neighbouring pairs take them: eight tiles of rows, then the next tile of columns, so that
+// the tiles in flight at a time form a block that shares its operands in L2.
+__device__ __forceinline__ void pair_tile(const PairArgs& a, uint32_t index, uint32_t& tile_m, uint32_t& tile_n) {
+  const uint32_t per_group = 8 * a.tiles_n, group = index / per_group, inside = index - group * per_group;
+  const uint32_t rows = min(8u, a.tiles_m - 8 * group);
+  tile_n = inside / rows;
+  tile_m = 8 * group + inside - tile_n * rows;
+}
+
+template <bool SINGLE>  // d is fp32
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
+    matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                       const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
+                       const __grid_constant__ CUtensorMap map_d, const PairArgs a) {
+  extern __shared__ uint8_t raw_shared[];
+  __shared__ __align__(8) uint64_t barriers[2 * kPairStages + 3];
+  __shared__ uint32_t tensor_base, failed, issued;
+  const uint32_t base = (smem_address(raw_shared) + 1023) & ~1023u;
+  const uint32_t scales = base + kPairStages * kPairStageBytes, staging = scales + kPairStages * kPairScaleBytes;
+  float* bias_tile = reinterpret_cast<float*>(raw_shared + (staging + kPairStaging - smem_address(raw_shared)));
+  const uint32_t full = smem_address(barriers), empty = full + 8 * kPairStages, done = empty + 8 * kPairStages, drained = done + 16;
+  const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
+  const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1, tiles = a.tiles_m * a.tiles_n;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2 * kPairStages + 2; ++i) mbarrier_init(full + 8 * i, 1);
+    mbarrier_init(drained, 8);  // the four reading warps of both blocks
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    failed = issued = 0;
+    prefetch_map(&map_a);
+    prefetch_map(&map_b);
+    prefetch_map(&map_sa);
+    prefetch_map(&map_sb);
+    prefetch_map(&map_d);
+  }
+  if (warp == 0) pair_tensor_alloc(smem_address(&tensor_base), 512);
+  tensor_fence_before();
+  cluster_sync();
+  tensor_fence_after();
+  const uint32_t sums = tensor_base;
+  grid_dependency_handshake();
+
+  if (warp == 4 && lane == 0) {  // loads, in both blocks; the even block's barrier counts the bytes of both
+    uint32_t i = 0;
+    bool ok = true;
+    for (uint32_t t = pair; t < tiles && ok; t += pairs) {
+      uint32_t tile_m, tile_n;
+      pair_tile(a, t, tile_m, tile_n);
+      const uint32_t row_a = tile_m * kPairTile + rank * 128, row_b = tile_n * kPairTile + rank * 128;
+      for (uint32_t b = 0; b < a.blocks; ++b, ++i) {
+        const uint32_t stage = i % kPairStages, round = i / kPairStages;
+        if (round > 0 && !mbarrier_wait(empty + 8 * stage, (round - 1) & 1)) { ok = false; break; }
+        const bool with_scales = (b & 3) == 0;
+        const uint32_t at = base + stage * kPairStageBytes, at_scales = scales + stage * kPairScaleBytes, bar = address_in(full + 8 * stage, 0);
+        if (rank == 0) mbarrier_expect_bytes(full + 8 * stage, 2 * (kPairStageBytes + (with_scales ? kPairScaleBytes : 0)) + kCopyAnnounceExtra);
+        pair_tile_load(at, &map_a, b * 128, row_a, bar);
+        pair_tile_load(at + 128 * 128, &map_b, b * 128, row_b, bar);
+        if (with_scales) {
+          pair_tile_load(at_scales, &map_sa, 0, (b >> 2) * a.atoms_a + tile_m * 2 + rank, bar);
+          pair_tile_load(at_scales + 512, &map_sb, 0, (b >> 2) * a.atoms_b + tile_n * 2, bar);
+        }
+      }
+    }
+    issued = i;
+    if (!ok) atomicExch(&failed, 1u);
+  } else if (warp == 5 && lane == 0 && rank == 0) {  // matrix instructions, for both blocks
+    uint32_t i = 0, unit = 0, scale_a = 0;
+    bool ok = true;
+    for (uint32_t t = pair; t < tiles && ok; t += pairs, ++unit) {
+      if (unit > 0 && !mbarrier_wait(drained, (unit - 1) & 1)) { ok = false; break; }
+      tensor_fence_after();
+      const uint32_t into = sums + (unit & 1 ? kPairSecond : 0);
+      for (uint32_t b = 0; b < a.blocks; ++b, ++i) {
+        const uint32_t stage = i % kPairStages, round = i / kPairStages;
+        if (!mbarrier_wait(full + 8 * stage, round & 1)) { ok = false; break; }
+        tensor_fence_after();
+        const uint32_t at = base + stage * kPairStageBytes;
+        if ((b & 3) == 0) {  // a word of scales serves four blocks of k
+          const uint32_t from = scales + stage * kPairScaleBytes;
+          scale_a = sums + kPairScaleColumn + 12 * stage;
+          pair_scale_copy(scale_a, scale_descriptor(from));
+          pair_scale_copy(scale_a + 4, scale_descriptor(from + 512));
+          pair_scale_copy(scale_a + 8, scale_descriptor(from + 1024));
+        }
+        const uint32_t instruction = with_scale_byte(a.instruction, b & 3);
+        const uint64_t da = operand_descriptor(at), db = operand_descriptor(at + 128 * 128);
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) pair_scaled_mma(into, da + 2 * k, db + 2 * k, instruction, scale_a, scale_a + 4, b > 0 || k > 0);
+        pair_mma_commit(empty + 8 * stage);
+      }
+      if (ok) pair_mma_commit(done + 8 * (unit & 1));
+    }
+    if (!ok) atomicExch(&failed, 1u);
+  } else if (warp < 4) {  // results
+    uint32_t unit = 0;
+    const uint32_t piece = staging + warp * 4096;
+    float* values = reinterpret_cast<float*>(raw_shared + (piece - smem_address(raw_shared)));
+    const uint32_t drained_at = address_in(drained, 0);
+    for (uint32_t t = pair; t < tiles; t += pairs, ++unit) {
+      uint32_t tile_m, tile_n;
+      pair_tile(a, t, tile_m, tile_n);
+      const uint32_t row0 = tile_m * kPairTile + rank * 128 + warp * 32, col0 = tile_n * kPairTile;
+      if (a.bias) {
+        asm volatile("bar.sync 1, 128;" ::: "memory");  // the last tile's values have been read
+        for (uint32_t c = threadIdx.x; c < kPairTile; c += 128) bias_tile[c] = col0 + c < a.n ? ld_c(a.bias + col0 + c) : 0.0f;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+      }
+      if (!mbarrier_wait(done + 8 * (unit & 1), (unit >> 1) & 1)) { atomicExch(&failed, 1u); break; }
+      tensor_fence_after();
+      const uint32_t from = sums + (unit & 1 ? kPairSecond : 0) + ((warp * 32) << 16);
+#pragma unroll 1
+      for (int half = 0; half < 8; ++half) {  // 32 columns at a time, those shared with the next tile first
+        const uint32_t c = 32 * (unit & 1 ? half : 7 - half);
+        float v[32];
+        tensor_read(from + c, v);
+        tensor_read_wait();
+        if (half == 2) {  // three of eight pieces: 96 columns
+          tensor_fence_before();
+          __syncwarp();
+          if (lane == 0) mbarrier_arrive_cluster(drained_at);
+        }
+        if (a.bias)
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] += bias_tile[c + j];
+        if (a.tile_stores) {
+          // row `lane` of the piece, its 16-byte units permuted as the tensor map's swizzle has them
+          if (lane == 0) store_wait_read();
+          __syncwarp();
+          if (SINGLE) {
+#pragma unroll
+            for (uint32_t u = 0; u < 8; ++u)
+              *reinterpret_cast<float4*>(values + lane * 32 + 4 * (u ^ (lane & 7))) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+          } else {
+#pragma unroll
+            for (uint32_t u = 0; u < 4; ++u) {
+              uint32_t w[4];
+#pragma unroll
+              for (uint32_t j = 0; j < 4; ++j) {
+                const float x = v[8 * u + 2 * j], y = v[8 * u + 2 * j + 1];
+                if (a.dtype_d == kBf16) {
+                  const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+                  memcpy(&w[j], &h, 4);
+                } else {
+                  const __half2 h = __floats2half2_rn(x, y);
+                  memcpy(&w[j], &h, 4);
+                }
+              }
+              *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(values) + lane * 64 + 16 * (u ^ ((lane >> 1) & 3))) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+          }
+          shared_to_async();
+          __syncwarp();
+          if (lane == 0 && row0 < a.m && col0 + c < a.n) {
+            if (SINGLE && a.accumulate) tile_add(&map_d, col0 + c, row0, piece);
+            else tile_store(&map_d, col0 + c, row0, piece);
+            store_commit();
+          }
+        } else {  // through shared memory so that a row's values leave side by side
+#pragma unroll
+          for (uint32_t u = 0; u < 8; ++u)
+            *reinterpret_cast<float4*>(values + lane * 32 + 4 * (u ^ (lane & 7))) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+          __syncwarp();
+          if (col0 + c + lane < a.n)
+            for (uint32_t r = 0; r < 32 && row0 + r < a.m; ++r)
+              store_value(a.d, a.dtype_d, (uint64_t)(row0 + r) * a.ldd + col0 + c + lane, values[r * 32 + 4 * ((lane >> 2) ^ (r & 7)) + (lane & 3)], a.accumulate);
+          __syncwarp();
+        }
+      }
+    }
+    if (lane == 0) store_wait();
+  }
+  __syncwarp();
+  __syncthreads();
+  if (threadIdx.x == 0 && *reinterpret_cast<volatile uint32_t*>(&failed)) {
+    atomicOr(a.status, kDevCopyTimeout);
+    // no copy may still be on its way when a block of the pair leaves
+    if (rank == 0)
+      for (uint32_t i = 0; i < issued && i < kPairStages; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kPairStages) & 1);
+  }
+  tensor_fence_before();
+  cluster_sync();
+  tensor_fence_after();
+  if (warp == 0) pair_tensor_free(sums, 512);
+}
+
 // k = 0: the sum is empty.
 __global__ void __launch_bounds__(256) matmul_empty_kernel(const MatmulArgs a) {
   grid_dependency_handshake();

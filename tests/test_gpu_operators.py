@@ -300,6 +300,8 @@ PRODUCTS = [
     (512, 512, 512, "e5m2", "e4m3", F32, False, True, 0), (1500, 1100, 700, "e4m3", "e4m3", BF16, True, False, 0),
     (2048, 2304, 640, "e4m3", "e4m3", BF16, True, False, 0), (640, 1280, 8300, "e5m2", "e4m3", F32, False, False, 0),
     (2600, 2600, 1160, "e4m3", "e4m3", F32, False, True, 0), (4100, 520, 2100, "e4m3", "e4m3", F16, True, False, 4),
+    (2305, 2311, 300, "e5m2", "e5m2", BF16, True, False, 0), (2048, 2100, 257, "e4m3", "e5m2", F16, False, True, 0), (5000, 1900, 1000, "e4m3", "e4m3", F32, True, False, 0),
+    (4000, 3333, 128, "e4m3", "e4m3", F32, False, True, 1), (7000, 2000, 1, "e5m2", "e4m3", BF16, True, False, 0),
 ]
 
 
