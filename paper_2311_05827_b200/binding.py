@@ -250,9 +250,13 @@ def _check(code: int, where: str) -> None:
 
 
 def _stream_handle(stream=None) -> int:
+    if stream is not None:
+        return int(stream.cuda_stream)
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return int(s.cuda_stream)
+    if not torch.cuda.is_initialized():
+        torch.cuda.init()
+    # the current stream's handle itself: building a torch.cuda.Stream object takes as long as a launch
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 # ---- size queries (host only) -------------------------------------------------------------

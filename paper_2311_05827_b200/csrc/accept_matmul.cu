@@ -64,15 +64,51 @@ bool result_map(CUtensorMap* map, void* d, int32_t dtype, uint64_t m, uint64_t n
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Products of at least this many tiles of 256 x 256 go to the pairs of SMs.
+// How a large product is dealt to the pairs of SMs: see matmul_pair_kernel.
+struct PairShape { uint64_t tiles; unsigned pairs; uint32_t whole, parts, chunks; };
+
+// Products of at least this many tiles of 256 x 256 go to the pairs.
 constexpr uint64_t kPairTilesLeast = 60;
 
+uint64_t pair_tiles(const accept_matmul_params* p) { return (up(p->m, 256) / 256) * (up(p->n, 256) / 256); }
+bool uses_pairs(const accept_matmul_params* p) { return p->k != 0 && pair_tiles(p) >= kPairTilesLeast; }
+
+PairShape pair_shape(const accept_matmul_params* p) {
+  PairShape s{};
+  const uint64_t blocks = up(p->k, 128) / 128;
+  s.tiles = pair_tiles(p);
+  s.pairs = kSms / 2;
+  const uint64_t left = s.tiles % s.pairs;
+  const uint32_t chunks = p->dtype_d == ACCEPT_DTYPE_F32 ? (uint32_t)((blocks + accept::kChunk - 1) / accept::kChunk) : 1;
+  s.chunks = chunks ? chunks : 1;
+  s.parts = 1;
+  s.whole = (uint32_t)s.tiles;
+  if (left != 0) {
+    // cut what is left so that one more round serves it; a part of fewer than 12 blocks of k costs more than it gives
+    uint64_t parts = s.pairs / left;
+    if (parts > blocks / 12) parts = blocks / 12;
+    if (parts > 8) parts = 8;
+    if (parts >= 2 && parts >= s.chunks) {
+      s.parts = (uint32_t)parts;
+      s.whole = (uint32_t)(s.tiles - left);
+    }
+  }
+  if (s.tiles * s.parts < s.pairs) s.pairs = (unsigned)(s.tiles * s.parts);
+  return s;
+}
+
+size_t pair_arrival_bytes(const PairShape& s) { return (size_t)up(32 * (s.tiles - s.whole), 16); }
+size_t pair_partial_bytes(const PairShape& s) { return (size_t)((s.tiles - s.whole) * s.parts * 256 * 256 * 4); }
+
 accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b, const void* d_b_scale,
-                           const MatmulArgs& base, cudaStream_t s) {
+                           const MatmulArgs& base, uint8_t* d_ws, cudaStream_t s) {
+  const PairShape shape = pair_shape(p);
   accept::PairArgs a{};
   a.bias = base.bias;
   a.d = base.d;
   a.status = base.status;
+  a.arrivals = reinterpret_cast<uint32_t*>(d_ws + 16);
+  a.partials = reinterpret_cast<float*>(d_ws + 16 + pair_arrival_bytes(shape));
   a.ldd = base.ldd;
   a.dtype_d = base.dtype_d;
   a.accumulate = base.accumulate;
@@ -83,6 +119,9 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
   a.atoms_b = (uint32_t)(up(p->n, 128) / 128);
   a.tiles_m = (uint32_t)(up(p->m, 256) / 256);
   a.tiles_n = (uint32_t)(up(p->n, 256) / 256);
+  a.whole = shape.whole;
+  a.parts = shape.parts;
+  a.chunks = shape.chunks;
   a.instruction = accept::scaled_instruction((uint32_t)p->format_a, (uint32_t)p->format_b, 256, 256);
   const bool single = p->dtype_d == ACCEPT_DTYPE_F32;
   a.tile_stores = is_aligned(a.d, 16) && a.ldd * value_size(p->dtype_d) % 16 == 0 && (single || !a.accumulate);
@@ -92,11 +131,10 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
       !scale_map(&map_sa, d_a_scale, groups * a.atoms_a, 1) || !scale_map(&map_sb, d_b_scale, groups * a.atoms_b, 2) ||
       (a.tile_stores && !result_map(&map_d, a.d, p->dtype_d, p->m, p->n, a.ldd)))
     return ACCEPT_ERR_CUDA;
-  const uint64_t tiles = (uint64_t)a.tiles_m * a.tiles_n;
-  const unsigned pairs = (unsigned)(tiles < kSms / 2 ? tiles : kSms / 2);
   auto fn = single ? accept::matmul_pair_kernel<true> : accept::matmul_pair_kernel<false>;
   if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::kPairSharedBytes) != cudaSuccess) return ACCEPT_ERR_CUDA;
-  ACCEPT_LAUNCH(accept::launch_overlapped_shared(fn, dim3(2 * pairs), accept::kMatmulThreads, accept::kPairSharedBytes, s, map_a, map_b, map_sa, map_sb, map_d, a));
+  if (a.parts > 1 && cudaMemsetAsync(a.arrivals, 0, pair_arrival_bytes(shape), s) != cudaSuccess) return ACCEPT_ERR_CUDA;
+  ACCEPT_LAUNCH(accept::launch_overlapped_shared(fn, dim3(2 * shape.pairs), accept::kMatmulThreads, accept::kPairSharedBytes, s, map_a, map_b, map_sa, map_sb, map_d, a));
   return ACCEPT_OK;
 }
 
@@ -141,7 +179,12 @@ accept_status accept_matmul_check_params(const accept_matmul_params* p) {
   return ACCEPT_OK;
 }
 
-size_t accept_matmul_workspace_size(const accept_matmul_params* p) { return accept_matmul_check_params(p) == ACCEPT_OK ? 16 : 0; }
+size_t accept_matmul_workspace_size(const accept_matmul_params* p) {
+  if (accept_matmul_check_params(p) != ACCEPT_OK) return 0;
+  if (!uses_pairs(p)) return 16;
+  const PairShape s = pair_shape(p);
+  return 16 + (s.parts > 1 ? pair_arrival_bytes(s) + pair_partial_bytes(s) : 0);
+}
 
 accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b,
                                   const void* d_b_scale, const float* d_bias, void* d_d, void* d_ws, size_t ws_bytes,
@@ -149,11 +192,11 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
   if (!p || !d_ws) return ACCEPT_ERR_NULL;
   const accept_status st = accept_matmul_check_params(p);
   if (st != ACCEPT_OK) return st;
-  if (ws_bytes < 16) return ACCEPT_ERR_TOO_SMALL;
+  if (ws_bytes < accept_matmul_workspace_size(p)) return ACCEPT_ERR_TOO_SMALL;
   if (p->m == 0 || p->n == 0) return ACCEPT_OK;
   if (!d_d || (p->k != 0 && (!d_a || !d_a_scale || !d_b || !d_b_scale))) return ACCEPT_ERR_NULL;
   if (!is_aligned(d_a, 16) || !is_aligned(d_a_scale, 16) || !is_aligned(d_b, 16) || !is_aligned(d_b_scale, 16) || !is_aligned(d_bias, 4) ||
-      !is_aligned(d_d, value_size(p->dtype_d)) || !is_aligned(d_ws, 4))
+      !is_aligned(d_d, value_size(p->dtype_d)) || !is_aligned(d_ws, 16))
     return ACCEPT_ERR_MISALIGNED;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
   MatmulArgs a{};
@@ -163,7 +206,8 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
   a.ldd = p->ldd;
   a.dtype_d = p->dtype_d;
   a.accumulate = p->accumulate;
-  ACCEPT_BOUNDS(s, bounds_list.add(d_bias, 4 * p->n, false); bounds_list.add(d_d, ((p->m - 1) * p->ldd + p->n) * value_size(p->dtype_d), true));
+  ACCEPT_BOUNDS(s, bounds_list.add(d_bias, 4 * p->n, false); bounds_list.add(d_d, ((p->m - 1) * p->ldd + p->n) * value_size(p->dtype_d), true);
+                bounds_list.add(d_ws, accept_matmul_workspace_size(p), true));
   if (p->k == 0) {
     a.rows_a = (uint32_t)p->m;
     a.rows_b = (uint32_t)p->n;
@@ -171,7 +215,7 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
     return ACCEPT_OK;
   }
 
-  if ((up(p->m, 256) / 256) * (up(p->n, 256) / 256) >= kPairTilesLeast) return launch_pairs(p, d_a, d_a_scale, d_b, d_b_scale, a, s);
+  if (uses_pairs(p)) return launch_pairs(p, d_a, d_a_scale, d_b, d_b_scale, a, static_cast<uint8_t*>(d_ws), s);
 
   const bool turned = p->m <= 128;  // few rows of a: b's rows take the 128 lanes
   const uint64_t rows_a = turned ? p->n : p->m, rows_b = turned ? p->m : p->n;
