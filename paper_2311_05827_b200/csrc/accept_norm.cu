@@ -10,84 +10,104 @@ using accept::NormArgs;
 
 constexpr unsigned kSms = 148;
 
-// Launch shape of a pass: octets per thread, threads, whether each warp has a row of its own, blocks.
-struct NormShape { int octets; unsigned threads; bool one_warp; bool longer; unsigned blocks; };
-
-NormShape norm_shape(const accept_layer_norm_params* p, bool backward) {
-  NormShape s{};
-  const uint64_t octets = (p->cols + 7) / 8;
-  if (octets <= 64) {
-    s.one_warp = true;
-    s.octets = octets <= 32 ? 1 : 2;
-    s.threads = 256;
-  } else {
-    s.octets = octets <= 256 || (backward && octets > 512) ? 1 : 2;
-    s.threads = (unsigned)(((octets + s.octets - 1) / s.octets + 31) / 32 * 32);
-    if ((octets + s.octets - 1) / s.octets > 1024) s.longer = true;
-  }
-  if (s.longer) s.threads = 1024;
-  const uint64_t units = s.one_warp ? (p->rows + 7) / 8 : p->rows;
-  const uint64_t per_sm = backward ? (s.octets == 2 ? 512 : 1024) / s.threads : 1024 / s.threads;
-  const uint64_t most = kSms * (per_sm ? per_sm : 1);
-  s.blocks = (unsigned)(units < most ? units : most);
-  return s;
-}
-
-// Partial sums of dgamma and dbeta that the backward pass leaves in the workspace.
-unsigned long_partials(const accept_layer_norm_params* p) { return (unsigned)(p->rows < 64 ? p->rows : 64); }
-
-uint64_t norm_partials(const accept_layer_norm_params* p) {
-  const NormShape s = norm_shape(p, true);
-  return s.longer ? long_partials(p) : s.blocks;
-}
-
-using KernelFn = void (*)(const NormArgs);
-
-template <typename TX, typename TY, bool WHOLE>
-KernelFn forward_for(const NormShape& s) {
-  if (s.one_warp) return s.octets == 1 ? accept::norm_forward_kernel<TX, TY, WHOLE, true, 1, 256> : accept::norm_forward_kernel<TX, TY, WHOLE, true, 2, 256>;
-  return s.octets == 1 ? accept::norm_forward_kernel<TX, TY, WHOLE, false, 1, 256>
-                       : s.threads <= 512 ? accept::norm_forward_kernel<TX, TY, WHOLE, false, 2, 512> : accept::norm_forward_kernel<TX, TY, WHOLE, false, 2, 1024>;
-}
-template <typename TX, typename TY, bool WHOLE>
-KernelFn backward_for(const NormShape& s) {
-  if (s.one_warp) return s.octets == 1 ? accept::norm_backward_kernel<TX, TY, WHOLE, true, 1, 256> : accept::norm_backward_kernel<TX, TY, WHOLE, true, 2, 256>;
-  return s.octets == 2 ? accept::norm_backward_kernel<TX, TY, WHOLE, false, 2, 256>
-                       : s.threads <= 256 ? accept::norm_backward_kernel<TX, TY, WHOLE, false, 1, 256> : accept::norm_backward_kernel<TX, TY, WHOLE, false, 1, 1024>;
-}
-
-struct Kernels { KernelFn one, sums; };
-
-template <typename TX, typename TY>
-Kernels kernels_for(const NormShape& s, bool backward, bool whole) {
-  if (s.longer) return backward ? Kernels{accept::norm_backward_long_kernel<TX, TY>, accept::norm_backward_long_sums_kernel<TX, TY>}
-                                : Kernels{accept::norm_forward_long_kernel<TX, TY>, nullptr};
-  if (backward) return {whole ? backward_for<TX, TY, true>(s) : backward_for<TX, TY, false>(s), nullptr};
-  return {whole ? forward_for<TX, TY, true>(s) : forward_for<TX, TY, false>(s), nullptr};
-}
-
-template <typename TX>
-Kernels kernels_for_y(const accept_layer_norm_params* p, const NormShape& s, bool backward, bool whole) {
-  switch (p->dtype_y) {
-    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, whole);
-    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, whole);
-    default: return kernels_for<TX, __half>(s, backward, whole);
-  }
-}
-
-Kernels select_kernels(const accept_layer_norm_params* p, const NormShape& s, bool backward, bool whole) {
-  switch (p->dtype_x) {
-    case ACCEPT_DTYPE_F32: return kernels_for_y<float>(p, s, backward, whole);
-    case ACCEPT_DTYPE_BF16: return kernels_for_y<__nv_bfloat16>(p, s, backward, whole);
-    default: return kernels_for_y<__half>(p, s, backward, whole);
-  }
-}
-
 size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
 bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF16 || d == ACCEPT_DTYPE_F16; }
 
 // rows that all start on 16-byte boundaries
 bool whole_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p, 16) && ld * value_size(dtype) % 16 == 0; }
+
+// Launch shape of a pass.  A row is shared by as many warps as hold it at 16 columns a thread; a block holds as many such
+// groups as fit 512 threads, fewer where there are too few rows for every SM, and fills shared memory with rows on their way.
+enum class NormPath { kRegisters, kWide, kLong };  // up to 8192 columns; up to 16384; more
+struct NormShape { NormPath path; unsigned warps, groups, stages, blocks; size_t shared; };
+
+constexpr size_t kNormShared = 200 * 1024;
+
+NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
+  NormShape s{};
+  const uint64_t warps = (p->cols + 32 * accept::kOwn - 1) / (32 * accept::kOwn);
+  if (warps > 32) {
+    s.path = NormPath::kLong;
+    s.blocks = (unsigned)(p->rows < kSms ? p->rows : kSms);
+    return s;
+  }
+  s.path = warps <= 16 ? NormPath::kRegisters : NormPath::kWide;
+  s.warps = (unsigned)warps;
+  const uint64_t spread = (p->rows + kSms - 1) / kSms, most = s.path == NormPath::kWide ? 1 : 16 / warps;
+  s.groups = (unsigned)(spread < most ? (spread ? spread : 1) : most);
+  const auto space = [&](int32_t dtype) {
+    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, 32 * s.warps, (uint32_t)p->cols)
+                                              : accept::row_space<uint16_t>(v, 32 * s.warps, (uint32_t)p->cols));
+  };
+  const size_t row = space(p->dtype_x) + (backward ? space(p->dtype_y) : 0);
+  while (s.groups > 1 && s.groups * row > kNormShared) --s.groups;
+  s.stages = 4;
+  while (s.stages > 1 && s.groups * s.stages * row > kNormShared) --s.stages;
+  s.shared = s.groups * s.stages * row;
+  // the groups of a block add up their column sums in the same memory
+  const size_t sums = backward && s.groups > 1 ? 2 * 4 * (size_t)accept::kOwn * 32 * s.warps : 0;
+  if (s.shared < sums) s.shared = sums;
+  const uint64_t units = (p->rows + s.groups - 1) / s.groups;
+  s.blocks = (unsigned)(units < kSms ? units : kSms);
+  return s;
+}
+
+// Partial sums of dgamma and dbeta that the backward pass leaves in the workspace: one for each block, or for each
+// slab of rows.
+constexpr unsigned kSlabs = 64;
+uint64_t norm_partials(const accept_layer_norm_params* p, const NormShape& s) {
+  return s.path == NormPath::kRegisters ? s.blocks : p->rows < kSlabs ? p->rows : kSlabs;
+}
+
+using KernelFn = void (*)(const NormArgs);
+struct Kernels { KernelFn rows, sums; };
+
+template <typename TX, typename TY, int V>
+KernelFn rows_kernel(NormPath path, bool backward) {
+  if (path == NormPath::kLong) return backward ? accept::norm_backward_long_kernel<TX, TY> : accept::norm_forward_long_kernel<TX, TY>;
+  if (path == NormPath::kWide)
+    return backward ? accept::norm_backward_kernel<TX, TY, V, false, 1024> : accept::norm_forward_kernel<TX, TY, V, 1024>;
+  return backward ? accept::norm_backward_kernel<TX, TY, V, true, 512> : accept::norm_forward_kernel<TX, TY, V, 512>;
+}
+
+template <typename TX, typename TY>
+Kernels kernels_for(NormPath path, bool backward, bool whole) {
+  constexpr int kUnit = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
+  return {whole ? rows_kernel<TX, TY, kUnit>(path, backward) : rows_kernel<TX, TY, 1>(path, backward), accept::norm_column_sums_kernel<TX, TY>};
+}
+
+template <typename TX>
+Kernels kernels_for_y(const accept_layer_norm_params* p, NormPath path, bool backward, bool whole) {
+  switch (p->dtype_y) {
+    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(path, backward, whole);
+    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(path, backward, whole);
+    default: return kernels_for<TX, __half>(path, backward, whole);
+  }
+}
+
+Kernels select_kernels(const accept_layer_norm_params* p, NormPath path, bool backward, bool whole) {
+  switch (p->dtype_x) {
+    case ACCEPT_DTYPE_F32: return kernels_for_y<float>(p, path, backward, whole);
+    case ACCEPT_DTYPE_BF16: return kernels_for_y<__nv_bfloat16>(p, path, backward, whole);
+    default: return kernels_for_y<__half>(p, path, backward, whole);
+  }
+}
+
+// Columns that a thread takes side by side where rows start on 16-byte boundaries (see column_of), else 1.
+int unit_of(const accept_layer_norm_params* p, bool whole) {
+  return !whole ? 1 : p->dtype_x == ACCEPT_DTYPE_F32 || p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 8;
+}
+
+cudaError_t launch_norm(KernelFn fn, const NormShape& shape, NormArgs& a, cudaStream_t s) {
+  a.warps = shape.warps;
+  a.stages = shape.stages;
+  const unsigned threads = shape.path == NormPath::kLong ? 1024 : 32 * shape.warps * shape.groups;
+  if (shape.shared > 32 * 1024) {  // with the static part, more than a kernel gets without asking
+    const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shape.shared);
+    if (err != cudaSuccess) return err;
+  }
+  return accept::launch_overlapped_shared(fn, dim3(shape.blocks), threads, shape.shared, s, a);
+}
 
 NormArgs norm_args(const accept_layer_norm_params* p) {
   NormArgs a{};
@@ -127,7 +147,8 @@ accept_status accept_layer_norm_check_params(const accept_layer_norm_params* p) 
 
 size_t accept_layer_norm_workspace_size(const accept_layer_norm_params* p) {
   if (accept_layer_norm_check_params(p) != ACCEPT_OK) return 0;
-  return 16 + (size_t)(norm_partials(p) * 8 * p->cols);
+  const NormShape s = norm_shape(p, true, 4);  // the partials depend on the rows and columns alone, not on their alignment
+  return 16 + (size_t)(norm_partials(p, s) * 8 * p->cols);
 }
 
 accept_status accept_layer_norm_forward(const accept_layer_norm_params* p, const void* d_x, const void* d_gamma,
@@ -153,10 +174,10 @@ accept_status accept_layer_norm_forward(const accept_layer_norm_params* p, const
                 bounds_list.add(d_gamma, p->cols * value_size(p->dtype_w), false);
                 bounds_list.add(d_beta, p->cols * value_size(p->dtype_w), false);
                 bounds_list.add(d_mean, 4 * p->rows, true); bounds_list.add(d_rstd, 4 * p->rows, true));
-  const NormShape shape = norm_shape(p, false);
   const bool whole = whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_y, p->ld_y, p->dtype_y);
-  const Kernels k = select_kernels(p, shape, false, whole);
-  ACCEPT_LAUNCH(launch_overlapped(k.one, dim3(shape.blocks), shape.threads, s, a));
+  a.whole_weights = is_aligned(d_gamma, 16) && is_aligned(d_beta, 16);
+  const NormShape shape = norm_shape(p, false, unit_of(p, whole));
+  ACCEPT_LAUNCH(launch_norm(select_kernels(p, shape.path, false, whole).rows, shape, a, s));
   return ACCEPT_OK;
 }
 
@@ -175,7 +196,8 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
       !is_aligned(d_dbeta, 4) || !is_aligned(d_ws, 16))
     return ACCEPT_ERR_MISALIGNED;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const NormShape shape = norm_shape(p, true);
+  const bool whole = whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_dy, p->ld_y, p->dtype_y) && is_aligned(d_dx, 16);
+  const NormShape shape = norm_shape(p, true, unit_of(p, whole));
   NormArgs a = norm_args(p);
   a.x = d_x;
   a.dy = d_dy;
@@ -184,7 +206,8 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
   a.rstd = d_rstd;
   a.dx = d_dx;
   a.partials = weights ? reinterpret_cast<float*>(static_cast<uint8_t*>(d_ws) + 16) : nullptr;
-  a.n_partials = (uint32_t)norm_partials(p);
+  a.n_partials = (uint32_t)norm_partials(p, shape);
+  a.whole_weights = is_aligned(d_gamma, 16);
   a.dgamma = d_dgamma;
   a.dbeta = d_dbeta;
   ACCEPT_BOUNDS(s, bounds_list.add(d_x, matrix_bytes(p->rows, p->cols, p->ld_x, p->dtype_x), false);
@@ -195,10 +218,10 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
                 bounds_list.add(d_dgamma, 4 * p->cols, true); bounds_list.add(d_dbeta, 4 * p->cols, true);
                 bounds_list.add(d_ws, accept_layer_norm_workspace_size(p), true));
   if (p->rows != 0) {
-    const bool whole = whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_dy, p->ld_y, p->dtype_y) && is_aligned(d_dx, 16);
-    const Kernels k = select_kernels(p, shape, true, whole);
-    if (!shape.longer || d_dx) ACCEPT_LAUNCH(launch_overlapped(k.one, dim3(shape.blocks), shape.threads, s, a));
-    if (shape.longer && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 255) / 256, a.n_partials), 256, s, a));
+    const Kernels k = select_kernels(p, shape.path, true, whole);
+    const bool apart = shape.path != NormPath::kRegisters;  // the sums over the rows are a pass of their own
+    if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
+    if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 127) / 128, a.n_partials), 128, s, a));
   }
   if (weights) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 256, s, a));
   return ACCEPT_OK;
