@@ -19,9 +19,18 @@ bool whole_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p
 // Launch shape of a pass.  A row is shared by as many warps as hold it at 16 columns a thread; a block holds as many such
 // groups as fit 512 threads, fewer where there are too few rows for every SM, and fills shared memory with rows on their way.
 enum class NormPath { kRegisters, kWide, kLong };  // up to 8192 columns; up to 16384; more
-struct NormShape { NormPath path; unsigned warps, groups, stages, blocks; size_t shared; };
+struct NormShape { NormPath path; unsigned warps, groups, blocks; size_t shared; };
 
-constexpr size_t kNormShared = 200 * 1024;
+// Rows of a group in shared memory.  A block of 512 threads holds 32 KB of an fp32 row's stage at most (64 KB backward):
+// three stages fit.  Rows of more than 8192 columns take twice that.
+template <typename TX, typename TY>
+constexpr int stages_of(NormPath path, bool backward) {
+  return path != NormPath::kWide || !backward ? 3 : 12 / (int)(sizeof(TX) + sizeof(TY));
+}
+int stages_of(const accept_layer_norm_params* p, NormPath path, bool backward) {
+  const int size = (p->dtype_x == ACCEPT_DTYPE_F32 ? 4 : 2) + (p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 2);
+  return path != NormPath::kWide || !backward ? 3 : 12 / size;
+}
 
 NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
   NormShape s{};
@@ -36,14 +45,10 @@ NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
   const uint64_t spread = (p->rows + kSms - 1) / kSms, most = s.path == NormPath::kWide ? 1 : 16 / warps;
   s.groups = (unsigned)(spread < most ? (spread ? spread : 1) : most);
   const auto space = [&](int32_t dtype) {
-    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, 32 * s.warps, (uint32_t)p->cols)
-                                              : accept::row_space<uint16_t>(v, 32 * s.warps, (uint32_t)p->cols));
+    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, s.warps, (uint32_t)p->cols)
+                                              : accept::row_space<uint16_t>(v, s.warps, (uint32_t)p->cols));
   };
-  const size_t row = space(p->dtype_x) + (backward ? space(p->dtype_y) : 0);
-  while (s.groups > 1 && s.groups * row > kNormShared) --s.groups;
-  s.stages = 4;
-  while (s.stages > 1 && s.groups * s.stages * row > kNormShared) --s.stages;
-  s.shared = s.groups * s.stages * row;
+  s.shared = s.groups * (size_t)stages_of(p, s.path, backward) * (space(p->dtype_x) + (backward ? space(p->dtype_y) : 0));
   // the groups of a block add up their column sums in the same memory
   const size_t sums = backward && s.groups > 1 ? 2 * 4 * (size_t)accept::kOwn * 32 * s.warps : 0;
   if (s.shared < sums) s.shared = sums;
@@ -62,26 +67,32 @@ uint64_t norm_partials(const accept_layer_norm_params* p, const NormShape& s) {
 using KernelFn = void (*)(const NormArgs);
 struct Kernels { KernelFn rows, sums; };
 
-template <typename TX, typename TY, int V>
+template <typename TX, typename TY, int V, bool FULL>
 KernelFn rows_kernel(NormPath path, bool backward) {
+  constexpr NormPath kReg = NormPath::kRegisters, kWide = NormPath::kWide;
   if (path == NormPath::kLong) return backward ? accept::norm_backward_long_kernel<TX, TY> : accept::norm_forward_long_kernel<TX, TY>;
-  if (path == NormPath::kWide)
-    return backward ? accept::norm_backward_kernel<TX, TY, V, false, 1024> : accept::norm_forward_kernel<TX, TY, V, 1024>;
-  return backward ? accept::norm_backward_kernel<TX, TY, V, true, 512> : accept::norm_forward_kernel<TX, TY, V, 512>;
+  if (path == kWide)
+    return backward ? accept::norm_backward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kWide, true), false, 1024>
+                    : accept::norm_forward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kWide, false), 1024>;
+  return backward ? accept::norm_backward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kReg, true), true, 512>
+                  : accept::norm_forward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kReg, false), 512>;
 }
 
+// whole: rows start on 16-byte boundaries; full: 512 columns for each warp
 template <typename TX, typename TY>
-Kernels kernels_for(NormPath path, bool backward, bool whole) {
+Kernels kernels_for(NormPath path, bool backward, bool whole, bool full) {
   constexpr int kUnit = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
-  return {whole ? rows_kernel<TX, TY, kUnit>(path, backward) : rows_kernel<TX, TY, 1>(path, backward), accept::norm_column_sums_kernel<TX, TY>};
+  return {!whole ? rows_kernel<TX, TY, 1, false>(path, backward)
+          : full ? rows_kernel<TX, TY, kUnit, true>(path, backward) : rows_kernel<TX, TY, kUnit, false>(path, backward),
+          accept::norm_column_sums_kernel<TX, TY>};
 }
 
 template <typename TX>
 Kernels kernels_for_y(const accept_layer_norm_params* p, NormPath path, bool backward, bool whole) {
   switch (p->dtype_y) {
-    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(path, backward, whole);
-    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(path, backward, whole);
-    default: return kernels_for<TX, __half>(path, backward, whole);
+    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(path, backward, whole, p->cols % 512 == 0);
+    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(path, backward, whole, p->cols % 512 == 0);
+    default: return kernels_for<TX, __half>(path, backward, whole, p->cols % 512 == 0);
   }
 }
 
@@ -100,7 +111,6 @@ int unit_of(const accept_layer_norm_params* p, bool whole) {
 
 cudaError_t launch_norm(KernelFn fn, const NormShape& shape, NormArgs& a, cudaStream_t s) {
   a.warps = shape.warps;
-  a.stages = shape.stages;
   const unsigned threads = shape.path == NormPath::kLong ? 1024 : 32 * shape.warps * shape.groups;
   if (shape.shared > 32 * 1024) {  // with the static part, more than a kernel gets without asking
     const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shape.shared);

@@ -27,20 +27,29 @@ struct NormArgs {
   uint32_t cols;
   uint32_t n_partials;
   uint32_t warps;        // that share a row
-  uint32_t stages;       // rows of a group in shared memory
   float eps, inv_cols;
   int dtype_w;
   int whole_weights;     // gamma and beta start on 16-byte boundaries
 };
 
-constexpr int kOwn = 16;  // columns of a row that a thread holds
+constexpr int kOwn = 16;         // columns of a row that a thread holds
+constexpr int kPairs = kOwn / 2;
 
-// How the columns of a row lie over the threads that share it: units of V neighbours, thread t holding units t, t + T, ...
-// V = 8 where both tensors are 16-bit types, 4 where one is fp32 (16 bytes at most for a thread, neighbours side by side),
-// 1 where rows do not start on 16-byte boundaries.
+// How the columns of a row lie over the threads that share it: a warp holds 512 neighbours, as units of V neighbours dealt
+// over its lanes, so that all addresses of a thread are one base and constants.  V = 8 where both tensors are 16-bit types,
+// 4 where one is fp32 (16 bytes at most for a thread, neighbours side by side), 1 where rows do not start on 16-byte
+// boundaries.
 template <int V>
-__device__ __forceinline__ uint32_t column_of(uint32_t t, uint32_t threads, int own) {
-  return V * (t + own / V * threads) + own % V;
+__device__ __forceinline__ uint32_t column_of(uint32_t t, int own) {
+  return (t >> 5) * (32 * kOwn) + V * (t & 31) + own / V * (32 * V) + own % V;
+}
+// Which of the thread's columns exist, a bit for each.
+template <int V>
+__device__ __forceinline__ uint32_t columns_mask(uint32_t t, uint32_t cols) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) m |= column_of<V>(t, i) < cols ? 1u << i : 0u;
+  return m;
 }
 
 template <int BYTES>
@@ -49,39 +58,47 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, uint32
   if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if (!bounds_ok(src, BYTES, false)) return;
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copy_wait(uint32_t pending) {  // all but the last `pending` groups have landed
-  switch (pending) {
-    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
-    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
-    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
-    default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
-  }
-}
+template <int PENDING>  // all but the last PENDING groups have landed
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
-// Bytes of shared memory that a row of T takes for `threads` threads (V = 1: the 16-byte pieces that hold it).
+// Bytes of shared memory that a row of T takes for `warps` warps (V = 1: the 16-byte pieces that hold it).
 template <typename T>
-__host__ __device__ constexpr uint32_t row_space(int v, uint32_t threads, uint32_t cols) {
-  return v > 1 ? threads * kOwn * (uint32_t)sizeof(T) : (cols * (uint32_t)sizeof(T) + 30) / 16 * 16;
+__host__ __device__ constexpr uint32_t row_space(int v, uint32_t warps, uint32_t cols) {
+  return v > 1 ? warps * 32 * kOwn * (uint32_t)sizeof(T) : (cols * (uint32_t)sizeof(T) + 30) / 16 * 16;
 }
 
-// Starts the copies of a row into `dst`.  `begin` and `end` bound the bytes of the matrix.
-template <typename T, int V>
+// Starts the copies of a row into `dst` (shared).  `begin` and `end` bound the values of the matrix; FULL: all columns of
+// every thread exist.
+template <typename T, int V, bool FULL>
 __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, uint32_t threads, const T* begin, const T* end) {
   if (V > 1) {
     constexpr int kBytes = V * (int)sizeof(T) < 16 ? 8 : 16;
-    constexpr int kCopies = V * (int)sizeof(T) / kBytes;  // of a unit: one, but for V = 8 of fp32, which does not occur
-    static_assert(kCopies == 1 || V == 1, "a unit is one copy");
+    static_assert(V == 1 || V * (int)sizeof(T) == kBytes, "a unit is one copy");
+    const uint32_t first = column_of<V>(t, 0);
+    const uint32_t to = dst + first * (uint32_t)sizeof(T);
+    const T* from = row + first;
 #pragma unroll
     for (int i = 0; i < kOwn / V; ++i) {
-      const uint32_t c = V * (t + i * threads);
-      const uint32_t bytes = c < cols ? min(cols - c, (uint32_t)V) * (uint32_t)sizeof(T) : 0;
-      copy_async<kBytes>(dst + (i * threads + t) * kBytes, row + (bytes ? c : 0), bytes);
+      if (FULL) {
+        copy_async<kBytes>(to + i * 32 * kBytes, from + i * 32 * V);
+      } else {
+        const uint32_t c = first + i * 32 * V;
+        const uint32_t bytes = c < cols ? min(cols - c, (uint32_t)V) * (uint32_t)sizeof(T) : 0;
+        copy_async<kBytes>(to + i * 32 * kBytes, bytes ? from + i * 32 * V : row, bytes);
+      }
     }
   } else {
     // the 16-byte pieces that hold the row; what lies outside the matrix is not read
     const uintptr_t from = reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15, to = reinterpret_cast<uintptr_t>(row + cols);
-    for (uint32_t i = t; from + 16ull * i < to; i += threads) {
+    const uint32_t pieces = (uint32_t)((to - from + 15) / 16);
+    for (uint32_t i = t; i < pieces; i += threads) {
       const uintptr_t at = from + 16ull * i;
       if (at >= reinterpret_cast<uintptr_t>(begin)) {
         const uint64_t left = reinterpret_cast<uintptr_t>(end) - at;
@@ -105,58 +122,72 @@ __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t c
   }
 }
 
-// Takes a row that has landed at `src` into registers; columns past the last are zero.
+// Takes a row that has landed at `src` (shared) into registers; columns that do not exist are zero.
 template <typename T, int V>
-__device__ __forceinline__ void take_row(const uint8_t* src, const T* row, uint32_t cols, uint32_t t, uint32_t threads, float (&v)[kOwn]) {
+__device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, uint32_t mask, float2 (&v)[kPairs]) {
   if (V > 1) {
+    const uint32_t from = src + column_of<V>(t, 0) * (uint32_t)sizeof(T);
 #pragma unroll
     for (int i = 0; i < kOwn / V; ++i) {
-      T w[V];
-      if (V * sizeof(T) == 16) {
-        const uint4 raw = *reinterpret_cast<const uint4*>(src + (i * threads + t) * 16);
-        memcpy(w, &raw, sizeof(w));
-      } else {
-        const uint2 raw = *reinterpret_cast<const uint2*>(src + (i * threads + t) * 8);
-        memcpy(w, &raw, sizeof(w));
-      }
+      uint32_t w[4] = {0, 0, 0, 0};
+      if (V * sizeof(T) == 16)
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from + i * 32 * 16));
+      else
+        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from + i * 32 * 8));
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[V * i + j] = to_float(w[j]);
+      for (int j = 0; j < V / 2; ++j) {
+        if constexpr (sizeof(T) == 4) v[(V * i / 2 + j) % kPairs] = make_float2(__uint_as_float(w[(2 * j) % 4]), __uint_as_float(w[(2 * j + 1) % 4]));
+        else v[(V * i / 2 + j) % kPairs] = word_to_pair<T>(w[j % 4]);
+      }
     }
   } else {
-    const T* p = reinterpret_cast<const T*>(src + (reinterpret_cast<uintptr_t>(row) & 15));
+    const uint32_t from = src + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + column_of<V>(t, 0) * (uint32_t)sizeof(T);
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
-      const uint32_t c = t + i * threads;
-      v[i] = c < cols ? to_float(p[c]) : 0.0f;
+      float f = 0.0f;
+      if (mask >> i & 1) {
+        if constexpr (sizeof(T) == 4) {
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(from + i * 32 * 4));
+        } else {
+          uint16_t w;
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(from + i * 32 * 2));
+          T h;
+          memcpy(&h, &w, 2);
+          f = to_float(h);
+        }
+      }
+      if (i % 2) v[i / 2].y = f;
+      else v[i / 2].x = f;
     }
   }
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void store_row(T* row, uint32_t cols, uint32_t t, uint32_t threads, const float (&v)[kOwn]) {
+template <typename T, int V, bool FULL>
+__device__ __forceinline__ void store_row(T* row, uint32_t t, uint32_t mask, const float2 (&v)[kPairs]) {
+  T* to = row + column_of<V>(t, 0);
 #pragma unroll
   for (int i = 0; i < kOwn / V; ++i) {
-    const uint32_t c = V * (t + i * threads);
-    if (V > 1 && c + V <= cols) {
+    constexpr uint32_t kUnit = (1u << V) - 1;
+    T* p = to + i * 32 * V;
+    if (V > 1 && (FULL || (mask >> (V * i) & kUnit) == kUnit)) {
+      uint32_t w[4];
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) {
+        const float2 f = v[(V * i / 2 + j) % kPairs];
+        if constexpr (sizeof(T) == 4) { w[(2 * j) % 4] = __float_as_uint(f.x); w[(2 * j + 1) % 4] = __float_as_uint(f.y); }
+        else w[j % 4] = pair_to_word<T>(f);
+      }
       if (V * sizeof(T) == 16) {
-        T w[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[j] = from_float<T>(v[V * i + j]);
-        uint4 raw;
-        memcpy(&raw, w, 16);
-        if (bounds_ok(row + c, 16, true)) __stcs(reinterpret_cast<uint4*>(row + c), raw);
+        if (bounds_ok(p, 16, true)) __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
       } else {
-        T w[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) w[j] = from_float<T>(v[V * i + j]);
-        uint2 raw;
-        memcpy(&raw, w, 8);
-        if (bounds_ok(row + c, 8, true)) __stcs(reinterpret_cast<uint2*>(row + c), raw);
+        if (bounds_ok(p, 8, true)) __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (c + j < cols) st_c(row + c + j, from_float<T>(v[V * i + j]));
+      for (int j = 0; j < V; ++j) {
+        const float2 f = v[(V * i + j) / 2];
+        if (mask >> (V * i + j) & 1) st_c(p + j, from_float<T>((V * i + j) % 2 ? f.y : f.x));
+      }
     }
   }
 }
@@ -171,37 +202,33 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, float absen
 
 // gamma or beta for this thread's columns: read once for all rows that it takes.
 template <int V>
-__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, float absent, uint32_t t, uint32_t threads, float (&v)[kOwn]) {
+__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, float absent, uint32_t t, float2 (&v)[kPairs]) {
 #pragma unroll
   for (int i = 0; i < kOwn; i += V) {
-    const uint32_t c = column_of<V>(t, threads, i);
+    const uint32_t c = column_of<V>(t, i);
     if (V > 1 && w && a.whole_weights && c + V <= a.cols) {
-      if (a.dtype_w == kF32) {
 #pragma unroll
-        for (int j = 0; j < V; j += 4) {
+      for (int j = 0; j < V; j += 4) {
+        float2 lo, hi;
+        if (a.dtype_w == kF32) {
           const float4 f = ld_c(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c + j));
-          v[i + j] = f.x; v[(i + j + 1) % kOwn] = f.y; v[(i + j + 2) % kOwn] = f.z; v[(i + j + 3) % kOwn] = f.w;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < V; j += 4) {
+          lo = make_float2(f.x, f.y);
+          hi = make_float2(f.z, f.w);
+        } else {
           const uint2 raw = ld_c(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(w) + c + j));
-          if (a.dtype_w == kBf16) {
-            __nv_bfloat16 h[4];
-            memcpy(h, &raw, 8);
-#pragma unroll
-            for (int l = 0; l < 4; ++l) v[(i + j + l) % kOwn] = to_float(h[l]);
-          } else {
-            __half h[4];
-            memcpy(h, &raw, 8);
-#pragma unroll
-            for (int l = 0; l < 4; ++l) v[(i + j + l) % kOwn] = to_float(h[l]);
-          }
+          lo = a.dtype_w == kBf16 ? word_to_pair<__nv_bfloat16>(raw.x) : word_to_pair<__half>(raw.x);
+          hi = a.dtype_w == kBf16 ? word_to_pair<__nv_bfloat16>(raw.y) : word_to_pair<__half>(raw.y);
         }
+        v[(i + j) / 2 % kPairs] = lo;
+        v[((i + j) / 2 + 1) % kPairs] = hi;
       }
     } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[i + j] = c + j < a.cols ? weight_at(w, a.dtype_w, absent, c + j) : absent;
+      for (int j = 0; j < V; ++j) {
+        const float f = c + j < a.cols ? weight_at(w, a.dtype_w, absent, c + j) : absent;
+        if ((i + j) % 2) v[(i + j) / 2].y = f;
+        else v[(i + j) / 2].x = f;
+      }
     }
   }
 }
@@ -223,164 +250,227 @@ struct Group {
     if (warps == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(threads) : "memory");
   }
-  // Sum over the group; `slot` holds a value of each warp and is used in turn with another (a barrier lies between).
+  // Sum over the group.  `slot`: 32 floats of the group, zero past its warps, used in turn with others (a barrier lies
+  // between two uses); every thread adds the warps' values up for itself.
   __device__ __forceinline__ float sum(float v, float* slot) const {
     v = warp_sum(v);
     if (warps == 1) return v;
     if ((t & 31) == 0) slot[t >> 5] = v;
     sync();
-    return warp_sum((t & 31) < warps ? slot[t & 31] : 0.0f);
+    float4 s = *reinterpret_cast<const float4*>(slot);
+    for (uint32_t w = 4; w < warps; w += 4) {
+      const float4 m = *reinterpret_cast<const float4*>(slot + w);
+      s.x += m.x; s.y += m.y; s.z += m.z; s.w += m.w;
+    }
+    return (s.x + s.y) + (s.z + s.w);
+  }
+  // Two sums with one barrier: after the first exchange the lower half of a warp adds up one of them, the upper half the
+  // other.  `slot`: 64 floats, pairs of both.
+  __device__ __forceinline__ float2 sum_two(float2 v, float* slot) const {
+    const bool upper = (t & 16) != 0;
+    float mine = upper ? v.y : v.x;
+    mine += __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, 16);
+#pragma unroll
+    for (int d = 8; d >= 1; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
+    if (warps == 1) {
+      const float other = __shfl_xor_sync(0xffffffffu, mine, 16);
+      return upper ? make_float2(other, mine) : make_float2(mine, other);
+    }
+    if ((t & 15) == 0) slot[t >> 4] = mine;
+    sync();
+    float4 s = *reinterpret_cast<const float4*>(slot);
+    for (uint32_t w = 2; w < warps; w += 2) {
+      const float4 m = *reinterpret_cast<const float4*>(slot + 2 * w);
+      s.x += m.x; s.y += m.y; s.z += m.z; s.w += m.w;
+    }
+    return make_float2(s.x + s.z, s.y + s.w);
   }
 };
+
+constexpr int kMostGroups = 16;
 
 extern __shared__ __align__(16) uint8_t norm_shared[];
 
 // Forward.  The mean first, then the sum of the squared distances from it, so that an offset much larger than the spread
 // costs no digits.
-template <typename TX, typename TY, int V, int MAX_THREADS>
+template <typename TX, typename TY, int V, bool FULL, int STAGES, int MAX_THREADS>
 __global__ void __launch_bounds__(MAX_THREADS) norm_forward_kernel(const NormArgs a) {
-  __shared__ float slots[2][32];
+  __shared__ __align__(16) float slots[kMostGroups][2][32];
   const Group g(a.warps);
   const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space = row_space<TX>(V, threads, a.cols);
-  const uint32_t offset = g.index * a.stages * space, shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + offset;
+  const uint32_t space = row_space<TX>(V, a.warps, a.cols);
+  const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space, shared_end = shared + STAGES * space;
+  const uint32_t mask = FULL ? 0 : columns_mask<V>(t, a.cols);
   const TX* x = static_cast<const TX*>(a.x);
   const TX* end = x + (a.rows - 1) * a.ld_x + a.cols;
-  const uint64_t first = (uint64_t)blockIdx.x * groups + g.index, step = (uint64_t)gridDim.x * groups;
+  const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
+  const uint32_t step = gridDim.x * groups;
+  if (a.warps > 1) {
+    float* zero = &slots[g.index][0][0];
+    for (uint32_t i = t; i < 64; i += threads) zero[i] = 0.0f;
+    g.sync();
+  }
   grid_dependency_handshake();
-  for (uint32_t s = 0; s + 1 < a.stages; ++s) {
-    const uint64_t r = first + s * step;
-    if (r < a.rows) start_row<TX, V>(shared + s * space, x + r * a.ld_x, a.cols, t, threads, x, end);
+  if (first >= a.rows) return;
+  const TX* row = x + first * a.ld_x;
+  TY* out = static_cast<TY*>(a.y) + first * a.ld_y;
+  const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
+#pragma unroll
+  for (int s = 0; s + 1 < STAGES; ++s) {
+    if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL>(shared + s * space, row + s * stride_x, a.cols, t, threads, x, end);
     copy_commit();
   }
-  float gamma[kOwn], beta[kOwn];
-  load_weights<V>(a, a.gamma, 1.0f, t, threads, gamma);
-  load_weights<V>(a, a.beta, 0.0f, t, threads, beta);
-  float* slot = slots[0] + g.index * a.warps;
-  uint32_t stage = 0;
-  for (uint64_t r = first; r < a.rows; r += step) {
-    const uint64_t ahead = r + (a.stages - 1) * step;
-    const uint32_t into = stage == 0 ? a.stages - 1 : stage - 1;  // where the row before lay (or this one, with one stage)
-    if (ahead < a.rows) start_row<TX, V>(shared + into * space, x + ahead * a.ld_x, a.cols, t, threads, x, end);
+  float2 gamma[kPairs], beta[kPairs];
+  load_weights<V>(a, a.gamma, 1.0f, t, gamma);
+  load_weights<V>(a, a.beta, 0.0f, t, beta);
+  uint32_t here = shared, ahead = shared + (STAGES - 1) * space;  // where this row lies, and where the one to start goes
+  uint64_t left = a.rows - first;                                 // rows from this one on
+  for (uint64_t r = first;; r += step) {
+    if (left > (uint64_t)(STAGES - 1) * step) start_row<TX, V, FULL>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, x, end);
     copy_commit();
-    copy_wait(a.stages - 1);
+    copy_wait<STAGES - 1>();
     if (V == 1) g.sync();
-    float v[kOwn];
-    take_row<TX, V>(norm_shared + offset + stage * space, x + r * a.ld_x, a.cols, t, threads, v);
-    stage = stage + 1 == a.stages ? 0 : stage + 1;
-    float sum = 0.0f;
+    float2 v[kPairs];
+    take_row<TX, V>(here, row, t, mask, v);
+    const float2 sum = add2(add2(add2(v[0], v[1]), add2(v[2], v[3])), add2(add2(v[4], v[5]), add2(v[6], v[7])));
+    const float mean = g.sum(sum.x + sum.y, slots[g.index][0]) * a.inv_cols;
+    float2 squares[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) sum += v[i];
-    const float mean = g.sum(sum, slot) * a.inv_cols;
-    float squares = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      v[i] = column_of<V>(t, threads, i) < a.cols ? v[i] - mean : 0.0f;
-      squares = fmaf(v[i], v[i], squares);
+    for (int i = 0; i < kPairs; ++i) {
+      v[i] = add2(v[i], both(-mean));
+      if (!FULL) {
+        if (!(mask >> (2 * i) & 1)) v[i].x = 0.0f;
+        if (!(mask >> (2 * i + 1) & 1)) v[i].y = 0.0f;
+      }
+      squares[i % 2] = fma2(v[i], v[i], squares[i % 2]);
     }
-    const float rstd = 1.0f / sqrtf(g.sum(squares, slot + 32) * a.inv_cols + a.eps);
+    squares[0] = add2(squares[0], squares[1]);
+    const float rstd = rsqrtf(g.sum(squares[0].x + squares[0].y, slots[g.index][1]) * a.inv_cols + a.eps);
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) v[i] = fmaf(v[i] * rstd, gamma[i], beta[i]);
-    store_row<TY, V>(static_cast<TY*>(a.y) + r * a.ld_y, a.cols, t, threads, v);
-    if (t == 0 && a.mean_out) st_c(a.mean_out + r, mean);
-    if (t == 0 && a.rstd_out) st_c(a.rstd_out + r, rstd);
+    for (int i = 0; i < kPairs; ++i) v[i] = fma2(mul2(v[i], both(rstd)), gamma[i], beta[i]);
+    store_row<TY, V, FULL>(out, t, mask, v);
+    if (t == 0) {
+      if (a.mean_out) st_c(a.mean_out + r, mean);
+      if (a.rstd_out) st_c(a.rstd_out + r, rstd);
+    }
+    if (left <= step) break;
+    left -= step;
+    row += stride_x;
+    out += stride_y;
+    ahead = here;
+    here = here + space == shared_end ? shared : here + space;
   }
 }
 
 // Backward.  dx needs two sums of a row, taken together; the gradients of gamma and beta are sums over the rows (SUMS),
 // held in registers over all rows of a group, added up over the block's groups and joined by norm_join_kernel.
-template <typename TX, typename TY, int V, bool SUMS, int MAX_THREADS>
+template <typename TX, typename TY, int V, bool FULL, int STAGES, bool SUMS, int MAX_THREADS>
 __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormArgs a) {
-  __shared__ float slots[4][32];
+  constexpr int kSums = SUMS ? kPairs : 1;
+  __shared__ __align__(16) float slots[kMostGroups][2][64];
   const Group g(a.warps);
   const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space_x = row_space<TX>(V, threads, a.cols), space = space_x + row_space<TY>(V, threads, a.cols);
-  const uint32_t offset = g.index * a.stages * space, shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + offset;
+  const uint32_t space_x = row_space<TX>(V, a.warps, a.cols), space = space_x + row_space<TY>(V, a.warps, a.cols);
+  const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space, shared_end = shared + STAGES * space;
+  const uint32_t mask = FULL ? 0 : columns_mask<V>(t, a.cols);
   const TX* x = static_cast<const TX*>(a.x);
   const TY* dy = static_cast<const TY*>(a.dy);
   const TX* end_x = x + (a.rows - 1) * a.ld_x + a.cols;
   const TY* end_y = dy + (a.rows - 1) * a.ld_y + a.cols;
-  const uint64_t first = (uint64_t)blockIdx.x * groups + g.index, step = (uint64_t)gridDim.x * groups;
-  grid_dependency_handshake();
-  for (uint32_t s = 0; s + 1 < a.stages; ++s) {
-    const uint64_t r = first + s * step;
-    if (r < a.rows) {
-      start_row<TX, V>(shared + s * space, x + r * a.ld_x, a.cols, t, threads, x, end_x);
-      start_row<TY, V>(shared + s * space + space_x, dy + r * a.ld_y, a.cols, t, threads, dy, end_y);
-    }
-    copy_commit();
+  const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
+  const uint32_t step = gridDim.x * groups;
+  if (a.warps > 1) {
+    float* zero = &slots[g.index][0][0];
+    for (uint32_t i = t; i < 128; i += threads) zero[i] = 0.0f;
+    g.sync();
   }
-  float gamma[kOwn], dgamma[SUMS ? kOwn : 1], dbeta[SUMS ? kOwn : 1];
-  load_weights<V>(a, a.gamma, 1.0f, t, threads, gamma);
+  grid_dependency_handshake();
+  float2 gamma[kPairs], dgamma[kSums], dbeta[kSums];
 #pragma unroll
-  for (int i = 0; i < (SUMS ? kOwn : 1); ++i) dgamma[i] = dbeta[i] = 0.0f;
-  float* slot = slots[0] + g.index * a.warps;
-  uint32_t stage = 0;
-  for (uint64_t r = first; r < a.rows; r += step) {
-    const uint64_t ahead = r + (a.stages - 1) * step;
-    const uint32_t into = stage == 0 ? a.stages - 1 : stage - 1;
-    const float mean = ld_c(a.mean + r), rstd = ld_c(a.rstd + r);
-    if (ahead < a.rows) {
-      start_row<TX, V>(shared + into * space, x + ahead * a.ld_x, a.cols, t, threads, x, end_x);
-      start_row<TY, V>(shared + into * space + space_x, dy + ahead * a.ld_y, a.cols, t, threads, dy, end_y);
-    }
-    copy_commit();
-    copy_wait(a.stages - 1);
-    if (V == 1) g.sync();
-    float xhat[kOwn], h[kOwn];
-    const uint8_t* landed = norm_shared + offset + stage * space;
-    take_row<TX, V>(landed, x + r * a.ld_x, a.cols, t, threads, xhat);
-    take_row<TY, V>(landed + space_x, dy + r * a.ld_y, a.cols, t, threads, h);
-    stage = stage + 1 == a.stages ? 0 : stage + 1;
-    float sum = 0.0f, along = 0.0f;
+  for (int i = 0; i < kSums; ++i) dgamma[i] = dbeta[i] = both(0.0f);
+  if (first < a.rows) {
+    const TX* row = x + first * a.ld_x;
+    const TY* drow = dy + first * a.ld_y;
+    TX* out = static_cast<TX*>(a.dx) + first * a.ld_x;
+    const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
-      xhat[i] = (xhat[i] - mean) * rstd;  // columns past the last: dy = 0, so what stands here counts nowhere
-      if (SUMS) {
-        dbeta[i % kOwn] += h[i];
-        dgamma[i % kOwn] = fmaf(h[i], xhat[i], dgamma[i % kOwn]);
+    for (int s = 0; s + 1 < STAGES; ++s) {
+      if (first + (uint64_t)s * step < a.rows) {
+        start_row<TX, V, FULL>(shared + s * space, row + s * stride_x, a.cols, t, threads, x, end_x);
+        start_row<TY, V, FULL>(shared + s * space + space_x, drow + s * stride_y, a.cols, t, threads, dy, end_y);
       }
-      h[i] *= gamma[i];
-      sum += h[i];
-      along = fmaf(h[i], xhat[i], along);
+      copy_commit();
     }
-    if (!a.dx) {
-      if (V == 1) g.sync();  // the row has been read: its place is free
-      continue;
-    }
-    // both sums with one barrier; the two pairs of slots are used in turn
-    sum = warp_sum(sum);
-    along = warp_sum(along);
-    if (a.warps > 1) {
-      const uint32_t lane = t & 31;
-      if (lane == 0) { slot[t >> 5] = sum; slot[32 + (t >> 5)] = along; }
-      g.sync();
-      sum = warp_sum(lane < a.warps ? slot[lane] : 0.0f);
-      along = warp_sum(lane < a.warps ? slot[32 + lane] : 0.0f);
-      slot += slot >= slots[2] ? -64 : 64;
-    }
-    sum *= a.inv_cols;
-    along *= a.inv_cols;
+    load_weights<V>(a, a.gamma, 1.0f, t, gamma);
+    uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;
+    uint64_t left = a.rows - first;
+    const float* means = a.mean + first;
+    const float* rstds = a.rstd + first;
+    float mean_next = ld_c(means), rstd_next = ld_c(rstds);
+    for (;;) {
+      if (left > (uint64_t)(STAGES - 1) * step) {
+        start_row<TX, V, FULL>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, x, end_x);
+        start_row<TY, V, FULL>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, threads, dy, end_y);
+      }
+      copy_commit();
+      const float mean = mean_next, rstd = rstd_next;
+      if (left > step) { mean_next = ld_c(means += step); rstd_next = ld_c(rstds += step); }
+      copy_wait<STAGES - 1>();
+      if (V == 1) g.sync();
+      float2 xhat[kPairs], h[kPairs];
+      take_row<TX, V>(here, row, t, mask, xhat);
+      take_row<TY, V>(here + space_x, drow, t, mask, h);
+      float2 sum[2] = {both(0.0f), both(0.0f)}, along[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) h[i] = rstd * (h[i] - sum - xhat[i] * along);
-    store_row<TX, V>(static_cast<TX*>(a.dx) + r * a.ld_x, a.cols, t, threads, h);
+      for (int i = 0; i < kPairs; ++i) {
+        xhat[i] = mul2(add2(xhat[i], both(-mean)), both(rstd));  // columns that do not exist: dy = 0, so this counts nowhere
+        if (SUMS) {
+          dbeta[i % kSums] = add2(dbeta[i % kSums], h[i]);
+          dgamma[i % kSums] = fma2(h[i], xhat[i], dgamma[i % kSums]);
+        }
+        h[i] = mul2(h[i], gamma[i]);
+        sum[i % 2] = add2(sum[i % 2], h[i]);
+        along[i % 2] = fma2(h[i], xhat[i], along[i % 2]);
+      }
+      if (a.dx) {
+        sum[0] = add2(sum[0], sum[1]);
+        along[0] = add2(along[0], along[1]);
+        float2 s = g.sum_two(make_float2(sum[0].x + sum[0].y, along[0].x + along[0].y), slots[g.index][turn]);
+        turn ^= 1;
+        s = mul2(s, both(-a.inv_cols));
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) h[i] = mul2(fma2(xhat[i], both(s.y), add2(h[i], both(s.x))), both(rstd));
+        store_row<TX, V, FULL>(out, t, mask, h);
+      } else if (V == 1) {
+        g.sync();  // the row has been read: its place is free
+      }
+      if (left <= step) break;
+      left -= step;
+      row += stride_x;
+      drow += stride_y;
+      out += stride_x;
+      ahead = here;
+      here = here + space == shared_end ? shared : here + space;
+    }
   }
   if (!SUMS || !a.partials) return;
   float* out = a.partials + (uint64_t)blockIdx.x * 2 * a.cols;
   if (groups > 1) {  // the block's groups add up their columns one after the other
-    float* sums = reinterpret_cast<float*>(norm_shared);
-    copy_wait(0);
+    float2* sums = reinterpret_cast<float2*>(norm_shared);
+    copy_wait<0>();
     __syncthreads();
     for (uint32_t k = 0; k < groups; ++k) {
       if (g.index == k) {
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          float* p = sums + i * threads + t;  // a place of its own for each of the thread's columns
-          float* q = p + kOwn * threads;
-          dgamma[i % kOwn] = k ? *p + dgamma[i % kOwn] : dgamma[i % kOwn];
-          dbeta[i % kOwn] = k ? *q + dbeta[i % kOwn] : dbeta[i % kOwn];
-          *p = dgamma[i % kOwn];
-          *q = dbeta[i % kOwn];
+        for (int i = 0; i < kPairs; ++i) {
+          float2* p = sums + i * threads + t;  // a place of its own for each pair of the thread's columns
+          float2* q = p + kPairs * threads;
+          if (k) {
+            dgamma[i % kSums] = add2(*p, dgamma[i % kSums]);
+            dbeta[i % kSums] = add2(*q, dbeta[i % kSums]);
+          }
+          *p = dgamma[i % kSums];
+          *q = dbeta[i % kSums];
         }
       }
       __syncthreads();
@@ -389,8 +479,9 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
   }
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
-    const uint32_t c = column_of<V>(t, threads, i);
-    if (c < a.cols) { st_c(out + c, dgamma[i % kOwn]); st_c(out + a.cols + c, dbeta[i % kOwn]); }
+    const uint32_t c = column_of<V>(t, i);
+    const float2 d = dgamma[i / 2 % kSums], e = dbeta[i / 2 % kSums];
+    if (c < a.cols) { st_c(out + c, i % 2 ? d.y : d.x); st_c(out + a.cols + c, i % 2 ? e.y : e.x); }
   }
 }
 
