@@ -25,11 +25,11 @@ struct NormShape { NormPath path; unsigned warps, groups, blocks; size_t shared;
 // three stages fit.  Rows of more than 8192 columns take twice that.
 template <typename TX, typename TY>
 constexpr int stages_of(NormPath path, bool backward) {
-  return path != NormPath::kWide || !backward ? 3 : 12 / (int)(sizeof(TX) + sizeof(TY));
+  return !backward && path == NormPath::kRegisters ? 4 : path != NormPath::kWide || !backward ? 3 : 12 / (int)(sizeof(TX) + sizeof(TY));
 }
 int stages_of(const accept_layer_norm_params* p, NormPath path, bool backward) {
   const int size = (p->dtype_x == ACCEPT_DTYPE_F32 ? 4 : 2) + (p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 2);
-  return path != NormPath::kWide || !backward ? 3 : 12 / size;
+  return !backward && path == NormPath::kRegisters ? 4 : path != NormPath::kWide || !backward ? 3 : 12 / size;
 }
 
 NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
@@ -146,8 +146,8 @@ extern "C" {
 accept_status accept_layer_norm_check_params(const accept_layer_norm_params* p) {
   if (!p) return ACCEPT_ERR_NULL;
   if (p->cols == 0 || p->cols > 0x7fffffffull || p->ld_x < p->cols || p->ld_y < p->cols) return ACCEPT_ERR_BAD_SIZE;
-  // every offset of a value must be a 63-bit number of bytes
-  if (p->rows > (1ull << 40) || p->ld_x > (1ull << 40) || p->ld_y > (1ull << 40) ||
+  // every offset of a value must be a 63-bit number of bytes, and the turns of a group of threads a 31-bit number
+  if (p->rows > (1ull << 38) || p->ld_x > (1ull << 40) || p->ld_y > (1ull << 40) ||
       (p->rows && (p->ld_x > (1ull << 60) / p->rows || p->ld_y > (1ull << 60) / p->rows)))
     return ACCEPT_ERR_BAD_SIZE;
   if (!is_dtype(p->dtype_x) || !is_dtype(p->dtype_y) || !is_dtype(p->dtype_w)) return ACCEPT_ERR_BAD_ENUM;
@@ -233,7 +233,7 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
     if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
     if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 127) / 128, a.n_partials), 128, s, a));
   }
-  if (weights) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 256, s, a));
+  if (weights) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 32 * accept::kJoinWarps, s, a));
   return ACCEPT_OK;
 }
 

@@ -58,11 +58,12 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, uint32
   if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
-  if (!bounds_ok(src, BYTES, false)) return;
-  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+// With offsets from the two addresses that the instruction holds.
+template <int BYTES, int TO, int FROM>
+__device__ __forceinline__ void copy_async_at(uint32_t dst, const void* src) {
+  if (!bounds_ok(static_cast<const uint8_t*>(src) + FROM, BYTES, false)) return;
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0+%2], [%1+%3], 16;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0+%2], [%1+%3], 8;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM) : "memory");
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING>  // all but the last PENDING groups have landed
@@ -84,11 +85,17 @@ __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t c
     const uint32_t first = column_of<V>(t, 0);
     const uint32_t to = dst + first * (uint32_t)sizeof(T);
     const T* from = row + first;
+    if (FULL) {
+      constexpr int kTo = 32 * kBytes, kFrom = 32 * V * (int)sizeof(T);
+      copy_async_at<kBytes, 0, 0>(to, from);
+      copy_async_at<kBytes, kTo, kFrom>(to, from);
+      if constexpr (kOwn / V == 4) {
+        copy_async_at<kBytes, 2 * kTo, 2 * kFrom>(to, from);
+        copy_async_at<kBytes, 3 * kTo, 3 * kFrom>(to, from);
+      }
+    } else {
 #pragma unroll
-    for (int i = 0; i < kOwn / V; ++i) {
-      if (FULL) {
-        copy_async<kBytes>(to + i * 32 * kBytes, from + i * 32 * V);
-      } else {
+      for (int i = 0; i < kOwn / V; ++i) {
         const uint32_t c = first + i * 32 * V;
         const uint32_t bytes = c < cols ? min(cols - c, (uint32_t)V) * (uint32_t)sizeof(T) : 0;
         copy_async<kBytes>(to + i * 32 * kBytes, bytes ? from + i * 32 * V : row, bytes);
@@ -122,26 +129,39 @@ __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t c
   }
 }
 
+// Unit I of the thread from shared memory.
+template <typename T, int V, int I>
+__device__ __forceinline__ void take_unit(uint32_t from, Pair (&v)[kPairs]) {
+  constexpr int kFirst = V * I / 2;
+  if constexpr (sizeof(T) == 4) {
+    asm volatile("ld.shared.v2.u64 {%0,%1}, [%2+%3];" : "=l"(v[kFirst % kPairs]), "=l"(v[(kFirst + 1) % kPairs]) : "r"(from), "n"(I * 32 * 16));
+  } else if constexpr (V == 8) {
+    uint32_t w[4];
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+%5];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from), "n"(I * 32 * 16));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[(kFirst + j) % kPairs] = word_to_pair<T>(w[j]);
+  } else {
+    uint32_t w[2];
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2+%3];" : "=r"(w[0]), "=r"(w[1]) : "r"(from), "n"(I * 32 * 8));
+    v[kFirst % kPairs] = word_to_pair<T>(w[0]);
+    v[(kFirst + 1) % kPairs] = word_to_pair<T>(w[1]);
+  }
+}
+
 // Takes a row that has landed at `src` (shared) into registers; columns that do not exist are zero.
 template <typename T, int V>
-__device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, uint32_t mask, float2 (&v)[kPairs]) {
+__device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, uint32_t mask, Pair (&v)[kPairs]) {
   if (V > 1) {
     const uint32_t from = src + column_of<V>(t, 0) * (uint32_t)sizeof(T);
-#pragma unroll
-    for (int i = 0; i < kOwn / V; ++i) {
-      uint32_t w[4] = {0, 0, 0, 0};
-      if (V * sizeof(T) == 16)
-        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from + i * 32 * 16));
-      else
-        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(from + i * 32 * 8));
-#pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        if constexpr (sizeof(T) == 4) v[(V * i / 2 + j) % kPairs] = make_float2(__uint_as_float(w[(2 * j) % 4]), __uint_as_float(w[(2 * j + 1) % 4]));
-        else v[(V * i / 2 + j) % kPairs] = word_to_pair<T>(w[j % 4]);
-      }
+    take_unit<T, V, 0>(from, v);
+    take_unit<T, V, 1>(from, v);
+    if constexpr (kOwn / V == 4) {
+      take_unit<T, V, 2>(from, v);
+      take_unit<T, V, 3>(from, v);
     }
   } else {
     const uint32_t from = src + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + column_of<V>(t, 0) * (uint32_t)sizeof(T);
+    float lo = 0.0f;
 #pragma unroll
     for (int i = 0; i < kOwn; ++i) {
       float f = 0.0f;
@@ -156,14 +176,14 @@ __device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t,
           f = to_float(h);
         }
       }
-      if (i % 2) v[i / 2].y = f;
-      else v[i / 2].x = f;
+      if (i % 2) v[i / 2] = pair_of(lo, f);
+      else lo = f;
     }
   }
 }
 
 template <typename T, int V, bool FULL>
-__device__ __forceinline__ void store_row(T* row, uint32_t t, uint32_t mask, const float2 (&v)[kPairs]) {
+__device__ __forceinline__ void store_row(T* row, uint32_t t, uint32_t mask, const Pair (&v)[kPairs]) {
   T* to = row + column_of<V>(t, 0);
 #pragma unroll
   for (int i = 0; i < kOwn / V; ++i) {
@@ -173,8 +193,8 @@ __device__ __forceinline__ void store_row(T* row, uint32_t t, uint32_t mask, con
       uint32_t w[4];
 #pragma unroll
       for (int j = 0; j < V / 2; ++j) {
-        const float2 f = v[(V * i / 2 + j) % kPairs];
-        if constexpr (sizeof(T) == 4) { w[(2 * j) % 4] = __float_as_uint(f.x); w[(2 * j + 1) % 4] = __float_as_uint(f.y); }
+        const Pair f = v[(V * i / 2 + j) % kPairs];
+        if constexpr (sizeof(T) == 4) { w[(2 * j) % 4] = __float_as_uint(split(f).x); w[(2 * j + 1) % 4] = __float_as_uint(split(f).y); }
         else w[j % 4] = pair_to_word<T>(f);
       }
       if (V * sizeof(T) == 16) {
@@ -185,7 +205,7 @@ __device__ __forceinline__ void store_row(T* row, uint32_t t, uint32_t mask, con
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float2 f = v[(V * i + j) / 2];
+        const float2 f = split(v[(V * i + j) / 2]);
         if (mask >> (V * i + j) & 1) st_c(p + j, from_float<T>((V * i + j) % 2 ? f.y : f.x));
       }
     }
@@ -202,18 +222,18 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, float absen
 
 // gamma or beta for this thread's columns: read once for all rows that it takes.
 template <int V>
-__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, float absent, uint32_t t, float2 (&v)[kPairs]) {
+__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, float absent, uint32_t t, Pair (&v)[kPairs]) {
 #pragma unroll
   for (int i = 0; i < kOwn; i += V) {
     const uint32_t c = column_of<V>(t, i);
     if (V > 1 && w && a.whole_weights && c + V <= a.cols) {
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
-        float2 lo, hi;
+        Pair lo, hi;
         if (a.dtype_w == kF32) {
           const float4 f = ld_c(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c + j));
-          lo = make_float2(f.x, f.y);
-          hi = make_float2(f.z, f.w);
+          lo = pair_of(f.x, f.y);
+          hi = pair_of(f.z, f.w);
         } else {
           const uint2 raw = ld_c(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(w) + c + j));
           lo = a.dtype_w == kBf16 ? word_to_pair<__nv_bfloat16>(raw.x) : word_to_pair<__half>(raw.x);
@@ -226,8 +246,8 @@ __device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, f
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float f = c + j < a.cols ? weight_at(w, a.dtype_w, absent, c + j) : absent;
-        if ((i + j) % 2) v[(i + j) / 2].y = f;
-        else v[(i + j) / 2].x = f;
+        if ((i + j) % 2) v[(i + j) / 2] = pair_of(split(v[(i + j) / 2]).x, f);
+        else v[(i + j) / 2] = both(f);
       }
     }
   }
@@ -258,7 +278,9 @@ struct Group {
     if ((t & 31) == 0) slot[t >> 5] = v;
     sync();
     float4 s = *reinterpret_cast<const float4*>(slot);
-    for (uint32_t w = 4; w < warps; w += 4) {
+#pragma unroll
+    for (uint32_t w = 4; w < 32; w += 4) {
+      if (w >= warps) break;
       const float4 m = *reinterpret_cast<const float4*>(slot + w);
       s.x += m.x; s.y += m.y; s.z += m.z; s.w += m.w;
     }
@@ -279,7 +301,9 @@ struct Group {
     if ((t & 15) == 0) slot[t >> 4] = mine;
     sync();
     float4 s = *reinterpret_cast<const float4*>(slot);
-    for (uint32_t w = 2; w < warps; w += 2) {
+#pragma unroll
+    for (uint32_t w = 2; w < 32; w += 2) {
+      if (w >= warps) break;
       const float4 m = *reinterpret_cast<const float4*>(slot + 2 * w);
       s.x += m.x; s.y += m.y; s.z += m.z; s.w += m.w;
     }
@@ -320,41 +344,40 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_forward_kernel(const NormArg
     if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL>(shared + s * space, row + s * stride_x, a.cols, t, threads, x, end);
     copy_commit();
   }
-  float2 gamma[kPairs], beta[kPairs];
+  Pair gamma[kPairs], beta[kPairs];
   load_weights<V>(a, a.gamma, 1.0f, t, gamma);
   load_weights<V>(a, a.beta, 0.0f, t, beta);
   uint32_t here = shared, ahead = shared + (STAGES - 1) * space;  // where this row lies, and where the one to start goes
-  uint64_t left = a.rows - first;                                 // rows from this one on
-  for (uint64_t r = first;; r += step) {
-    if (left > (uint64_t)(STAGES - 1) * step) start_row<TX, V, FULL>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, x, end);
+  uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);  // rows of this group from this one on
+  float* mean_out = a.mean_out && t == 0 ? a.mean_out + first : nullptr;
+  float* rstd_out = a.rstd_out && t == 0 ? a.rstd_out + first : nullptr;
+  for (;;) {
+    if (left > STAGES - 1) start_row<TX, V, FULL>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, x, end);
     copy_commit();
     copy_wait<STAGES - 1>();
     if (V == 1) g.sync();
-    float2 v[kPairs];
+    Pair v[kPairs];
     take_row<TX, V>(here, row, t, mask, v);
-    const float2 sum = add2(add2(add2(v[0], v[1]), add2(v[2], v[3])), add2(add2(v[4], v[5]), add2(v[6], v[7])));
-    const float mean = g.sum(sum.x + sum.y, slots[g.index][0]) * a.inv_cols;
-    float2 squares[2] = {both(0.0f), both(0.0f)};
+    const Pair sum = add2(add2(add2(v[0], v[1]), add2(v[2], v[3])), add2(add2(v[4], v[5]), add2(v[6], v[7])));
+    const float mean = g.sum(sum_of(sum), slots[g.index][0]) * a.inv_cols;
+    Pair squares[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       v[i] = add2(v[i], both(-mean));
       if (!FULL) {
-        if (!(mask >> (2 * i) & 1)) v[i].x = 0.0f;
-        if (!(mask >> (2 * i + 1) & 1)) v[i].y = 0.0f;
+        const float2 f = split(v[i]);
+        v[i] = pair_of(mask >> (2 * i) & 1 ? f.x : 0.0f, mask >> (2 * i + 1) & 1 ? f.y : 0.0f);
       }
       squares[i % 2] = fma2(v[i], v[i], squares[i % 2]);
     }
     squares[0] = add2(squares[0], squares[1]);
-    const float rstd = rsqrtf(g.sum(squares[0].x + squares[0].y, slots[g.index][1]) * a.inv_cols + a.eps);
+    const float rstd = rsqrtf(g.sum(sum_of(squares[0]), slots[g.index][1]) * a.inv_cols + a.eps);
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) v[i] = fma2(mul2(v[i], both(rstd)), gamma[i], beta[i]);
     store_row<TY, V, FULL>(out, t, mask, v);
-    if (t == 0) {
-      if (a.mean_out) st_c(a.mean_out + r, mean);
-      if (a.rstd_out) st_c(a.rstd_out + r, rstd);
-    }
-    if (left <= step) break;
-    left -= step;
+    if (mean_out) { st_c(mean_out, mean); mean_out += step; }
+    if (rstd_out) { st_c(rstd_out, rstd); rstd_out += step; }
+    if (--left == 0) break;
     row += stride_x;
     out += stride_y;
     ahead = here;
@@ -385,7 +408,7 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
     g.sync();
   }
   grid_dependency_handshake();
-  float2 gamma[kPairs], dgamma[kSums], dbeta[kSums];
+  Pair gamma[kPairs], dgamma[kSums], dbeta[kSums];
 #pragma unroll
   for (int i = 0; i < kSums; ++i) dgamma[i] = dbeta[i] = both(0.0f);
   if (first < a.rows) {
@@ -403,24 +426,24 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
     }
     load_weights<V>(a, a.gamma, 1.0f, t, gamma);
     uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;
-    uint64_t left = a.rows - first;
+    uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);
     const float* means = a.mean + first;
     const float* rstds = a.rstd + first;
     float mean_next = ld_c(means), rstd_next = ld_c(rstds);
     for (;;) {
-      if (left > (uint64_t)(STAGES - 1) * step) {
+      if (left > STAGES - 1) {
         start_row<TX, V, FULL>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, x, end_x);
         start_row<TY, V, FULL>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, threads, dy, end_y);
       }
       copy_commit();
       const float mean = mean_next, rstd = rstd_next;
-      if (left > step) { mean_next = ld_c(means += step); rstd_next = ld_c(rstds += step); }
+      if (left > 1) { mean_next = ld_c(means += step); rstd_next = ld_c(rstds += step); }
       copy_wait<STAGES - 1>();
       if (V == 1) g.sync();
-      float2 xhat[kPairs], h[kPairs];
+      Pair xhat[kPairs], h[kPairs];
       take_row<TX, V>(here, row, t, mask, xhat);
       take_row<TY, V>(here + space_x, drow, t, mask, h);
-      float2 sum[2] = {both(0.0f), both(0.0f)}, along[2] = {both(0.0f), both(0.0f)};
+      Pair sum[2] = {both(0.0f), both(0.0f)}, along[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
         xhat[i] = mul2(add2(xhat[i], both(-mean)), both(rstd));  // columns that do not exist: dy = 0, so this counts nowhere
@@ -435,17 +458,16 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
       if (a.dx) {
         sum[0] = add2(sum[0], sum[1]);
         along[0] = add2(along[0], along[1]);
-        float2 s = g.sum_two(make_float2(sum[0].x + sum[0].y, along[0].x + along[0].y), slots[g.index][turn]);
+        const float2 s = g.sum_two(make_float2(sum_of(sum[0]), sum_of(along[0])), slots[g.index][turn]);
         turn ^= 1;
-        s = mul2(s, both(-a.inv_cols));
+        const Pair less = both(-s.x * a.inv_cols), slope = both(-s.y * a.inv_cols);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) h[i] = mul2(fma2(xhat[i], both(s.y), add2(h[i], both(s.x))), both(rstd));
+        for (int i = 0; i < kPairs; ++i) h[i] = mul2(fma2(xhat[i], slope, add2(h[i], less)), both(rstd));
         store_row<TX, V, FULL>(out, t, mask, h);
       } else if (V == 1) {
         g.sync();  // the row has been read: its place is free
       }
-      if (left <= step) break;
-      left -= step;
+      if (--left == 0) break;
       row += stride_x;
       drow += stride_y;
       out += stride_x;
@@ -456,15 +478,15 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
   if (!SUMS || !a.partials) return;
   float* out = a.partials + (uint64_t)blockIdx.x * 2 * a.cols;
   if (groups > 1) {  // the block's groups add up their columns one after the other
-    float2* sums = reinterpret_cast<float2*>(norm_shared);
+    Pair* sums = reinterpret_cast<Pair*>(norm_shared);
     copy_wait<0>();
     __syncthreads();
     for (uint32_t k = 0; k < groups; ++k) {
       if (g.index == k) {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-          float2* p = sums + i * threads + t;  // a place of its own for each pair of the thread's columns
-          float2* q = p + kPairs * threads;
+          Pair* p = sums + i * threads + t;  // a place of its own for each pair of the thread's columns
+          Pair* q = p + kPairs * threads;
           if (k) {
             dgamma[i % kSums] = add2(*p, dgamma[i % kSums]);
             dbeta[i % kSums] = add2(*q, dbeta[i % kSums]);
@@ -477,10 +499,21 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
     }
     if (g.index + 1 != groups) return;
   }
+  const bool pairs = V > 1 && FULL;  // both runs of a unit are 16 bytes and more, on 16-byte boundaries
+#pragma unroll
+  for (int i = 0; i < kOwn; i += 4) {
+    if (!pairs) break;
+    const uint32_t c = column_of<V>(t, i);
+    const float2 d0 = split(dgamma[i / 2 % kSums]), d1 = split(dgamma[(i / 2 + 1) % kSums]);
+    const float2 e0 = split(dbeta[i / 2 % kSums]), e1 = split(dbeta[(i / 2 + 1) % kSums]);
+    st_c(reinterpret_cast<float4*>(out + c), make_float4(d0.x, d0.y, d1.x, d1.y));
+    st_c(reinterpret_cast<float4*>(out + a.cols + c), make_float4(e0.x, e0.y, e1.x, e1.y));
+  }
+  if (pairs) return;
 #pragma unroll
   for (int i = 0; i < kOwn; ++i) {
     const uint32_t c = column_of<V>(t, i);
-    const float2 d = dgamma[i / 2 % kSums], e = dbeta[i / 2 % kSums];
+    const float2 d = split(dgamma[i / 2 % kSums]), e = split(dbeta[i / 2 % kSums]);
     if (c < a.cols) { st_c(out + c, i % 2 ? d.y : d.x); st_c(out + a.cols + c, i % 2 ? e.y : e.x); }
   }
 }
@@ -562,31 +595,33 @@ __global__ void __launch_bounds__(128) norm_column_sums_kernel(const NormArgs a)
   st_c(out + a.cols + c, dbeta);
 }
 
-// dgamma and dbeta from the blocks' partial sums: 32 columns a block, the partials dealt over its eight warps and
-// added in a fixed order.
-__global__ void __launch_bounds__(256) norm_join_kernel(const NormArgs a) {
-  __shared__ float part[8][33];
+// dgamma and dbeta from the blocks' partial sums: 32 columns a block, the partials dealt over its sixteen warps, all of a
+// warp's loads on their way at once, and added in a fixed order.
+constexpr int kJoinWarps = 16;
+__global__ void __launch_bounds__(32 * kJoinWarps) norm_join_kernel(const NormArgs a) {
+  __shared__ float part[kJoinWarps][33];
   grid_dependency_handshake();
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;  // over dgamma, then dbeta
   const uint64_t width = 2ull * a.cols;
-  float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+  float s = 0.0f;
   if (c < width) {
-    uint32_t i = warp;
-    for (; i + 24 < a.n_partials; i += 32) {
-      s0 += ld_c(a.partials + (uint64_t)i * width + c);
-      s1 += ld_c(a.partials + (uint64_t)(i + 8) * width + c);
-      s2 += ld_c(a.partials + (uint64_t)(i + 16) * width + c);
-      s3 += ld_c(a.partials + (uint64_t)(i + 24) * width + c);
+    const float* p = a.partials + c;
+    constexpr int kAtOnce = 10;  // 148 blocks over 16 warps
+    for (uint32_t i = warp; i < a.n_partials; i += kAtOnce * kJoinWarps) {
+      float v[kAtOnce];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) v[j] = i + j * kJoinWarps < a.n_partials ? ld_c(p + (uint64_t)(i + j * kJoinWarps) * width) : 0.0f;
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j) s += v[j];
     }
-    for (; i < a.n_partials; i += 8) s0 += ld_c(a.partials + (uint64_t)i * width + c);
   }
-  part[warp][lane] = (s0 + s1) + (s2 + s3);
+  part[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && c < width) {
-    float s = 0.0f;
+    s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += part[w][lane];
+    for (int w = 0; w < kJoinWarps; ++w) s += part[w][lane];
     float* out = c < a.cols ? a.dgamma : a.dbeta;
     if (out) st_c(out + (c < a.cols ? c : c - a.cols), s);
   }

@@ -18,50 +18,59 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(f
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
 // ---- pairs: sm_100 adds, multiplies and fuses two fp32 values with one instruction, each rounded as by itself ----
-__device__ __forceinline__ unsigned long long bits(float2 v) {
-  unsigned long long r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(v.x), "f"(v.y));
+// A pair is one 64-bit register pair from its load to its store.
+typedef unsigned long long Pair;
+__device__ __forceinline__ Pair pair_of(float lo, float hi) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
   return r;
 }
-__device__ __forceinline__ float2 pair_of(unsigned long long b) {
+__device__ __forceinline__ float2 split(Pair b) {
   float2 v;
   asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(b));
   return v;
 }
-__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  unsigned long long r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
-  return pair_of(r);
+__device__ __forceinline__ Pair both(float v) { return pair_of(v, v); }
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  unsigned long long r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)));
-  return pair_of(r);
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  unsigned long long r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
-  return pair_of(r);
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ float sum_of(Pair v) {
+  const float2 f = split(v);
+  return f.x + f.y;
 }
 // Two 16-bit values of a word, the lower first.
-template <typename T> __device__ __forceinline__ float2 word_to_pair(uint32_t w);
-template <> __device__ __forceinline__ float2 word_to_pair<__nv_bfloat16>(uint32_t w) {  // bf16 is the upper half of an fp32
-  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+template <typename T> __device__ __forceinline__ Pair word_to_pair(uint32_t w);
+template <> __device__ __forceinline__ Pair word_to_pair<__nv_bfloat16>(uint32_t w) {  // bf16 is the upper half of an fp32
+  return pair_of(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
-template <> __device__ __forceinline__ float2 word_to_pair<__half>(uint32_t w) {
+template <> __device__ __forceinline__ Pair word_to_pair<__half>(uint32_t w) {
   __half2 h;
   memcpy(&h, &w, 4);
-  return __half22float2(h);
+  const float2 f = __half22float2(h);
+  return pair_of(f.x, f.y);
 }
-template <typename T> __device__ __forceinline__ uint32_t pair_to_word(float2 v);
-template <> __device__ __forceinline__ uint32_t pair_to_word<__nv_bfloat16>(float2 v) {
+template <typename T> __device__ __forceinline__ uint32_t pair_to_word(Pair v);
+template <> __device__ __forceinline__ uint32_t pair_to_word<__nv_bfloat16>(Pair p) {
+  const float2 v = split(p);
   const __nv_bfloat162 h = __floats2bfloat162_rn(v.x, v.y);
   uint32_t w;
   memcpy(&w, &h, 4);
   return w;
 }
-template <> __device__ __forceinline__ uint32_t pair_to_word<__half>(float2 v) {
+template <> __device__ __forceinline__ uint32_t pair_to_word<__half>(Pair p) {
+  const float2 v = split(p);
   const __half2 h = __floats2half2_rn(v.x, v.y);
   uint32_t w;
   memcpy(&w, &h, 4);
