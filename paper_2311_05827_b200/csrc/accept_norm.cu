@@ -16,41 +16,42 @@ bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF1
 // rows that all start on 16-byte boundaries
 bool whole_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p, 16) && ld * value_size(dtype) % 16 == 0; }
 
-// Launch shape of a pass.  A row is shared by as many warps as hold it at 16 columns a thread; a block holds as many such
-// groups as fit 512 threads, fewer where there are too few rows for every SM, and fills shared memory with rows on their way.
-enum class NormPath { kRegisters, kWide, kLong };  // up to 8192 columns; up to 16384; more
-struct NormShape { NormPath path; unsigned warps, groups, blocks; size_t shared; };
+// Launch shape of a pass.  A row is shared by as many warps as hold it at `own` columns a thread; a block holds as many
+// such groups as fit 512 threads, fewer where there are too few rows for every SM.  16 columns a thread, 32 for rows of more
+// than 8192 (32 everywhere: 16384 x 4096 fp32 to bf16 62 -> 77 us, 8 x 4096 bf16 2.6 -> 3.7 us, for want of registers).  The
+// backward pass over more than 8192 columns has no registers for the sums over the rows and leaves them to a pass of their
+// own (kApart); rows of more than 16384 columns are not held (kLong).
+enum class NormPath { kRegisters, kApart, kLong };
+struct NormShape { NormPath path; int own; unsigned warps, groups, blocks; size_t shared; };
 
-// Rows of a group in shared memory.  A block of 512 threads holds 32 KB of an fp32 row's stage at most (64 KB backward):
-// three stages fit.  Rows of more than 8192 columns take twice that.
-template <typename TX, typename TY>
-constexpr int stages_of(NormPath path, bool backward) {
-  return !backward && path == NormPath::kRegisters ? 4 : path != NormPath::kWide || !backward ? 3 : 12 / (int)(sizeof(TX) + sizeof(TY));
+// Rows of a group in shared memory: up to 192 KB for the block.
+constexpr int stages_for(bool backward, int own, int size_x, int size_y) {
+  const int row = 512 * own * (size_x + (backward ? size_y : 0));
+  return 196608 / row < 4 ? 196608 / row : 4;
 }
-int stages_of(const accept_layer_norm_params* p, NormPath path, bool backward) {
-  const int size = (p->dtype_x == ACCEPT_DTYPE_F32 ? 4 : 2) + (p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 2);
-  return !backward && path == NormPath::kRegisters ? 4 : path != NormPath::kWide || !backward ? 3 : 12 / size;
+int stages_of(const accept_layer_norm_params* p, bool backward, int own) {
+  return stages_for(backward, own, p->dtype_x == ACCEPT_DTYPE_F32 ? 4 : 2, p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 2);
 }
 
 NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
   NormShape s{};
-  const uint64_t warps = (p->cols + 32 * accept::kOwn - 1) / (32 * accept::kOwn);
-  if (warps > 32) {
+  if (p->cols > 16384) {
     s.path = NormPath::kLong;
     s.blocks = (unsigned)(p->rows < kSms ? p->rows : kSms);
     return s;
   }
-  s.path = warps <= 16 ? NormPath::kRegisters : NormPath::kWide;
-  s.warps = (unsigned)warps;
-  const uint64_t spread = (p->rows + kSms - 1) / kSms, most = s.path == NormPath::kWide ? 1 : 16 / warps;
+  s.path = backward && p->cols > 8192 ? NormPath::kApart : NormPath::kRegisters;
+  s.own = p->cols > 8192 ? 32 : 16;
+  s.warps = (unsigned)((p->cols + 32 * s.own - 1) / (32 * s.own));
+  const uint64_t spread = (p->rows + kSms - 1) / kSms, most = 16 / s.warps;
   s.groups = (unsigned)(spread < most ? (spread ? spread : 1) : most);
   const auto space = [&](int32_t dtype) {
-    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, s.warps, (uint32_t)p->cols)
-                                              : accept::row_space<uint16_t>(v, s.warps, (uint32_t)p->cols));
+    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, s.own, s.warps, (uint32_t)p->cols)
+                                              : accept::row_space<uint16_t>(v, s.own, s.warps, (uint32_t)p->cols));
   };
-  s.shared = s.groups * (size_t)stages_of(p, s.path, backward) * (space(p->dtype_x) + (backward ? space(p->dtype_y) : 0));
-  // the groups of a block add up their column sums in the same memory
-  const size_t sums = backward && s.groups > 1 ? 2 * 4 * (size_t)accept::kOwn * 32 * s.warps : 0;
+  s.shared = s.groups * (size_t)stages_of(p, backward, s.own) * (space(p->dtype_x) + (backward ? space(p->dtype_y) : 0));
+  // the column sums of the block's groups take the same memory
+  const size_t sums = backward && s.path == NormPath::kRegisters ? 2 * 4 * (size_t)s.own * 32 * s.warps * s.groups : 0;
   if (s.shared < sums) s.shared = sums;
   const uint64_t units = (p->rows + s.groups - 1) / s.groups;
   s.blocks = (unsigned)(units < kSms ? units : kSms);
@@ -68,39 +69,39 @@ using KernelFn = void (*)(const NormArgs);
 struct Kernels { KernelFn rows, sums; };
 
 template <typename TX, typename TY, int V, bool FULL>
-KernelFn rows_kernel(NormPath path, bool backward) {
-  constexpr NormPath kReg = NormPath::kRegisters, kWide = NormPath::kWide;
-  if (path == NormPath::kLong) return backward ? accept::norm_backward_long_kernel<TX, TY> : accept::norm_forward_long_kernel<TX, TY>;
-  if (path == kWide)
-    return backward ? accept::norm_backward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kWide, true), false, 1024>
-                    : accept::norm_forward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kWide, false), 1024>;
-  return backward ? accept::norm_backward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kReg, true), true, 512>
-                  : accept::norm_forward_kernel<TX, TY, V, FULL, stages_of<TX, TY>(kReg, false), 512>;
+KernelFn rows_kernel(const NormShape& s, bool backward) {
+  constexpr int kX = (int)sizeof(TX), kY = (int)sizeof(TY);
+  if (s.path == NormPath::kLong) return backward ? accept::norm_backward_long_kernel<TX, TY> : accept::norm_forward_long_kernel<TX, TY>;
+  if (!backward)
+    return s.own == 32 ? accept::norm_forward_kernel<TX, TY, V, FULL, 32, stages_for(false, 32, kX, kY)>
+                       : accept::norm_forward_kernel<TX, TY, V, FULL, 16, stages_for(false, 16, kX, kY)>;
+  return s.own == 32 ? accept::norm_backward_kernel<TX, TY, V, FULL, 32, stages_for(true, 32, kX, kY), false>
+                     : accept::norm_backward_kernel<TX, TY, V, FULL, 16, stages_for(true, 16, kX, kY), true>;
 }
 
-// whole: rows start on 16-byte boundaries; full: 512 columns for each warp
+// whole: rows start on 16-byte boundaries; full: every thread has all its columns
 template <typename TX, typename TY>
-Kernels kernels_for(NormPath path, bool backward, bool whole, bool full) {
+Kernels kernels_for(const NormShape& s, bool backward, bool whole, bool full) {
   constexpr int kUnit = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
-  return {!whole ? rows_kernel<TX, TY, 1, false>(path, backward)
-          : full ? rows_kernel<TX, TY, kUnit, true>(path, backward) : rows_kernel<TX, TY, kUnit, false>(path, backward),
+  return {!whole ? rows_kernel<TX, TY, 1, false>(s, backward)
+          : full ? rows_kernel<TX, TY, kUnit, true>(s, backward) : rows_kernel<TX, TY, kUnit, false>(s, backward),
           accept::norm_column_sums_kernel<TX, TY>};
 }
 
 template <typename TX>
-Kernels kernels_for_y(const accept_layer_norm_params* p, NormPath path, bool backward, bool whole) {
+Kernels kernels_for_y(const accept_layer_norm_params* p, const NormShape& s, bool backward, bool whole) {
   switch (p->dtype_y) {
-    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(path, backward, whole, p->cols % 512 == 0);
-    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(path, backward, whole, p->cols % 512 == 0);
-    default: return kernels_for<TX, __half>(path, backward, whole, p->cols % 512 == 0);
+    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, whole, s.own != 0 && p->cols % (32 * s.own) == 0);
+    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, whole, s.own != 0 && p->cols % (32 * s.own) == 0);
+    default: return kernels_for<TX, __half>(s, backward, whole, s.own != 0 && p->cols % (32 * s.own) == 0);
   }
 }
 
-Kernels select_kernels(const accept_layer_norm_params* p, NormPath path, bool backward, bool whole) {
+Kernels select_kernels(const accept_layer_norm_params* p, const NormShape& s, bool backward, bool whole) {
   switch (p->dtype_x) {
-    case ACCEPT_DTYPE_F32: return kernels_for_y<float>(p, path, backward, whole);
-    case ACCEPT_DTYPE_BF16: return kernels_for_y<__nv_bfloat16>(p, path, backward, whole);
-    default: return kernels_for_y<__half>(p, path, backward, whole);
+    case ACCEPT_DTYPE_F32: return kernels_for_y<float>(p, s, backward, whole);
+    case ACCEPT_DTYPE_BF16: return kernels_for_y<__nv_bfloat16>(p, s, backward, whole);
+    default: return kernels_for_y<__half>(p, s, backward, whole);
   }
 }
 
@@ -187,7 +188,7 @@ accept_status accept_layer_norm_forward(const accept_layer_norm_params* p, const
   const bool whole = whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_y, p->ld_y, p->dtype_y);
   a.whole_weights = is_aligned(d_gamma, 16) && is_aligned(d_beta, 16);
   const NormShape shape = norm_shape(p, false, unit_of(p, whole));
-  ACCEPT_LAUNCH(launch_norm(select_kernels(p, shape.path, false, whole).rows, shape, a, s));
+  ACCEPT_LAUNCH(launch_norm(select_kernels(p, shape, false, whole).rows, shape, a, s));
   return ACCEPT_OK;
 }
 
@@ -228,8 +229,8 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
                 bounds_list.add(d_dgamma, 4 * p->cols, true); bounds_list.add(d_dbeta, 4 * p->cols, true);
                 bounds_list.add(d_ws, accept_layer_norm_workspace_size(p), true));
   if (p->rows != 0) {
-    const Kernels k = select_kernels(p, shape.path, true, whole);
-    const bool apart = shape.path != NormPath::kRegisters;  // the sums over the rows are a pass of their own
+    const Kernels k = select_kernels(p, shape, true, whole);
+    const bool apart = shape.path != NormPath::kRegisters;
     if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
     if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 127) / 128, a.n_partials), 128, s, a));
   }

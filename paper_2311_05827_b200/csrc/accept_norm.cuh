@@ -1,7 +1,7 @@
 // Layer norm, forward and backward (sm_100a).
 //
 // Bound by memory: each value is read once and written once, and a row stays in the registers of the threads that
-// share it (16 columns each) while its sums are taken.  A row's sums need barriers, during which its threads load
+// share it (OWN = 16 or 32 columns each) while its sums are taken.  A row's sums need barriers, during which its threads load
 // nothing; so the next rows are already on their way into shared memory by asynchronous copies.  Each thread copies what it
 // will itself read, so the copies need no barrier of their own.
 #pragma once
@@ -32,25 +32,37 @@ struct NormArgs {
   int whole_weights;     // gamma and beta start on 16-byte boundaries
 };
 
-constexpr int kOwn = 16;         // columns of a row that a thread holds
-constexpr int kPairs = kOwn / 2;
-
-// How the columns of a row lie over the threads that share it: a warp holds 512 neighbours, as units of V neighbours dealt
+// How the columns of a row lie over the threads that share it: a warp holds 32 OWN neighbours, as units of V neighbours dealt
 // over its lanes, so that all addresses of a thread are one base and constants.  V = 8 where both tensors are 16-bit types,
 // 4 where one is fp32 (16 bytes at most for a thread, neighbours side by side), 1 where rows do not start on 16-byte
 // boundaries.
-template <int V>
+template <int V, int OWN>
 __device__ __forceinline__ uint32_t column_of(uint32_t t, int own) {
-  return (t >> 5) * (32 * kOwn) + V * (t & 31) + own / V * (32 * V) + own % V;
+  return (t >> 5) * (32 * OWN) + V * (t & 31) + own / V * (32 * V) + own % V;
 }
-// Which of the thread's columns exist, a bit for each.
-template <int V>
-__device__ __forceinline__ uint32_t columns_mask(uint32_t t, uint32_t cols) {
-  uint32_t m = 0;
+// How many values of each of the thread's units exist (V = 1: a bit for each).  FULL: all of them.
+template <int V, bool FULL, int OWN>
+struct Own {
+  static constexpr int kUnits = V > 1 ? OWN / V : 1;
+  uint32_t count[kUnits];
+  __device__ __forceinline__ Own(uint32_t t, uint32_t cols) {
 #pragma unroll
-  for (int i = 0; i < kOwn; ++i) m |= column_of<V>(t, i) < cols ? 1u << i : 0u;
-  return m;
-}
+    for (int i = 0; i < kUnits; ++i) {
+      if (V > 1) {
+        const uint32_t c = column_of<V, OWN>(t, V * i);
+        count[i] = c < cols ? min(cols - c, (uint32_t)V) : 0;
+      } else {
+        count[0] = 0;
+#pragma unroll
+        for (int j = 0; j < OWN; ++j) count[0] |= column_of<1, OWN>(t, j) < cols ? 1u << j : 0u;
+      }
+    }
+  }
+  __device__ __forceinline__ uint32_t of(int unit) const { return FULL ? V : count[unit % kUnits]; }
+  __device__ __forceinline__ bool has(int value) const {  // value of the thread's OWN
+    return FULL || (V > 1 ? (uint32_t)(value % V) < count[value / V % kUnits] : (count[0] >> value & 1) != 0);
+  }
+};
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, uint32_t bytes) {  // the rest of BYTES is zero
@@ -65,42 +77,39 @@ __device__ __forceinline__ void copy_async_at(uint32_t dst, const void* src) {
   if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0+%2], [%1+%3], 16;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0+%2], [%1+%3], 8;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM) : "memory");
 }
+template <int BYTES, int TO, int FROM>
+__device__ __forceinline__ void copy_async_at(uint32_t dst, const void* src, uint32_t bytes) {  // the rest of BYTES is zero
+  if (!bounds_ok(static_cast<const uint8_t*>(src) + FROM, bytes, false)) return;
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0+%2], [%1+%3], 16, %4;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM), "r"(bytes) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0+%2], [%1+%3], 8, %4;" ::"r"(dst), "l"(src), "n"(TO), "n"(FROM), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int PENDING>  // all but the last PENDING groups have landed
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
 // Bytes of shared memory that a row of T takes for `warps` warps (V = 1: the 16-byte pieces that hold it).
 template <typename T>
-__host__ __device__ constexpr uint32_t row_space(int v, uint32_t warps, uint32_t cols) {
-  return v > 1 ? warps * 32 * kOwn * (uint32_t)sizeof(T) : (cols * (uint32_t)sizeof(T) + 30) / 16 * 16;
+__host__ __device__ constexpr uint32_t row_space(int v, int own, uint32_t warps, uint32_t cols) {
+  return v > 1 ? warps * 32 * own * (uint32_t)sizeof(T) : (cols * (uint32_t)sizeof(T) + 30) / 16 * 16;
 }
 
-// Starts the copies of a row into `dst` (shared).  `begin` and `end` bound the values of the matrix; FULL: all columns of
-// every thread exist.
-template <typename T, int V, bool FULL>
-__device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, uint32_t threads, const T* begin, const T* end) {
-  if (V > 1) {
-    constexpr int kBytes = V * (int)sizeof(T) < 16 ? 8 : 16;
-    static_assert(V == 1 || V * (int)sizeof(T) == kBytes, "a unit is one copy");
-    const uint32_t first = column_of<V>(t, 0);
-    const uint32_t to = dst + first * (uint32_t)sizeof(T);
+// Starts the copies of a row into `dst` (shared).  `begin` and `end` bound the values of the matrix.  Units that do not
+// exist are not copied: their places hold zeros from the start (clear_row).
+template <typename T, int V, bool FULL, int OWN, int I = 0>
+__device__ __forceinline__ void start_units(uint32_t to, const T* from, const Own<V, FULL, OWN>& own) {
+  constexpr int kBytes = V * (int)sizeof(T), kTo = I * 32 * kBytes, kFrom = I * 32 * V * (int)sizeof(T);
+  static_assert(kBytes == 8 || kBytes == 16, "a unit is one copy");
+  if (FULL) copy_async_at<kBytes, kTo, kFrom>(to, from);
+  else if (own.of(I)) copy_async_at<kBytes, kTo, kFrom>(to, from, own.of(I) * (uint32_t)sizeof(T));
+  if constexpr (I + 1 < OWN / V) start_units<T, V, FULL, OWN, I + 1>(to, from, own);
+}
+template <typename T, int V, bool FULL, int OWN>
+__device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, uint32_t threads, const Own<V, FULL, OWN>& own,
+                                          const T* begin, const T* end) {
+  if constexpr (V > 1) {
+    const uint32_t first = column_of<V, OWN>(t, 0), to = dst + first * (uint32_t)sizeof(T);
     const T* from = row + first;
-    if (FULL) {
-      constexpr int kTo = 32 * kBytes, kFrom = 32 * V * (int)sizeof(T);
-      copy_async_at<kBytes, 0, 0>(to, from);
-      copy_async_at<kBytes, kTo, kFrom>(to, from);
-      if constexpr (kOwn / V == 4) {
-        copy_async_at<kBytes, 2 * kTo, 2 * kFrom>(to, from);
-        copy_async_at<kBytes, 3 * kTo, 3 * kFrom>(to, from);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kOwn / V; ++i) {
-        const uint32_t c = first + i * 32 * V;
-        const uint32_t bytes = c < cols ? min(cols - c, (uint32_t)V) * (uint32_t)sizeof(T) : 0;
-        copy_async<kBytes>(to + i * 32 * kBytes, bytes ? from + i * 32 * V : row, bytes);
-      }
-    }
+    start_units(to, from, own);
   } else {
     // the 16-byte pieces that hold the row; what lies outside the matrix is not read
     const uintptr_t from = reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15, to = reinterpret_cast<uintptr_t>(row + cols);
@@ -129,43 +138,52 @@ __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t c
   }
 }
 
-// Unit I of the thread from shared memory.
-template <typename T, int V, int I>
-__device__ __forceinline__ void take_unit(uint32_t from, Pair (&v)[kPairs]) {
+// Zeros where this thread's units that do not exist would lie.
+template <typename T, int V, bool FULL, int OWN>
+__device__ __forceinline__ void clear_row(uint32_t dst, uint32_t t, const Own<V, FULL, OWN>& own) {
+  if (V == 1 || FULL) return;
+#pragma unroll
+  for (int i = 0; i < OWN / V; ++i) {
+    if (own.of(i)) continue;
+    const uint32_t at = dst + column_of<V, OWN>(t, V * i) * (uint32_t)sizeof(T);
+#pragma unroll
+    for (int j = 0; j < V * (int)sizeof(T); j += 8) asm volatile("st.shared.u64 [%0], %1;" ::"r"(at + j), "l"(0ull) : "memory");
+  }
+}
+
+// Units I and after of the thread from shared memory.
+template <typename T, int V, int OWN, int I = 0>
+__device__ __forceinline__ void take_units(uint32_t from, Pair (&v)[OWN / 2]) {
   constexpr int kFirst = V * I / 2;
   if constexpr (sizeof(T) == 4) {
-    asm volatile("ld.shared.v2.u64 {%0,%1}, [%2+%3];" : "=l"(v[kFirst % kPairs]), "=l"(v[(kFirst + 1) % kPairs]) : "r"(from), "n"(I * 32 * 16));
+    asm volatile("ld.shared.v2.u64 {%0,%1}, [%2+%3];" : "=l"(v[kFirst % (OWN / 2)]), "=l"(v[(kFirst + 1) % (OWN / 2)]) : "r"(from), "n"(I * 32 * 16));
   } else if constexpr (V == 8) {
     uint32_t w[4];
     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+%5];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from), "n"(I * 32 * 16));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[(kFirst + j) % kPairs] = word_to_pair<T>(w[j]);
+    for (int j = 0; j < 4; ++j) v[(kFirst + j) % (OWN / 2)] = word_to_pair<T>(w[j]);
   } else {
     uint32_t w[2];
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2+%3];" : "=r"(w[0]), "=r"(w[1]) : "r"(from), "n"(I * 32 * 8));
-    v[kFirst % kPairs] = word_to_pair<T>(w[0]);
-    v[(kFirst + 1) % kPairs] = word_to_pair<T>(w[1]);
+    v[kFirst % (OWN / 2)] = word_to_pair<T>(w[0]);
+    v[(kFirst + 1) % (OWN / 2)] = word_to_pair<T>(w[1]);
   }
+  if constexpr (I + 1 < OWN / V) take_units<T, V, OWN, I + 1>(from, v);
 }
 
 // Takes a row that has landed at `src` (shared) into registers; columns that do not exist are zero.
-template <typename T, int V>
-__device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, uint32_t mask, Pair (&v)[kPairs]) {
-  if (V > 1) {
-    const uint32_t from = src + column_of<V>(t, 0) * (uint32_t)sizeof(T);
-    take_unit<T, V, 0>(from, v);
-    take_unit<T, V, 1>(from, v);
-    if constexpr (kOwn / V == 4) {
-      take_unit<T, V, 2>(from, v);
-      take_unit<T, V, 3>(from, v);
-    }
+template <typename T, int V, bool FULL, int OWN>
+__device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, const Own<V, FULL, OWN>& own, Pair (&v)[OWN / 2]) {
+  if constexpr (V > 1) {
+    const uint32_t from = src + column_of<V, OWN>(t, 0) * (uint32_t)sizeof(T);
+    take_units<T, V, OWN>(from, v);
   } else {
-    const uint32_t from = src + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + column_of<V>(t, 0) * (uint32_t)sizeof(T);
+    const uint32_t from = src + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + column_of<V, OWN>(t, 0) * (uint32_t)sizeof(T);
     float lo = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kOwn; ++i) {
+    for (int i = 0; i < OWN; ++i) {
       float f = 0.0f;
-      if (mask >> i & 1) {
+      if (own.has(i)) {
         if constexpr (sizeof(T) == 4) {
           asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(from + i * 32 * 4));
         } else {
@@ -182,18 +200,17 @@ __device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t,
   }
 }
 
-template <typename T, int V, bool FULL>
-__device__ __forceinline__ void store_row(T* row, uint32_t t, uint32_t mask, const Pair (&v)[kPairs]) {
-  T* to = row + column_of<V>(t, 0);
+template <typename T, int V, bool FULL, int OWN>
+__device__ __forceinline__ void store_row(T* row, uint32_t t, const Own<V, FULL, OWN>& own, const Pair (&v)[OWN / 2]) {
+  T* to = row + column_of<V, OWN>(t, 0);
 #pragma unroll
-  for (int i = 0; i < kOwn / V; ++i) {
-    constexpr uint32_t kUnit = (1u << V) - 1;
+  for (int i = 0; i < OWN / V; ++i) {
     T* p = to + i * 32 * V;
-    if (V > 1 && (FULL || (mask >> (V * i) & kUnit) == kUnit)) {
+    if (V > 1 && own.of(i) == V) {
       uint32_t w[4];
 #pragma unroll
       for (int j = 0; j < V / 2; ++j) {
-        const Pair f = v[(V * i / 2 + j) % kPairs];
+        const Pair f = v[(V * i / 2 + j) % (OWN / 2)];
         if constexpr (sizeof(T) == 4) { w[(2 * j) % 4] = __float_as_uint(split(f).x); w[(2 * j + 1) % 4] = __float_as_uint(split(f).y); }
         else w[j % 4] = pair_to_word<T>(f);
       }
@@ -202,11 +219,11 @@ __device__ __forceinline__ void store_row(T* row, uint32_t t, uint32_t mask, con
       } else {
         if (bounds_ok(p, 8, true)) __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
       }
-    } else {
+    } else if (V == 1 || own.of(i) != 0) {
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         const float2 f = split(v[(V * i + j) / 2]);
-        if (mask >> (V * i + j) & 1) st_c(p + j, from_float<T>((V * i + j) % 2 ? f.y : f.x));
+        if (own.has(V * i + j)) st_c(p + j, from_float<T>((V * i + j) % 2 ? f.y : f.x));
       }
     }
   }
@@ -221,11 +238,11 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, float absen
 }
 
 // gamma or beta for this thread's columns: read once for all rows that it takes.
-template <int V>
-__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, float absent, uint32_t t, Pair (&v)[kPairs]) {
+template <int V, int OWN>
+__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
 #pragma unroll
-  for (int i = 0; i < kOwn; i += V) {
-    const uint32_t c = column_of<V>(t, i);
+  for (int i = 0; i < OWN; i += V) {
+    const uint32_t c = column_of<V, OWN>(t, i);
     if (V > 1 && w && a.whole_weights && c + V <= a.cols) {
 #pragma unroll
       for (int j = 0; j < V; j += 4) {
@@ -239,8 +256,8 @@ __device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, f
           lo = a.dtype_w == kBf16 ? word_to_pair<__nv_bfloat16>(raw.x) : word_to_pair<__half>(raw.x);
           hi = a.dtype_w == kBf16 ? word_to_pair<__nv_bfloat16>(raw.y) : word_to_pair<__half>(raw.y);
         }
-        v[(i + j) / 2 % kPairs] = lo;
-        v[((i + j) / 2 + 1) % kPairs] = hi;
+        v[(i + j) / 2 % (OWN / 2)] = lo;
+        v[((i + j) / 2 + 1) % (OWN / 2)] = hi;
       }
     } else {
 #pragma unroll
@@ -270,7 +287,7 @@ struct Group {
     if (warps == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(threads) : "memory");
   }
-  // Sum over the group.  `slot`: 32 floats of the group, zero past its warps, used in turn with others (a barrier lies
+  // Sum over the group.  `slot`: 16 floats of the group, zero past its warps, used in turn with others (a barrier lies
   // between two uses); every thread adds the warps' values up for itself.
   __device__ __forceinline__ float sum(float v, float* slot) const {
     v = warp_sum(v);
@@ -279,7 +296,7 @@ struct Group {
     sync();
     float4 s = *reinterpret_cast<const float4*>(slot);
 #pragma unroll
-    for (uint32_t w = 4; w < 32; w += 4) {
+    for (uint32_t w = 4; w < 16; w += 4) {
       if (w >= warps) break;
       const float4 m = *reinterpret_cast<const float4*>(slot + w);
       s.x += m.x; s.y += m.y; s.z += m.z; s.w += m.w;
@@ -287,7 +304,7 @@ struct Group {
     return (s.x + s.y) + (s.z + s.w);
   }
   // Two sums with one barrier: after the first exchange the lower half of a warp adds up one of them, the upper half the
-  // other.  `slot`: 64 floats, pairs of both.
+  // other.  `slot`: 32 floats, pairs of both.
   __device__ __forceinline__ float2 sum_two(float2 v, float* slot) const {
     const bool upper = (t & 16) != 0;
     float mine = upper ? v.y : v.x;
@@ -302,7 +319,7 @@ struct Group {
     sync();
     float4 s = *reinterpret_cast<const float4*>(slot);
 #pragma unroll
-    for (uint32_t w = 2; w < 32; w += 2) {
+    for (uint32_t w = 2; w < 16; w += 2) {
       if (w >= warps) break;
       const float4 m = *reinterpret_cast<const float4*>(slot + 2 * w);
       s.x += m.x; s.y += m.y; s.z += m.z; s.w += m.w;
@@ -317,23 +334,28 @@ extern __shared__ __align__(16) uint8_t norm_shared[];
 
 // Forward.  The mean first, then the sum of the squared distances from it, so that an offset much larger than the spread
 // costs no digits.
-template <typename TX, typename TY, int V, bool FULL, int STAGES, int MAX_THREADS>
-__global__ void __launch_bounds__(MAX_THREADS) norm_forward_kernel(const NormArgs a) {
-  __shared__ __align__(16) float slots[kMostGroups][2][32];
+template <typename TX, typename TY, int V, bool FULL, int OWN, int STAGES>
+__global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a) {
+  __shared__ __align__(16) float slots[kMostGroups][2][16];
   const Group g(a.warps);
   const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space = row_space<TX>(V, a.warps, a.cols);
+  const uint32_t space = row_space<TX>(V, OWN, a.warps, a.cols);
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space, shared_end = shared + STAGES * space;
-  const uint32_t mask = FULL ? 0 : columns_mask<V>(t, a.cols);
+  const Own<V, FULL, OWN> own(t, a.cols);
+  bool ends_inside = false;
+#pragma unroll
+  for (int i = 0; i < OWN / V; ++i) ends_inside |= V > 1 && own.of(i) % V != 0;
   const TX* x = static_cast<const TX*>(a.x);
   const TX* end = x + (a.rows - 1) * a.ld_x + a.cols;
   const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
   const uint32_t step = gridDim.x * groups;
   if (a.warps > 1) {
     float* zero = &slots[g.index][0][0];
-    for (uint32_t i = t; i < 64; i += threads) zero[i] = 0.0f;
+    for (uint32_t i = t; i < 32; i += threads) zero[i] = 0.0f;
     g.sync();
   }
+#pragma unroll
+  for (int i = 0; i < STAGES; ++i) clear_row<TX, V, FULL, OWN>(shared + i * space, t, own);
   grid_dependency_handshake();
   if (first >= a.rows) return;
   const TX* row = x + first * a.ld_x;
@@ -341,40 +363,45 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_forward_kernel(const NormArg
   const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) {
-    if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL>(shared + s * space, row + s * stride_x, a.cols, t, threads, x, end);
+    if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL, OWN>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end);
     copy_commit();
   }
-  Pair gamma[kPairs], beta[kPairs];
-  load_weights<V>(a, a.gamma, 1.0f, t, gamma);
-  load_weights<V>(a, a.beta, 0.0f, t, beta);
+  Pair gamma[OWN / 2], beta[OWN / 2];
+  load_weights<V, OWN>(a, a.gamma, 1.0f, t, gamma);
+  load_weights<V, OWN>(a, a.beta, 0.0f, t, beta);
   uint32_t here = shared, ahead = shared + (STAGES - 1) * space;  // where this row lies, and where the one to start goes
   uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);  // rows of this group from this one on
   float* mean_out = a.mean_out && t == 0 ? a.mean_out + first : nullptr;
   float* rstd_out = a.rstd_out && t == 0 ? a.rstd_out + first : nullptr;
   for (;;) {
-    if (left > STAGES - 1) start_row<TX, V, FULL>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, x, end);
+    if (left > STAGES - 1) start_row<TX, V, FULL, OWN>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end);
     copy_commit();
     copy_wait<STAGES - 1>();
     if (V == 1) g.sync();
-    Pair v[kPairs];
-    take_row<TX, V>(here, row, t, mask, v);
-    const Pair sum = add2(add2(add2(v[0], v[1]), add2(v[2], v[3])), add2(add2(v[4], v[5]), add2(v[6], v[7])));
+    Pair v[OWN / 2];
+    take_row<TX, V, FULL, OWN>(here, row, t, own, v);
+    Pair sums[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+    for (int i = 4; i < OWN / 2; ++i) sums[i % 4] = add2(sums[i % 4], v[i]);
+    const Pair sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
     const float mean = g.sum(sum_of(sum), slots[g.index][0]) * a.inv_cols;
     Pair squares[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) {
-      v[i] = add2(v[i], both(-mean));
-      if (!FULL) {
+    for (int i = 0; i < OWN / 2; ++i) {
+      // a unit that does not exist stays zero; one that ends inside (one thread's) is masked value by value
+      if (V > 1) v[i] = add2(v[i], both(own.of(2 * i / V) ? -mean : 0.0f));
+      else v[i] = add2(v[i], pair_of(own.has(2 * i) ? -mean : 0.0f, own.has(2 * i + 1) ? -mean : 0.0f));
+      if (!FULL && V > 1 && ends_inside) {
         const float2 f = split(v[i]);
-        v[i] = pair_of(mask >> (2 * i) & 1 ? f.x : 0.0f, mask >> (2 * i + 1) & 1 ? f.y : 0.0f);
+        v[i] = pair_of(own.has(2 * i) ? f.x : 0.0f, own.has(2 * i + 1) ? f.y : 0.0f);
       }
       squares[i % 2] = fma2(v[i], v[i], squares[i % 2]);
     }
     squares[0] = add2(squares[0], squares[1]);
     const float rstd = rsqrtf(g.sum(sum_of(squares[0]), slots[g.index][1]) * a.inv_cols + a.eps);
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) v[i] = fma2(mul2(v[i], both(rstd)), gamma[i], beta[i]);
-    store_row<TY, V, FULL>(out, t, mask, v);
+    for (int i = 0; i < OWN / 2; ++i) v[i] = fma2(mul2(v[i], both(rstd)), gamma[i], beta[i]);
+    store_row<TY, V, FULL, OWN>(out, t, own, v);
     if (mean_out) { st_c(mean_out, mean); mean_out += step; }
     if (rstd_out) { st_c(rstd_out, rstd); rstd_out += step; }
     if (--left == 0) break;
@@ -387,15 +414,15 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_forward_kernel(const NormArg
 
 // Backward.  dx needs two sums of a row, taken together; the gradients of gamma and beta are sums over the rows (SUMS),
 // held in registers over all rows of a group, added up over the block's groups and joined by norm_join_kernel.
-template <typename TX, typename TY, int V, bool FULL, int STAGES, bool SUMS, int MAX_THREADS>
-__global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormArgs a) {
-  constexpr int kSums = SUMS ? kPairs : 1;
-  __shared__ __align__(16) float slots[kMostGroups][2][64];
+template <typename TX, typename TY, int V, bool FULL, int OWN, int STAGES, bool SUMS>
+__global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
+  constexpr int kSums = SUMS ? OWN / 2 : 1;
+  __shared__ __align__(16) float slots[kMostGroups][2][32];
   const Group g(a.warps);
   const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space_x = row_space<TX>(V, a.warps, a.cols), space = space_x + row_space<TY>(V, a.warps, a.cols);
+  const uint32_t space_x = row_space<TX>(V, OWN, a.warps, a.cols), space = space_x + row_space<TY>(V, OWN, a.warps, a.cols);
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space, shared_end = shared + STAGES * space;
-  const uint32_t mask = FULL ? 0 : columns_mask<V>(t, a.cols);
+  const Own<V, FULL, OWN> own(t, a.cols);
   const TX* x = static_cast<const TX*>(a.x);
   const TY* dy = static_cast<const TY*>(a.dy);
   const TX* end_x = x + (a.rows - 1) * a.ld_x + a.cols;
@@ -404,11 +431,16 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
   const uint32_t step = gridDim.x * groups;
   if (a.warps > 1) {
     float* zero = &slots[g.index][0][0];
-    for (uint32_t i = t; i < 128; i += threads) zero[i] = 0.0f;
+    for (uint32_t i = t; i < 64; i += threads) zero[i] = 0.0f;
     g.sync();
   }
+#pragma unroll
+  for (int i = 0; i < STAGES; ++i) {
+    clear_row<TX, V, FULL, OWN>(shared + i * space, t, own);
+    clear_row<TY, V, FULL, OWN>(shared + i * space + space_x, t, own);
+  }
   grid_dependency_handshake();
-  Pair gamma[kPairs], dgamma[kSums], dbeta[kSums];
+  Pair gamma[OWN / 2], dgamma[kSums], dbeta[kSums];
 #pragma unroll
   for (int i = 0; i < kSums; ++i) dgamma[i] = dbeta[i] = both(0.0f);
   if (first < a.rows) {
@@ -419,12 +451,12 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
 #pragma unroll
     for (int s = 0; s + 1 < STAGES; ++s) {
       if (first + (uint64_t)s * step < a.rows) {
-        start_row<TX, V, FULL>(shared + s * space, row + s * stride_x, a.cols, t, threads, x, end_x);
-        start_row<TY, V, FULL>(shared + s * space + space_x, drow + s * stride_y, a.cols, t, threads, dy, end_y);
+        start_row<TX, V, FULL, OWN>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end_x);
+        start_row<TY, V, FULL, OWN>(shared + s * space + space_x, drow + s * stride_y, a.cols, t, threads, own, dy, end_y);
       }
       copy_commit();
     }
-    load_weights<V>(a, a.gamma, 1.0f, t, gamma);
+    load_weights<V, OWN>(a, a.gamma, 1.0f, t, gamma);
     uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;
     uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);
     const float* means = a.mean + first;
@@ -432,20 +464,20 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
     float mean_next = ld_c(means), rstd_next = ld_c(rstds);
     for (;;) {
       if (left > STAGES - 1) {
-        start_row<TX, V, FULL>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, x, end_x);
-        start_row<TY, V, FULL>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, threads, dy, end_y);
+        start_row<TX, V, FULL, OWN>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end_x);
+        start_row<TY, V, FULL, OWN>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, threads, own, dy, end_y);
       }
       copy_commit();
       const float mean = mean_next, rstd = rstd_next;
       if (left > 1) { mean_next = ld_c(means += step); rstd_next = ld_c(rstds += step); }
       copy_wait<STAGES - 1>();
       if (V == 1) g.sync();
-      Pair xhat[kPairs], h[kPairs];
-      take_row<TX, V>(here, row, t, mask, xhat);
-      take_row<TY, V>(here + space_x, drow, t, mask, h);
+      Pair xhat[OWN / 2], h[OWN / 2];
+      take_row<TX, V, FULL, OWN>(here, row, t, own, xhat);
+      take_row<TY, V, FULL, OWN>(here + space_x, drow, t, own, h);
       Pair sum[2] = {both(0.0f), both(0.0f)}, along[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
+      for (int i = 0; i < OWN / 2; ++i) {
         xhat[i] = mul2(add2(xhat[i], both(-mean)), both(rstd));  // columns that do not exist: dy = 0, so this counts nowhere
         if (SUMS) {
           dbeta[i % kSums] = add2(dbeta[i % kSums], h[i]);
@@ -462,8 +494,8 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
         turn ^= 1;
         const Pair less = both(-s.x * a.inv_cols), slope = both(-s.y * a.inv_cols);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) h[i] = mul2(fma2(xhat[i], slope, add2(h[i], less)), both(rstd));
-        store_row<TX, V, FULL>(out, t, mask, h);
+        for (int i = 0; i < OWN / 2; ++i) h[i] = mul2(fma2(xhat[i], slope, add2(h[i], less)), both(rstd));
+        store_row<TX, V, FULL, OWN>(out, t, own, h);
       } else if (V == 1) {
         g.sync();  // the row has been read: its place is free
       }
@@ -477,44 +509,44 @@ __global__ void __launch_bounds__(MAX_THREADS) norm_backward_kernel(const NormAr
   }
   if (!SUMS || !a.partials) return;
   float* out = a.partials + (uint64_t)blockIdx.x * 2 * a.cols;
-  if (groups > 1) {  // the block's groups add up their columns one after the other
-    Pair* sums = reinterpret_cast<Pair*>(norm_shared);
-    copy_wait<0>();
-    __syncthreads();
-    for (uint32_t k = 0; k < groups; ++k) {
-      if (g.index == k) {
+  if (groups == 1) {
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-          Pair* p = sums + i * threads + t;  // a place of its own for each pair of the thread's columns
-          Pair* q = p + kPairs * threads;
-          if (k) {
-            dgamma[i % kSums] = add2(*p, dgamma[i % kSums]);
-            dbeta[i % kSums] = add2(*q, dbeta[i % kSums]);
-          }
-          *p = dgamma[i % kSums];
-          *q = dbeta[i % kSums];
-        }
-      }
-      __syncthreads();
+    for (int i = 0; i < OWN; ++i) {
+      const uint32_t c = column_of<V, OWN>(t, i);
+      const float2 d = split(dgamma[i / 2 % kSums]), e = split(dbeta[i / 2 % kSums]);
+      if (c < a.cols) { st_c(out + c, i % 2 ? d.y : d.x); st_c(out + a.cols + c, i % 2 ? e.y : e.x); }
     }
-    if (g.index + 1 != groups) return;
+    return;
   }
-  const bool pairs = V > 1 && FULL;  // both runs of a unit are 16 bytes and more, on 16-byte boundaries
+  // the groups of the block lay their sums side by side in shared memory; all threads add them up, group after group
+  const uint32_t width = a.warps * 32 * OWN;
+  float* sums = reinterpret_cast<float*>(norm_shared);
+  copy_wait<0>();
+  __syncthreads();
+  float* mine = sums + (uint64_t)g.index * 2 * width;
 #pragma unroll
-  for (int i = 0; i < kOwn; i += 4) {
-    if (!pairs) break;
-    const uint32_t c = column_of<V>(t, i);
-    const float2 d0 = split(dgamma[i / 2 % kSums]), d1 = split(dgamma[(i / 2 + 1) % kSums]);
-    const float2 e0 = split(dbeta[i / 2 % kSums]), e1 = split(dbeta[(i / 2 + 1) % kSums]);
-    st_c(reinterpret_cast<float4*>(out + c), make_float4(d0.x, d0.y, d1.x, d1.y));
-    st_c(reinterpret_cast<float4*>(out + a.cols + c), make_float4(e0.x, e0.y, e1.x, e1.y));
+  for (int i = 0; i < OWN / 2; ++i) {
+    const uint32_t c = column_of<V, OWN>(t, 2 * i);
+    if (V > 1) {
+      *reinterpret_cast<Pair*>(mine + c) = dgamma[i % kSums];
+      *reinterpret_cast<Pair*>(mine + width + c) = dbeta[i % kSums];
+    } else {
+      const float2 d = split(dgamma[i % kSums]), e = split(dbeta[i % kSums]);
+      mine[c] = d.x;
+      mine[c + 32] = d.y;
+      mine[width + c] = e.x;
+      mine[width + c + 32] = e.y;
+    }
   }
-  if (pairs) return;
-#pragma unroll
-  for (int i = 0; i < kOwn; ++i) {
-    const uint32_t c = column_of<V>(t, i);
-    const float2 d = split(dgamma[i / 2 % kSums]), e = split(dbeta[i / 2 % kSums]);
-    if (c < a.cols) { st_c(out + c, i % 2 ? d.y : d.x); st_c(out + a.cols + c, i % 2 ? e.y : e.x); }
+  __syncthreads();
+  for (uint32_t c = threadIdx.x; c < a.cols; c += blockDim.x) {
+    float d = 0.0f, e = 0.0f;
+    for (uint32_t k = 0; k < groups; ++k) {
+      d += sums[(uint64_t)k * 2 * width + c];
+      e += sums[(uint64_t)k * 2 * width + width + c];
+    }
+    st_c(out + c, d);
+    st_c(out + a.cols + c, e);
   }
 }
 
