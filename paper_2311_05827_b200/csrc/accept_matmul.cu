@@ -64,28 +64,27 @@ bool result_map(CUtensorMap* map, void* d, int32_t dtype, uint64_t m, uint64_t n
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// How a large product is dealt to the pairs of SMs: see matmul_pair_kernel.
-struct PairShape { uint64_t tiles; unsigned pairs; uint32_t whole, parts, chunks; };
+// ---- more than kFewRows rows: pairs of SMs ----
+constexpr uint64_t kFewRows = 128;
+bool uses_pairs(const accept_matmul_params* p) { return p->k != 0 && p->m > kFewRows; }
 
-// Products of at least this many tiles of 256 x 256 go to the pairs.
-constexpr uint64_t kPairTilesLeast = 60;
+// How a product is dealt to the pairs of SMs: see matmul_pair_kernel.
+struct PairPlan { unsigned nt; uint64_t tiles; unsigned pairs; uint32_t whole, parts, chunks; };
 
-uint64_t pair_tiles(const accept_matmul_params* p) { return (up(p->m, 256) / 256) * (up(p->n, 256) / 256); }
-bool uses_pairs(const accept_matmul_params* p) { return p->k != 0 && pair_tiles(p) >= kPairTilesLeast; }
-
-PairShape pair_shape(const accept_matmul_params* p) {
-  PairShape s{};
-  const uint64_t blocks = up(p->k, 128) / 128;
-  s.tiles = pair_tiles(p);
-  s.pairs = kSms / 2;
-  const uint64_t left = s.tiles % s.pairs;
-  const uint32_t chunks = p->dtype_d == ACCEPT_DTYPE_F32 ? (uint32_t)((blocks + accept::kChunk - 1) / accept::kChunk) : 1;
-  s.chunks = chunks ? chunks : 1;
+// The plan with tiles of 256 x nt, and about how many cycles it takes.
+PairPlan pair_plan(const accept_matmul_params* p, unsigned nt, uint64_t* cycles) {
+  PairPlan s{};
+  const uint64_t blocks = up(p->k, 128) / 128, pairs = kSms / 2;
+  s.nt = nt;
+  s.tiles = (up(p->m, 256) / 256) * (up(p->n, nt) / nt);
+  s.pairs = (unsigned)pairs;
+  const uint64_t left = s.tiles % pairs;
+  s.chunks = p->dtype_d == ACCEPT_DTYPE_F32 ? (uint32_t)((blocks + accept::kChunk - 1) / accept::kChunk) : 1;
   s.parts = 1;
   s.whole = (uint32_t)s.tiles;
   if (left != 0) {
     // cut what is left so that one more round serves it; a part of fewer than 12 blocks of k costs more than it gives
-    uint64_t parts = s.pairs / left;
+    uint64_t parts = pairs / left;
     if (parts > blocks / 12) parts = blocks / 12;
     if (parts > 8) parts = 8;
     if (parts >= 2 && parts >= s.chunks) {
@@ -94,21 +93,39 @@ PairShape pair_shape(const accept_matmul_params* p) {
     }
   }
   if (s.tiles * s.parts < s.pairs) s.pairs = (unsigned)(s.tiles * s.parts);
+  // measured: 545 cycles a block of k and 1300 a tile with 256 columns, 310 and 900 with 128; a cut tile's join 3000
+  const uint64_t block = nt == 256 ? 545 : 310, tile = nt == 256 ? 1300 : 900;
+  *cycles = (s.whole + pairs - 1) / pairs * (blocks * block + tile) + (s.whole < s.tiles ? (blocks + s.parts - 1) / s.parts * block + tile + 3000 : 0);
   return s;
 }
+PairPlan pair_plan(const accept_matmul_params* p) {
+  uint64_t large, small;
+  const PairPlan a = pair_plan(p, 256, &large), b = pair_plan(p, 128, &small);
+  return small < large ? b : a;
+}
 
-size_t pair_arrival_bytes(const PairShape& s) { return (size_t)up(32 * (s.tiles - s.whole), 16); }
-size_t pair_partial_bytes(const PairShape& s) { return (size_t)((s.tiles - s.whole) * s.parts * 256 * 256 * 4); }
+size_t pair_arrival_bytes(const PairPlan& s) { return (size_t)up(32 * (s.tiles - s.whole), 16); }
+size_t pair_partial_bytes(const PairPlan& s) { return (size_t)((s.tiles - s.whole) * s.parts * 256 * s.nt * 4); }
+
+template <int NT>
+cudaError_t launch_pair_kernel(bool single, unsigned pairs, cudaStream_t s, const CUtensorMap& map_a, const CUtensorMap& map_b, const CUtensorMap& map_sa,
+                               const CUtensorMap& map_sb, const CUtensorMap& map_d, const accept::PairArgs& a) {
+  constexpr int kBytes = accept::PairShape<NT>::kSharedBytes;
+  auto fn = single ? accept::matmul_pair_kernel<NT, true> : accept::matmul_pair_kernel<NT, false>;
+  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+  if (err != cudaSuccess) return err;
+  return accept::launch_overlapped_shared(fn, dim3(2 * pairs), accept::kPairThreads, kBytes, s, map_a, map_b, map_sa, map_sb, map_d, a);
+}
 
 accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b, const void* d_b_scale,
                            const MatmulArgs& base, uint8_t* d_ws, cudaStream_t s) {
-  const PairShape shape = pair_shape(p);
+  const PairPlan plan = pair_plan(p);
   accept::PairArgs a{};
   a.bias = base.bias;
   a.d = base.d;
   a.status = base.status;
   a.arrivals = reinterpret_cast<uint32_t*>(d_ws + 16);
-  a.partials = reinterpret_cast<float*>(d_ws + 16 + pair_arrival_bytes(shape));
+  a.partials = reinterpret_cast<float*>(d_ws + 16 + pair_arrival_bytes(plan));
   a.ldd = base.ldd;
   a.dtype_d = base.dtype_d;
   a.accumulate = base.accumulate;
@@ -118,43 +135,44 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
   a.atoms_a = (uint32_t)(up(p->m, 128) / 128);
   a.atoms_b = (uint32_t)(up(p->n, 128) / 128);
   a.tiles_m = (uint32_t)(up(p->m, 256) / 256);
-  a.tiles_n = (uint32_t)(up(p->n, 256) / 256);
-  a.whole = shape.whole;
-  a.parts = shape.parts;
-  a.chunks = shape.chunks;
-  a.instruction = accept::scaled_instruction((uint32_t)p->format_a, (uint32_t)p->format_b, 256, 256);
+  a.tiles_n = (uint32_t)(up(p->n, plan.nt) / plan.nt);
+  a.whole = plan.whole;
+  a.parts = plan.parts;
+  a.chunks = plan.chunks;
+  a.instruction = accept::scaled_instruction((uint32_t)p->format_a, (uint32_t)p->format_b, 256, plan.nt);
   const bool single = p->dtype_d == ACCEPT_DTYPE_F32;
   a.tile_stores = is_aligned(a.d, 16) && a.ldd * value_size(p->dtype_d) % 16 == 0 && (single || !a.accumulate);
+  a.word_stores = is_aligned(a.d, 4) && a.ldd % 2 == 0;
   const uint64_t groups = (a.blocks + 3) / 4;
   CUtensorMap map_a, map_b, map_sa, map_sb, map_d{};
-  if (!operand_map(&map_a, d_a, p->m, p->k, 128) || !operand_map(&map_b, d_b, p->n, p->k, 128) ||
-      !scale_map(&map_sa, d_a_scale, groups * a.atoms_a, 1) || !scale_map(&map_sb, d_b_scale, groups * a.atoms_b, 2) ||
+  if (!operand_map(&map_a, d_a, p->m, p->k, 128) || !operand_map(&map_b, d_b, p->n, p->k, plan.nt / 2) ||
+      !scale_map(&map_sa, d_a_scale, groups * a.atoms_a, 1) || !scale_map(&map_sb, d_b_scale, groups * a.atoms_b, plan.nt / 128) ||
       (a.tile_stores && !result_map(&map_d, a.d, p->dtype_d, p->m, p->n, a.ldd)))
     return ACCEPT_ERR_CUDA;
-  auto fn = single ? accept::matmul_pair_kernel<true> : accept::matmul_pair_kernel<false>;
-  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::kPairSharedBytes) != cudaSuccess) return ACCEPT_ERR_CUDA;
-  if (a.parts > 1 && cudaMemsetAsync(a.arrivals, 0, pair_arrival_bytes(shape), s) != cudaSuccess) return ACCEPT_ERR_CUDA;
-  ACCEPT_LAUNCH(accept::launch_overlapped_shared(fn, dim3(2 * shape.pairs), accept::kMatmulThreads, accept::kPairSharedBytes, s, map_a, map_b, map_sa, map_sb, map_d, a));
+  if (a.parts > 1 && cudaMemsetAsync(a.arrivals, 0, pair_arrival_bytes(plan), s) != cudaSuccess) return ACCEPT_ERR_CUDA;
+  if (plan.nt == 256) ACCEPT_LAUNCH(launch_pair_kernel<256>(single, plan.pairs, s, map_a, map_b, map_sa, map_sb, map_d, a));
+  else ACCEPT_LAUNCH(launch_pair_kernel<128>(single, plan.pairs, s, map_a, map_b, map_sa, map_sb, map_d, a));
   return ACCEPT_OK;
 }
 
-template <int NT, bool TURNED>
-cudaError_t launch_matmul(const CUtensorMap& map_a, const CUtensorMap& map_b, const MatmulArgs& a, unsigned tiles, unsigned parts, cudaStream_t s) {
-  auto fn = accept::matmul_kernel<NT, TURNED>;
-  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::matmul_shared_bytes(NT));
+// ---- few rows ----
+template <int NT>
+cudaError_t launch_few(const CUtensorMap& map_a, const CUtensorMap& map_b, const MatmulArgs& a, unsigned tiles, unsigned parts, cudaStream_t s) {
+  auto fn = accept::matmul_few_kernel<NT>;
+  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::kFewShared);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(tiles, 1, parts);
-  cfg.blockDim = dim3(accept::kMatmulThreads, 1, 1);
-  cfg.dynamicSmemBytes = accept::matmul_shared_bytes(NT);
+  cfg.gridDim = dim3(tiles, parts, 1);
+  cfg.blockDim = dim3(accept::kFewThreads, 1, 1);
+  cfg.dynamicSmemBytes = accept::kFewShared;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = 1;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = parts;
+  attr[1].val.clusterDim.y = parts;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, fn, map_a, map_b, a);
@@ -182,7 +200,7 @@ accept_status accept_matmul_check_params(const accept_matmul_params* p) {
 size_t accept_matmul_workspace_size(const accept_matmul_params* p) {
   if (accept_matmul_check_params(p) != ACCEPT_OK) return 0;
   if (!uses_pairs(p)) return 16;
-  const PairShape s = pair_shape(p);
+  const PairPlan s = pair_plan(p);
   return 16 + (s.parts > 1 ? pair_arrival_bytes(s) + pair_partial_bytes(s) : 0);
 }
 
@@ -208,37 +226,31 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
   a.accumulate = p->accumulate;
   ACCEPT_BOUNDS(s, bounds_list.add(d_bias, 4 * p->n, false); bounds_list.add(d_d, ((p->m - 1) * p->ldd + p->n) * value_size(p->dtype_d), true);
                 bounds_list.add(d_ws, accept_matmul_workspace_size(p), true));
+  a.m = (uint32_t)p->m;
+  a.n = (uint32_t)p->n;
   if (p->k == 0) {
-    a.rows_a = (uint32_t)p->m;
-    a.rows_b = (uint32_t)p->n;
     ACCEPT_LAUNCH(launch_overlapped(accept::matmul_empty_kernel, dim3((unsigned)((p->m * p->n + 255) / 256)), 256, s, a));
     return ACCEPT_OK;
   }
-
   if (uses_pairs(p)) return launch_pairs(p, d_a, d_a_scale, d_b, d_b_scale, a, static_cast<uint8_t*>(d_ws), s);
 
-  const bool turned = p->m <= 128;  // few rows of a: b's rows take the 128 lanes
-  const uint64_t rows_a = turned ? p->n : p->m, rows_b = turned ? p->m : p->n;
-  const unsigned nt = !turned ? 128 : p->m <= 16 ? 16 : p->m <= 32 ? 32 : p->m <= 64 ? 64 : 128;
-  a.scale_a = static_cast<const uint8_t*>(turned ? d_b_scale : d_a_scale);
-  a.scale_b = static_cast<const uint8_t*>(turned ? d_a_scale : d_b_scale);
-  a.rows_a = (uint32_t)rows_a;
-  a.rows_b = (uint32_t)rows_b;
+  const unsigned nt = p->m <= 16 ? 16 : p->m <= 32 ? 32 : p->m <= 64 ? 64 : 128;
+  a.scale_a = static_cast<const uint8_t*>(d_b_scale);
+  a.scale_b = static_cast<const uint8_t*>(d_a_scale);
   a.blocks = (uint32_t)(up(p->k, 128) / 128);
-  a.atoms_a = (uint32_t)(up(rows_a, 128) / 128);
-  a.atoms_b = (uint32_t)(up(rows_b, 128) / 128);
-  a.tiles_a = a.atoms_a;
-  a.instruction = accept::scaled_instruction((uint32_t)(turned ? p->format_b : p->format_a), (uint32_t)(turned ? p->format_a : p->format_b), 128, nt);
+  a.atoms_a = (uint32_t)(up(p->n, 128) / 128);
+  a.atoms_b = 1;
+  a.instruction = accept::scaled_instruction((uint32_t)p->format_b, (uint32_t)p->format_a, 128, nt);
+  a.wide_stores = !a.accumulate && is_aligned(a.d, 4 * value_size(p->dtype_d)) && a.ldd % 4 == 0;
   CUtensorMap map_a, map_b;
-  if (!operand_map(&map_a, turned ? d_b : d_a, rows_a, p->k, 128) || !operand_map(&map_b, turned ? d_a : d_b, rows_b, p->k, nt)) return ACCEPT_ERR_CUDA;
-  const uint64_t tiles = (uint64_t)a.tiles_a * (up(rows_b, nt) / nt);
+  if (!operand_map(&map_a, d_b, p->n, p->k, 128) || !operand_map(&map_b, d_a, p->m, p->k, nt)) return ACCEPT_ERR_CUDA;
+  const unsigned tiles = a.atoms_a;
   unsigned parts = 1;
-  while (parts < 8 && tiles * parts * 2 <= kSms && a.blocks >= parts * 4) parts *= 2;
-  if (!turned) ACCEPT_LAUNCH((launch_matmul<128, false>(map_a, map_b, a, (unsigned)tiles, parts, s)));
-  else if (nt == 16) ACCEPT_LAUNCH((launch_matmul<16, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
-  else if (nt == 32) ACCEPT_LAUNCH((launch_matmul<32, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
-  else if (nt == 64) ACCEPT_LAUNCH((launch_matmul<64, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
-  else ACCEPT_LAUNCH((launch_matmul<128, true>(map_a, map_b, a, (unsigned)tiles, parts, s)));
+  while (parts < 8 && (uint64_t)tiles * parts * 2 <= kSms && a.blocks >= parts * 4) parts *= 2;
+  if (nt == 16) ACCEPT_LAUNCH(launch_few<16>(map_a, map_b, a, tiles, parts, s));
+  else if (nt == 32) ACCEPT_LAUNCH(launch_few<32>(map_a, map_b, a, tiles, parts, s));
+  else if (nt == 64) ACCEPT_LAUNCH(launch_few<64>(map_a, map_b, a, tiles, parts, s));
+  else ACCEPT_LAUNCH(launch_few<128>(map_a, map_b, a, tiles, parts, s));
   return ACCEPT_OK;
 }
 

@@ -9,28 +9,19 @@
 namespace accept {
 
 struct MatmulArgs {
-  const uint8_t* scale_a;  // of the operand on the instruction's M side
-  const uint8_t* scale_b;
+  const uint8_t* scale_a;  // of the operand on the instruction's M side: b's rows, the columns of d
+  const uint8_t* scale_b;  // of a
   const float* bias;       // may be null
   void* d;
   uint32_t* status;
   uint64_t ldd;
-  uint32_t rows_a, rows_b;    // rows of the two operands
+  uint32_t m, n;
   uint32_t blocks;            // ceil(k / 128)
   uint32_t atoms_a, atoms_b;  // groups of 128 rows in the scales
-  uint32_t tiles_a;           // tiles along the M side
   uint32_t instruction;
   int dtype_d, accumulate;
+  int wide_stores;            // four neighbours of d are stored at once (aligned rows, nothing to add)
 };
-
-constexpr int kTileA = 128;      // rows of the M side of a tile: one lane of tensor memory each
-constexpr int kStageBlocks = 6;  // blocks of k in flight
-constexpr int kMatmulThreads = 192;
-
-// Shared memory of a block of threads: stages, each the two operand tiles and 1 KB of scales; the same memory holds the
-// finished tile in fp32 afterwards.
-__host__ __device__ constexpr int stage_bytes(int nt) { return (kTileA + nt) * 128 + 1024; }
-__host__ __device__ constexpr int matmul_shared_bytes(int nt) { return 1024 + kStageBlocks * stage_bytes(nt); }
 
 __device__ __forceinline__ void store_value(void* d, int dtype, uint64_t at, float v, bool accumulate) {
   if (dtype == kF32) {
@@ -44,29 +35,42 @@ __device__ __forceinline__ void store_value(void* d, int dtype, uint64_t at, flo
     st_c(p, __float2half_rn(accumulate ? v + __half2float(ld_c(p)) : v));
   }
 }
+__device__ __forceinline__ uint32_t two_values(int dtype, float x, float y) {  // 16-bit types
+  return dtype == kBf16 ? pair_to_word<__nv_bfloat16>(pair_of(x, y)) : pair_to_word<__half>(pair_of(x, y));
+}
 
-// One tile of 128 rows of the M-side operand by NT rows of the other, over this block's share of k; the blocks of a
-// cluster (z) share k and add their sums in the order of their ranks.  TURNED: the M side is b (few rows of a), the
-// tile's rows are columns of d.
-template <int NT, bool TURNED>
-__global__ void __launch_bounds__(kMatmulThreads) matmul_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                                const MatmulArgs a) {
-  constexpr int kStage = stage_bytes(NT);
-  constexpr int kScaleSlots = 4;             // words of scales in tensor memory, used in turn
-  constexpr uint32_t kColumns = NT <= 32 ? 64 : NT <= 64 ? 128 : 256;  // NT sums and 32 columns of scales, a power of two
-  constexpr uint32_t kScaleColumn = kColumns - 8 * kScaleSlots;
+// ---- few rows of a (at most 128): single tokens and small batches -----------------------------------------------------
+//
+// Bound by the bytes of b.  b's rows take the 128 lanes of the instruction's M side and a's rows its N side (NT = 16 to
+// 128), so nothing is loaded or multiplied for rows that are not there; there are only n / 128 such tiles, so the blocks of
+// a cluster share k, up to eight ways, and add their sums through each other's shared memory in the order of their
+// ranks.  Every block asks for as much of its share of b at once as shared memory holds.
+constexpr int kTileA = 128;
+constexpr int kFewThreads = 192;
+constexpr int kFewShared = 224 * 1024;
+__host__ __device__ constexpr int few_stage_bytes(int nt) { return (kTileA + nt) * 128 + 1024; }  // both tiles and 1 KB of scales
+__host__ __device__ constexpr int few_stages(int nt) { return (kFewShared - 1024) / few_stage_bytes(nt); }
+
+template <int NT>
+__global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                                 const MatmulArgs a) {
+  constexpr int kStage = few_stage_bytes(NT), kStages = few_stages(NT);
+  constexpr int kWords = 4;  // of scales in tensor memory, used in turn
+  static_assert(kStages <= 13, "a word comes round again thirteen blocks on, when the stage says that its products are done");
+  constexpr uint32_t kColumns = NT <= 32 ? 64 : NT <= 64 ? 128 : 256;  // NT sums and the scales, a power of two
+  constexpr uint32_t kScaleColumn = kColumns - 8 * kWords;
   extern __shared__ uint8_t raw_shared[];
-  __shared__ __align__(8) uint64_t barriers[2 * kStageBlocks + 1];
+  __shared__ __align__(8) uint64_t barriers[2 * kStages + 1];
   __shared__ uint32_t tensor_base, failed, issued;
   const uint32_t base = (smem_address(raw_shared) + 1023) & ~1023u;  // 128-byte swizzle repeats every 1024 bytes
-  const uint32_t full = smem_address(barriers), empty = full + 8 * kStageBlocks, done = empty + 8 * kStageBlocks;
+  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t parts = gridDim.z, rank = blockIdx.z;
+  const uint32_t parts = gridDim.y, rank = blockIdx.y;
   const uint32_t first = (uint32_t)((uint64_t)a.blocks * rank / parts), last = (uint32_t)((uint64_t)a.blocks * (rank + 1) / parts);
-  const uint32_t row_a = blockIdx.x % a.tiles_a * kTileA, row_b = blockIdx.x / a.tiles_a * NT;
+  const uint32_t row_a = blockIdx.x * kTileA;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2 * kStageBlocks + 1; ++i) mbarrier_init(full + 8 * i, 1);
+    for (int i = 0; i < 2 * kStages + 1; ++i) mbarrier_init(full + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     failed = issued = 0;
     prefetch_map(&map_a);
@@ -79,72 +83,78 @@ __global__ void __launch_bounds__(kMatmulThreads) matmul_kernel(const __grid_con
   const uint32_t sums = tensor_base;
   grid_dependency_handshake();
 
-  if (warp == 4 && lane == 0) {  // loads
+  if (warp == 4) {  // loads
+    const bool leader = elect_one();
+    uint32_t stage = 0, parity = 1;  // a fresh barrier passes for the phase before its first
     uint32_t b = first;
     for (; b < last; ++b) {
-      const uint32_t i = b - first, stage = i % kStageBlocks, round = i / kStageBlocks;
-      if (round > 0 && !mbarrier_wait(empty + 8 * stage, (round - 1) & 1)) { atomicExch(&failed, 1u); break; }
-      const uint32_t at = base + stage * kStage, bar = full + 8 * stage;
-      const bool scales = i == 0 || (b & 3) == 0;  // a word of scales serves four blocks of k
-      mbarrier_expect_bytes(bar, (kTileA + NT) * 128 + (scales ? 1024 : 0) + kCopyAnnounceExtra);
-      tile_load(at, &map_a, b * 128, row_a, bar);
-      tile_load(at + kTileA * 128, &map_b, b * 128, row_b, bar);
-      if (scales) {
-        bulk_copy_to_shared(at + (kTileA + NT) * 128, a.scale_a + ((uint64_t)(b >> 2) * a.atoms_a + row_a / 128) * 512, 512, bar);
-        bulk_copy_to_shared(at + (kTileA + NT) * 128 + 512, a.scale_b + ((uint64_t)(b >> 2) * a.atoms_b + row_b / 128) * 512, 512, bar);
+      if (!mbarrier_wait_warp(empty + 8 * stage, parity)) break;
+      if (leader) {
+        const uint32_t at = base + stage * kStage, bar = full + 8 * stage;
+        const bool scales = b == first || (b & 3) == 0;  // a word of scales serves four blocks of k
+        mbarrier_expect_bytes(bar, (kTileA + NT) * 128 + (scales ? 1024 : 0) + kCopyAnnounceExtra);
+        tile_load(at, &map_a, b * 128, row_a, bar);
+        tile_load(at + kTileA * 128, &map_b, b * 128, 0, bar);
+        if (scales) {
+          bulk_copy_to_shared(at + (kTileA + NT) * 128, a.scale_a + ((uint64_t)(b >> 2) * a.atoms_a + blockIdx.x) * 512, 512, bar);
+          bulk_copy_to_shared(at + (kTileA + NT) * 128 + 512, a.scale_b + (uint64_t)(b >> 2) * a.atoms_b * 512, 512, bar);
+        }
       }
+      if (++stage == kStages) { stage = 0; parity ^= 1; }
     }
-    issued = b - first;
-  } else if (warp == 5 && lane == 0) {  // matrix instructions
-    uint32_t slot = 0, scale_a = 0, scale_b = 0;
-    bool ok = true;
-    for (uint32_t b = first; b < last && ok; ++b) {
-      const uint32_t i = b - first, stage = i % kStageBlocks, round = i / kStageBlocks;
-      ok = mbarrier_wait(full + 8 * stage, round & 1);
-      if (!ok) break;
+    if (leader) {
+      issued = b - first;
+      if (b < last) atomicExch(&failed, 1u);
+    }
+  } else if (warp == 5) {  // matrix instructions
+    const bool leader = elect_one();
+    const uint32_t tensor = __shfl_sync(0xffffffffu, sums, 0);
+    uint32_t stage = 0, parity = 0, word = kWords - 1, b = first;
+    for (; b < last; ++b) {
+      if (!mbarrier_wait_warp(full + 8 * stage, parity)) break;
       tensor_fence_after();
-      const uint32_t at = base + stage * kStage;
-      if (i == 0 || (b & 3) == 0) {
-        scale_a = sums + kScaleColumn + 8 * slot;
-        scale_b = scale_a + 4;
-        slot = (slot + 1) % kScaleSlots;
-        scale_copy(scale_a, scale_descriptor(at + (kTileA + NT) * 128));
-        scale_copy(scale_b, scale_descriptor(at + (kTileA + NT) * 128 + 512));
-      }
+      // A word of scales serves four blocks of k and comes round again after three others, thirteen blocks after the last
+      // that used it (only a share's first and last word serve fewer); this stage was filled again, so the products of
+      // kStages blocks back are done.
+      const bool fresh = b == first || (b & 3) == 0;
+      if (fresh) word = word + 1 == kWords ? 0 : word + 1;
+      const uint32_t at = base + stage * kStage, scale_a = tensor + kScaleColumn + 8 * word;
       const uint32_t instruction = with_scale_byte(a.instruction, b & 3);
-      const uint64_t da = operand_descriptor(at), db = operand_descriptor(at + kTileA * 128);
+      const uint64_t da = operand_descriptor(at), db = operand_descriptor(at + kTileA * 128), ds = scale_descriptor(at + (kTileA + NT) * 128);
+      if (leader) {
+        if (fresh) {
+          scale_copy(scale_a, ds);
+          scale_copy(scale_a + 4, ds + 32);
+        }
 #pragma unroll
-      for (uint32_t k = 0; k < 4; ++k)  // 32 values of k: 32 bytes further in the swizzled rows
-        scaled_mma(sums, da + 2 * k, db + 2 * k, instruction, scale_a, scale_b + (row_b % 128) / 32, i > 0 || k > 0);
-      mma_commit(empty + 8 * stage);
+        for (uint32_t k = 0; k < 4; ++k)  // 32 values of k: 32 bytes further in the swizzled rows
+          scaled_mma(tensor, da + 2 * k, db + 2 * k, instruction, scale_a, scale_a + 4, b > first || k > 0);
+        mma_commit(empty + 8 * stage);
+      }
+      if (++stage == kStages) { stage = 0; parity ^= 1; }
     }
-    if (ok) mma_commit(done);
-    else atomicExch(&failed, 1u);
+    if (leader) {
+      if (b == last) mma_commit(done);
+      else atomicExch(&failed, 1u);
+    }
   }
   __syncwarp();
 
-  // The finished tile goes through shared memory as fp32, a row of d in a row of it.
-  constexpr int kRows = TURNED ? NT : kTileA, kCols = TURNED ? kTileA : NT, kPitch = TURNED ? kTileA : NT + 4;
+  // The block's sums go through shared memory as fp32, a row of d (a row of a) in 128 floats.
   float* tile = reinterpret_cast<float*>(raw_shared + (base - smem_address(raw_shared)));
   if (warp < 4) {
-    const bool ok = mbarrier_wait(done, 0);
+    const bool ok = mbarrier_wait_warp(done, 0);
     if (!ok) atomicExch(&failed, 1u);
     tensor_fence_after();
     if (ok) {
-      const uint32_t l = warp * 32 + lane;
-#pragma unroll
-      for (int c = 0; c < NT; c += 16) {
-        float v[16];
+      constexpr int kPiece = NT < 32 ? 16 : 32;
+#pragma unroll 1
+      for (uint32_t c = 0; c < NT && c < a.m; c += kPiece) {
+        float v[kPiece];
         tensor_read(sums + ((warp * 32) << 16) + c, v);
         tensor_read_wait();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          if (first == last) v[j] = 0.0f;  // no share of k: nothing was written there
-          if (TURNED) tile[(c + j) * kPitch + l] = v[j];
-        }
-        if (!TURNED)
-#pragma unroll
-          for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(tile + l * kPitch + c + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        for (int j = 0; j < kPiece; ++j) tile[(c + j) * kTileA + warp * 32 + lane] = first == last ? 0.0f : v[j];  // no share of k: nothing was summed
       }
     }
     tensor_fence_before();
@@ -156,45 +166,59 @@ __global__ void __launch_bounds__(kMatmulThreads) matmul_kernel(const __grid_con
     tensor_free(sums, kColumns);
   }
 
-  // Rows of the tile are dealt over the blocks of the cluster; each adds all blocks' sums and stores.
   const bool failure = *reinterpret_cast<volatile uint32_t*>(&failed) != 0;
   if (failure) {
     if (threadIdx.x == 0) {
       atomicOr(a.status, kDevCopyTimeout);
       // no copy of this block may still be on its way when it leaves
-      for (uint32_t i = 0; i < issued && i < kStageBlocks; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kStageBlocks) & 1);
+      for (uint32_t i = 0; i < issued && i < kStages; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kStages) & 1);
     }
   } else {
-    const uint32_t d_rows = TURNED ? a.rows_b : a.rows_a, d_cols = TURNED ? a.rows_a : a.rows_b;
-    const uint32_t row0 = TURNED ? row_b : row_a, col0 = TURNED ? row_a : row_b;
+    // quarter rows (32 columns, eight lanes) are dealt over the cluster's blocks and their warps
     const uint32_t tile_address = smem_address(tile);
-    for (uint32_t r = rank + parts * warp; r < kRows && row0 + r < d_rows; r += parts * (kMatmulThreads / 32)) {
-      for (uint32_t c = 4 * lane; c < kCols && col0 + c < d_cols; c += 128) {
-        float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (uint32_t p = 0; p < parts; ++p) {
-          const uint32_t at = tile_address + 4 * (r * kPitch + c);
-          const float4 v = parts > 1 ? ld_cluster(address_in(at, p)) : *reinterpret_cast<const float4*>(tile + r * kPitch + c);
-          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-        }
-        const float out[4] = {s.x, s.y, s.z, s.w};
+    const uint32_t c = 4 * (lane & 7), col0 = row_a;
+    for (uint32_t q = (rank * (kFewThreads / 32) + warp) * 4 + (lane >> 3); q < 4 * a.m; q += parts * (kFewThreads / 32) * 4) {
+      const uint32_t r = q >> 2, col = col0 + 32 * (q & 3) + c;
+      if (col >= a.n) continue;
+      const uint32_t at = tile_address + 4 * (r * kTileA + 32 * (q & 3) + c);
+      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (parts == 1) {
+        s = *reinterpret_cast<const float4*>(tile + r * kTileA + 32 * (q & 3) + c);
+      } else {
+        float4 v[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t col = col0 + c + j;
-          if (col < d_cols) store_value(a.d, a.dtype_d, (uint64_t)(row0 + r) * a.ldd + col, out[j] + (a.bias ? ld_c(a.bias + col) : 0.0f), a.accumulate);
-        }
+        for (uint32_t p = 0; p < 8; ++p)
+          if (p < parts) v[p] = ld_cluster(address_in(at, p));
+#pragma unroll
+        for (uint32_t p = 0; p < 8; ++p)
+          if (p < parts) { s.x += v[p].x; s.y += v[p].y; s.z += v[p].z; s.w += v[p].w; }
+      }
+      float out[4] = {s.x, s.y, s.z, s.w};
+      if (a.bias)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[j] += col + j < a.n ? ld_c(a.bias + col + j) : 0.0f;
+      const uint64_t to = (uint64_t)r * a.ldd + col;
+      if (a.wide_stores && col + 4 <= a.n) {
+        if (a.dtype_d == kF32) st_c(reinterpret_cast<float4*>(static_cast<float*>(a.d) + to), make_float4(out[0], out[1], out[2], out[3]));
+        else st_c(reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.d) + to), make_uint2(two_values(a.dtype_d, out[0], out[1]), two_values(a.dtype_d, out[2], out[3])));
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (col + j < a.n) store_value(a.d, a.dtype_d, to + j, out[j], a.accumulate);
       }
     }
   }
   if (parts > 1) cluster_sync();  // the other blocks may still be reading this one's tile
 }
 
-// ---- large products: pairs of SMs, tiles of 256 x 256, persistent -----------------------------------------------------
+// ---- more rows: pairs of SMs, tiles of 256 x NT, persistent ---------------------------------------------------------
 //
 // Bound by the tensor cores.  A pair of blocks holds one tile (128 rows of it in each block's tensor memory); each
 // block loads its own 128 rows of a and half of b, so an operand byte in shared memory feeds twice the products it would
 // feed for one SM alone.  Each pair keeps taking units of work; the sums of the next one are formed while the last one's
-// are read.  Two tiles of sums (2 x 256 columns) and the scales do not fit 512 columns side by side, so the two overlap by
-// 24 columns: those are read first, and the next unit's products start once they are.
+// are read.  NT = 256 for large products; two tiles of sums (2 x 256 columns) and the scales do not fit 512 columns side by
+// side, so the two overlap by 24 columns: those are read first, and the next unit's products start once they are.
+// NT = 128 where tiles of 256 would leave pairs without work.
 //
 // A unit is a tile over all of k; the tiles that are left when every pair has had the same number (whole tiles) are cut
 // along k into `parts`, so that all pairs share the last round.  A part's sums go to the workspace; the warp that
@@ -202,21 +226,28 @@ __global__ void __launch_bounds__(kMatmulThreads) matmul_kernel(const __grid_con
 //
 // Sums that go out in fp32 are taken over at most kChunk blocks of k at a time and the chunks added one after the other
 // (in d): the tensor cores' own sums over 16384 values of k are off by 1.1e-6 of the result's norm, over 8192 by 0.8e-6.
-constexpr int kPairTile = 256;
-constexpr int kPairStages = 6;
-constexpr int kPairStageBytes = 2 * 128 * 128;            // 128 rows of a and 128 of b, 128 bytes each
-constexpr int kPairScaleBytes = 512 + 1024;               // scales of 128 rows of a, of 256 of b, four blocks of k
-constexpr int kPairStaging = 4 * 4096;                    // a piece of the result for each of four warps: 32 rows of 128 bytes
-constexpr int kPairSharedBytes = 1024 + kPairStages * (kPairStageBytes + kPairScaleBytes) + kPairStaging + 4 * 4 * kPairTile;  // and each warp's copy of the bias
-constexpr uint32_t kPairScaleColumn = 512 - 2 * 12;            // two words of scales in turn: 4 columns of a, 8 of b each
-constexpr uint32_t kPairSecond = kPairScaleColumn - kPairTile; // where the second tile of sums starts
+constexpr int kPairThreads = 192;
+constexpr uint32_t kPairRows = 256;
 constexpr uint32_t kChunk = 64;
+
+template <int NT>
+struct PairShape {
+  static constexpr int kStages = NT == 256 ? 6 : 8;
+  static constexpr int kOperandBytes = (128 + NT / 2) * 128;             // a block's rows of a and of b, 128 bytes each
+  static constexpr int kScaleBytes = 512 + 4 * NT;                       // scales of 128 rows of a, of NT of b, four blocks of k
+  static constexpr int kStaging = 4 * 4096;                              // a piece of the result for each of four warps
+  static constexpr int kSharedBytes = 1024 + kStages * (kOperandBytes + kScaleBytes) + kStaging + 4 * 4 * NT;  // and each warp's copy of the bias
+  static constexpr uint32_t kWordColumns = 4 + NT / 32;                  // a word of scales in tensor memory: of a, of b
+  static constexpr uint32_t kScaleColumn = 512 - 2 * kWordColumns;       // two words in turn
+  static constexpr uint32_t kSecond = kScaleColumn - NT < (uint32_t)NT ? kScaleColumn - NT : NT;  // the second tile of sums
+  static constexpr bool kOverlap = kSecond < (uint32_t)NT;
+};
 
 struct PairArgs {
   const float* bias;
   void* d;
   uint32_t* status;
-  float* partials;     // parts of cut tiles: (tile, part) x 256 x 256 values
+  float* partials;     // parts of cut tiles: (tile, part) x 256 x NT values
   uint32_t* arrivals;  // eight for each cut tile (two blocks of four warps), zero at the start
   uint64_t ldd;
   uint32_t m, n, blocks;
@@ -228,6 +259,7 @@ struct PairArgs {
   uint32_t instruction;
   int dtype_d, accumulate;
   int tile_stores;     // d is stored through its tensor map (16-byte aligned rows, nothing to add but in fp32)
+  int word_stores;     // rows of a 16-bit d start on 4-byte boundaries
 };
 
 // One accumulation: blocks [first, last) of k of a tile.
@@ -274,75 +306,99 @@ __device__ __forceinline__ bool pair_unit(const PairArgs& a, uint32_t pair, uint
 template <bool SINGLE>
 __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap* map_d, uint8_t* piece, uint32_t piece_address, uint32_t lane,
                                            uint32_t row0, uint32_t col, bool add, uint32_t turn, float (&v)[32]) {
-  if (a.tile_stores) {
-    // row `lane` of the piece, its 16-byte units permuted as the tensor map's swizzle has them
-    if (SINGLE) {
-      if (lane == 0) store_wait_read<0>();
+  if (!SINGLE && !add) {
+    // row `lane` of the piece in 64 bytes, its 16-byte units permuted as the tensor map's swizzle has them; two pieces in turn
+    if (a.tile_stores) {
+      if (lane == 0) store_wait_read<1>();
       __syncwarp();
+    }
+    piece += 2048 * (turn & 1);
+    piece_address += 2048 * (turn & 1);
 #pragma unroll
-      for (uint32_t u = 0; u < 8; ++u)
-        *reinterpret_cast<float4*>(piece + lane * 128 + 16 * (u ^ (lane & 7))) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+    for (uint32_t u = 0; u < 4; ++u) {
+      uint32_t w[4];
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j) w[j] = two_values(a.dtype_d, v[8 * u + 2 * j], v[8 * u + 2 * j + 1]);
+      *reinterpret_cast<uint4*>(piece + lane * 64 + 16 * (u ^ ((lane >> 1) & 3))) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    if (a.tile_stores) {
+      shared_to_async();
+      __syncwarp();
+      if (lane == 0) {
+        if (row0 < a.m && col < a.n) tile_store(map_d, col, row0, piece_address);
+        store_commit();
+      }
+      return;
+    }
+    __syncwarp();
+    const uint32_t rows = row0 < a.m ? min(a.m - row0, 32u) : 0;
+    if (a.word_stores) {  // two rows at a time, a word for each lane
+      const uint32_t c = 2 * (lane & 15), unit = c >> 3, in_unit = 2 * (c & 7);
+      uint16_t* p = static_cast<uint16_t*>(a.d) + (uint64_t)(row0 + (lane >> 4)) * a.ldd + col + c;
+#pragma unroll 4
+      for (uint32_t r = lane >> 4; r < rows; r += 2, p += 2 * a.ldd) {
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(piece + r * 64 + 16 * (unit ^ ((r >> 1) & 3)) + in_unit);
+        if (col + c + 1 < a.n) st_c(reinterpret_cast<uint32_t*>(p), w);
+        else if (col + c < a.n) st_c(p, (uint16_t)w);
+      }
     } else {
-      if (lane == 0) store_wait_read<1>();  // two pieces of 2 KB in turn
-      __syncwarp();
-      piece += 2048 * (turn & 1);
-      piece_address += 2048 * (turn & 1);
-#pragma unroll
-      for (uint32_t u = 0; u < 4; ++u) {
-        uint32_t w[4];
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-          const float x = v[8 * u + 2 * j], y = v[8 * u + 2 * j + 1];
-          if (a.dtype_d == kBf16) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
-            memcpy(&w[j], &h, 4);
-          } else {
-            const __half2 h = __floats2half2_rn(x, y);
-            memcpy(&w[j], &h, 4);
-          }
-        }
-        *reinterpret_cast<uint4*>(piece + lane * 64 + 16 * (u ^ ((lane >> 1) & 3))) = make_uint4(w[0], w[1], w[2], w[3]);
+      uint16_t* p = static_cast<uint16_t*>(a.d) + (uint64_t)row0 * a.ldd + col + lane;
+#pragma unroll 4
+      for (uint32_t r = 0; r < rows; ++r, p += a.ldd) {
+        const uint16_t w = *reinterpret_cast<const uint16_t*>(piece + r * 64 + 16 * ((lane >> 3) ^ ((r >> 1) & 3)) + 2 * (lane & 7));
+        if (col + lane < a.n) st_c(p, w);
       }
     }
+    __syncwarp();
+    return;
+  }
+  // fp32, 128 bytes a row
+  if (SINGLE && a.tile_stores) {
+    if (lane == 0) store_wait_read<0>();
+    __syncwarp();
+  }
+#pragma unroll
+  for (uint32_t u = 0; u < 8; ++u)
+    *reinterpret_cast<float4*>(piece + lane * 128 + 16 * (u ^ (lane & 7))) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
+  if (SINGLE && a.tile_stores) {
     shared_to_async();
     __syncwarp();
     if (lane == 0) {
       if (row0 < a.m && col < a.n) {
-        if (SINGLE && add) tile_add(map_d, col, row0, piece_address);
+        if (add) tile_add(map_d, col, row0, piece_address);
         else tile_store(map_d, col, row0, piece_address);
       }
       store_commit();
     }
-  } else {  // through shared memory so that a row's values leave side by side
-#pragma unroll
-    for (uint32_t u = 0; u < 8; ++u)
-      *reinterpret_cast<float4*>(piece + lane * 128 + 16 * (u ^ (lane & 7))) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
-    __syncwarp();
-    if (col + lane < a.n)
-      for (uint32_t r = 0; r < 32 && row0 + r < a.m; ++r)
-        store_value(a.d, a.dtype_d, (uint64_t)(row0 + r) * a.ldd + col + lane,
-                    *reinterpret_cast<const float*>(piece + r * 128 + 16 * ((lane >> 2) ^ (r & 7)) + 4 * (lane & 3)), add);
-    __syncwarp();
+    return;
   }
+  __syncwarp();
+  if (col + lane < a.n)
+    for (uint32_t r = 0; r < 32 && row0 + r < a.m; ++r)
+      store_value(a.d, a.dtype_d, (uint64_t)(row0 + r) * a.ldd + col + lane,
+                  *reinterpret_cast<const float*>(piece + r * 128 + 16 * ((lane >> 2) ^ (r & 7)) + 4 * (lane & 3)), add);
+  __syncwarp();
 }
 
-template <bool SINGLE>  // d is fp32
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
+template <int NT, bool SINGLE>  // SINGLE: d is fp32
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
     matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                        const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
                        const __grid_constant__ CUtensorMap map_d, const PairArgs a) {
+  using S = PairShape<NT>;
+  constexpr int kStages = S::kStages;
   extern __shared__ uint8_t raw_shared[];
-  __shared__ __align__(8) uint64_t barriers[2 * kPairStages + 3];
+  __shared__ __align__(8) uint64_t barriers[2 * kStages + 4];
   __shared__ uint32_t tensor_base, failed, issued;
   const uint32_t base = (smem_address(raw_shared) + 1023) & ~1023u;
-  const uint32_t scales = base + kPairStages * kPairStageBytes, staging = scales + kPairStages * kPairScaleBytes;
-  const uint32_t full = smem_address(barriers), empty = full + 8 * kPairStages, done = empty + 8 * kPairStages, drained = done + 16;
+  const uint32_t scales = base + kStages * S::kOperandBytes, staging = scales + kStages * S::kScaleBytes;
+  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < 2 * kPairStages + 2; ++i) mbarrier_init(full + 8 * i, 1);
-    mbarrier_init(drained, 8);  // the four reading warps of both blocks
+    for (int i = 0; i < 2 * kStages + 2; ++i) mbarrier_init(full + 8 * i, 1);
+    for (int i = 0; i < 2; ++i) mbarrier_init(drained + 8 * i, 8);  // the four reading warps of both blocks, for each tile of sums
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     failed = issued = 0;
     prefetch_map(&map_a);
@@ -365,21 +421,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
     bool ok = true;
     Unit u;
     for (uint32_t unit = 0; ok && pair_unit(a, pair, pairs, unit, u); ++unit) {
-      const uint32_t row_a = u.tile_m * kPairTile + rank * 128, row_b = u.tile_n * kPairTile + rank * 128;
+      const uint32_t row_a = u.tile_m * kPairRows + rank * 128, row_b = u.tile_n * NT + rank * (NT / 2);
       for (uint32_t b = u.first; b < u.last; ++b, ++i) {
         if (!mbarrier_wait_warp(empty + 8 * stage, parity)) { ok = false; break; }
         if (leader) {
           const bool with_scales = b == u.first || (b & 3) == 0;
-          const uint32_t at = base + stage * kPairStageBytes, at_scales = scales + stage * kPairScaleBytes, bar = full_cluster + 8 * stage;
-          if (rank == 0) mbarrier_expect_bytes(full + 8 * stage, 2 * (kPairStageBytes + (with_scales ? kPairScaleBytes : 0)) + kCopyAnnounceExtra);
+          const uint32_t at = base + stage * S::kOperandBytes, at_scales = scales + stage * S::kScaleBytes, bar = full_cluster + 8 * stage;
+          if (rank == 0) mbarrier_expect_bytes(full + 8 * stage, 2 * (S::kOperandBytes + (with_scales ? S::kScaleBytes : 0)) + kCopyAnnounceExtra);
           pair_tile_load(at, &map_a, b * 128, row_a, bar);
           pair_tile_load(at + 128 * 128, &map_b, b * 128, row_b, bar);
           if (with_scales) {
             pair_tile_load(at_scales, &map_sa, 0, (b >> 2) * a.atoms_a + u.tile_m * 2 + rank, bar);
-            pair_tile_load(at_scales + 512, &map_sb, 0, (b >> 2) * a.atoms_b + u.tile_n * 2, bar);
+            pair_tile_load(at_scales + 512, &map_sb, 0, (b >> 2) * a.atoms_b + u.tile_n * (NT / 128), bar);
           }
         }
-        if (++stage == kPairStages) { stage = 0; parity ^= 1; }
+        if (++stage == kStages) { stage = 0; parity ^= 1; }
       }
     }
     if (leader) {
@@ -394,9 +450,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
     bool ok = true;
     Unit u;
     for (uint32_t unit = 0; ok && pair_unit(a, pair, pairs, unit, u); ++unit) {
-      if (unit > 0 && !mbarrier_wait_warp(drained, (unit - 1) & 1)) { ok = false; break; }
+      // the columns shared with the last unit's sums, or the unit's before that
+      constexpr uint32_t kBack = S::kOverlap ? 1 : 2;
+      if (unit >= kBack && !mbarrier_wait_warp(drained + 8 * ((unit - kBack) & 1), ((unit - kBack) >> 1) & 1)) { ok = false; break; }
       tensor_fence_after();
-      const uint32_t into = tensor + (unit & 1 ? kPairSecond : 0);
+      const uint32_t into = tensor + (unit & 1 ? S::kSecond : 0);
       for (uint32_t b = u.first; b < u.last; ++b) {
         if (!mbarrier_wait_warp(full + 8 * stage, parity)) { ok = false; break; }
         tensor_fence_after();
@@ -405,25 +463,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
           // the products that used this word before must be done (at most five blocks back: that phase is the latest)
           word ^= 1;
           const uint32_t before = word ? used[1] : used[0];
-          if (before != 0 && !mbarrier_wait_warp(empty + 8 * ((before - 1) % kPairStages), ((before - 1) / kPairStages) & 1)) { ok = false; break; }
+          if (before != 0 && !mbarrier_wait_warp(empty + 8 * ((before - 1) % kStages), ((before - 1) / kStages) & 1)) { ok = false; break; }
         }
         ++i;
         if (word) used[1] = i;
         else used[0] = i;
-        const uint32_t at = base + stage * kPairStageBytes, scale_a = tensor + kPairScaleColumn + 12 * word;
+        const uint32_t at = base + stage * S::kOperandBytes, scale_a = tensor + S::kScaleColumn + S::kWordColumns * word;
         const uint32_t instruction = with_scale_byte(a.instruction, b & 3);
-        const uint64_t da = operand_descriptor(at), db = operand_descriptor(at + 128 * 128), ds = scale_descriptor(scales + stage * kPairScaleBytes);
+        const uint64_t da = operand_descriptor(at), db = operand_descriptor(at + 128 * 128), ds = scale_descriptor(scales + stage * S::kScaleBytes);
         if (leader) {
           if (fresh) {
             pair_scale_copy(scale_a, ds);
             pair_scale_copy(scale_a + 4, ds + 32);
-            pair_scale_copy(scale_a + 8, ds + 64);
+            if (NT == 256) pair_scale_copy(scale_a + 8, ds + 64);
           }
 #pragma unroll
           for (uint32_t k = 0; k < 4; ++k) pair_scaled_mma(into, da + 2 * k, db + 2 * k, instruction, scale_a, scale_a + 4, b > u.first || k > 0);
           pair_mma_commit(empty + 8 * stage);
         }
-        if (++stage == kPairStages) { stage = 0; parity ^= 1; }
+        if (++stage == kStages) { stage = 0; parity ^= 1; }
       }
       if (ok && leader) pair_mma_commit(done + 8 * (unit & 1));
     }
@@ -431,34 +489,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
   } else if (warp < 4) {  // results
     const uint32_t piece_address = staging + warp * 4096;
     uint8_t* piece = raw_shared + (piece_address - smem_address(raw_shared));
-    float* bias_tile = reinterpret_cast<float*>(raw_shared + (staging + kPairStaging - smem_address(raw_shared))) + warp * kPairTile;
+    float* bias_tile = reinterpret_cast<float*>(raw_shared + (staging + S::kStaging - smem_address(raw_shared))) + warp * NT;
     const uint32_t drained_at = address_in(drained, 0);
     Unit u;
     for (uint32_t unit = 0; pair_unit(a, pair, pairs, unit, u); ++unit) {
-      const uint32_t row0 = u.tile_m * kPairTile + rank * 128 + warp * 32, col0 = u.tile_n * kPairTile;
+      const uint32_t row0 = u.tile_m * kPairRows + rank * 128 + warp * 32, col0 = u.tile_n * NT;
       const bool with_bias = a.bias && u.chunk == 0;
       if (with_bias) {
         __syncwarp();
-        for (uint32_t c = lane; c < kPairTile; c += 32) bias_tile[c] = col0 + c < a.n ? ld_c(a.bias + col0 + c) : 0.0f;
+        for (uint32_t c = lane; c < NT; c += 32) bias_tile[c] = col0 + c < a.n ? ld_c(a.bias + col0 + c) : 0.0f;
         __syncwarp();
       }
       if (!mbarrier_wait(done + 8 * (unit & 1), (unit >> 1) & 1)) { atomicExch(&failed, 1u); break; }
       tensor_fence_after();
-      const uint32_t from = sums + (unit & 1 ? kPairSecond : 0) + ((warp * 32) << 16);
-      // a cut tile: this warp's 32 x 256 values of each part, as 8 x 8 x 32 pieces of four
-      float4* partial = u.cut == ~0u ? nullptr : reinterpret_cast<float4*>(a.partials) + (((uint64_t)u.cut * a.parts * 2 + rank) * 4 + warp) * 2048;
-      const uint64_t part_stride = 2 * 4 * 2048;
+      const uint32_t from = sums + (unit & 1 ? S::kSecond : 0) + ((warp * 32) << 16);
+      // a cut tile: this warp's 32 x NT values of each part, four neighbours of each lane's row side by side
+      float4* partial = u.cut == ~0u ? nullptr : reinterpret_cast<float4*>(a.partials) + (((uint64_t)u.cut * a.parts * 2 + rank) * 4 + warp) * (8 * NT);
+      const uint64_t part_stride = 2 * 4 * (8 * NT);
       if (u.chunk > 0 && lane == 0) store_wait();  // the chunk before must lie in d
 #pragma unroll 1
-      for (uint32_t turn = 0; turn < 8; ++turn) {  // 32 columns at a time, those shared with the next unit's sums first
-        const uint32_t c = 32 * (unit & 1 ? turn : 7 - turn);
+      for (uint32_t turn = 0; turn < NT / 32; ++turn) {  // 32 columns at a time, those shared with the next unit's sums first
+        const uint32_t c = 32 * (unit & 1 ? turn : NT / 32 - 1 - turn);
         float v[32];
         tensor_read(from + c, v);
         tensor_read_wait();
-        if (turn == 0) {
+        if (turn == (S::kOverlap ? 0 : NT / 32 - 1)) {
           tensor_fence_before();
           __syncwarp();
-          if (lane == 0) mbarrier_arrive_cluster(drained_at);
+          if (lane == 0) mbarrier_arrive_cluster(drained_at + 8 * (unit & 1));
         }
         if (partial) {
 #pragma unroll
@@ -480,7 +538,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
         if (before + 1 == a.parts) {  // all parts are there: add them in their order
           __threadfence();
 #pragma unroll 1
-          for (uint32_t turn = 0; turn < 8; ++turn) {
+          for (uint32_t turn = 0; turn < NT / 32; ++turn) {
             const uint32_t c = 32 * turn;
             float v[32];
 #pragma unroll
@@ -507,7 +565,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
     atomicOr(a.status, kDevCopyTimeout);
     // no copy may still be on its way when a block of the pair leaves
     if (rank == 0)
-      for (uint32_t i = 0; i < issued && i < kPairStages; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kPairStages) & 1);
+      for (uint32_t i = 0; i < issued && i < kStages; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kStages) & 1);
   }
   tensor_fence_before();
   cluster_sync();
@@ -518,8 +576,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kMatmulThreads)
 // k = 0: the sum is empty.
 __global__ void __launch_bounds__(256) matmul_empty_kernel(const MatmulArgs a) {
   grid_dependency_handshake();
-  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = i / a.rows_b, col = i % a.rows_b;
-  if (row < a.rows_a) store_value(a.d, a.dtype_d, row * a.ldd + col, a.bias ? ld_c(a.bias + col) : 0.0f, a.accumulate);
+  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = i / a.n, col = i % a.n;
+  if (row < a.m) store_value(a.d, a.dtype_d, row * a.ldd + col, a.bias ? ld_c(a.bias + col) : 0.0f, a.accumulate);
 }
 
 }  // namespace accept
