@@ -367,7 +367,8 @@ typedef struct {
 
 accept_status accept_matmul_check_params(const accept_matmul_params* p);
 size_t accept_matmul_workspace_size(const accept_matmul_params* p);
-/* bias: n fp32 values, or NULL.  d_ws: 16-byte aligned.  The status word gets ACCEPT_DEV_COPY_TIMEOUT if a wait inside the kernel ran out. */
+/* bias: n fp32 values, or NULL.  d_ws: 16-byte aligned; zero before its first use by this entry point and after a call
+ * whose status word is not zero (calls leave it ready for the next, of any sizes).  The status word gets ACCEPT_DEV_COPY_TIMEOUT if a wait inside the kernel ran out. */
 accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b,
                                   const void* d_b_scale, const float* d_bias, void* d_d, void* d_ws, size_t ws_bytes,
                                   void* cuda_stream);

@@ -68,6 +68,10 @@ bool result_map(CUtensorMap* map, void* d, int32_t dtype, uint64_t m, uint64_t n
 constexpr uint64_t kFewRows = 128;
 bool uses_pairs(const accept_matmul_params* p) { return p->k != 0 && p->m > kFewRows; }
 
+// Arrival counts at the start of the workspace, for 73 cut tiles of 16 warps at most: a fixed place, so that calls of
+// different sizes can share a workspace.
+constexpr size_t kArrivalBytes = 74 * 64;
+
 // How a product is dealt to the pairs of SMs: see matmul_pair_kernel.
 struct PairPlan { unsigned nt; uint64_t tiles; unsigned pairs; uint32_t whole, parts, chunks; };
 
@@ -82,20 +86,22 @@ PairPlan pair_plan(const accept_matmul_params* p, unsigned nt, uint64_t* cycles)
   s.chunks = p->dtype_d == ACCEPT_DTYPE_F32 ? (uint32_t)((blocks + accept::kChunk - 1) / accept::kChunk) : 1;
   s.parts = 1;
   s.whole = (uint32_t)s.tiles;
-  if (left != 0) {
-    // cut what is left so that one more round serves it; a part of fewer than 12 blocks of k costs more than it gives
-    uint64_t parts = pairs / left;
-    if (parts > blocks / 12) parts = blocks / 12;
-    if (parts > 8) parts = 8;
-    if (parts >= 2 && parts >= s.chunks) {
+  // Measured at 16 to 128 blocks of k, one to four rounds: a block of k takes about 600 cycles with 256 columns and 480
+  // with 128 (whose operands' way into the SM binds it), a tile 2500 and 1500 more, the join of a cut tile 11000.
+  const uint64_t block = nt == 256 ? 600 : 480, tile = nt == 256 ? 2500 : 1500, join = 11000;
+  uint64_t last = left ? blocks * block + tile : 0;
+  if (left != 0) {  // cut what is left so that all pairs share the last round, where the join costs less than that saves
+    const uint64_t most = nt == 256 ? 8 : 6;  // parts that the join has room for
+    for (uint64_t parts = s.chunks < 2 ? 2 : s.chunks; parts <= most && parts * left <= pairs && parts <= blocks; ++parts) {
+      const uint64_t cost = (blocks + parts - 1) / parts * block + tile + join;
+      if (cost >= last) continue;
+      last = cost;
       s.parts = (uint32_t)parts;
       s.whole = (uint32_t)(s.tiles - left);
     }
   }
   if (s.tiles * s.parts < s.pairs) s.pairs = (unsigned)(s.tiles * s.parts);
-  // measured: 545 cycles a block of k and 1300 a tile with 256 columns, 310 and 900 with 128; a cut tile's join 3000
-  const uint64_t block = nt == 256 ? 545 : 310, tile = nt == 256 ? 1300 : 900;
-  *cycles = (s.whole + pairs - 1) / pairs * (blocks * block + tile) + (s.whole < s.tiles ? (blocks + s.parts - 1) / s.parts * block + tile + 3000 : 0);
+  *cycles = s.tiles / pairs * (blocks * block + tile) + last;
   return s;
 }
 PairPlan pair_plan(const accept_matmul_params* p) {
@@ -104,7 +110,6 @@ PairPlan pair_plan(const accept_matmul_params* p) {
   return small < large ? b : a;
 }
 
-size_t pair_arrival_bytes(const PairPlan& s) { return (size_t)up(32 * (s.tiles - s.whole), 16); }
 size_t pair_partial_bytes(const PairPlan& s) { return (size_t)((s.tiles - s.whole) * s.parts * 256 * s.nt * 4); }
 
 template <int NT>
@@ -114,7 +119,7 @@ cudaError_t launch_pair_kernel(bool single, unsigned pairs, cudaStream_t s, cons
   auto fn = single ? accept::matmul_pair_kernel<NT, true> : accept::matmul_pair_kernel<NT, false>;
   const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
   if (err != cudaSuccess) return err;
-  return accept::launch_overlapped_shared(fn, dim3(2 * pairs), accept::kPairThreads, kBytes, s, map_a, map_b, map_sa, map_sb, map_d, a);
+  return accept::launch_overlapped_shared(fn, dim3(2 * pairs), accept::PairShape<NT>::kThreads, kBytes, s, map_a, map_b, map_sa, map_sb, map_d, a);
 }
 
 accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b, const void* d_b_scale,
@@ -125,7 +130,7 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
   a.d = base.d;
   a.status = base.status;
   a.arrivals = reinterpret_cast<uint32_t*>(d_ws + 16);
-  a.partials = reinterpret_cast<float*>(d_ws + 16 + pair_arrival_bytes(plan));
+  a.partials = reinterpret_cast<float*>(d_ws + 16 + kArrivalBytes);
   a.ldd = base.ldd;
   a.dtype_d = base.dtype_d;
   a.accumulate = base.accumulate;
@@ -149,7 +154,6 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
       !scale_map(&map_sa, d_a_scale, groups * a.atoms_a, 1) || !scale_map(&map_sb, d_b_scale, groups * a.atoms_b, plan.nt / 128) ||
       (a.tile_stores && !result_map(&map_d, a.d, p->dtype_d, p->m, p->n, a.ldd)))
     return ACCEPT_ERR_CUDA;
-  if (a.parts > 1 && cudaMemsetAsync(a.arrivals, 0, pair_arrival_bytes(plan), s) != cudaSuccess) return ACCEPT_ERR_CUDA;
   if (plan.nt == 256) ACCEPT_LAUNCH(launch_pair_kernel<256>(single, plan.pairs, s, map_a, map_b, map_sa, map_sb, map_d, a));
   else ACCEPT_LAUNCH(launch_pair_kernel<128>(single, plan.pairs, s, map_a, map_b, map_sa, map_sb, map_d, a));
   return ACCEPT_OK;
@@ -201,7 +205,7 @@ size_t accept_matmul_workspace_size(const accept_matmul_params* p) {
   if (accept_matmul_check_params(p) != ACCEPT_OK) return 0;
   if (!uses_pairs(p)) return 16;
   const PairPlan s = pair_plan(p);
-  return 16 + (s.parts > 1 ? pair_arrival_bytes(s) + pair_partial_bytes(s) : 0);
+  return 16 + (s.parts > 1 ? kArrivalBytes + pair_partial_bytes(s) : 0);
 }
 
 accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b,

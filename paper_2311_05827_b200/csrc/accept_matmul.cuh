@@ -221,26 +221,30 @@ __global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_co
 // NT = 128 where tiles of 256 would leave pairs without work.
 //
 // A unit is a tile over all of k; the tiles that are left when every pair has had the same number (whole tiles) are cut
-// along k into `parts`, so that all pairs share the last round.  A part's sums go to the workspace; the warp that
-// is the last to bring its 32 rows of a tile adds all parts in their order.  No block waits for another pair.
+// along k into `parts`, so that all pairs share the last round: one part at most for each pair, its last unit.  A part's
+// sums go to the workspace; the warp that is the last to bring its rows and columns of a tile fetches the other parts' sums
+// into the shared memory that the operands have left and adds all parts in their order.  No block waits for another pair.
 //
 // Sums that go out in fp32 are taken over at most kChunk blocks of k at a time and the chunks added one after the other
 // (in d): the tensor cores' own sums over 16384 values of k are off by 1.1e-6 of the result's norm, over 8192 by 0.8e-6.
-constexpr int kPairThreads = 192;
 constexpr uint32_t kPairRows = 256;
 constexpr uint32_t kChunk = 64;
 
 template <int NT>
 struct PairShape {
-  static constexpr int kStages = NT == 256 ? 6 : 8;
+  static constexpr int kReaders = NT == 256 ? 4 : 8;                     // warps that read sums: two share 32 rows where tiles are small
+  static constexpr int kThreads = 32 * (kReaders + 2);
+  static constexpr int kStages = NT == 256 ? 6 : 7;
   static constexpr int kOperandBytes = (128 + NT / 2) * 128;             // a block's rows of a and of b, 128 bytes each
   static constexpr int kScaleBytes = 512 + 4 * NT;                       // scales of 128 rows of a, of NT of b, four blocks of k
-  static constexpr int kStaging = 4 * 4096;                              // a piece of the result for each of four warps
-  static constexpr int kSharedBytes = 1024 + kStages * (kOperandBytes + kScaleBytes) + kStaging + 4 * 4 * NT;  // and each warp's copy of the bias
+  static constexpr int kStaging = kReaders * 4096;                       // a piece of the result for each of those warps
+  static constexpr int kSharedBytes = 1024 + kStages * (kOperandBytes + kScaleBytes) + kStaging + kReaders * 4 * NT;  // and each warp's copy of the bias
   static constexpr uint32_t kWordColumns = 4 + NT / 32;                  // a word of scales in tensor memory: of a, of b
   static constexpr uint32_t kScaleColumn = 512 - 2 * kWordColumns;       // two words in turn
   static constexpr uint32_t kSecond = kScaleColumn - NT < (uint32_t)NT ? kScaleColumn - NT : NT;  // the second tile of sums
   static constexpr bool kOverlap = kSecond < (uint32_t)NT;
+  // pieces of other parts' sums (32 rows x 32 columns, 4 KB) that a reading warp can have in shared memory at the end
+  static constexpr uint32_t kSlots = kStages * kOperandBytes / kReaders / 4096;
 };
 
 struct PairArgs {
@@ -248,7 +252,7 @@ struct PairArgs {
   void* d;
   uint32_t* status;
   float* partials;     // parts of cut tiles: (tile, part) x 256 x NT values
-  uint32_t* arrivals;  // eight for each cut tile (two blocks of four warps), zero at the start
+  uint32_t* arrivals;  // one for each reading warp of both blocks and each cut tile; zero, and zero again after the call
   uint64_t ldd;
   uint32_t m, n, blocks;
   uint32_t atoms_a, atoms_b;
@@ -381,24 +385,25 @@ __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap*
 }
 
 template <int NT, bool SINGLE>  // SINGLE: d is fp32
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThreads)
     matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                        const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
                        const __grid_constant__ CUtensorMap map_d, const PairArgs a) {
   using S = PairShape<NT>;
-  constexpr int kStages = S::kStages;
+  constexpr int kStages = S::kStages, kReaders = S::kReaders, kShare = kReaders / 4;  // warps that share 32 rows
   extern __shared__ uint8_t raw_shared[];
-  __shared__ __align__(8) uint64_t barriers[2 * kStages + 4];
+  __shared__ __align__(8) uint64_t barriers[2 * kStages + 4 + kReaders];
   __shared__ uint32_t tensor_base, failed, issued;
   const uint32_t base = (smem_address(raw_shared) + 1023) & ~1023u;
   const uint32_t scales = base + kStages * S::kOperandBytes, staging = scales + kStages * S::kScaleBytes;
-  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16;
+  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16, joined = drained + 16;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2 * kStages + 2; ++i) mbarrier_init(full + 8 * i, 1);
-    for (int i = 0; i < 2; ++i) mbarrier_init(drained + 8 * i, 8);  // the four reading warps of both blocks, for each tile of sums
+    for (int i = 0; i < 2; ++i) mbarrier_init(drained + 8 * i, S::kOverlap ? 8 : 2 * kReaders);  // warps of both blocks that read what is waited for
+    for (int i = 0; i < kReaders; ++i) mbarrier_init(joined + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     failed = issued = 0;
     prefetch_map(&map_a);
@@ -414,7 +419,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
   const uint32_t sums = tensor_base;
   grid_dependency_handshake();
 
-  if (warp == 4) {  // loads, in both blocks; the even block's barrier counts the bytes of both
+  if (warp == kReaders) {  // loads, in both blocks; the even block's barrier counts the bytes of both
     const bool leader = elect_one();
     const uint32_t full_cluster = address_in(full, 0);
     uint32_t i = 0, stage = 0, parity = 1;  // a fresh barrier passes for the phase before its first
@@ -442,7 +447,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
       issued = i;
       if (!ok) atomicExch(&failed, 1u);
     }
-  } else if (warp == 5 && rank == 0) {  // matrix instructions, for both blocks
+  } else if (warp == kReaders + 1 && rank == 0) {  // matrix instructions, for both blocks
     const bool leader = elect_one();
     const uint32_t tensor = __shfl_sync(0xffffffffu, sums, 0);
     uint32_t i = 0, stage = 0, parity = 0, word = 0;
@@ -486,14 +491,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
       if (ok && leader) pair_mma_commit(done + 8 * (unit & 1));
     }
     if (!ok && leader) atomicExch(&failed, 1u);
-  } else if (warp < 4) {  // results
+  } else if (warp < kReaders) {  // results
     const uint32_t piece_address = staging + warp * 4096;
     uint8_t* piece = raw_shared + (piece_address - smem_address(raw_shared));
     float* bias_tile = reinterpret_cast<float*>(raw_shared + (staging + S::kStaging - smem_address(raw_shared))) + warp * NT;
     const uint32_t drained_at = address_in(drained, 0);
     Unit u;
     for (uint32_t unit = 0; pair_unit(a, pair, pairs, unit, u); ++unit) {
-      const uint32_t row0 = u.tile_m * kPairRows + rank * 128 + warp * 32, col0 = u.tile_n * NT;
+      const uint32_t row0 = u.tile_m * kPairRows + rank * 128 + (warp & 3) * 32, col0 = u.tile_n * NT;
       const bool with_bias = a.bias && u.chunk == 0;
       if (with_bias) {
         __syncwarp();
@@ -502,18 +507,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
       }
       if (!mbarrier_wait(done + 8 * (unit & 1), (unit >> 1) & 1)) { atomicExch(&failed, 1u); break; }
       tensor_fence_after();
-      const uint32_t from = sums + (unit & 1 ? S::kSecond : 0) + ((warp * 32) << 16);
+      const uint32_t from = sums + (unit & 1 ? S::kSecond : 0) + (((warp & 3) * 32) << 16);
       // a cut tile: this warp's 32 x NT values of each part, four neighbours of each lane's row side by side
-      float4* partial = u.cut == ~0u ? nullptr : reinterpret_cast<float4*>(a.partials) + (((uint64_t)u.cut * a.parts * 2 + rank) * 4 + warp) * (8 * NT);
+      float4* partial = u.cut == ~0u ? nullptr : reinterpret_cast<float4*>(a.partials) + (((uint64_t)u.cut * a.parts * 2 + rank) * 4 + (warp & 3)) * (8 * NT);
       const uint64_t part_stride = 2 * 4 * (8 * NT);
       if (u.chunk > 0 && lane == 0) store_wait();  // the chunk before must lie in d
 #pragma unroll 1
-      for (uint32_t turn = 0; turn < NT / 32; ++turn) {  // 32 columns at a time, those shared with the next unit's sums first
-        const uint32_t c = 32 * (unit & 1 ? turn : NT / 32 - 1 - turn);
+      for (uint32_t turn = warp >> 2; turn < NT / 32; turn += kShare) {  // 32 columns at a time, those shared with the next unit's sums first
+        const uint32_t c = 32 * (unit & 1 || !S::kOverlap ? turn : NT / 32 - 1 - turn);
         float v[32];
         tensor_read(from + c, v);
         tensor_read_wait();
-        if (turn == (S::kOverlap ? 0 : NT / 32 - 1)) {
+        if (S::kOverlap ? turn == 0 : turn + kShare >= NT / 32) {
           tensor_fence_before();
           __syncwarp();
           if (lane == 0) mbarrier_arrive_cluster(drained_at + 8 * (unit & 1));
@@ -526,38 +531,67 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads)
           if (with_bias)
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += bias_tile[c + j];
-          pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate || u.chunk > 0, turn, v);
+          pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate || u.chunk > 0, turn / kShare, v);
         }
       }
       if (partial) {
         __threadfence();
         __syncwarp();
         uint32_t before = 0;
-        if (lane == 0) before = atomicAdd(a.arrivals + (u.cut * 2 + rank) * 4 + warp, 1u);
+        // counts from 0 to parts - 1 and back to 0
+        if (lane == 0) before = atomicInc(a.arrivals + (u.cut * 2 + rank) * kReaders + warp, a.parts - 1);
         before = __shfl_sync(0xffffffffu, before, 0);
-        if (before + 1 == a.parts) {  // all parts are there: add them in their order
+        if (before + 1 == a.parts) {  // all parts are there: add them in their order, this one's from tensor memory
           __threadfence();
-#pragma unroll 1
-          for (uint32_t turn = 0; turn < NT / 32; ++turn) {
-            const uint32_t c = 32 * turn;
-            float v[32];
+          asm volatile("fence.proxy.async;" ::: "memory");
+          const uint32_t others = a.parts - 1, batch = S::kSlots / others, slots = base + warp * S::kSlots * 4096, bar = joined + 8 * warp;
+          const uint32_t pieces = (NT / 32 - (warp >> 2) + kShare - 1) / kShare;
+          bool landed = true;
+          for (uint32_t start = 0, phase = 0; start < pieces && landed; start += batch, phase ^= 1) {
+            const uint32_t stop = min(start + batch, pieces);
+            __syncwarp();
+            if (lane == 0) {
+              mbarrier_expect_bytes(bar, (stop - start) * others * 4096 + kCopyAnnounceExtra);
+              for (uint32_t i = start; i < stop; ++i)
+                for (uint32_t o = 0; o < others; ++o)
+                  bulk_copy_to_shared(slots + ((i - start) * others + o) * 4096, partial + (o + (o >= u.part)) * part_stride + 8 * ((warp >> 2) + i * kShare) * 32, 4096, bar);
+            }
+            landed = mbarrier_wait_warp(bar, phase);
+            for (uint32_t i = start; i < stop && landed; ++i) {
+              const uint32_t c = 32 * ((warp >> 2) + i * kShare);
+              float own[32], v[32];
+              tensor_read(from + c, own);
+              tensor_read_wait();
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = 0.0f;
-            for (uint32_t p = 0; p < a.parts; ++p)
+              for (int j = 0; j < 32; ++j) v[j] = u.part == 0 ? own[j] : 0.0f;
+              for (uint32_t o = 0; o < others; ++o) {
+                if (o == u.part && o > 0)
 #pragma unroll
-              for (uint32_t j = 0; j < 8; ++j) {
-                const float4 w = ld_c(partial + p * part_stride + (c / 4 + j) * 32 + lane);
-                v[4 * j] += w.x; v[4 * j + 1] += w.y; v[4 * j + 2] += w.z; v[4 * j + 3] += w.w;
+                  for (int j = 0; j < 32; ++j) v[j] += own[j];
+                const float4* w = reinterpret_cast<const float4*>(raw_shared + (slots + ((i - start) * others + o) * 4096 - smem_address(raw_shared))) + lane;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                  const float4 f = w[32 * j];
+                  v[4 * j] += f.x; v[4 * j + 1] += f.y; v[4 * j + 2] += f.z; v[4 * j + 3] += f.w;
+                }
               }
-            if (with_bias)
+              if (u.part == others)
 #pragma unroll
-              for (int j = 0; j < 32; ++j) v[j] += bias_tile[c + j];
-            pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate, turn, v);
+                for (int j = 0; j < 32; ++j) v[j] += own[j];
+              if (with_bias)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) v[j] += bias_tile[c + j];
+              pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate, i, v);
+            }
+          }
+          if (!landed) {
+            if (lane == 0) atomicExch(&failed, 1u);
+            break;
           }
         }
       }
     }
-    if (lane == 0) store_wait();
+    if (lane == 0) store_wait_read<0>();  // the block may leave: its shared memory has been read
   }
   __syncwarp();
   __syncthreads();
