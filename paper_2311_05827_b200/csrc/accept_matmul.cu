@@ -64,10 +64,7 @@ bool result_map(CUtensorMap* map, void* d, int32_t dtype, uint64_t m, uint64_t n
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// ---- more than kFewRows rows: pairs of SMs ----
-constexpr uint64_t kFewRows = 128;
-bool uses_pairs(const accept_matmul_params* p) { return p->k != 0 && p->m > kFewRows; }
-
+// ---- large products: pairs of SMs ----
 // Arrival counts at the start of the workspace, for 73 cut tiles of 16 warps at most: a fixed place, so that calls of
 // different sizes can share a workspace.
 constexpr size_t kArrivalBytes = 74 * 64;
@@ -108,6 +105,27 @@ PairPlan pair_plan(const accept_matmul_params* p) {
   uint64_t large, small;
   const PairPlan a = pair_plan(p, 256, &large), b = pair_plan(p, 128, &small);
   return small < large ? b : a;
+}
+
+// ---- small products: a block for each tile of 128 x 128 (or 128 x m), or a cluster of blocks that share its k ----
+uint64_t small_tiles(const accept_matmul_params* p) { return (up(p->m, 128) / 128) * (up(p->n, 128) / 128); }
+unsigned small_parts(const accept_matmul_params* p) {
+  unsigned parts = 1;
+  while (parts < 8 && small_tiles(p) * parts * 2 <= kSms && up(p->k, 128) / 128 >= parts * 4) parts *= 2;
+  return parts;
+}
+
+// Products of up to 128 rows, whose bytes bind them, are small; others where one block for each tile does them sooner than
+// the pairs.  Measured: 7500 cycles and 700 a block of k (where all SMs ask for operands; their way into the SM binds it)
+// against 10000 and the plan's (1000 x 2048 x 1544: 9.0 us against 9.7; 237 x 270 x 171: 5.2 against 6.4).
+bool uses_pairs(const accept_matmul_params* p) {
+  if (p->k == 0 || p->m <= 128) return false;
+  if (small_tiles(p) > kSms) return true;
+  uint64_t large, small;
+  pair_plan(p, 256, &large);
+  pair_plan(p, 128, &small);
+  const uint64_t parts = small_parts(p), blocks = up(p->k, 128) / 128;
+  return 7500 + (blocks + parts - 1) / parts * 700 > 10000 + (small < large ? small : large);
 }
 
 size_t pair_partial_bytes(const PairPlan& s) { return (size_t)((s.tiles - s.whole) * s.parts * 256 * s.nt * 4); }
@@ -159,16 +177,15 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
   return ACCEPT_OK;
 }
 
-// ---- few rows ----
 template <int NT>
-cudaError_t launch_few(const CUtensorMap& map_a, const CUtensorMap& map_b, const MatmulArgs& a, unsigned tiles, unsigned parts, cudaStream_t s) {
-  auto fn = accept::matmul_few_kernel<NT>;
-  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::kFewShared);
+cudaError_t launch_small(const CUtensorMap& map_a, const CUtensorMap& map_b, const MatmulArgs& a, unsigned tiles, unsigned parts, cudaStream_t s) {
+  auto fn = accept::matmul_small_kernel<NT>;
+  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::kSmallShared);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(tiles, parts, 1);
-  cfg.blockDim = dim3(accept::kFewThreads, 1, 1);
-  cfg.dynamicSmemBytes = accept::kFewShared;
+  cfg.blockDim = dim3(accept::kSmallThreads, 1, 1);
+  cfg.dynamicSmemBytes = accept::kSmallShared;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -243,18 +260,18 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
   a.scale_b = static_cast<const uint8_t*>(d_a_scale);
   a.blocks = (uint32_t)(up(p->k, 128) / 128);
   a.atoms_a = (uint32_t)(up(p->n, 128) / 128);
-  a.atoms_b = 1;
+  a.atoms_b = (uint32_t)(up(p->m, 128) / 128);
+  a.tiles = a.atoms_a;
   a.instruction = accept::scaled_instruction((uint32_t)p->format_b, (uint32_t)p->format_a, 128, nt);
   a.wide_stores = !a.accumulate && is_aligned(a.d, 4 * value_size(p->dtype_d)) && a.ldd % 4 == 0;
   CUtensorMap map_a, map_b;
   if (!operand_map(&map_a, d_b, p->n, p->k, 128) || !operand_map(&map_b, d_a, p->m, p->k, nt)) return ACCEPT_ERR_CUDA;
-  const unsigned tiles = a.atoms_a;
-  unsigned parts = 1;
-  while (parts < 8 && (uint64_t)tiles * parts * 2 <= kSms && a.blocks >= parts * 4) parts *= 2;
-  if (nt == 16) ACCEPT_LAUNCH(launch_few<16>(map_a, map_b, a, tiles, parts, s));
-  else if (nt == 32) ACCEPT_LAUNCH(launch_few<32>(map_a, map_b, a, tiles, parts, s));
-  else if (nt == 64) ACCEPT_LAUNCH(launch_few<64>(map_a, map_b, a, tiles, parts, s));
-  else ACCEPT_LAUNCH(launch_few<128>(map_a, map_b, a, tiles, parts, s));
+  const unsigned tiles = a.tiles * (unsigned)(up(p->m, nt) / nt);
+  const unsigned parts = small_parts(p);
+  if (nt == 16) ACCEPT_LAUNCH(launch_small<16>(map_a, map_b, a, tiles, parts, s));
+  else if (nt == 32) ACCEPT_LAUNCH(launch_small<32>(map_a, map_b, a, tiles, parts, s));
+  else if (nt == 64) ACCEPT_LAUNCH(launch_small<64>(map_a, map_b, a, tiles, parts, s));
+  else ACCEPT_LAUNCH(launch_small<128>(map_a, map_b, a, tiles, parts, s));
   return ACCEPT_OK;
 }
 

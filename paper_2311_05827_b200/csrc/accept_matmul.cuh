@@ -18,43 +18,100 @@ struct MatmulArgs {
   uint32_t m, n;
   uint32_t blocks;            // ceil(k / 128)
   uint32_t atoms_a, atoms_b;  // groups of 128 rows in the scales
+  uint32_t tiles;             // along n
   uint32_t instruction;
   int dtype_d, accumulate;
   int wide_stores;            // four neighbours of d are stored at once (aligned rows, nothing to add)
 };
 
-__device__ __forceinline__ void store_value(void* d, int dtype, uint64_t at, float v, bool accumulate) {
-  if (dtype == kF32) {
-    float* p = static_cast<float*>(d) + at;
-    st_c(p, accumulate ? v + ld_c(p) : v);
-  } else if (dtype == kBf16) {
-    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(d) + at;
-    st_c(p, __float2bfloat16_rn(accumulate ? v + __bfloat162float(ld_c(p)) : v));
-  } else {
-    __half* p = static_cast<__half*>(d) + at;
-    st_c(p, __float2half_rn(accumulate ? v + __half2float(ld_c(p)) : v));
-  }
+__device__ __forceinline__ float load_value(const void* d, int dtype, uint64_t at) {
+  if (dtype == kF32) return ld_c(static_cast<const float*>(d) + at);
+  if (dtype == kBf16) return __bfloat162float(ld_c(static_cast<const __nv_bfloat16*>(d) + at));
+  return __half2float(ld_c(static_cast<const __half*>(d) + at));
+}
+__device__ __forceinline__ void store_value(void* d, int dtype, uint64_t at, float v) {
+  if (dtype == kF32) st_c(static_cast<float*>(d) + at, v);
+  else if (dtype == kBf16) st_c(static_cast<__nv_bfloat16*>(d) + at, __float2bfloat16_rn(v));
+  else st_c(static_cast<__half*>(d) + at, __float2half_rn(v));
 }
 __device__ __forceinline__ uint32_t two_values(int dtype, float x, float y) {  // 16-bit types
   return dtype == kBf16 ? pair_to_word<__nv_bfloat16>(pair_of(x, y)) : pair_to_word<__half>(pair_of(x, y));
 }
 
-// ---- few rows of a (at most 128): single tokens and small batches -----------------------------------------------------
+// ---- small products: single tokens, small batches, few tiles ---------------------------------------------------------
 //
-// Bound by the bytes of b.  b's rows take the 128 lanes of the instruction's M side and a's rows its N side (NT = 16 to
-// 128), so nothing is loaded or multiplied for rows that are not there; there are only n / 128 such tiles, so the blocks of
-// a cluster share k, up to eight ways, and add their sums through each other's shared memory in the order of their
-// ranks.  Every block asks for as much of its share of b at once as shared memory holds.
+// Bound by the bytes of b, or by the time of a launch.  b's rows take the 128 lanes of the instruction's M side and a's rows
+// its N side (NT = 16 to 128), so nothing is loaded or multiplied for rows that are not there.  Where there are few tiles
+// the blocks of a cluster share k, up to eight ways, and add their sums through each other's shared memory in the order of
+// their ranks.  Every block asks for as much of its share at once as shared memory holds.
 constexpr int kTileA = 128;
-constexpr int kFewThreads = 192;
-constexpr int kFewShared = 224 * 1024;
-__host__ __device__ constexpr int few_stage_bytes(int nt) { return (kTileA + nt) * 128 + 1024; }  // both tiles and 1 KB of scales
-__host__ __device__ constexpr int few_stages(int nt) { return (kFewShared - 1024) / few_stage_bytes(nt); }
+constexpr int kSmallReaders = 8;  // warps that read the sums: two share 32 lanes
+constexpr int kSmallThreads = 32 * (kSmallReaders + 2);
+constexpr int kSmallShared = 224 * 1024;
+__host__ __device__ constexpr int small_stage_bytes(int nt) { return (kTileA + nt) * 128 + 1024; }  // both tiles and 1 KB of scales
+__host__ __device__ constexpr int small_stages(int nt) { return (kSmallShared - 1024) / small_stage_bytes(nt); }
+
+// The finished rows to d, dealt over the cluster's blocks and their warps; several rows' reads are on their way at once.
+template <bool WIDE, uint32_t PARTS>
+__device__ __forceinline__ void small_store(const MatmulArgs& a, uint32_t tile, uint32_t col0, uint32_t row0, uint32_t rows, uint32_t rank,
+                                            uint32_t warp, uint32_t lane) {
+  constexpr uint32_t kWarps = kSmallThreads / 32, kAtOnce = PARTS < 4 ? 4 : 2, kPartsAtOnce = PARTS < 4 ? PARTS : 4;
+  const uint32_t c = WIDE ? 4 * lane : lane, stride = PARTS * kWarps;
+  float bias[4];
+#pragma unroll
+  for (uint32_t j = 0; j < 4; ++j) {
+    const uint32_t col = col0 + c + j * (WIDE ? 1 : 32);
+    bias[j] = a.bias && col < a.n ? ldg_c(a.bias + col) : 0.0f;
+  }
+  for (uint32_t r0 = rank * kWarps + warp; r0 < rows; r0 += kAtOnce * stride) {
+    float4 v[kAtOnce];
+#pragma unroll
+    for (uint32_t i = 0; i < kAtOnce; ++i) v[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (uint32_t p = 0; p < PARTS; p += kPartsAtOnce) {
+      float4 f[kPartsAtOnce][kAtOnce];
+#pragma unroll
+      for (uint32_t q = 0; q < kPartsAtOnce; ++q) {
+        const uint32_t from = address_in(tile, p + q);
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) {
+          const uint32_t at = from + 4 * (min(r0 + i * stride, rows - 1) * kTileA + c);  // rows past the last are read and dropped
+          if (WIDE) f[q][i] = ld_cluster(at);
+          else f[q][i] = make_float4(ld_cluster_one(at), ld_cluster_one(at + 128), ld_cluster_one(at + 256), ld_cluster_one(at + 384));
+        }
+      }
+#pragma unroll
+      for (uint32_t q = 0; q < kPartsAtOnce; ++q)
+#pragma unroll
+        for (uint32_t i = 0; i < kAtOnce; ++i) { v[i].x += f[q][i].x; v[i].y += f[q][i].y; v[i].z += f[q][i].z; v[i].w += f[q][i].w; }
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kAtOnce; ++i) {
+      const uint32_t r = r0 + i * stride;
+      if (r >= rows) break;
+      const uint64_t to = (uint64_t)(row0 + r) * a.ldd + col0 + c;
+      const float out[4] = {v[i].x + bias[0], v[i].y + bias[1], v[i].z + bias[2], v[i].w + bias[3]};
+      if (WIDE) {
+        if (a.dtype_d == kF32) st_c(reinterpret_cast<float4*>(static_cast<float*>(a.d) + to), make_float4(out[0], out[1], out[2], out[3]));
+        else st_c(reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.d) + to), make_uint2(two_values(a.dtype_d, out[0], out[1]), two_values(a.dtype_d, out[2], out[3])));
+      } else {
+        float old[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (a.accumulate)
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j)
+            if (col0 + c + 32 * j < a.n) old[j] = load_value(a.d, a.dtype_d, to + 32 * j);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+          if (col0 + c + 32 * j < a.n) store_value(a.d, a.dtype_d, to + 32 * j, a.accumulate ? out[j] + old[j] : out[j]);
+      }
+    }
+  }
+}
 
 template <int NT>
-__global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+__global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                  const MatmulArgs a) {
-  constexpr int kStage = few_stage_bytes(NT), kStages = few_stages(NT);
+  constexpr int kStage = small_stage_bytes(NT), kStages = small_stages(NT);
   constexpr int kWords = 4;  // of scales in tensor memory, used in turn
   static_assert(kStages <= 13, "a word comes round again thirteen blocks on, when the stage says that its products are done");
   constexpr uint32_t kColumns = NT <= 32 ? 64 : NT <= 64 ? 128 : 256;  // NT sums and the scales, a power of two
@@ -67,7 +124,8 @@ __global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_co
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t parts = gridDim.y, rank = blockIdx.y;
   const uint32_t first = (uint32_t)((uint64_t)a.blocks * rank / parts), last = (uint32_t)((uint64_t)a.blocks * (rank + 1) / parts);
-  const uint32_t row_a = blockIdx.x * kTileA;
+  const uint32_t tile_b = blockIdx.x / a.tiles, tile_a = blockIdx.x - tile_b * a.tiles;
+  const uint32_t row_a = tile_a * kTileA, row_b = tile_b * NT, rows = min(a.m - row_b, (uint32_t)NT);
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2 * kStages + 1; ++i) mbarrier_init(full + 8 * i, 1);
@@ -83,7 +141,7 @@ __global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_co
   const uint32_t sums = tensor_base;
   grid_dependency_handshake();
 
-  if (warp == 4) {  // loads
+  if (warp == kSmallReaders) {  // loads
     const bool leader = elect_one();
     uint32_t stage = 0, parity = 1;  // a fresh barrier passes for the phase before its first
     uint32_t b = first;
@@ -94,10 +152,10 @@ __global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_co
         const bool scales = b == first || (b & 3) == 0;  // a word of scales serves four blocks of k
         mbarrier_expect_bytes(bar, (kTileA + NT) * 128 + (scales ? 1024 : 0) + kCopyAnnounceExtra);
         tile_load(at, &map_a, b * 128, row_a, bar);
-        tile_load(at + kTileA * 128, &map_b, b * 128, 0, bar);
+        tile_load(at + kTileA * 128, &map_b, b * 128, row_b, bar);
         if (scales) {
-          bulk_copy_to_shared(at + (kTileA + NT) * 128, a.scale_a + ((uint64_t)(b >> 2) * a.atoms_a + blockIdx.x) * 512, 512, bar);
-          bulk_copy_to_shared(at + (kTileA + NT) * 128 + 512, a.scale_b + (uint64_t)(b >> 2) * a.atoms_b * 512, 512, bar);
+          bulk_copy_to_shared(at + (kTileA + NT) * 128, a.scale_a + ((uint64_t)(b >> 2) * a.atoms_a + tile_a) * 512, 512, bar);
+          bulk_copy_to_shared(at + (kTileA + NT) * 128 + 512, a.scale_b + ((uint64_t)(b >> 2) * a.atoms_b + tile_b) * 512, 512, bar);  // NT < 128: one tile
         }
       }
       if (++stage == kStages) { stage = 0; parity ^= 1; }
@@ -106,7 +164,7 @@ __global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_co
       issued = b - first;
       if (b < last) atomicExch(&failed, 1u);
     }
-  } else if (warp == 5) {  // matrix instructions
+  } else if (warp == kSmallReaders + 1) {  // matrix instructions
     const bool leader = elect_one();
     const uint32_t tensor = __shfl_sync(0xffffffffu, sums, 0);
     uint32_t stage = 0, parity = 0, word = kWords - 1, b = first;
@@ -142,19 +200,19 @@ __global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_co
 
   // The block's sums go through shared memory as fp32, a row of d (a row of a) in 128 floats.
   float* tile = reinterpret_cast<float*>(raw_shared + (base - smem_address(raw_shared)));
-  if (warp < 4) {
+  if (warp < kSmallReaders) {
     const bool ok = mbarrier_wait_warp(done, 0);
     if (!ok) atomicExch(&failed, 1u);
     tensor_fence_after();
     if (ok) {
       constexpr int kPiece = NT < 32 ? 16 : 32;
 #pragma unroll 1
-      for (uint32_t c = 0; c < NT && c < a.m; c += kPiece) {
+      for (uint32_t c = kPiece * (warp >> 2); c < rows; c += 2 * kPiece) {
         float v[kPiece];
-        tensor_read(sums + ((warp * 32) << 16) + c, v);
+        tensor_read(sums + (((warp & 3) * 32) << 16) + c, v);
         tensor_read_wait();
 #pragma unroll
-        for (int j = 0; j < kPiece; ++j) tile[(c + j) * kTileA + warp * 32 + lane] = first == last ? 0.0f : v[j];  // no share of k: nothing was summed
+        for (int j = 0; j < kPiece; ++j) tile[(c + j) * kTileA + (warp & 3) * 32 + lane] = first == last ? 0.0f : v[j];  // no share of k: nothing was summed
       }
     }
     tensor_fence_before();
@@ -174,39 +232,13 @@ __global__ void __launch_bounds__(kFewThreads) matmul_few_kernel(const __grid_co
       for (uint32_t i = 0; i < issued && i < kStages; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kStages) & 1);
     }
   } else {
-    // quarter rows (32 columns, eight lanes) are dealt over the cluster's blocks and their warps
-    const uint32_t tile_address = smem_address(tile);
-    const uint32_t c = 4 * (lane & 7), col0 = row_a;
-    for (uint32_t q = (rank * (kFewThreads / 32) + warp) * 4 + (lane >> 3); q < 4 * a.m; q += parts * (kFewThreads / 32) * 4) {
-      const uint32_t r = q >> 2, col = col0 + 32 * (q & 3) + c;
-      if (col >= a.n) continue;
-      const uint32_t at = tile_address + 4 * (r * kTileA + 32 * (q & 3) + c);
-      float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (parts == 1) {
-        s = *reinterpret_cast<const float4*>(tile + r * kTileA + 32 * (q & 3) + c);
-      } else {
-        float4 v[8];
-#pragma unroll
-        for (uint32_t p = 0; p < 8; ++p)
-          if (p < parts) v[p] = ld_cluster(address_in(at, p));
-#pragma unroll
-        for (uint32_t p = 0; p < 8; ++p)
-          if (p < parts) { s.x += v[p].x; s.y += v[p].y; s.z += v[p].z; s.w += v[p].w; }
-      }
-      float out[4] = {s.x, s.y, s.z, s.w};
-      if (a.bias)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) out[j] += col + j < a.n ? ld_c(a.bias + col + j) : 0.0f;
-      const uint64_t to = (uint64_t)r * a.ldd + col;
-      if (a.wide_stores && col + 4 <= a.n) {
-        if (a.dtype_d == kF32) st_c(reinterpret_cast<float4*>(static_cast<float*>(a.d) + to), make_float4(out[0], out[1], out[2], out[3]));
-        else st_c(reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.d) + to), make_uint2(two_values(a.dtype_d, out[0], out[1]), two_values(a.dtype_d, out[2], out[3])));
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (col + j < a.n) store_value(a.d, a.dtype_d, to + j, out[j], a.accumulate);
-      }
-    }
+    // wide: a lane has four neighbours of a row; otherwise four columns 32 apart, so that a row leaves in runs
+    const bool wide = a.wide_stores && row_a + kTileA <= a.n;
+    const uint32_t at = smem_address(tile);
+    if (parts == 1) wide ? small_store<true, 1>(a, at, row_a, row_b, rows, rank, warp, lane) : small_store<false, 1>(a, at, row_a, row_b, rows, rank, warp, lane);
+    else if (parts == 2) wide ? small_store<true, 2>(a, at, row_a, row_b, rows, rank, warp, lane) : small_store<false, 2>(a, at, row_a, row_b, rows, rank, warp, lane);
+    else if (parts == 4) wide ? small_store<true, 4>(a, at, row_a, row_b, rows, rank, warp, lane) : small_store<false, 4>(a, at, row_a, row_b, rows, rank, warp, lane);
+    else wide ? small_store<true, 8>(a, at, row_a, row_b, rows, rank, warp, lane) : small_store<false, 8>(a, at, row_a, row_b, rows, rank, warp, lane);
   }
   if (parts > 1) cluster_sync();  // the other blocks may still be reading this one's tile
 }
@@ -377,10 +409,21 @@ __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap*
     return;
   }
   __syncwarp();
-  if (col + lane < a.n)
-    for (uint32_t r = 0; r < 32 && row0 + r < a.m; ++r)
-      store_value(a.d, a.dtype_d, (uint64_t)(row0 + r) * a.ldd + col + lane,
-                  *reinterpret_cast<const float*>(piece + r * 128 + 16 * ((lane >> 2) ^ (r & 7)) + 4 * (lane & 3)), add);
+  if (col + lane < a.n) {
+    const uint32_t rows = row0 < a.m ? min(a.m - row0, 32u) : 0;
+    uint64_t at = (uint64_t)row0 * a.ldd + col + lane;
+    for (uint32_t r = 0; r < rows; r += 8) {  // eight rows' old values are on their way at once
+      float old[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) old[j] = add && r + j < rows ? load_value(a.d, a.dtype_d, at + j * a.ldd) : 0.0f;
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) {
+        const float x = *reinterpret_cast<const float*>(piece + (r + j) * 128 + 16 * ((lane >> 2) ^ ((r + j) & 7)) + 4 * (lane & 3));
+        if (r + j < rows) store_value(a.d, a.dtype_d, at + j * a.ldd, add ? x + old[j] : x);
+      }
+      at += 8 * a.ldd;
+    }
+  }
   __syncwarp();
 }
 
@@ -611,7 +654,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
 __global__ void __launch_bounds__(256) matmul_empty_kernel(const MatmulArgs a) {
   grid_dependency_handshake();
   const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = i / a.n, col = i % a.n;
-  if (row < a.m) store_value(a.d, a.dtype_d, row * a.ldd + col, a.bias ? ld_c(a.bias + col) : 0.0f, a.accumulate);
+  if (row < a.m) {
+    const float v = a.bias ? ld_c(a.bias + col) : 0.0f;
+    store_value(a.d, a.dtype_d, row * a.ldd + col, a.accumulate ? v + load_value(a.d, a.dtype_d, row * a.ldd + col) : v);
+  }
 }
 
 }  // namespace accept

@@ -237,36 +237,55 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, float absen
   return to_float(ld_c(static_cast<const __half*>(w) + c));
 }
 
-// gamma or beta for this thread's columns: read once for all rows that it takes.
-template <int V, int OWN>
-__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
+// gamma or beta for this thread's columns: read once for all rows that it takes, all loads on their way at once.
+template <typename T, int V, bool FULL, int OWN>
+__device__ __forceinline__ void load_weights_of(const T* w, bool whole, const Own<V, FULL, OWN>& own, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
+  w += column_of<V, OWN>(t, 0);
+  if (V > 1 && FULL && whole) {
+    uint4 raw[OWN * sizeof(T) / 16];
+    constexpr int kEach = 16 / (int)sizeof(T), kOf = V >= kEach ? V / kEach : 1;  // values of a load, loads of a unit
+    if constexpr (V >= kEach) {
 #pragma unroll
-  for (int i = 0; i < OWN; i += V) {
-    const uint32_t c = column_of<V, OWN>(t, i);
-    if (V > 1 && w && a.whole_weights && c + V <= a.cols) {
+      for (int i = 0; i < OWN / kEach; ++i) raw[i] = ld_c(reinterpret_cast<const uint4*>(w + i / kOf * (32 * V) + i % kOf * kEach));
+    } else {  // units of four 16-bit values
 #pragma unroll
-      for (int j = 0; j < V; j += 4) {
-        Pair lo, hi;
-        if (a.dtype_w == kF32) {
-          const float4 f = ld_c(reinterpret_cast<const float4*>(static_cast<const float*>(w) + c + j));
-          lo = pair_of(f.x, f.y);
-          hi = pair_of(f.z, f.w);
-        } else {
-          const uint2 raw = ld_c(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(w) + c + j));
-          lo = a.dtype_w == kBf16 ? word_to_pair<__nv_bfloat16>(raw.x) : word_to_pair<__half>(raw.x);
-          hi = a.dtype_w == kBf16 ? word_to_pair<__nv_bfloat16>(raw.y) : word_to_pair<__half>(raw.y);
-        }
-        v[(i + j) / 2 % (OWN / 2)] = lo;
-        v[((i + j) / 2 + 1) % (OWN / 2)] = hi;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const float f = c + j < a.cols ? weight_at(w, a.dtype_w, absent, c + j) : absent;
-        if ((i + j) % 2) v[(i + j) / 2] = pair_of(split(v[(i + j) / 2]).x, f);
-        else v[(i + j) / 2] = both(f);
+      for (int i = 0; i < OWN / V; i += 2) {
+        const uint2 lo = ld_c(reinterpret_cast<const uint2*>(w + i * (32 * V))), hi = ld_c(reinterpret_cast<const uint2*>(w + (i + 1) * (32 * V)));
+        raw[i / 2] = make_uint4(lo.x, lo.y, hi.x, hi.y);
       }
     }
+#pragma unroll
+    for (int i = 0; i < OWN / kEach; ++i) {
+      if constexpr (sizeof(T) == 4) {
+        v[2 * i] = pair_of(__uint_as_float(raw[i].x), __uint_as_float(raw[i].y));
+        v[2 * i + 1] = pair_of(__uint_as_float(raw[i].z), __uint_as_float(raw[i].w));
+      } else {
+        v[4 * i] = word_to_pair<T>(raw[i].x);
+        v[4 * i + 1] = word_to_pair<T>(raw[i].y);
+        v[4 * i + 2] = word_to_pair<T>(raw[i].z);
+        v[4 * i + 3] = word_to_pair<T>(raw[i].w);
+      }
+    }
+  } else {
+    T raw[OWN];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i)
+      if (own.has(i)) raw[i] = ld_c(w + i / V * (32 * V) + i % V);
+#pragma unroll
+    for (int i = 0; i < OWN; i += 2) v[i / 2] = pair_of(own.has(i) ? to_float(raw[i]) : absent, own.has(i + 1) ? to_float(raw[i + 1]) : absent);
+  }
+}
+template <int V, bool FULL, int OWN>
+__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, const Own<V, FULL, OWN>& own, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
+  if (!w) {
+#pragma unroll
+    for (int i = 0; i < OWN / 2; ++i) v[i] = both(absent);
+  } else if (a.dtype_w == kF32) {
+    load_weights_of<float, V, FULL, OWN>(static_cast<const float*>(w), a.whole_weights, own, absent, t, v);
+  } else if (a.dtype_w == kBf16) {
+    load_weights_of<__nv_bfloat16, V, FULL, OWN>(static_cast<const __nv_bfloat16*>(w), a.whole_weights, own, absent, t, v);
+  } else {
+    load_weights_of<__half, V, FULL, OWN>(static_cast<const __half*>(w), a.whole_weights, own, absent, t, v);
   }
 }
 
@@ -367,8 +386,8 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a) {
     copy_commit();
   }
   Pair gamma[OWN / 2], beta[OWN / 2];
-  load_weights<V, OWN>(a, a.gamma, 1.0f, t, gamma);
-  load_weights<V, OWN>(a, a.beta, 0.0f, t, beta);
+  load_weights<V, FULL, OWN>(a, a.gamma, own, 1.0f, t, gamma);
+  load_weights<V, FULL, OWN>(a, a.beta, own, 0.0f, t, beta);
   uint32_t here = shared, ahead = shared + (STAGES - 1) * space;  // where this row lies, and where the one to start goes
   uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);  // rows of this group from this one on
   float* mean_out = a.mean_out && t == 0 ? a.mean_out + first : nullptr;
@@ -456,7 +475,7 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
       }
       copy_commit();
     }
-    load_weights<V, OWN>(a, a.gamma, 1.0f, t, gamma);
+    load_weights<V, FULL, OWN>(a, a.gamma, own, 1.0f, t, gamma);
     uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;
     uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);
     const float* means = a.mean + first;
