@@ -50,17 +50,17 @@ bool scale_map(CUtensorMap* map, const void* scales, uint64_t atoms, uint32_t bo
                 CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Pieces of 32 x 32 values of d, each row a swizzle span (64 bytes for 16-bit types, 128 for fp32).
+// Pieces of 32 rows of 64 bytes of d, the span of the swizzle.
 bool result_map(CUtensorMap* map, void* d, int32_t dtype, uint64_t m, uint64_t n, uint64_t ldd) {
   const EncodeFn encode = tensor_map_encoder();
   if (!encode) return false;
   const cuuint64_t dims[2] = {n, m}, strides[1] = {ldd * value_size(dtype)};
-  const cuuint32_t box[2] = {32, 32}, steps[2] = {1, 1};
+  const cuuint32_t box[2] = {64 / (cuuint32_t)value_size(dtype), 32}, steps[2] = {1, 1};
   const CUtensorMapDataType type = dtype == ACCEPT_DTYPE_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                                    : dtype == ACCEPT_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                                 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
   return encode(map, type, 2, d, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                dtype == ACCEPT_DTYPE_F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -88,7 +88,7 @@ PairPlan pair_plan(const accept_matmul_params* p, unsigned nt, uint64_t* cycles)
   const uint64_t block = nt == 256 ? 600 : 480, tile = nt == 256 ? 2500 : 1500, join = 11000;
   uint64_t last = left ? blocks * block + tile : 0;
   if (left != 0) {  // cut what is left so that all pairs share the last round, where the join costs less than that saves
-    const uint64_t most = nt == 256 ? 8 : 6;  // parts that the join has room for
+    const uint64_t most = 6;  // parts that the join has room for
     for (uint64_t parts = s.chunks < 2 ? 2 : s.chunks; parts <= most && parts * left <= pairs && parts <= blocks; ++parts) {
       const uint64_t cost = (blocks + parts - 1) / parts * block + tile + join;
       if (cost >= last) continue;

@@ -264,17 +264,18 @@ constexpr uint32_t kChunk = 64;
 
 template <int NT>
 struct PairShape {
-  static constexpr int kReaders = NT == 256 ? 4 : 8;                     // warps that read sums: two share 32 rows where tiles are small
+  static constexpr int kReaders = 8;                                     // warps that read sums: two share 32 rows
   static constexpr int kThreads = 32 * (kReaders + 2);
-  static constexpr int kStages = NT == 256 ? 6 : 7;
+  static constexpr int kStages = NT == 256 ? 6 : 8;
   static constexpr int kOperandBytes = (128 + NT / 2) * 128;             // a block's rows of a and of b, 128 bytes each
   static constexpr int kScaleBytes = 512 + 4 * NT;                       // scales of 128 rows of a, of NT of b, four blocks of k
-  static constexpr int kStaging = kReaders * 4096;                       // a piece of the result for each of those warps
+  static constexpr int kStaging = kReaders * 2048;                       // a piece of the result for each of those warps: 32 rows of 64 bytes
   static constexpr int kSharedBytes = 1024 + kStages * (kOperandBytes + kScaleBytes) + kStaging + kReaders * 4 * NT;  // and each warp's copy of the bias
   static constexpr uint32_t kWordColumns = 4 + NT / 32;                  // a word of scales in tensor memory: of a, of b
   static constexpr uint32_t kScaleColumn = 512 - 2 * kWordColumns;       // two words in turn
   static constexpr uint32_t kSecond = kScaleColumn - NT < (uint32_t)NT ? kScaleColumn - NT : NT;  // the second tile of sums
   static constexpr bool kOverlap = kSecond < (uint32_t)NT;
+  static_assert(kStages * kScaleBytes % 1024 == 0, "the pieces lie on the boundaries that the tensor map's swizzle counts from");
   // pieces of other parts' sums (32 rows x 32 columns, 4 KB) that a reading warp can have in shared memory at the end
   static constexpr uint32_t kSlots = kStages * kOperandBytes / kReaders / 4096;
 };
@@ -338,40 +339,40 @@ __device__ __forceinline__ bool pair_unit(const PairArgs& a, uint32_t pair, uint
   return true;
 }
 
-// 32 columns of a warp's 32 rows to d.  `piece`: the warp's 4 KB of shared memory.
+// 32 columns of a warp's 32 rows to d, through the warp's 2 KB of shared memory (`piece`): 32 rows of 64 bytes, 16-byte units
+// permuted as the tensor map's swizzle has them.
 template <bool SINGLE>
 __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap* map_d, uint8_t* piece, uint32_t piece_address, uint32_t lane,
-                                           uint32_t row0, uint32_t col, bool add, uint32_t turn, float (&v)[32]) {
+                                           uint32_t row0, uint32_t col, bool add, float (&v)[32]) {
+  const uint32_t rows = row0 < a.m ? min(a.m - row0, 32u) : 0;
+  uint8_t* mine = piece + lane * 64;
+  const uint32_t swap = (lane >> 1) & 3;
   if (!SINGLE && !add) {
-    // row `lane` of the piece in 64 bytes, its 16-byte units permuted as the tensor map's swizzle has them; two pieces in turn
     if (a.tile_stores) {
-      if (lane == 0) store_wait_read<1>();
+      if (lane == 0) store_wait_read<0>();
       __syncwarp();
     }
-    piece += 2048 * (turn & 1);
-    piece_address += 2048 * (turn & 1);
 #pragma unroll
     for (uint32_t u = 0; u < 4; ++u) {
       uint32_t w[4];
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j) w[j] = two_values(a.dtype_d, v[8 * u + 2 * j], v[8 * u + 2 * j + 1]);
-      *reinterpret_cast<uint4*>(piece + lane * 64 + 16 * (u ^ ((lane >> 1) & 3))) = make_uint4(w[0], w[1], w[2], w[3]);
+      *reinterpret_cast<uint4*>(mine + 16 * (u ^ swap)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
     if (a.tile_stores) {
       shared_to_async();
       __syncwarp();
       if (lane == 0) {
-        if (row0 < a.m && col < a.n) tile_store(map_d, col, row0, piece_address);
+        if (rows && col < a.n) tile_store(map_d, col, row0, piece_address);
         store_commit();
       }
       return;
     }
     __syncwarp();
-    const uint32_t rows = row0 < a.m ? min(a.m - row0, 32u) : 0;
     if (a.word_stores) {  // two rows at a time, a word for each lane
       const uint32_t c = 2 * (lane & 15), unit = c >> 3, in_unit = 2 * (c & 7);
       uint16_t* p = static_cast<uint16_t*>(a.d) + (uint64_t)(row0 + (lane >> 4)) * a.ldd + col + c;
-#pragma unroll 4
+#pragma unroll 8
       for (uint32_t r = lane >> 4; r < rows; r += 2, p += 2 * a.ldd) {
         const uint32_t w = *reinterpret_cast<const uint32_t*>(piece + r * 64 + 16 * (unit ^ ((r >> 1) & 3)) + in_unit);
         if (col + c + 1 < a.n) st_c(reinterpret_cast<uint32_t*>(p), w);
@@ -379,7 +380,7 @@ __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap*
       }
     } else {
       uint16_t* p = static_cast<uint16_t*>(a.d) + (uint64_t)row0 * a.ldd + col + lane;
-#pragma unroll 4
+#pragma unroll 8
       for (uint32_t r = 0; r < rows; ++r, p += a.ldd) {
         const uint16_t w = *reinterpret_cast<const uint16_t*>(piece + r * 64 + 16 * ((lane >> 3) ^ ((r >> 1) & 3)) + 2 * (lane & 7));
         if (col + lane < a.n) st_c(p, w);
@@ -388,43 +389,51 @@ __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap*
     __syncwarp();
     return;
   }
-  // fp32, 128 bytes a row
-  if (SINGLE && a.tile_stores) {
-    if (lane == 0) store_wait_read<0>();
+  // in fp32, sixteen columns at a time
+#pragma unroll
+  for (uint32_t half = 0; half < 32; half += 16) {
+    if (SINGLE && a.tile_stores) {
+      if (lane == 0) store_wait_read<0>();
+      __syncwarp();
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < 4; ++u)
+      *reinterpret_cast<float4*>(mine + 16 * (u ^ swap)) = make_float4(v[half + 4 * u], v[half + 4 * u + 1], v[half + 4 * u + 2], v[half + 4 * u + 3]);
+    if (SINGLE && a.tile_stores) {
+      shared_to_async();
+      __syncwarp();
+      if (lane == 0) {
+        if (rows && col + half < a.n) {
+          if (add) tile_add(map_d, col + half, row0, piece_address);
+          else tile_store(map_d, col + half, row0, piece_address);
+        }
+        store_commit();
+      }
+      continue;
+    }
+    __syncwarp();
+    const uint32_t c = col + half + (lane & 15);
+    if (c < a.n) {  // two rows at a time; eight such pairs' sums, and the old values that they are added to, at once
+      uint64_t at = (uint64_t)(row0 + (lane >> 4)) * a.ldd + c;
+#pragma unroll 1
+      for (uint32_t r = lane >> 4; r < rows; r += 16, at += 16 * a.ldd) {
+        float x[8], old[8];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+          x[j] = *reinterpret_cast<const float*>(piece + (r + 2 * j) * 64 + 16 * (((lane & 15) >> 2) ^ (((r >> 1) + j) & 3)) + 4 * (lane & 3));
+          old[j] = 0.0f;
+          if (add && r + 2 * j < rows) old[j] = SINGLE ? ld_c(static_cast<const float*>(a.d) + at + 2 * j * a.ldd) : load_value(a.d, a.dtype_d, at + 2 * j * a.ldd);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j)
+          if (r + 2 * j < rows) {
+            if (SINGLE) st_c(static_cast<float*>(a.d) + at + 2 * j * a.ldd, add ? x[j] + old[j] : x[j]);
+            else store_value(a.d, a.dtype_d, at + 2 * j * a.ldd, x[j] + old[j]);
+          }
+      }
+    }
     __syncwarp();
   }
-#pragma unroll
-  for (uint32_t u = 0; u < 8; ++u)
-    *reinterpret_cast<float4*>(piece + lane * 128 + 16 * (u ^ (lane & 7))) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
-  if (SINGLE && a.tile_stores) {
-    shared_to_async();
-    __syncwarp();
-    if (lane == 0) {
-      if (row0 < a.m && col < a.n) {
-        if (add) tile_add(map_d, col, row0, piece_address);
-        else tile_store(map_d, col, row0, piece_address);
-      }
-      store_commit();
-    }
-    return;
-  }
-  __syncwarp();
-  if (col + lane < a.n) {
-    const uint32_t rows = row0 < a.m ? min(a.m - row0, 32u) : 0;
-    uint64_t at = (uint64_t)row0 * a.ldd + col + lane;
-    for (uint32_t r = 0; r < rows; r += 8) {  // eight rows' old values are on their way at once
-      float old[8];
-#pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) old[j] = add && r + j < rows ? load_value(a.d, a.dtype_d, at + j * a.ldd) : 0.0f;
-#pragma unroll
-      for (uint32_t j = 0; j < 8; ++j) {
-        const float x = *reinterpret_cast<const float*>(piece + (r + j) * 128 + 16 * ((lane >> 2) ^ ((r + j) & 7)) + 4 * (lane & 3));
-        if (r + j < rows) store_value(a.d, a.dtype_d, at + j * a.ldd, add ? x + old[j] : x);
-      }
-      at += 8 * a.ldd;
-    }
-  }
-  __syncwarp();
 }
 
 template <int NT, bool SINGLE>  // SINGLE: d is fp32
@@ -433,7 +442,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
                        const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
                        const __grid_constant__ CUtensorMap map_d, const PairArgs a) {
   using S = PairShape<NT>;
-  constexpr int kStages = S::kStages, kReaders = S::kReaders, kShare = kReaders / 4;  // warps that share 32 rows
+  constexpr int kStages = S::kStages, kReaders = S::kReaders, kShare = kReaders / 4, kPer = NT / 32 / kShare;  // warps that share 32 rows, pieces of 32 columns for each
   extern __shared__ uint8_t raw_shared[];
   __shared__ __align__(8) uint64_t barriers[2 * kStages + 4 + kReaders];
   __shared__ uint32_t tensor_base, failed, issued;
@@ -535,7 +544,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
     }
     if (!ok && leader) atomicExch(&failed, 1u);
   } else if (warp < kReaders) {  // results
-    const uint32_t piece_address = staging + warp * 4096;
+    const uint32_t piece_address = staging + warp * 2048;
     uint8_t* piece = raw_shared + (piece_address - smem_address(raw_shared));
     float* bias_tile = reinterpret_cast<float*>(raw_shared + (staging + S::kStaging - smem_address(raw_shared))) + warp * NT;
     const uint32_t drained_at = address_in(drained, 0);
@@ -556,12 +565,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
       const uint64_t part_stride = 2 * 4 * (8 * NT);
       if (u.chunk > 0 && lane == 0) store_wait();  // the chunk before must lie in d
 #pragma unroll 1
-      for (uint32_t turn = warp >> 2; turn < NT / 32; turn += kShare) {  // 32 columns at a time, those shared with the next unit's sums first
-        const uint32_t c = 32 * (unit & 1 || !S::kOverlap ? turn : NT / 32 - 1 - turn);
+      for (uint32_t turn = 0; turn < kPer; ++turn) {  // 32 columns at a time, those shared with the next unit's sums first
+        const uint32_t c = 32 * ((warp >> 2) * kPer + (unit & 1 || !S::kOverlap ? turn : kPer - 1 - turn));
         float v[32];
         tensor_read(from + c, v);
         tensor_read_wait();
-        if (S::kOverlap ? turn == 0 : turn + kShare >= NT / 32) {
+        if (S::kOverlap ? turn == 0 && (warp >> 2) == (unit & 1 ? 0 : kShare - 1) : turn + 1 == kPer) {
           tensor_fence_before();
           __syncwarp();
           if (lane == 0) mbarrier_arrive_cluster(drained_at + 8 * (unit & 1));
@@ -574,7 +583,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
           if (with_bias)
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += bias_tile[c + j];
-          pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate || u.chunk > 0, turn / kShare, v);
+          pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate || u.chunk > 0, v);
         }
       }
       if (partial) {
@@ -588,20 +597,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
           __threadfence();
           asm volatile("fence.proxy.async;" ::: "memory");
           const uint32_t others = a.parts - 1, batch = S::kSlots / others, slots = base + warp * S::kSlots * 4096, bar = joined + 8 * warp;
-          const uint32_t pieces = (NT / 32 - (warp >> 2) + kShare - 1) / kShare;
           bool landed = true;
-          for (uint32_t start = 0, phase = 0; start < pieces && landed; start += batch, phase ^= 1) {
-            const uint32_t stop = min(start + batch, pieces);
+          for (uint32_t start = 0, phase = 0; start < kPer && landed; start += batch, phase ^= 1) {
+            const uint32_t stop = min(start + batch, (uint32_t)kPer);
             __syncwarp();
             if (lane == 0) {
               mbarrier_expect_bytes(bar, (stop - start) * others * 4096 + kCopyAnnounceExtra);
               for (uint32_t i = start; i < stop; ++i)
                 for (uint32_t o = 0; o < others; ++o)
-                  bulk_copy_to_shared(slots + ((i - start) * others + o) * 4096, partial + (o + (o >= u.part)) * part_stride + 8 * ((warp >> 2) + i * kShare) * 32, 4096, bar);
+                  bulk_copy_to_shared(slots + ((i - start) * others + o) * 4096, partial + (o + (o >= u.part)) * part_stride + 8 * ((warp >> 2) * kPer + i) * 32, 4096, bar);
             }
             landed = mbarrier_wait_warp(bar, phase);
             for (uint32_t i = start; i < stop && landed; ++i) {
-              const uint32_t c = 32 * ((warp >> 2) + i * kShare);
+              const uint32_t c = 32 * ((warp >> 2) * kPer + i);
               float own[32], v[32];
               tensor_read(from + c, own);
               tensor_read_wait();
@@ -624,7 +632,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
               if (with_bias)
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] += bias_tile[c + j];
-              pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate, i, v);
+              pair_store<SINGLE>(a, &map_d, piece, piece_address, lane, row0, col0 + c, a.accumulate, v);
             }
           }
           if (!landed) {
