@@ -9,6 +9,7 @@ using accept::launch_overlapped;
 using accept::NormArgs;
 
 constexpr unsigned kSms = 148;
+uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
 size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
 bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF16 || d == ACCEPT_DTYPE_F16; }
@@ -20,9 +21,10 @@ bool whole_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p
 // such groups as fit 512 threads, fewer where there are too few rows for every SM.  16 columns a thread, 32 for rows of more
 // than 8192 (32 everywhere: 16384 x 4096 fp32 to bf16 62 -> 77 us, 8 x 4096 bf16 2.6 -> 3.7 us, for want of registers).  The
 // backward pass over more than 8192 columns has no registers for the sums over the rows and leaves them to a pass of their
-// own (kApart); rows of more than 16384 columns are not held (kLong).
+// own (kApart); rows of more than 16384 columns are not held (kLong).  Rows of up to 128 columns take eight lanes each: with
+// a warp each, 14400 x 105 bf16 took 13.4 us.
 enum class NormPath { kRegisters, kApart, kLong };
-struct NormShape { NormPath path; int own; unsigned warps, groups, blocks; size_t shared; };
+struct NormShape { NormPath path; int own, lanes; unsigned warps, groups, blocks; size_t shared; };
 
 // Rows of a group in shared memory: up to 192 KB for the block.
 constexpr int stages_for(bool backward, int own, int size_x, int size_y) {
@@ -42,16 +44,18 @@ NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
   }
   s.path = backward && p->cols > 8192 ? NormPath::kApart : NormPath::kRegisters;
   s.own = p->cols > 8192 ? 32 : 16;
-  s.warps = (unsigned)((p->cols + 32 * s.own - 1) / (32 * s.own));
-  const uint64_t spread = (p->rows + kSms - 1) / kSms, most = 16 / s.warps;
+  s.lanes = p->cols <= 128 ? 8 : 32;
+  s.warps = (unsigned)((p->cols + s.lanes * s.own - 1) / (s.lanes * s.own));
+  const uint64_t spread = (p->rows + kSms - 1) / kSms, most = 512 / (s.lanes * s.warps);
   s.groups = (unsigned)(spread < most ? (spread ? spread : 1) : most);
+  if (s.lanes < 32) s.groups = (unsigned)up(s.groups, 32 / s.lanes);  // whole warps
   const auto space = [&](int32_t dtype) {
-    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, s.own, s.warps, (uint32_t)p->cols)
-                                              : accept::row_space<uint16_t>(v, s.own, s.warps, (uint32_t)p->cols));
+    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, s.own, s.lanes * s.warps, (uint32_t)p->cols)
+                                              : accept::row_space<uint16_t>(v, s.own, s.lanes * s.warps, (uint32_t)p->cols));
   };
   s.shared = s.groups * (size_t)stages_of(p, backward, s.own) * (space(p->dtype_x) + (backward ? space(p->dtype_y) : 0));
   // the column sums of the block's groups take the same memory
-  const size_t sums = backward && s.path == NormPath::kRegisters ? 2 * 4 * (size_t)s.own * 32 * s.warps * s.groups : 0;
+  const size_t sums = backward && s.path == NormPath::kRegisters ? 2 * 4 * (size_t)s.own * s.lanes * s.warps * s.groups : 0;
   if (s.shared < sums) s.shared = sums;
   const uint64_t units = (p->rows + s.groups - 1) / s.groups;
   s.blocks = (unsigned)(units < kSms ? units : kSms);
@@ -59,41 +63,42 @@ NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
 }
 
 // Partial sums of dgamma and dbeta that the backward pass leaves in the workspace: one for each block, or for each
-// slab of rows.
-constexpr unsigned kSlabs = 64;
+// slab of rows (512 at least: a slab of its own costs a launch that joins them).
 uint64_t norm_partials(const accept_layer_norm_params* p, const NormShape& s) {
-  return s.path == NormPath::kRegisters ? s.blocks : p->rows < kSlabs ? p->rows : kSlabs;
+  if (s.path == NormPath::kRegisters) return s.blocks;
+  const uint64_t slabs = (p->rows + 511) / 512;
+  return slabs < 32 ? slabs : 32;
 }
 
 using KernelFn = void (*)(const NormArgs);
 struct Kernels { KernelFn rows, sums; };
 
-template <typename TX, typename TY, int V, bool FULL>
+template <typename TX, typename TY, int V>
 KernelFn rows_kernel(const NormShape& s, bool backward) {
   constexpr int kX = (int)sizeof(TX), kY = (int)sizeof(TY);
   if (s.path == NormPath::kLong) return backward ? accept::norm_backward_long_kernel<TX, TY> : accept::norm_forward_long_kernel<TX, TY>;
   if (!backward)
-    return s.own == 32 ? accept::norm_forward_kernel<TX, TY, V, FULL, 32, stages_for(false, 32, kX, kY)>
-                       : accept::norm_forward_kernel<TX, TY, V, FULL, 16, stages_for(false, 16, kX, kY)>;
-  return s.own == 32 ? accept::norm_backward_kernel<TX, TY, V, FULL, 32, stages_for(true, 32, kX, kY), false>
-                     : accept::norm_backward_kernel<TX, TY, V, FULL, 16, stages_for(true, 16, kX, kY), true>;
+    return s.own == 32     ? accept::norm_forward_kernel<TX, TY, V, 32, 32, stages_for(false, 32, kX, kY)>
+           : s.lanes == 32 ? accept::norm_forward_kernel<TX, TY, V, 16, 32, stages_for(false, 16, kX, kY)>
+                           : accept::norm_forward_kernel<TX, TY, V, 16, 8, stages_for(false, 16, kX, kY)>;
+  return s.own == 32     ? accept::norm_backward_kernel<TX, TY, V, 32, 32, stages_for(true, 32, kX, kY), false>
+         : s.lanes == 32 ? accept::norm_backward_kernel<TX, TY, V, 16, 32, stages_for(true, 16, kX, kY), true>
+                         : accept::norm_backward_kernel<TX, TY, V, 16, 8, stages_for(true, 16, kX, kY), true>;
 }
 
-// whole: rows start on 16-byte boundaries; full: every thread has all its columns
+// whole: rows start on 16-byte boundaries
 template <typename TX, typename TY>
-Kernels kernels_for(const NormShape& s, bool backward, bool whole, bool full) {
+Kernels kernels_for(const NormShape& s, bool backward, bool whole) {
   constexpr int kUnit = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
-  return {!whole ? rows_kernel<TX, TY, 1, false>(s, backward)
-          : full ? rows_kernel<TX, TY, kUnit, true>(s, backward) : rows_kernel<TX, TY, kUnit, false>(s, backward),
-          accept::norm_column_sums_kernel<TX, TY>};
+  return {whole ? rows_kernel<TX, TY, kUnit>(s, backward) : rows_kernel<TX, TY, 1>(s, backward), accept::norm_column_sums_kernel<TX, TY>};
 }
 
 template <typename TX>
 Kernels kernels_for_y(const accept_layer_norm_params* p, const NormShape& s, bool backward, bool whole) {
   switch (p->dtype_y) {
-    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, whole, s.own != 0 && p->cols % (32 * s.own) == 0);
-    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, whole, s.own != 0 && p->cols % (32 * s.own) == 0);
-    default: return kernels_for<TX, __half>(s, backward, whole, s.own != 0 && p->cols % (32 * s.own) == 0);
+    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, whole);
+    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, whole);
+    default: return kernels_for<TX, __half>(s, backward, whole);
   }
 }
 
@@ -112,7 +117,7 @@ int unit_of(const accept_layer_norm_params* p, bool whole) {
 
 cudaError_t launch_norm(KernelFn fn, const NormShape& shape, NormArgs& a, cudaStream_t s) {
   a.warps = shape.warps;
-  const unsigned threads = shape.path == NormPath::kLong ? 1024 : 32 * shape.warps * shape.groups;
+  const unsigned threads = shape.path == NormPath::kLong ? 1024 : shape.lanes * shape.warps * shape.groups;
   if (shape.shared > 32 * 1024) {  // with the static part, more than a kernel gets without asking
     const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shape.shared);
     if (err != cudaSuccess) return err;
@@ -232,9 +237,10 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
     const Kernels k = select_kernels(p, shape, true, whole);
     const bool apart = shape.path != NormPath::kRegisters;
     if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
-    if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 127) / 128, a.n_partials), 128, s, a));
+    if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 31) / 32, a.n_partials), 256, s, a));
   }
-  if (weights) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 32 * accept::kJoinWarps, s, a));
+  const bool summed = shape.path != NormPath::kRegisters && p->rows != 0 && a.n_partials == 1;
+  if (weights && !summed) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 32 * accept::kJoinWarps, s, a));
   return ACCEPT_OK;
 }
 

@@ -32,16 +32,19 @@ struct NormArgs {
   int whole_weights;     // gamma and beta start on 16-byte boundaries
 };
 
-// How the columns of a row lie over the threads that share it: a warp holds 32 OWN neighbours, as units of V neighbours dealt
-// over its lanes, so that all addresses of a thread are one base and constants.  V = 8 where both tensors are 16-bit types,
+// How the columns of a row lie over the threads that share it: L lanes (a warp, or eight lanes where a row is short) hold
+// L OWN neighbours, as units of V neighbours dealt over them, so that all addresses of a thread are one base and constants.  V = 8 where both tensors are 16-bit types,
 // 4 where one is fp32 (16 bytes at most for a thread, neighbours side by side), 1 where rows do not start on 16-byte
 // boundaries.
-template <int V, int OWN>
+template <int V, int OWN, int L>
 __device__ __forceinline__ uint32_t column_of(uint32_t t, int own) {
-  return (t >> 5) * (32 * OWN) + V * (t & 31) + own / V * (32 * V) + own % V;
+  return t / L * (L * OWN) + V * (t % L) + own / V * (L * V) + own % V;
 }
+template <int OWN, int L>  // all columns of the L lanes exist
+__device__ __forceinline__ bool lanes_are_full(uint32_t t, uint32_t cols) { return (t / L + 1) * (L * OWN) <= cols; }
+
 // How many values of each of the thread's units exist (V = 1: a bit for each).  FULL: all of them.
-template <int V, bool FULL, int OWN>
+template <int V, bool FULL, int OWN, int L>
 struct Own {
   static constexpr int kUnits = V > 1 ? OWN / V : 1;
   uint32_t count[kUnits];
@@ -49,12 +52,12 @@ struct Own {
 #pragma unroll
     for (int i = 0; i < kUnits; ++i) {
       if (V > 1) {
-        const uint32_t c = column_of<V, OWN>(t, V * i);
+        const uint32_t c = column_of<V, OWN, L>(t, V * i);
         count[i] = c < cols ? min(cols - c, (uint32_t)V) : 0;
       } else {
         count[0] = 0;
 #pragma unroll
-        for (int j = 0; j < OWN; ++j) count[0] |= column_of<1, OWN>(t, j) < cols ? 1u << j : 0u;
+        for (int j = 0; j < OWN; ++j) count[0] |= column_of<1, OWN, L>(t, j) < cols ? 1u << j : 0u;
       }
     }
   }
@@ -87,27 +90,27 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int PENDING>  // all but the last PENDING groups have landed
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
-// Bytes of shared memory that a row of T takes for `warps` warps (V = 1: the 16-byte pieces that hold it).
+// Bytes of shared memory that a row of T takes for `threads` threads (V = 1: the 16-byte pieces that hold it).
 template <typename T>
-__host__ __device__ constexpr uint32_t row_space(int v, int own, uint32_t warps, uint32_t cols) {
-  return v > 1 ? warps * 32 * own * (uint32_t)sizeof(T) : (cols * (uint32_t)sizeof(T) + 30) / 16 * 16;
+__host__ __device__ constexpr uint32_t row_space(int v, int own, uint32_t threads, uint32_t cols) {
+  return v > 1 ? threads * own * (uint32_t)sizeof(T) : (cols * (uint32_t)sizeof(T) + 30) / 16 * 16;
 }
 
 // Starts the copies of a row into `dst` (shared).  `begin` and `end` bound the values of the matrix.  Units that do not
 // exist are not copied: their places hold zeros from the start (clear_row).
-template <typename T, int V, bool FULL, int OWN, int I = 0>
-__device__ __forceinline__ void start_units(uint32_t to, const T* from, const Own<V, FULL, OWN>& own) {
-  constexpr int kBytes = V * (int)sizeof(T), kTo = I * 32 * kBytes, kFrom = I * 32 * V * (int)sizeof(T);
+template <typename T, int V, bool FULL, int OWN, int L, int I = 0>
+__device__ __forceinline__ void start_units(uint32_t to, const T* from, const Own<V, FULL, OWN, L>& own) {
+  constexpr int kBytes = V * (int)sizeof(T), kTo = I * L * kBytes, kFrom = I * L * V * (int)sizeof(T);
   static_assert(kBytes == 8 || kBytes == 16, "a unit is one copy");
   if (FULL) copy_async_at<kBytes, kTo, kFrom>(to, from);
   else if (own.of(I)) copy_async_at<kBytes, kTo, kFrom>(to, from, own.of(I) * (uint32_t)sizeof(T));
-  if constexpr (I + 1 < OWN / V) start_units<T, V, FULL, OWN, I + 1>(to, from, own);
+  if constexpr (I + 1 < OWN / V) start_units<T, V, FULL, OWN, L, I + 1>(to, from, own);
 }
-template <typename T, int V, bool FULL, int OWN>
-__device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, uint32_t threads, const Own<V, FULL, OWN>& own,
+template <typename T, int V, bool FULL, int OWN, int L>
+__device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, uint32_t threads, const Own<V, FULL, OWN, L>& own,
                                           const T* begin, const T* end) {
   if constexpr (V > 1) {
-    const uint32_t first = column_of<V, OWN>(t, 0), to = dst + first * (uint32_t)sizeof(T);
+    const uint32_t first = column_of<V, OWN, L>(t, 0), to = dst + first * (uint32_t)sizeof(T);
     const T* from = row + first;
     start_units(to, from, own);
   } else {
@@ -139,56 +142,56 @@ __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t c
 }
 
 // Zeros where this thread's units that do not exist would lie.
-template <typename T, int V, bool FULL, int OWN>
-__device__ __forceinline__ void clear_row(uint32_t dst, uint32_t t, const Own<V, FULL, OWN>& own) {
-  if (V == 1 || FULL) return;
+template <typename T, int V, int OWN, int L>
+__device__ __forceinline__ void clear_row(uint32_t dst, uint32_t t, uint32_t cols) {
+  if (V == 1) return;
 #pragma unroll
-  for (int i = 0; i < OWN / V; ++i) {
-    if (own.of(i)) continue;
-    const uint32_t at = dst + column_of<V, OWN>(t, V * i) * (uint32_t)sizeof(T);
+  for (int i = 0; i < OWN; i += V) {
+    if (column_of<V, OWN, L>(t, i) < cols) continue;
+    const uint32_t at = dst + column_of<V, OWN, L>(t, i) * (uint32_t)sizeof(T);
 #pragma unroll
     for (int j = 0; j < V * (int)sizeof(T); j += 8) asm volatile("st.shared.u64 [%0], %1;" ::"r"(at + j), "l"(0ull) : "memory");
   }
 }
 
 // Units I and after of the thread from shared memory.
-template <typename T, int V, int OWN, int I = 0>
+template <typename T, int V, int OWN, int L, int I = 0>
 __device__ __forceinline__ void take_units(uint32_t from, Pair (&v)[OWN / 2]) {
   constexpr int kFirst = V * I / 2;
   if constexpr (sizeof(T) == 4) {
-    asm volatile("ld.shared.v2.u64 {%0,%1}, [%2+%3];" : "=l"(v[kFirst % (OWN / 2)]), "=l"(v[(kFirst + 1) % (OWN / 2)]) : "r"(from), "n"(I * 32 * 16));
+    asm volatile("ld.shared.v2.u64 {%0,%1}, [%2+%3];" : "=l"(v[kFirst % (OWN / 2)]), "=l"(v[(kFirst + 1) % (OWN / 2)]) : "r"(from), "n"(I * L * 16));
   } else if constexpr (V == 8) {
     uint32_t w[4];
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+%5];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from), "n"(I * 32 * 16));
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4+%5];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(from), "n"(I * L * 16));
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[(kFirst + j) % (OWN / 2)] = word_to_pair<T>(w[j]);
   } else {
     uint32_t w[2];
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2+%3];" : "=r"(w[0]), "=r"(w[1]) : "r"(from), "n"(I * 32 * 8));
+    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2+%3];" : "=r"(w[0]), "=r"(w[1]) : "r"(from), "n"(I * L * 8));
     v[kFirst % (OWN / 2)] = word_to_pair<T>(w[0]);
     v[(kFirst + 1) % (OWN / 2)] = word_to_pair<T>(w[1]);
   }
-  if constexpr (I + 1 < OWN / V) take_units<T, V, OWN, I + 1>(from, v);
+  if constexpr (I + 1 < OWN / V) take_units<T, V, OWN, L, I + 1>(from, v);
 }
 
 // Takes a row that has landed at `src` (shared) into registers; columns that do not exist are zero.
-template <typename T, int V, bool FULL, int OWN>
-__device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, const Own<V, FULL, OWN>& own, Pair (&v)[OWN / 2]) {
+template <typename T, int V, bool FULL, int OWN, int L>
+__device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, const Own<V, FULL, OWN, L>& own, Pair (&v)[OWN / 2]) {
   if constexpr (V > 1) {
-    const uint32_t from = src + column_of<V, OWN>(t, 0) * (uint32_t)sizeof(T);
-    take_units<T, V, OWN>(from, v);
+    const uint32_t from = src + column_of<V, OWN, L>(t, 0) * (uint32_t)sizeof(T);
+    take_units<T, V, OWN, L>(from, v);
   } else {
-    const uint32_t from = src + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + column_of<V, OWN>(t, 0) * (uint32_t)sizeof(T);
+    const uint32_t from = src + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + column_of<V, OWN, L>(t, 0) * (uint32_t)sizeof(T);
     float lo = 0.0f;
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
       float f = 0.0f;
       if (own.has(i)) {
         if constexpr (sizeof(T) == 4) {
-          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(from + i * 32 * 4));
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(from + i * L * 4));
         } else {
           uint16_t w;
-          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(from + i * 32 * 2));
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(from + i * L * 2));
           T h;
           memcpy(&h, &w, 2);
           f = to_float(h);
@@ -200,12 +203,12 @@ __device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t,
   }
 }
 
-template <typename T, int V, bool FULL, int OWN>
-__device__ __forceinline__ void store_row(T* row, uint32_t t, const Own<V, FULL, OWN>& own, const Pair (&v)[OWN / 2]) {
-  T* to = row + column_of<V, OWN>(t, 0);
+template <typename T, int V, bool FULL, int OWN, int L>
+__device__ __forceinline__ void store_row(T* row, uint32_t t, const Own<V, FULL, OWN, L>& own, const Pair (&v)[OWN / 2]) {
+  T* to = row + column_of<V, OWN, L>(t, 0);
 #pragma unroll
   for (int i = 0; i < OWN / V; ++i) {
-    T* p = to + i * 32 * V;
+    T* p = to + i * L * V;
     if (V > 1 && own.of(i) == V) {
       uint32_t w[4];
 #pragma unroll
@@ -238,19 +241,19 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, float absen
 }
 
 // gamma or beta for this thread's columns: read once for all rows that it takes, all loads on their way at once.
-template <typename T, int V, bool FULL, int OWN>
-__device__ __forceinline__ void load_weights_of(const T* w, bool whole, const Own<V, FULL, OWN>& own, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
-  w += column_of<V, OWN>(t, 0);
+template <typename T, int V, bool FULL, int OWN, int L>
+__device__ __forceinline__ void load_weights_of(const T* w, bool whole, const Own<V, FULL, OWN, L>& own, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
+  w += column_of<V, OWN, L>(t, 0);
   if (V > 1 && FULL && whole) {
     uint4 raw[OWN * sizeof(T) / 16];
     constexpr int kEach = 16 / (int)sizeof(T), kOf = V >= kEach ? V / kEach : 1;  // values of a load, loads of a unit
     if constexpr (V >= kEach) {
 #pragma unroll
-      for (int i = 0; i < OWN / kEach; ++i) raw[i] = ld_c(reinterpret_cast<const uint4*>(w + i / kOf * (32 * V) + i % kOf * kEach));
+      for (int i = 0; i < OWN / kEach; ++i) raw[i] = ld_c(reinterpret_cast<const uint4*>(w + i / kOf * (L * V) + i % kOf * kEach));
     } else {  // units of four 16-bit values
 #pragma unroll
       for (int i = 0; i < OWN / V; i += 2) {
-        const uint2 lo = ld_c(reinterpret_cast<const uint2*>(w + i * (32 * V))), hi = ld_c(reinterpret_cast<const uint2*>(w + (i + 1) * (32 * V)));
+        const uint2 lo = ld_c(reinterpret_cast<const uint2*>(w + i * (L * V))), hi = ld_c(reinterpret_cast<const uint2*>(w + (i + 1) * (L * V)));
         raw[i / 2] = make_uint4(lo.x, lo.y, hi.x, hi.y);
       }
     }
@@ -270,22 +273,22 @@ __device__ __forceinline__ void load_weights_of(const T* w, bool whole, const Ow
     T raw[OWN];
 #pragma unroll
     for (int i = 0; i < OWN; ++i)
-      if (own.has(i)) raw[i] = ld_c(w + i / V * (32 * V) + i % V);
+      if (own.has(i)) raw[i] = ld_c(w + i / V * (L * V) + i % V);
 #pragma unroll
     for (int i = 0; i < OWN; i += 2) v[i / 2] = pair_of(own.has(i) ? to_float(raw[i]) : absent, own.has(i + 1) ? to_float(raw[i + 1]) : absent);
   }
 }
-template <int V, bool FULL, int OWN>
-__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, const Own<V, FULL, OWN>& own, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
+template <int V, bool FULL, int OWN, int L>
+__device__ __forceinline__ void load_weights(const NormArgs& a, const void* w, const Own<V, FULL, OWN, L>& own, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
   if (!w) {
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) v[i] = both(absent);
   } else if (a.dtype_w == kF32) {
-    load_weights_of<float, V, FULL, OWN>(static_cast<const float*>(w), a.whole_weights, own, absent, t, v);
+    load_weights_of<float, V, FULL, OWN, L>(static_cast<const float*>(w), a.whole_weights, own, absent, t, v);
   } else if (a.dtype_w == kBf16) {
-    load_weights_of<__nv_bfloat16, V, FULL, OWN>(static_cast<const __nv_bfloat16*>(w), a.whole_weights, own, absent, t, v);
+    load_weights_of<__nv_bfloat16, V, FULL, OWN, L>(static_cast<const __nv_bfloat16*>(w), a.whole_weights, own, absent, t, v);
   } else {
-    load_weights_of<__half, V, FULL, OWN>(static_cast<const __half*>(w), a.whole_weights, own, absent, t, v);
+    load_weights_of<__half, V, FULL, OWN, L>(static_cast<const __half*>(w), a.whole_weights, own, absent, t, v);
   }
 }
 
@@ -295,22 +298,25 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// The threads that share a row: `warps` warps, one of the block's groups.
+// The threads that share a row, one of the block's groups: `warps` warps (L = 32), or eight lanes of a warp (L = 8).
+template <int L>
 struct Group {
-  uint32_t index, warps, threads, t;
-  __device__ __forceinline__ explicit Group(uint32_t warps_) : warps(warps_), threads(32 * warps_) {
-    index = (threadIdx.x >> 5) / warps;
+  uint32_t index, warps, threads, t, mask;  // mask: the lanes that take part in an exchange
+  __device__ __forceinline__ explicit Group(uint32_t warps_) : warps(warps_), threads(L * warps_) {
+    index = L == 32 ? (threadIdx.x >> 5) / warps : threadIdx.x / L;
     t = threadIdx.x - index * threads;
+    mask = L == 32 ? 0xffffffffu : ((1u << L % 32) - 1) << (threadIdx.x & 31 & ~(L - 1));
   }
   __device__ __forceinline__ void sync() const {
-    if (warps == 1) __syncwarp();
+    if (L < 32 || warps == 1) __syncwarp(mask);
     else asm volatile("bar.sync %0, %1;" ::"r"(index + 1), "r"(threads) : "memory");
   }
   // Sum over the group.  `slot`: 16 floats of the group, zero past its warps, used in turn with others (a barrier lies
   // between two uses); every thread adds the warps' values up for itself.
   __device__ __forceinline__ float sum(float v, float* slot) const {
-    v = warp_sum(v);
-    if (warps == 1) return v;
+#pragma unroll
+    for (int d = L / 2; d >= 1; d >>= 1) v += __shfl_xor_sync(mask, v, d);
+    if (L < 32 || warps == 1) return v;
     if ((t & 31) == 0) slot[t >> 5] = v;
     sync();
     float4 s = *reinterpret_cast<const float4*>(slot);
@@ -322,16 +328,17 @@ struct Group {
     }
     return (s.x + s.y) + (s.z + s.w);
   }
-  // Two sums with one barrier: after the first exchange the lower half of a warp adds up one of them, the upper half the
+  // Two sums with one barrier: after the first exchange the lower half of the lanes adds up one of them, the upper half the
   // other.  `slot`: 32 floats, pairs of both.
   __device__ __forceinline__ float2 sum_two(float2 v, float* slot) const {
-    const bool upper = (t & 16) != 0;
+    constexpr int kHalf = L / 2;
+    const bool upper = (t & kHalf) != 0;
     float mine = upper ? v.y : v.x;
-    mine += __shfl_xor_sync(0xffffffffu, upper ? v.x : v.y, 16);
+    mine += __shfl_xor_sync(mask, upper ? v.x : v.y, kHalf);
 #pragma unroll
-    for (int d = 8; d >= 1; d >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, d);
-    if (warps == 1) {
-      const float other = __shfl_xor_sync(0xffffffffu, mine, 16);
+    for (int d = kHalf / 2; d >= 1; d >>= 1) mine += __shfl_xor_sync(mask, mine, d);
+    if (L < 32 || warps == 1) {
+      const float other = __shfl_xor_sync(mask, mine, kHalf);
       return upper ? make_float2(other, mine) : make_float2(mine, other);
     }
     if ((t & 15) == 0) slot[t >> 4] = mine;
@@ -347,63 +354,48 @@ struct Group {
   }
 };
 
-constexpr int kMostGroups = 16;
+constexpr int kMostGroups = 8;  // of several warps
 
 extern __shared__ __align__(16) uint8_t norm_shared[];
 
 // Forward.  The mean first, then the sum of the squared distances from it, so that an offset much larger than the spread
-// costs no digits.
-template <typename TX, typename TY, int V, bool FULL, int OWN, int STAGES>
-__global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a) {
-  __shared__ __align__(16) float slots[kMostGroups][2][16];
-  const Group g(a.warps);
-  const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space = row_space<TX>(V, OWN, a.warps, a.cols);
-  const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space, shared_end = shared + STAGES * space;
-  const Own<V, FULL, OWN> own(t, a.cols);
+// costs no digits.  FULL: all columns of this warp exist (the warps of a group meet at the same barriers either way).
+template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES>
+__device__ __forceinline__ void forward_rows(const NormArgs& a, const Group<L>& g, float (&slots)[2][16], uint32_t shared, uint32_t space, uint64_t first, uint32_t step) {
+  const uint32_t t = g.t, threads = g.threads, shared_end = shared + STAGES * space;
+  const Own<V, FULL, OWN, L> own(t, a.cols);
   bool ends_inside = false;
 #pragma unroll
   for (int i = 0; i < OWN / V; ++i) ends_inside |= V > 1 && own.of(i) % V != 0;
   const TX* x = static_cast<const TX*>(a.x);
   const TX* end = x + (a.rows - 1) * a.ld_x + a.cols;
-  const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
-  const uint32_t step = gridDim.x * groups;
-  if (a.warps > 1) {
-    float* zero = &slots[g.index][0][0];
-    for (uint32_t i = t; i < 32; i += threads) zero[i] = 0.0f;
-    g.sync();
-  }
-#pragma unroll
-  for (int i = 0; i < STAGES; ++i) clear_row<TX, V, FULL, OWN>(shared + i * space, t, own);
-  grid_dependency_handshake();
-  if (first >= a.rows) return;
   const TX* row = x + first * a.ld_x;
   TY* out = static_cast<TY*>(a.y) + first * a.ld_y;
   const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) {
-    if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL, OWN>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end);
+    if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL, OWN, L>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end);
     copy_commit();
   }
   Pair gamma[OWN / 2], beta[OWN / 2];
-  load_weights<V, FULL, OWN>(a, a.gamma, own, 1.0f, t, gamma);
-  load_weights<V, FULL, OWN>(a, a.beta, own, 0.0f, t, beta);
+  load_weights<V, FULL, OWN, L>(a, a.gamma, own, 1.0f, t, gamma);
+  load_weights<V, FULL, OWN, L>(a, a.beta, own, 0.0f, t, beta);
   uint32_t here = shared, ahead = shared + (STAGES - 1) * space;  // where this row lies, and where the one to start goes
   uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);  // rows of this group from this one on
   float* mean_out = a.mean_out && t == 0 ? a.mean_out + first : nullptr;
   float* rstd_out = a.rstd_out && t == 0 ? a.rstd_out + first : nullptr;
   for (;;) {
-    if (left > STAGES - 1) start_row<TX, V, FULL, OWN>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end);
+    if (left > STAGES - 1) start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end);
     copy_commit();
     copy_wait<STAGES - 1>();
     if (V == 1) g.sync();
     Pair v[OWN / 2];
-    take_row<TX, V, FULL, OWN>(here, row, t, own, v);
+    take_row<TX, V, FULL, OWN, L>(here, row, t, own, v);
     Pair sums[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
     for (int i = 4; i < OWN / 2; ++i) sums[i % 4] = add2(sums[i % 4], v[i]);
     const Pair sum = add2(add2(sums[0], sums[1]), add2(sums[2], sums[3]));
-    const float mean = g.sum(sum_of(sum), slots[g.index][0]) * a.inv_cols;
+    const float mean = g.sum(sum_of(sum), slots[0]) * a.inv_cols;
     Pair squares[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) {
@@ -417,10 +409,10 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a) {
       squares[i % 2] = fma2(v[i], v[i], squares[i % 2]);
     }
     squares[0] = add2(squares[0], squares[1]);
-    const float rstd = rsqrtf(g.sum(sum_of(squares[0]), slots[g.index][1]) * a.inv_cols + a.eps);
+    const float rstd = rsqrtf(g.sum(sum_of(squares[0]), slots[1]) * a.inv_cols + a.eps);
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) v[i] = fma2(mul2(v[i], both(rstd)), gamma[i], beta[i]);
-    store_row<TY, V, FULL, OWN>(out, t, own, v);
+    store_row<TY, V, FULL, OWN, L>(out, t, own, v);
     if (mean_out) { st_c(mean_out, mean); mean_out += step; }
     if (rstd_out) { st_c(rstd_out, rstd); rstd_out += step; }
     if (--left == 0) break;
@@ -431,130 +423,180 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a) {
   }
 }
 
+template <typename TX, typename TY, int V, int OWN, int L, int STAGES>
+__global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a) {
+  __shared__ __align__(16) float slots[kMostGroups][2][16];
+  const Group<L> g(a.warps);
+  const uint32_t groups = blockDim.x / g.threads;
+  const uint32_t space = row_space<TX>(V, OWN, L * a.warps, a.cols);
+  const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space;
+  const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
+  const uint32_t step = gridDim.x * groups;
+  const bool full = lanes_are_full<OWN, L>(g.t, a.cols);
+  if (!full)
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) clear_row<TX, V, OWN, L>(shared + i * space, g.t, a.cols);
+  if (L == 32 && a.warps > 1) {
+    float* zero = &slots[g.index][0][0];
+    for (uint32_t i = g.t; i < 32; i += g.threads) zero[i] = 0.0f;
+    g.sync();
+  }
+  grid_dependency_handshake();
+  if (first >= a.rows) return;
+  if (full) forward_rows<TX, TY, V, true, OWN, L, STAGES>(a, g, slots[g.index % kMostGroups], shared, space, first, step);
+  else forward_rows<TX, TY, V, false, OWN, L, STAGES>(a, g, slots[g.index % kMostGroups], shared, space, first, step);
+}
+
 // Backward.  dx needs two sums of a row, taken together; the gradients of gamma and beta are sums over the rows (SUMS),
 // held in registers over all rows of a group, added up over the block's groups and joined by norm_join_kernel.
-template <typename TX, typename TY, int V, bool FULL, int OWN, int STAGES, bool SUMS>
-__global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
+template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES, bool SUMS>
+__device__ __forceinline__ void backward_rows(const NormArgs& a, const Group<L>& g, float (&slots)[2][32], uint32_t shared, uint32_t space, uint32_t space_x,
+                                              uint64_t first, uint32_t step, Pair (&dgamma)[SUMS ? OWN / 2 : 1], Pair (&dbeta)[SUMS ? OWN / 2 : 1]) {
   constexpr int kSums = SUMS ? OWN / 2 : 1;
-  __shared__ __align__(16) float slots[kMostGroups][2][32];
-  const Group g(a.warps);
-  const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space_x = row_space<TX>(V, OWN, a.warps, a.cols), space = space_x + row_space<TY>(V, OWN, a.warps, a.cols);
-  const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space, shared_end = shared + STAGES * space;
-  const Own<V, FULL, OWN> own(t, a.cols);
+  const uint32_t t = g.t, threads = g.threads, shared_end = shared + STAGES * space;
+  const Own<V, FULL, OWN, L> own(t, a.cols);
   const TX* x = static_cast<const TX*>(a.x);
   const TY* dy = static_cast<const TY*>(a.dy);
   const TX* end_x = x + (a.rows - 1) * a.ld_x + a.cols;
   const TY* end_y = dy + (a.rows - 1) * a.ld_y + a.cols;
+  Pair gamma[OWN / 2];
+  const TX* row = x + first * a.ld_x;
+  const TY* drow = dy + first * a.ld_y;
+  TX* out = static_cast<TX*>(a.dx) + first * a.ld_x;
+  const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
+#pragma unroll
+  for (int s = 0; s + 1 < STAGES; ++s) {
+    if (first + (uint64_t)s * step < a.rows) {
+      start_row<TX, V, FULL, OWN, L>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end_x);
+      start_row<TY, V, FULL, OWN, L>(shared + s * space + space_x, drow + s * stride_y, a.cols, t, threads, own, dy, end_y);
+    }
+    copy_commit();
+  }
+  load_weights<V, FULL, OWN, L>(a, a.gamma, own, 1.0f, t, gamma);
+  uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;
+  uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);
+  const float* means = a.mean + first;
+  const float* rstds = a.rstd + first;
+  float mean_next = ld_c(means), rstd_next = ld_c(rstds);
+  for (;;) {
+    if (left > STAGES - 1) {
+      start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end_x);
+      start_row<TY, V, FULL, OWN, L>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, threads, own, dy, end_y);
+    }
+    copy_commit();
+    const float mean = mean_next, rstd = rstd_next;
+    if (left > 1) { mean_next = ld_c(means += step); rstd_next = ld_c(rstds += step); }
+    copy_wait<STAGES - 1>();
+    if (V == 1) g.sync();
+    Pair xhat[OWN / 2], h[OWN / 2];
+    take_row<TX, V, FULL, OWN, L>(here, row, t, own, xhat);
+    take_row<TY, V, FULL, OWN, L>(here + space_x, drow, t, own, h);
+    Pair sum[2] = {both(0.0f), both(0.0f)}, along[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+    for (int i = 0; i < OWN / 2; ++i) {
+      xhat[i] = mul2(add2(xhat[i], both(-mean)), both(rstd));  // columns that do not exist: dy = 0, so this counts nowhere
+      if (SUMS) {
+        dbeta[i % kSums] = add2(dbeta[i % kSums], h[i]);
+        dgamma[i % kSums] = fma2(h[i], xhat[i], dgamma[i % kSums]);
+      }
+      h[i] = mul2(h[i], gamma[i]);
+      sum[i % 2] = add2(sum[i % 2], h[i]);
+      along[i % 2] = fma2(h[i], xhat[i], along[i % 2]);
+    }
+    if (a.dx) {
+      sum[0] = add2(sum[0], sum[1]);
+      along[0] = add2(along[0], along[1]);
+      const float2 s = g.sum_two(make_float2(sum_of(sum[0]), sum_of(along[0])), slots[turn]);
+      turn ^= 1;
+      const Pair less = both(-s.x * a.inv_cols), slope = both(-s.y * a.inv_cols);
+#pragma unroll
+      for (int i = 0; i < OWN / 2; ++i) h[i] = mul2(fma2(xhat[i], slope, add2(h[i], less)), both(rstd));
+      store_row<TX, V, FULL, OWN, L>(out, t, own, h);
+    } else if (V == 1) {
+      g.sync();  // the row has been read: its place is free
+    }
+    if (--left == 0) break;
+    row += stride_x;
+    drow += stride_y;
+    out += stride_x;
+    ahead = here;
+    here = here + space == shared_end ? shared : here + space;
+  }
+}
+
+template <typename TX, typename TY, int V, int OWN, int L, int STAGES, bool SUMS>
+__global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
+  constexpr int kSums = SUMS ? OWN / 2 : 1;
+  __shared__ __align__(16) float slots[kMostGroups][2][32];
+  const Group<L> g(a.warps);
+  const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
+  const uint32_t space_x = row_space<TX>(V, OWN, L * a.warps, a.cols), space = space_x + row_space<TY>(V, OWN, L * a.warps, a.cols);
+  const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space;
   const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
   const uint32_t step = gridDim.x * groups;
-  if (a.warps > 1) {
+  const bool full = lanes_are_full<OWN, L>(t, a.cols);
+  if (!full) {
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) {
+      clear_row<TX, V, OWN, L>(shared + i * space, t, a.cols);
+      clear_row<TY, V, OWN, L>(shared + i * space + space_x, t, a.cols);
+    }
+  }
+  if (L == 32 && a.warps > 1) {
     float* zero = &slots[g.index][0][0];
     for (uint32_t i = t; i < 64; i += threads) zero[i] = 0.0f;
     g.sync();
   }
-#pragma unroll
-  for (int i = 0; i < STAGES; ++i) {
-    clear_row<TX, V, FULL, OWN>(shared + i * space, t, own);
-    clear_row<TY, V, FULL, OWN>(shared + i * space + space_x, t, own);
-  }
   grid_dependency_handshake();
-  Pair gamma[OWN / 2], dgamma[kSums], dbeta[kSums];
+  Pair dgamma[kSums], dbeta[kSums];
 #pragma unroll
   for (int i = 0; i < kSums; ++i) dgamma[i] = dbeta[i] = both(0.0f);
   if (first < a.rows) {
-    const TX* row = x + first * a.ld_x;
-    const TY* drow = dy + first * a.ld_y;
-    TX* out = static_cast<TX*>(a.dx) + first * a.ld_x;
-    const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
-#pragma unroll
-    for (int s = 0; s + 1 < STAGES; ++s) {
-      if (first + (uint64_t)s * step < a.rows) {
-        start_row<TX, V, FULL, OWN>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end_x);
-        start_row<TY, V, FULL, OWN>(shared + s * space + space_x, drow + s * stride_y, a.cols, t, threads, own, dy, end_y);
-      }
-      copy_commit();
-    }
-    load_weights<V, FULL, OWN>(a, a.gamma, own, 1.0f, t, gamma);
-    uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;
-    uint32_t left = (uint32_t)((a.rows - first + step - 1) / step);
-    const float* means = a.mean + first;
-    const float* rstds = a.rstd + first;
-    float mean_next = ld_c(means), rstd_next = ld_c(rstds);
-    for (;;) {
-      if (left > STAGES - 1) {
-        start_row<TX, V, FULL, OWN>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end_x);
-        start_row<TY, V, FULL, OWN>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, threads, own, dy, end_y);
-      }
-      copy_commit();
-      const float mean = mean_next, rstd = rstd_next;
-      if (left > 1) { mean_next = ld_c(means += step); rstd_next = ld_c(rstds += step); }
-      copy_wait<STAGES - 1>();
-      if (V == 1) g.sync();
-      Pair xhat[OWN / 2], h[OWN / 2];
-      take_row<TX, V, FULL, OWN>(here, row, t, own, xhat);
-      take_row<TY, V, FULL, OWN>(here + space_x, drow, t, own, h);
-      Pair sum[2] = {both(0.0f), both(0.0f)}, along[2] = {both(0.0f), both(0.0f)};
-#pragma unroll
-      for (int i = 0; i < OWN / 2; ++i) {
-        xhat[i] = mul2(add2(xhat[i], both(-mean)), both(rstd));  // columns that do not exist: dy = 0, so this counts nowhere
-        if (SUMS) {
-          dbeta[i % kSums] = add2(dbeta[i % kSums], h[i]);
-          dgamma[i % kSums] = fma2(h[i], xhat[i], dgamma[i % kSums]);
-        }
-        h[i] = mul2(h[i], gamma[i]);
-        sum[i % 2] = add2(sum[i % 2], h[i]);
-        along[i % 2] = fma2(h[i], xhat[i], along[i % 2]);
-      }
-      if (a.dx) {
-        sum[0] = add2(sum[0], sum[1]);
-        along[0] = add2(along[0], along[1]);
-        const float2 s = g.sum_two(make_float2(sum_of(sum[0]), sum_of(along[0])), slots[g.index][turn]);
-        turn ^= 1;
-        const Pair less = both(-s.x * a.inv_cols), slope = both(-s.y * a.inv_cols);
-#pragma unroll
-        for (int i = 0; i < OWN / 2; ++i) h[i] = mul2(fma2(xhat[i], slope, add2(h[i], less)), both(rstd));
-        store_row<TX, V, FULL, OWN>(out, t, own, h);
-      } else if (V == 1) {
-        g.sync();  // the row has been read: its place is free
-      }
-      if (--left == 0) break;
-      row += stride_x;
-      drow += stride_y;
-      out += stride_x;
-      ahead = here;
-      here = here + space == shared_end ? shared : here + space;
-    }
+    if (full) backward_rows<TX, TY, V, true, OWN, L, STAGES, SUMS>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step, dgamma, dbeta);
+    else backward_rows<TX, TY, V, false, OWN, L, STAGES, SUMS>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step, dgamma, dbeta);
   }
   if (!SUMS || !a.partials) return;
   float* out = a.partials + (uint64_t)blockIdx.x * 2 * a.cols;
   if (groups == 1) {
+    if (V > 1 && a.cols % 4 == 0) {
+#pragma unroll
+      for (int i = 0; i < OWN; i += 4) {
+        const uint32_t c = column_of<V, OWN, L>(t, i);
+        const float2 d0 = split(dgamma[i / 2 % kSums]), d1 = split(dgamma[(i / 2 + 1) % kSums]);
+        const float2 e0 = split(dbeta[i / 2 % kSums]), e1 = split(dbeta[(i / 2 + 1) % kSums]);
+        if (c < a.cols) {
+          st_c(reinterpret_cast<float4*>(out + c), make_float4(d0.x, d0.y, d1.x, d1.y));
+          st_c(reinterpret_cast<float4*>(out + a.cols + c), make_float4(e0.x, e0.y, e1.x, e1.y));
+        }
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < OWN; ++i) {
-      const uint32_t c = column_of<V, OWN>(t, i);
+      const uint32_t c = column_of<V, OWN, L>(t, i);
       const float2 d = split(dgamma[i / 2 % kSums]), e = split(dbeta[i / 2 % kSums]);
       if (c < a.cols) { st_c(out + c, i % 2 ? d.y : d.x); st_c(out + a.cols + c, i % 2 ? e.y : e.x); }
     }
     return;
   }
   // the groups of the block lay their sums side by side in shared memory; all threads add them up, group after group
-  const uint32_t width = a.warps * 32 * OWN;
+  const uint32_t width = a.warps * L * OWN;
   float* sums = reinterpret_cast<float*>(norm_shared);
   copy_wait<0>();
   __syncthreads();
   float* mine = sums + (uint64_t)g.index * 2 * width;
 #pragma unroll
   for (int i = 0; i < OWN / 2; ++i) {
-    const uint32_t c = column_of<V, OWN>(t, 2 * i);
+    const uint32_t c = column_of<V, OWN, L>(t, 2 * i);
     if (V > 1) {
       *reinterpret_cast<Pair*>(mine + c) = dgamma[i % kSums];
       *reinterpret_cast<Pair*>(mine + width + c) = dbeta[i % kSums];
     } else {
       const float2 d = split(dgamma[i % kSums]), e = split(dbeta[i % kSums]);
       mine[c] = d.x;
-      mine[c + 32] = d.y;
+      mine[c + L] = d.y;
       mine[width + c] = e.x;
-      mine[width + c + 32] = e.y;
+      mine[width + c + L] = e.y;
     }
   }
   __syncthreads();
@@ -627,23 +669,48 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const NormArgs
   }
 }
 
-// Sums over the rows where the pass over dx does not hold them (rows of more than 8192 values): one column for
-// each thread; blockIdx.y takes every gridDim.y-th row into its own partial, eight rows in flight.
+// Sums over the rows where the pass over dx does not hold them (rows of more than 8192 values): 32 columns a block, the
+// rows of its slab (blockIdx.y) dealt over eight warps, eight rows on their way for each.  With one slab the sums are
+// the results.
 template <typename TX, typename TY>
-__global__ void __launch_bounds__(128) norm_column_sums_kernel(const NormArgs a) {
+__global__ void __launch_bounds__(256) norm_column_sums_kernel(const NormArgs a) {
+  __shared__ float part[2][8][33];
   grid_dependency_handshake();
-  const uint32_t c = blockIdx.x * 128 + threadIdx.x;
-  if (c >= a.cols) return;
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
   float dgamma = 0.0f, dbeta = 0.0f;
-#pragma unroll 8
-  for (uint64_t r = blockIdx.y; r < a.rows; r += gridDim.y) {
-    const float dy = to_float(ld_c(static_cast<const TY*>(a.dy) + r * a.ld_y + c));
-    dbeta += dy;
-    dgamma = fmaf(dy, (to_float(ld_c(static_cast<const TX*>(a.x) + r * a.ld_x + c)) - ld_c(a.mean + r)) * ld_c(a.rstd + r), dgamma);
+  if (c < a.cols) {
+    const TX* x = static_cast<const TX*>(a.x) + c;
+    const TY* dy = static_cast<const TY*>(a.dy) + c;
+    const uint64_t step = 8ull * gridDim.y;
+#pragma unroll 1
+    for (uint64_t r = blockIdx.y * 8 + warp; r < a.rows; r += 8 * step) {
+      float u[8], v[8], mean[8], rstd[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint64_t row = r + j * step;
+        const bool there = row < a.rows;
+        u[j] = there ? to_float(ld_c(dy + row * a.ld_y)) : 0.0f;
+        v[j] = there ? to_float(ld_c(x + row * a.ld_x)) : 0.0f;
+        mean[j] = there ? ld_c(a.mean + row) : 0.0f;
+        rstd[j] = there ? ld_c(a.rstd + row) : 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        dbeta += u[j];
+        dgamma = fmaf(u[j], (v[j] - mean[j]) * rstd[j], dgamma);
+      }
+    }
   }
-  float* out = a.partials + (uint64_t)blockIdx.y * 2 * a.cols;
-  st_c(out + c, dgamma);
-  st_c(out + a.cols + c, dbeta);
+  part[0][warp][lane] = dgamma;
+  part[1][warp][lane] = dbeta;
+  __syncthreads();
+  if (warp >= 2 || c >= a.cols) return;
+  float s = 0.0f;
+#pragma unroll
+  for (int w = 0; w < 8; ++w) s += part[warp][w][lane];
+  float* out = gridDim.y > 1 ? a.partials + (2ull * blockIdx.y + warp) * a.cols : warp == 0 ? a.dgamma : a.dbeta;
+  if (out) st_c(out + c, s);
 }
 
 // dgamma and dbeta from the blocks' partial sums: 32 columns a block, the partials dealt over its sixteen warps, all of a

@@ -66,6 +66,8 @@ NORMS = [
     (41, 2056, 0, 0, 0, BF16, F32, F32), (1200, 4096, 0, 0, 0, BF16, BF16, F32), (65, 4096, 0, 0, 3, F32, BF16, BF16), (12, 4104, 0, 0, 0, F32, BF16, F32),
     (10, 8192, 0, 0, 0, BF16, BF16, BF16), (7, 8200, 0, 1, 0, F32, F32, F32), (5, 16384, 0, 0, 0, F16, BF16, F32), (3, 16391, 0, 0, 0, F32, F32, F32),
     (70, 20000, 0, 0, 0, BF16, F16, BF16), (2, 40000, 0, 0, 0, F32, F32, F32),
+    (5000, 64, 0, 0, 0, BF16, BF16, BF16), (3001, 128, 0, 0, 0, BF16, BF16, F32), (700, 100, 8, 8, 0, F32, BF16, F32), (601, 127, 0, 0, 1, F16, F16, F16),
+    (1100, 9001, 0, 0, 0, BF16, BF16, F32), (600, 8200, 0, 0, 0, F32, F32, F32), (300, 4480, 0, 0, 0, F16, F16, F16),
 ]
 
 
