@@ -14,8 +14,9 @@ uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
 bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF16 || d == ACCEPT_DTYPE_F16; }
 
-// rows that all start on 16-byte boundaries
+// rows that all start on 16-byte boundaries, or on 4-byte ones
 bool whole_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p, 16) && ld * value_size(dtype) % 16 == 0; }
+bool word_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p, 4) && ld * value_size(dtype) % 4 == 0; }
 
 // Launch shape of a pass.  A row is shared by as many warps as hold it at `own` columns a thread; a block holds as many
 // such groups as fit 512 threads, fewer where there are too few rows for every SM.  16 columns a thread, 32 for rows of more
@@ -50,8 +51,8 @@ NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
   s.groups = (unsigned)(spread < most ? (spread ? spread : 1) : most);
   if (s.lanes < 32) s.groups = (unsigned)up(s.groups, 32 / s.lanes);  // whole warps
   const auto space = [&](int32_t dtype) {
-    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, s.own, s.lanes * s.warps, (uint32_t)p->cols)
-                                              : accept::row_space<uint16_t>(v, s.own, s.lanes * s.warps, (uint32_t)p->cols));
+    return (size_t)(dtype == ACCEPT_DTYPE_F32 ? accept::row_space<float>(v, s.own, s.lanes, s.warps)
+                                              : accept::row_space<uint16_t>(v, s.own, s.lanes, s.warps));
   };
   s.shared = s.groups * (size_t)stages_of(p, backward, s.own) * (space(p->dtype_x) + (backward ? space(p->dtype_y) : 0));
   // the column sums of the block's groups take the same memory
@@ -86,33 +87,44 @@ KernelFn rows_kernel(const NormShape& s, bool backward) {
                          : accept::norm_backward_kernel<TX, TY, V, 16, 8, stages_for(true, 16, kX, kY), true>;
 }
 
-// whole: rows start on 16-byte boundaries
 template <typename TX, typename TY>
-Kernels kernels_for(const NormShape& s, bool backward, bool whole) {
+KernelFn loose_kernel(const NormShape& s, bool backward) {
+  if constexpr (sizeof(TX) + sizeof(TY) < 8) return rows_kernel<TX, TY, 1>(s, backward);
+  else return nullptr;  // fp32 values start on 4-byte boundaries
+}
+
+// How rows lie: all tensors' on 16-byte boundaries, or the 16-bit tensors' on 4-byte boundaries, or neither.
+enum class RowStarts { kWhole, kWords, kLoose };
+
+template <typename TX, typename TY>
+Kernels kernels_for(const NormShape& s, bool backward, RowStarts starts) {
   constexpr int kUnit = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
-  return {whole ? rows_kernel<TX, TY, kUnit>(s, backward) : rows_kernel<TX, TY, 1>(s, backward), accept::norm_column_sums_kernel<TX, TY>};
+  return {starts == RowStarts::kWhole   ? rows_kernel<TX, TY, kUnit>(s, backward)
+          : starts == RowStarts::kWords ? rows_kernel<TX, TY, 2>(s, backward) : loose_kernel<TX, TY>(s, backward),
+          accept::norm_column_sums_kernel<TX, TY>};
 }
 
 template <typename TX>
-Kernels kernels_for_y(const accept_layer_norm_params* p, const NormShape& s, bool backward, bool whole) {
+Kernels kernels_for_y(const accept_layer_norm_params* p, const NormShape& s, bool backward, RowStarts starts) {
   switch (p->dtype_y) {
-    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, whole);
-    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, whole);
-    default: return kernels_for<TX, __half>(s, backward, whole);
+    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, starts);
+    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, starts);
+    default: return kernels_for<TX, __half>(s, backward, starts);
   }
 }
 
-Kernels select_kernels(const accept_layer_norm_params* p, const NormShape& s, bool backward, bool whole) {
+Kernels select_kernels(const accept_layer_norm_params* p, const NormShape& s, bool backward, RowStarts starts) {
   switch (p->dtype_x) {
-    case ACCEPT_DTYPE_F32: return kernels_for_y<float>(p, s, backward, whole);
-    case ACCEPT_DTYPE_BF16: return kernels_for_y<__nv_bfloat16>(p, s, backward, whole);
-    default: return kernels_for_y<__half>(p, s, backward, whole);
+    case ACCEPT_DTYPE_F32: return kernels_for_y<float>(p, s, backward, starts);
+    case ACCEPT_DTYPE_BF16: return kernels_for_y<__nv_bfloat16>(p, s, backward, starts);
+    default: return kernels_for_y<__half>(p, s, backward, starts);
   }
 }
 
-// Columns that a thread takes side by side where rows start on 16-byte boundaries (see column_of), else 1.
-int unit_of(const accept_layer_norm_params* p, bool whole) {
-  return !whole ? 1 : p->dtype_x == ACCEPT_DTYPE_F32 || p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 8;
+// Columns that a thread takes side by side (see column_of).
+int unit_of(const accept_layer_norm_params* p, RowStarts starts) {
+  if (starts != RowStarts::kWhole) return starts == RowStarts::kWords ? 2 : 1;
+  return p->dtype_x == ACCEPT_DTYPE_F32 || p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 8;
 }
 
 cudaError_t launch_norm(KernelFn fn, const NormShape& shape, NormArgs& a, cudaStream_t s) {
@@ -190,10 +202,11 @@ accept_status accept_layer_norm_forward(const accept_layer_norm_params* p, const
                 bounds_list.add(d_gamma, p->cols * value_size(p->dtype_w), false);
                 bounds_list.add(d_beta, p->cols * value_size(p->dtype_w), false);
                 bounds_list.add(d_mean, 4 * p->rows, true); bounds_list.add(d_rstd, 4 * p->rows, true));
-  const bool whole = whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_y, p->ld_y, p->dtype_y);
+  const RowStarts starts = whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_y, p->ld_y, p->dtype_y)  ? RowStarts::kWhole
+                           : word_rows(d_x, p->ld_x, p->dtype_x) && word_rows(d_y, p->ld_y, p->dtype_y) ? RowStarts::kWords : RowStarts::kLoose;
   a.whole_weights = is_aligned(d_gamma, 16) && is_aligned(d_beta, 16);
-  const NormShape shape = norm_shape(p, false, unit_of(p, whole));
-  ACCEPT_LAUNCH(launch_norm(select_kernels(p, shape, false, whole).rows, shape, a, s));
+  const NormShape shape = norm_shape(p, false, unit_of(p, starts));
+  ACCEPT_LAUNCH(launch_norm(select_kernels(p, shape, false, starts).rows, shape, a, s));
   return ACCEPT_OK;
 }
 
@@ -212,8 +225,10 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
       !is_aligned(d_dbeta, 4) || !is_aligned(d_ws, 16))
     return ACCEPT_ERR_MISALIGNED;
   cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-  const bool whole = whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_dy, p->ld_y, p->dtype_y) && is_aligned(d_dx, 16);
-  const NormShape shape = norm_shape(p, true, unit_of(p, whole));
+  const RowStarts starts =
+      whole_rows(d_x, p->ld_x, p->dtype_x) && whole_rows(d_dy, p->ld_y, p->dtype_y) && is_aligned(d_dx, 16) ? RowStarts::kWhole
+      : word_rows(d_x, p->ld_x, p->dtype_x) && word_rows(d_dy, p->ld_y, p->dtype_y) && is_aligned(d_dx, 4) ? RowStarts::kWords : RowStarts::kLoose;
+  const NormShape shape = norm_shape(p, true, unit_of(p, starts));
   NormArgs a = norm_args(p);
   a.x = d_x;
   a.dy = d_dy;
@@ -234,7 +249,7 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
                 bounds_list.add(d_dgamma, 4 * p->cols, true); bounds_list.add(d_dbeta, 4 * p->cols, true);
                 bounds_list.add(d_ws, accept_layer_norm_workspace_size(p), true));
   if (p->rows != 0) {
-    const Kernels k = select_kernels(p, shape, true, whole);
+    const Kernels k = select_kernels(p, shape, true, starts);
     const bool apart = shape.path != NormPath::kRegisters;
     if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
     if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 31) / 32, a.n_partials), 256, s, a));

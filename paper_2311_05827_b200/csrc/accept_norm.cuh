@@ -2,8 +2,8 @@
 //
 // Bound by memory: each value is read once and written once, and a row stays in the registers of the threads that
 // share it (OWN = 16 or 32 columns each) while its sums are taken.  A row's sums need barriers, during which its threads load
-// nothing; so the next rows are already on their way into shared memory by asynchronous copies.  Each thread copies what it
-// will itself read, so the copies need no barrier of their own.
+// nothing; so the next rows are already on their way into shared memory by asynchronous copies.  Each thread (where rows
+// are not aligned, each warp) copies what it will itself read, so the copies need no barrier of their own.
 #pragma once
 #include "accept_types.cuh"
 
@@ -34,8 +34,8 @@ struct NormArgs {
 
 // How the columns of a row lie over the threads that share it: L lanes (a warp, or eight lanes where a row is short) hold
 // L OWN neighbours, as units of V neighbours dealt over them, so that all addresses of a thread are one base and constants.  V = 8 where both tensors are 16-bit types,
-// 4 where one is fp32 (16 bytes at most for a thread, neighbours side by side), 1 where rows do not start on 16-byte
-// boundaries.
+// 4 where one is fp32 (16 bytes at most for a thread, neighbours side by side); where rows do not start on 16-byte
+// boundaries, 2 if those of the 16-bit tensors start on 4-byte ones, else 1.
 template <int V, int OWN, int L>
 __device__ __forceinline__ uint32_t column_of(uint32_t t, int own) {
   return t / L * (L * OWN) + V * (t % L) + own / V * (L * V) + own % V;
@@ -43,27 +43,29 @@ __device__ __forceinline__ uint32_t column_of(uint32_t t, int own) {
 template <int OWN, int L>  // all columns of the L lanes exist
 __device__ __forceinline__ bool lanes_are_full(uint32_t t, uint32_t cols) { return (t / L + 1) * (L * OWN) <= cols; }
 
-// How many values of each of the thread's units exist (V = 1: a bit for each).  FULL: all of them.
+// How many values of each of the thread's units exist (V = 1 and 2: a bit for each value).  FULL: all of them.
 template <int V, bool FULL, int OWN, int L>
 struct Own {
-  static constexpr int kUnits = V > 1 ? OWN / V : 1;
+  static constexpr int kUnits = V > 2 ? OWN / V : 1;
   uint32_t count[kUnits];
   __device__ __forceinline__ Own(uint32_t t, uint32_t cols) {
+    if (V > 2) {
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) {
-      if (V > 1) {
+      for (int i = 0; i < kUnits; ++i) {
         const uint32_t c = column_of<V, OWN, L>(t, V * i);
         count[i] = c < cols ? min(cols - c, (uint32_t)V) : 0;
-      } else {
-        count[0] = 0;
-#pragma unroll
-        for (int j = 0; j < OWN; ++j) count[0] |= column_of<1, OWN, L>(t, j) < cols ? 1u << j : 0u;
       }
+    } else {
+      count[0] = 0;
+#pragma unroll
+      for (int j = 0; j < OWN; ++j) count[0] |= column_of<V, OWN, L>(t, j) < cols ? 1u << j : 0u;
     }
   }
-  __device__ __forceinline__ uint32_t of(int unit) const { return FULL ? V : count[unit % kUnits]; }
+  __device__ __forceinline__ uint32_t of(int unit) const {
+    return FULL ? V : V > 2 ? count[unit % kUnits] : V == 2 ? (count[0] >> 2 * unit & 1) + (count[0] >> (2 * unit + 1) & 1) : count[0] >> unit & 1;
+  }
   __device__ __forceinline__ bool has(int value) const {  // value of the thread's OWN
-    return FULL || (V > 1 ? (uint32_t)(value % V) < count[value / V % kUnits] : (count[0] >> value & 1) != 0);
+    return FULL || (V > 2 ? (uint32_t)(value % V) < count[value / V % kUnits] : (count[0] >> value & 1) != 0);
   }
 };
 
@@ -90,10 +92,11 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 template <int PENDING>  // all but the last PENDING groups have landed
 __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(PENDING) : "memory"); }
 
-// Bytes of shared memory that a row of T takes for `threads` threads (V = 1: the 16-byte pieces that hold it).
+// Bytes of shared memory that a row of T takes for `warps` times `lanes` threads (V = 1 and 2: for each of the warps the
+// 16-byte pieces that hold its columns).
 template <typename T>
-__host__ __device__ constexpr uint32_t row_space(int v, int own, uint32_t threads, uint32_t cols) {
-  return v > 1 ? threads * own * (uint32_t)sizeof(T) : (cols * (uint32_t)sizeof(T) + 30) / 16 * 16;
+__host__ __device__ constexpr uint32_t row_space(int v, int own, uint32_t lanes, uint32_t warps) {
+  return warps * (lanes * own * (uint32_t)sizeof(T) + (v > 2 ? 0 : 16));
 }
 
 // Starts the copies of a row into `dst` (shared).  `begin` and `end` bound the values of the matrix.  Units that do not
@@ -109,31 +112,51 @@ __device__ __forceinline__ void start_units(uint32_t to, const T* from, const Ow
 template <typename T, int V, bool FULL, int OWN, int L>
 __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, uint32_t threads, const Own<V, FULL, OWN, L>& own,
                                           const T* begin, const T* end) {
-  if constexpr (V > 1) {
+  if constexpr (V > 2) {
     const uint32_t first = column_of<V, OWN, L>(t, 0), to = dst + first * (uint32_t)sizeof(T);
     const T* from = row + first;
     start_units(to, from, own);
   } else {
-    // the 16-byte pieces that hold the row; what lies outside the matrix is not read
-    const uintptr_t from = reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15, to = reinterpret_cast<uintptr_t>(row + cols);
-    const uint32_t pieces = (uint32_t)((to - from + 15) / 16);
-    for (uint32_t i = t; i < pieces; i += threads) {
-      const uintptr_t at = from + 16ull * i;
-      if (at >= reinterpret_cast<uintptr_t>(begin)) {
-        const uint64_t left = reinterpret_cast<uintptr_t>(end) - at;
-        copy_async<16>(dst + 16 * i, reinterpret_cast<const void*>(at), left < 16 ? (uint32_t)left : 16u);
-      } else {  // the matrix starts inside this piece
-        for (const T* p = begin; reinterpret_cast<uintptr_t>(p) < at + 16 && p < end; ++p) {
-          const T v = ld_c(p);
-          const uint32_t to_byte = dst + 16 * i + (uint32_t)(reinterpret_cast<uintptr_t>(p) - at);
-          if (sizeof(T) == 4) {
-            uint32_t w;
-            memcpy(&w, &v, sizeof(T));
-            asm volatile("st.shared.u32 [%0], %1;" ::"r"(to_byte), "r"(w) : "memory");
-          } else {
-            uint16_t w;
-            memcpy(&w, &v, 2);
-            asm volatile("st.shared.u16 [%0], %1;" ::"r"(to_byte), "h"(w) : "memory");
+    // the 16-byte pieces that hold the L lanes' columns; what lies outside the matrix is not read
+    constexpr uint32_t kBytes = L * OWN * (uint32_t)sizeof(T);
+    const uint32_t part = t / L, lane = t % L;
+    dst += part * (kBytes + 16) + 16 * lane;
+    const T* begins = row + part * (L * OWN);
+    const uintptr_t from = (reinterpret_cast<uintptr_t>(begins) & ~(uintptr_t)15) + 16 * lane;
+    if (FULL && row != begin && row + cols != end) {
+      const void* p = reinterpret_cast<const void*>(from);
+      copy_async_at<16, 0, 0>(dst, p);
+      copy_async_at<16, 16 * L, 16 * L>(dst, p);
+      if constexpr (kBytes > 32 * L) {
+        copy_async_at<16, 32 * L, 32 * L>(dst, p);
+        copy_async_at<16, 48 * L, 48 * L>(dst, p);
+      }
+      if constexpr (kBytes > 64 * L) {
+        copy_async_at<16, 64 * L, 64 * L>(dst, p);
+        copy_async_at<16, 80 * L, 80 * L>(dst, p);
+        copy_async_at<16, 96 * L, 96 * L>(dst, p);
+        copy_async_at<16, 112 * L, 112 * L>(dst, p);
+      }
+      if (lane == 0) copy_async_at<16, kBytes, kBytes>(dst, p);  // the columns end inside one more piece, or before it
+    } else {
+      const T* ends = part * (L * OWN) + L * OWN < cols ? begins + L * OWN : row + cols;
+      for (uintptr_t at = from; at < reinterpret_cast<uintptr_t>(ends); at += 16 * L, dst += 16 * L) {
+        if (at >= reinterpret_cast<uintptr_t>(begin)) {
+          const uint64_t left = reinterpret_cast<uintptr_t>(end) - at;
+          copy_async<16>(dst, reinterpret_cast<const void*>(at), left < 16 ? (uint32_t)left : 16u);
+        } else {  // the matrix starts inside this piece
+          for (const T* p = begin; reinterpret_cast<uintptr_t>(p) < at + 16 && p < end; ++p) {
+            const T v = ld_c(p);
+            const uint32_t to_byte = dst + (uint32_t)(reinterpret_cast<uintptr_t>(p) - at);
+            if (sizeof(T) == 4) {
+              uint32_t w;
+              memcpy(&w, &v, sizeof(T));
+              asm volatile("st.shared.u32 [%0], %1;" ::"r"(to_byte), "r"(w) : "memory");
+            } else {
+              uint16_t w;
+              memcpy(&w, &v, 2);
+              asm volatile("st.shared.u16 [%0], %1;" ::"r"(to_byte), "h"(w) : "memory");
+            }
           }
         }
       }
@@ -144,7 +167,7 @@ __device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t c
 // Zeros where this thread's units that do not exist would lie.
 template <typename T, int V, int OWN, int L>
 __device__ __forceinline__ void clear_row(uint32_t dst, uint32_t t, uint32_t cols) {
-  if (V == 1) return;
+  if (V <= 2) return;
 #pragma unroll
   for (int i = 0; i < OWN; i += V) {
     if (column_of<V, OWN, L>(t, i) < cols) continue;
@@ -177,28 +200,34 @@ __device__ __forceinline__ void take_units(uint32_t from, Pair (&v)[OWN / 2]) {
 // Takes a row that has landed at `src` (shared) into registers; columns that do not exist are zero.
 template <typename T, int V, bool FULL, int OWN, int L>
 __device__ __forceinline__ void take_row(uint32_t src, const T* row, uint32_t t, const Own<V, FULL, OWN, L>& own, Pair (&v)[OWN / 2]) {
-  if constexpr (V > 1) {
+  if constexpr (V > 2) {
     const uint32_t from = src + column_of<V, OWN, L>(t, 0) * (uint32_t)sizeof(T);
     take_units<T, V, OWN, L>(from, v);
   } else {
-    const uint32_t from = src + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + column_of<V, OWN, L>(t, 0) * (uint32_t)sizeof(T);
-    float lo = 0.0f;
+    const uint32_t from = src + t / L * (L * OWN * (uint32_t)sizeof(T) + 16) + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15) + V * (t % L) * (uint32_t)sizeof(T);
+    // what lies where a column does not exist (it is inside the warp's space) is read and dropped
 #pragma unroll
-    for (int i = 0; i < OWN; ++i) {
-      float f = 0.0f;
-      if (own.has(i)) {
-        if constexpr (sizeof(T) == 4) {
-          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(from + i * L * 4));
-        } else {
-          uint16_t w;
-          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(from + i * L * 2));
-          T h;
-          memcpy(&h, &w, 2);
-          f = to_float(h);
-        }
+    for (int i = 0; i < OWN; i += 2) {
+      float lo, hi;
+      if constexpr (sizeof(T) == 4) {
+        constexpr int kNext = V == 2 ? 4 : 4 * L;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lo) : "r"(from + i / V * (L * V) * 4));
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(hi) : "r"(from + i / V * (L * V) * 4 + kNext));
+      } else if constexpr (V == 2) {
+        uint32_t w;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(from + i * L * 2));
+        const float2 f = split(word_to_pair<T>(w));
+        lo = f.x;
+        hi = f.y;
+      } else {
+        uint16_t w0, w1;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w0) : "r"(from + i * L * 2));
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w1) : "r"(from + (i + 1) * L * 2));
+        const float2 f = split(word_to_pair<T>(w0 | (uint32_t)w1 << 16));
+        lo = f.x;
+        hi = f.y;
       }
-      if (i % 2) v[i / 2] = pair_of(lo, f);
-      else lo = f;
+      v[i / 2] = FULL ? pair_of(lo, hi) : pair_of(own.has(i) ? lo : 0.0f, own.has(i + 1) ? hi : 0.0f);
     }
   }
 }
@@ -209,7 +238,15 @@ __device__ __forceinline__ void store_row(T* row, uint32_t t, const Own<V, FULL,
 #pragma unroll
   for (int i = 0; i < OWN / V; ++i) {
     T* p = to + i * L * V;
-    if (V > 1 && own.of(i) == V) {
+    if (V == 2 && own.of(i) == 2) {
+      if constexpr (sizeof(T) == 2) {
+        st_c(reinterpret_cast<uint32_t*>(p), pair_to_word<T>(v[i % (OWN / 2)]));
+      } else {
+        const float2 f = split(v[i % (OWN / 2)]);
+        st_c(p, from_float<T>(f.x));
+        st_c(p + 1, from_float<T>(f.y));
+      }
+    } else if (V > 2 && own.of(i) == V) {
       uint32_t w[4];
 #pragma unroll
       for (int j = 0; j < V / 2; ++j) {
@@ -244,7 +281,7 @@ __device__ __forceinline__ float weight_at(const void* w, int dtype, float absen
 template <typename T, int V, bool FULL, int OWN, int L>
 __device__ __forceinline__ void load_weights_of(const T* w, bool whole, const Own<V, FULL, OWN, L>& own, float absent, uint32_t t, Pair (&v)[OWN / 2]) {
   w += column_of<V, OWN, L>(t, 0);
-  if (V > 1 && FULL && whole) {
+  if (V > 2 && FULL && whole) {
     uint4 raw[OWN * sizeof(T) / 16];
     constexpr int kEach = 16 / (int)sizeof(T), kOf = V >= kEach ? V / kEach : 1;  // values of a load, loads of a unit
     if constexpr (V >= kEach) {
@@ -366,7 +403,7 @@ __device__ __forceinline__ void forward_rows(const NormArgs& a, const Group<L>& 
   const Own<V, FULL, OWN, L> own(t, a.cols);
   bool ends_inside = false;
 #pragma unroll
-  for (int i = 0; i < OWN / V; ++i) ends_inside |= V > 1 && own.of(i) % V != 0;
+  for (int i = 0; i < OWN / V; ++i) ends_inside |= V > 2 && own.of(i) % V != 0;
   const TX* x = static_cast<const TX*>(a.x);
   const TX* end = x + (a.rows - 1) * a.ld_x + a.cols;
   const TX* row = x + first * a.ld_x;
@@ -388,7 +425,7 @@ __device__ __forceinline__ void forward_rows(const NormArgs& a, const Group<L>& 
     if (left > STAGES - 1) start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end);
     copy_commit();
     copy_wait<STAGES - 1>();
-    if (V == 1) g.sync();
+    if (V <= 2) __syncwarp(g.mask);  // other lanes of the warp have copied for this one
     Pair v[OWN / 2];
     take_row<TX, V, FULL, OWN, L>(here, row, t, own, v);
     Pair sums[4] = {v[0], v[1], v[2], v[3]};
@@ -400,9 +437,9 @@ __device__ __forceinline__ void forward_rows(const NormArgs& a, const Group<L>& 
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) {
       // a unit that does not exist stays zero; one that ends inside (one thread's) is masked value by value
-      if (V > 1) v[i] = add2(v[i], both(own.of(2 * i / V) ? -mean : 0.0f));
+      if (FULL || V > 2) v[i] = add2(v[i], both(own.of(2 * i / V) ? -mean : 0.0f));
       else v[i] = add2(v[i], pair_of(own.has(2 * i) ? -mean : 0.0f, own.has(2 * i + 1) ? -mean : 0.0f));
-      if (!FULL && V > 1 && ends_inside) {
+      if (!FULL && V > 2 && ends_inside) {
         const float2 f = split(v[i]);
         v[i] = pair_of(own.has(2 * i) ? f.x : 0.0f, own.has(2 * i + 1) ? f.y : 0.0f);
       }
@@ -428,7 +465,7 @@ __global__ void __launch_bounds__(512) norm_forward_kernel(const NormArgs a) {
   __shared__ __align__(16) float slots[kMostGroups][2][16];
   const Group<L> g(a.warps);
   const uint32_t groups = blockDim.x / g.threads;
-  const uint32_t space = row_space<TX>(V, OWN, L * a.warps, a.cols);
+  const uint32_t space = row_space<TX>(V, OWN, L, a.warps);
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space;
   const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
   const uint32_t step = gridDim.x * groups;
@@ -487,7 +524,7 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const Group<L>&
     const float mean = mean_next, rstd = rstd_next;
     if (left > 1) { mean_next = ld_c(means += step); rstd_next = ld_c(rstds += step); }
     copy_wait<STAGES - 1>();
-    if (V == 1) g.sync();
+    if (V <= 2) __syncwarp(g.mask);  // other lanes of the warp have copied for this one
     Pair xhat[OWN / 2], h[OWN / 2];
     take_row<TX, V, FULL, OWN, L>(here, row, t, own, xhat);
     take_row<TY, V, FULL, OWN, L>(here + space_x, drow, t, own, h);
@@ -512,8 +549,8 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const Group<L>&
 #pragma unroll
       for (int i = 0; i < OWN / 2; ++i) h[i] = mul2(fma2(xhat[i], slope, add2(h[i], less)), both(rstd));
       store_row<TX, V, FULL, OWN, L>(out, t, own, h);
-    } else if (V == 1) {
-      g.sync();  // the row has been read: its place is free
+    } else if (V <= 2) {
+      __syncwarp(g.mask);  // the row has been read: its place is free
     }
     if (--left == 0) break;
     row += stride_x;
@@ -530,7 +567,7 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
   __shared__ __align__(16) float slots[kMostGroups][2][32];
   const Group<L> g(a.warps);
   const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space_x = row_space<TX>(V, OWN, L * a.warps, a.cols), space = space_x + row_space<TY>(V, OWN, L * a.warps, a.cols);
+  const uint32_t space_x = row_space<TX>(V, OWN, L, a.warps), space = space_x + row_space<TY>(V, OWN, L, a.warps);
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(norm_shared) + g.index * STAGES * space;
   const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
   const uint32_t step = gridDim.x * groups;
@@ -558,7 +595,7 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
   if (!SUMS || !a.partials) return;
   float* out = a.partials + (uint64_t)blockIdx.x * 2 * a.cols;
   if (groups == 1) {
-    if (V > 1 && a.cols % 4 == 0) {
+    if (V > 2 && a.cols % 4 == 0) {
 #pragma unroll
       for (int i = 0; i < OWN; i += 4) {
         const uint32_t c = column_of<V, OWN, L>(t, i);

@@ -68,6 +68,8 @@ NORMS = [
     (70, 20000, 0, 0, 0, BF16, F16, BF16), (2, 40000, 0, 0, 0, F32, F32, F32),
     (5000, 64, 0, 0, 0, BF16, BF16, BF16), (3001, 128, 0, 0, 0, BF16, BF16, F32), (700, 100, 8, 8, 0, F32, BF16, F32), (601, 127, 0, 0, 1, F16, F16, F16),
     (1100, 9001, 0, 0, 0, BF16, BF16, F32), (600, 8200, 0, 0, 0, F32, F32, F32), (300, 4480, 0, 0, 0, F16, F16, F16),
+    (50, 1030, 0, 0, 0, BF16, BF16, BF16), (33, 2051, 1, 3, 2, F16, F16, F16), (31, 1031, 0, 0, 0, BF16, BF16, F32), (400, 98, 0, 0, 0, BF16, BF16, BF16),
+    (20, 515, 0, 1, 0, F32, BF16, F32), (20, 515, 2, 0, 1, F32, F32, F32), (9, 8190, 0, 0, 0, F16, BF16, F16), (3, 9003, 1, 1, 0, BF16, F32, BF16),
 ]
 
 
