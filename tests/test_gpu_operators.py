@@ -486,3 +486,15 @@ def test_product_whose_copies_do_not_arrive_reports_it_and_leaves_the_gpu_usable
         A.accept_block_matmul(p, a, sa, b, sb, None, d, ws)
         assert A.accept_last_device_status(ws) == A.DEV_COPY_TIMEOUT
     check_product(A, m, n, k, "e4m3", "e4m3", BF16, True, False, 0)
+
+
+# ---- the operators together ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("tokens,width,features", [(256, 512, 384), (130, 328, 200)])
+def test_linear_stage_step(tokens, width, features):
+    """A training step of the example: 8-bit operands (E4M3: 2^-4 relative rounding at most, a third of that on average;
+    E5M2: twice that) leave the products within 10 %, gradients of sums over tokens included."""
+    from examples import linear_stage
+    errors = linear_stage.run(tokens, width, features, seed=3)
+    assert set(errors) == {"y", "dx", "dweight", "dgamma", "dbeta"}
+    assert max(errors.values()) < 0.1, errors
