@@ -97,19 +97,19 @@ KernelFn loose_kernel(const NormShape& s, bool backward) {
 enum class RowStarts { kWhole, kWords, kLoose };
 
 template <typename TX, typename TY>
-Kernels kernels_for(const NormShape& s, bool backward, RowStarts starts) {
+Kernels kernels_for(const NormShape& s, bool backward, RowStarts starts, bool wide_sums) {
   constexpr int kUnit = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
   return {starts == RowStarts::kWhole   ? rows_kernel<TX, TY, kUnit>(s, backward)
           : starts == RowStarts::kWords ? rows_kernel<TX, TY, 2>(s, backward) : loose_kernel<TX, TY>(s, backward),
-          accept::norm_column_sums_kernel<TX, TY>};
+          wide_sums ? accept::norm_column_sums_kernel<TX, TY, 4> : accept::norm_column_sums_kernel<TX, TY, 1>};
 }
 
 template <typename TX>
 Kernels kernels_for_y(const accept_layer_norm_params* p, const NormShape& s, bool backward, RowStarts starts) {
   switch (p->dtype_y) {
-    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, starts);
-    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, starts);
-    default: return kernels_for<TX, __half>(s, backward, starts);
+    case ACCEPT_DTYPE_F32: return kernels_for<TX, float>(s, backward, starts, p->cols % 4 == 0 && starts == RowStarts::kWhole);
+    case ACCEPT_DTYPE_BF16: return kernels_for<TX, __nv_bfloat16>(s, backward, starts, p->cols % 4 == 0 && starts == RowStarts::kWhole);
+    default: return kernels_for<TX, __half>(s, backward, starts, p->cols % 4 == 0 && starts == RowStarts::kWhole);
   }
 }
 
@@ -250,9 +250,10 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
                 bounds_list.add(d_ws, accept_layer_norm_workspace_size(p), true));
   if (p->rows != 0) {
     const Kernels k = select_kernels(p, shape, true, starts);
+    const unsigned columns = p->cols % 4 == 0 && starts == RowStarts::kWhole ? 128 : 32;  // a block of the sums
     const bool apart = shape.path != NormPath::kRegisters;
     if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
-    if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + 31) / 32, a.n_partials), 256, s, a));
+    if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + columns - 1) / columns, a.n_partials), 256, s, a));
   }
   const bool summed = shape.path != NormPath::kRegisters && p->rows != 0 && a.n_partials == 1;
   if (weights && !summed) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 32 * accept::kJoinWarps, s, a));

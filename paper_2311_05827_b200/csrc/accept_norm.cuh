@@ -706,48 +706,79 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const NormArgs
   }
 }
 
-// Sums over the rows where the pass over dx does not hold them (rows of more than 8192 values): 32 columns a block, the
-// rows of its slab (blockIdx.y) dealt over eight warps, eight rows on their way for each.  With one slab the sums are
-// the results.
-template <typename TX, typename TY>
+// C neighbouring values at p, in fp32; one read where C = 4.
+template <typename T, int C>
+__device__ __forceinline__ void ld_neighbours(const T* p, float (&v)[C]) {
+  if constexpr (C == 1) {
+    v[0] = to_float(ld_c(p));
+  } else if constexpr (sizeof(T) == 4) {
+    const float4 f = ld_c(reinterpret_cast<const float4*>(p));
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+  } else {
+    const uint2 w = ld_c(reinterpret_cast<const uint2*>(p));
+    const float2 lo = split(word_to_pair<T>(w.x)), hi = split(word_to_pair<T>(w.y));
+    v[0] = lo.x; v[1] = lo.y; v[2] = hi.x; v[3] = hi.y;
+  }
+}
+
+// Sums over the rows where the pass over dx does not hold them (rows of more than 8192 values): 32 C columns a block (C = 4
+// where rows start on 16-byte boundaries and their length divides by 4), the rows of its slab (blockIdx.y) dealt over
+// eight warps, several rows on their way for each.  With one slab the sums are the results.
+template <typename TX, typename TY, int C>
 __global__ void __launch_bounds__(256) norm_column_sums_kernel(const NormArgs a) {
-  __shared__ float part[2][8][33];
+  __shared__ float part[2][8][32 * C + 1];
+  constexpr int kAtOnce = C == 1 ? 8 : 4;
   grid_dependency_handshake();
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint64_t c = (uint64_t)blockIdx.x * 32 + lane;
-  float dgamma = 0.0f, dbeta = 0.0f;
+  const uint64_t c = ((uint64_t)blockIdx.x * 32 + lane) * C;
+  float dgamma[C], dbeta[C];
+#pragma unroll
+  for (int k = 0; k < C; ++k) dgamma[k] = dbeta[k] = 0.0f;
   if (c < a.cols) {
     const TX* x = static_cast<const TX*>(a.x) + c;
     const TY* dy = static_cast<const TY*>(a.dy) + c;
     const uint64_t step = 8ull * gridDim.y;
 #pragma unroll 1
-    for (uint64_t r = blockIdx.y * 8 + warp; r < a.rows; r += 8 * step) {
-      float u[8], v[8], mean[8], rstd[8];
+    for (uint64_t r = blockIdx.y * 8 + warp; r < a.rows; r += kAtOnce * step) {
+      float u[kAtOnce][C], v[kAtOnce][C], mean[kAtOnce], rstd[kAtOnce];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
+      for (int j = 0; j < kAtOnce; ++j) {
         const uint64_t row = r + j * step;
-        const bool there = row < a.rows;
-        u[j] = there ? to_float(ld_c(dy + row * a.ld_y)) : 0.0f;
-        v[j] = there ? to_float(ld_c(x + row * a.ld_x)) : 0.0f;
-        mean[j] = there ? ld_c(a.mean + row) : 0.0f;
-        rstd[j] = there ? ld_c(a.rstd + row) : 0.0f;
+        mean[j] = rstd[j] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < C; ++k) u[j][k] = v[j][k] = 0.0f;
+        if (row < a.rows) {
+          ld_neighbours<TY, C>(dy + row * a.ld_y, u[j]);
+          ld_neighbours<TX, C>(x + row * a.ld_x, v[j]);
+          mean[j] = ld_c(a.mean + row);
+          rstd[j] = ld_c(a.rstd + row);
+        }
       }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dbeta += u[j];
-        dgamma = fmaf(u[j], (v[j] - mean[j]) * rstd[j], dgamma);
-      }
+      for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+        for (int k = 0; k < C; ++k) {
+          dbeta[k] += u[j][k];
+          dgamma[k] = fmaf(u[j][k], (v[j][k] - mean[j]) * rstd[j], dgamma[k]);
+        }
     }
   }
-  part[0][warp][lane] = dgamma;
-  part[1][warp][lane] = dbeta;
-  __syncthreads();
-  if (warp >= 2 || c >= a.cols) return;
-  float s = 0.0f;
 #pragma unroll
-  for (int w = 0; w < 8; ++w) s += part[warp][w][lane];
-  float* out = gridDim.y > 1 ? a.partials + (2ull * blockIdx.y + warp) * a.cols : warp == 0 ? a.dgamma : a.dbeta;
-  if (out) st_c(out + c, s);
+  for (int k = 0; k < C; ++k) {
+    part[0][warp][lane * C + k] = dgamma[k];
+    part[1][warp][lane * C + k] = dbeta[k];
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < 64 * C; i += 256) {
+    const uint32_t which = i / (32 * C), at = i - which * (32 * C);
+    const uint64_t col = (uint64_t)blockIdx.x * (32 * C) + at;
+    if (col >= a.cols) continue;
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += part[which][w][at];
+    float* out = gridDim.y > 1 ? a.partials + (2ull * blockIdx.y + which) * a.cols : which == 0 ? a.dgamma : a.dbeta;
+    if (out) st_c(out + col, s);
+  }
 }
 
 // dgamma and dbeta from the blocks' partial sums: 32 columns a block, the partials dealt over its sixteen warps, all of a
