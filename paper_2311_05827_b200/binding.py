@@ -249,14 +249,19 @@ def _check(code: int, where: str) -> None:
         raise AcceptError(code, where)
 
 
+_raw_stream = None  # (current stream of a device, current device) of torch, once it has been imported
+
+
 def _stream_handle(stream=None) -> int:
+    global _raw_stream
     if stream is not None:
         return int(stream.cuda_stream)
-    import torch
-    if not torch.cuda.is_initialized():
+    if _raw_stream is None:
+        import torch
         torch.cuda.init()
-    # the current stream's handle itself: building a torch.cuda.Stream object takes as long as a launch
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        # the current stream's handle itself: building a torch.cuda.Stream object takes as long as a launch
+        _raw_stream = (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+    return _raw_stream[0](_raw_stream[1]())
 
 
 # ---- size queries (host only) -------------------------------------------------------------
