@@ -25,7 +25,7 @@ bool word_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p,
 // own (kApart); rows of more than 16384 columns are not held (kLong).  Rows of up to 128 columns take eight lanes each: with
 // a warp each, 14400 x 105 bf16 took 13.4 us.
 enum class NormPath { kRegisters, kApart, kLong };
-struct NormShape { NormPath path; int own, lanes; unsigned warps, groups, blocks; size_t shared; };
+struct NormShape { NormPath path; int own, lanes; unsigned warps, groups, blocks; bool joins; size_t shared; };
 
 // Rows of a group in shared memory: up to 192 KB for the block.
 constexpr int stages_for(bool backward, int own, int size_x, int size_y) {
@@ -47,7 +47,13 @@ NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
   s.own = p->cols > 8192 ? 32 : 16;
   s.lanes = p->cols <= 128 ? 8 : 32;
   s.warps = (unsigned)((p->cols + s.lanes * s.own - 1) / (s.lanes * s.own));
-  const uint64_t spread = (p->rows + kSms - 1) / kSms, most = 512 / (s.lanes * s.warps);
+  const uint64_t most = 512 / (s.lanes * s.warps);
+  // So few rows that eight blocks take them in two turns: one cluster, which adds up dgamma and dbeta itself.  That saves the
+  // launch that would join them (64 x 1024 fp32: 7.4 us a call with it, the host's time for two launches, 5.6 without); the
+  // cluster's own adding up outweighs it for wider rows (5 x 4356 bf16: 8.3 us against 7.4) and for more groups (640 x 79 fp16:
+  // 8.9 us).
+  s.joins = backward && s.path == NormPath::kRegisters && p->cols <= 2048 && p->rows != 0 && p->rows <= 16 * most && p->rows <= 256;
+  const uint64_t over = s.joins ? 8 : kSms, spread = (p->rows + over - 1) / over;
   s.groups = (unsigned)(spread < most ? (spread ? spread : 1) : most);
   if (s.lanes < 32) s.groups = (unsigned)up(s.groups, 32 / s.lanes);  // whole warps
   const auto space = [&](int32_t dtype) {
@@ -59,14 +65,14 @@ NormShape norm_shape(const accept_layer_norm_params* p, bool backward, int v) {
   const size_t sums = backward && s.path == NormPath::kRegisters ? 2 * 4 * (size_t)s.own * s.lanes * s.warps * s.groups : 0;
   if (s.shared < sums) s.shared = sums;
   const uint64_t units = (p->rows + s.groups - 1) / s.groups;
-  s.blocks = (unsigned)(units < kSms ? units : kSms);
+  s.blocks = (unsigned)(units < over ? units : over);
   return s;
 }
 
 // Partial sums of dgamma and dbeta that the backward pass leaves in the workspace: one for each block, or for each
 // slab of rows (512 at least: a slab of its own costs a launch that joins them).
 uint64_t norm_partials(const accept_layer_norm_params* p, const NormShape& s) {
-  if (s.path == NormPath::kRegisters) return s.blocks;
+  if (s.path == NormPath::kRegisters) return s.joins ? 0 : s.blocks;
   const uint64_t slabs = (p->rows + 511) / 512;
   return slabs < 32 ? slabs : 32;
 }
@@ -134,7 +140,22 @@ cudaError_t launch_norm(KernelFn fn, const NormShape& shape, NormArgs& a, cudaSt
     const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shape.shared);
     if (err != cudaSuccess) return err;
   }
-  return accept::launch_overlapped_shared(fn, dim3(shape.blocks), threads, shape.shared, s, a);
+  if (!shape.joins) return accept::launch_overlapped_shared(fn, dim3(shape.blocks), threads, shape.shared, s, a);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(shape.blocks, 1, 1);
+  cfg.blockDim = dim3(threads, 1, 1);
+  cfg.dynamicSmemBytes = shape.shared;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = shape.blocks;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, fn, a);
 }
 
 NormArgs norm_args(const accept_layer_norm_params* p) {
@@ -236,7 +257,8 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
   a.mean = d_mean;
   a.rstd = d_rstd;
   a.dx = d_dx;
-  a.partials = weights ? reinterpret_cast<float*>(static_cast<uint8_t*>(d_ws) + 16) : nullptr;
+  a.joins = shape.joins;
+  a.partials = weights && !shape.joins ? reinterpret_cast<float*>(static_cast<uint8_t*>(d_ws) + 16) : nullptr;
   a.n_partials = (uint32_t)norm_partials(p, shape);
   a.whole_weights = is_aligned(d_gamma, 16);
   a.dgamma = d_dgamma;
@@ -255,7 +277,7 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
     if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
     if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + columns - 1) / columns, a.n_partials), 256, s, a));
   }
-  const bool summed = shape.path != NormPath::kRegisters && p->rows != 0 && a.n_partials == 1;
+  const bool summed = shape.joins || (shape.path != NormPath::kRegisters && p->rows != 0 && a.n_partials == 1);
   if (weights && !summed) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 32 * accept::kJoinWarps, s, a));
   return ACCEPT_OK;
 }

@@ -5,6 +5,7 @@
 // nothing; so the next rows are already on their way into shared memory by asynchronous copies.  Each thread (where rows
 // are not aligned, each warp) copies what it will itself read, so the copies need no barrier of their own.
 #pragma once
+#include "accept_tensor.cuh"
 #include "accept_types.cuh"
 
 namespace accept {
@@ -21,6 +22,7 @@ struct NormArgs {
   const float* rstd;
   void* dx;              // backward, may be null
   float* partials;       // backward: n_partials x 2 x cols, or null
+  int joins;             // backward: the grid is one cluster, which adds up dgamma and dbeta itself
   float* dgamma;
   float* dbeta;
   uint64_t rows, ld_x, ld_y;
@@ -592,9 +594,9 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
     if (full) backward_rows<TX, TY, V, true, OWN, L, STAGES, SUMS>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step, dgamma, dbeta);
     else backward_rows<TX, TY, V, false, OWN, L, STAGES, SUMS>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step, dgamma, dbeta);
   }
-  if (!SUMS || !a.partials) return;
+  if (!SUMS || !(a.partials || (a.joins && (a.dgamma || a.dbeta)))) return;
   float* out = a.partials + (uint64_t)blockIdx.x * 2 * a.cols;
-  if (groups == 1) {
+  if (groups == 1 && !a.joins) {
     if (V > 2 && a.cols % 4 == 0) {
 #pragma unroll
       for (int i = 0; i < OWN; i += 4) {
@@ -637,15 +639,38 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const NormArgs a) {
     }
   }
   __syncthreads();
-  for (uint32_t c = threadIdx.x; c < a.cols; c += blockDim.x) {
+#pragma unroll 2
+  for (uint32_t c = threadIdx.x; c < a.cols && groups > 1; c += blockDim.x) {
     float d = 0.0f, e = 0.0f;
+#pragma unroll 4
     for (uint32_t k = 0; k < groups; ++k) {
       d += sums[(uint64_t)k * 2 * width + c];
       e += sums[(uint64_t)k * 2 * width + width + c];
     }
-    st_c(out + c, d);
-    st_c(out + a.cols + c, e);
+    if (a.joins) {
+      sums[c] = d;
+      sums[width + c] = e;
+    } else {
+      st_c(out + c, d);
+      st_c(out + a.cols + c, e);
+    }
   }
+  if (!a.joins) return;
+  // few rows: the blocks of the one cluster take the columns in turn and add up what each of them has, in their order
+  cluster_sync();
+  const uint32_t from = smem_address(sums);
+#pragma unroll 2
+  for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < 2 * a.cols; i += gridDim.x * blockDim.x) {
+    const uint32_t which = i >= a.cols ? 1 : 0, c = i - which * a.cols, at = from + 4 * (which * width + c);
+    float v[8], d = 0.0f;
+#pragma unroll
+    for (uint32_t r = 0; r < 8; ++r) v[r] = r < gridDim.x ? ld_cluster_one(address_in(at, r)) : 0.0f;
+#pragma unroll
+    for (uint32_t r = 0; r < 8; ++r) d += v[r];
+    float* result = which ? a.dbeta : a.dgamma;
+    if (result) st_c(result + c, d);
+  }
+  cluster_sync();  // no block leaves while others read its sums
 }
 
 // Rows longer than the registers of a block: the same formulas, each row read again for each of its sums.
