@@ -251,6 +251,10 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
 // are read.  NT = 256 for large products; two tiles of sums (2 x 256 columns) and the scales do not fit 512 columns side by
 // side, so the two overlap by 24 columns: those are read first, and the next unit's products start once they are.
 // NT = 128 where tiles of 256 would leave pairs without work.
+// The products of unit i so wait twice: for the last read of unit i - 2, whose columns they take over (`drained`: all reading
+// warps of both blocks), and, where the two tiles overlap, for the first reads of unit i - 1 by the warps that hold the shared
+// columns (`shared_read`).  The second does not imply the first: the warps that hold no shared columns of unit i - 1 may still
+// be storing what they read of unit i - 2.
 //
 // A unit is a tile over all of k; the tiles that are left when every pair has had the same number (whole tiles) are cut
 // along k into `parts`, so that all pairs share the last round: one part at most for each pair, its last unit.  A part's
@@ -444,17 +448,20 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
   using S = PairShape<NT>;
   constexpr int kStages = S::kStages, kReaders = S::kReaders, kShare = kReaders / 4, kPer = NT / 32 / kShare;  // warps that share 32 rows, pieces of 32 columns for each
   extern __shared__ uint8_t raw_shared[];
-  __shared__ __align__(8) uint64_t barriers[2 * kStages + 4 + kReaders];
+  __shared__ __align__(8) uint64_t barriers[2 * kStages + 6 + kReaders];
   __shared__ uint32_t tensor_base, failed, issued;
   const uint32_t base = (smem_address(raw_shared) + 1023) & ~1023u;
   const uint32_t scales = base + kStages * S::kOperandBytes, staging = scales + kStages * S::kScaleBytes;
-  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16, joined = drained + 16;
+  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 16, shared_read = drained + 16, joined = shared_read + 16;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = cluster_rank();
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2 * kStages + 2; ++i) mbarrier_init(full + 8 * i, 1);
-    for (int i = 0; i < 2; ++i) mbarrier_init(drained + 8 * i, S::kOverlap ? 8 : 2 * kReaders);  // warps of both blocks that read what is waited for
+    for (int i = 0; i < 2; ++i) {  // warps of both blocks
+      mbarrier_init(drained + 8 * i, 2 * kReaders);
+      mbarrier_init(shared_read + 8 * i, 2 * 4);
+    }
     for (int i = 0; i < kReaders; ++i) mbarrier_init(joined + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     failed = issued = 0;
@@ -507,9 +514,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
     bool ok = true;
     Unit u;
     for (uint32_t unit = 0; ok && pair_unit(a, pair, pairs, unit, u); ++unit) {
-      // the columns shared with the last unit's sums, or the unit's before that
-      constexpr uint32_t kBack = S::kOverlap ? 1 : 2;
-      if (unit >= kBack && !mbarrier_wait_warp(drained + 8 * ((unit - kBack) & 1), ((unit - kBack) >> 1) & 1)) { ok = false; break; }
+      if (unit >= 2 && !mbarrier_wait_warp(drained + 8 * (unit & 1), ((unit - 2) >> 1) & 1)) { ok = false; break; }
+      if (S::kOverlap && unit >= 1 && !mbarrier_wait_warp(shared_read + 8 * ((unit - 1) & 1), ((unit - 1) >> 1) & 1)) { ok = false; break; }
       tensor_fence_after();
       const uint32_t into = tensor + (unit & 1 ? S::kSecond : 0);
       for (uint32_t b = u.first; b < u.last; ++b) {
@@ -547,7 +553,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
     const uint32_t piece_address = staging + warp * 2048;
     uint8_t* piece = raw_shared + (piece_address - smem_address(raw_shared));
     float* bias_tile = reinterpret_cast<float*>(raw_shared + (staging + S::kStaging - smem_address(raw_shared))) + warp * NT;
-    const uint32_t drained_at = address_in(drained, 0);
+    const uint32_t drained_at = address_in(drained, 0), shared_read_at = address_in(shared_read, 0);
     Unit u;
     for (uint32_t unit = 0; pair_unit(a, pair, pairs, unit, u); ++unit) {
       const uint32_t row0 = u.tile_m * kPairRows + rank * 128 + (warp & 3) * 32, col0 = u.tile_n * NT;
@@ -570,10 +576,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
         float v[32];
         tensor_read(from + c, v);
         tensor_read_wait();
-        if (S::kOverlap ? turn == 0 && (warp >> 2) == (unit & 1 ? 0 : kShare - 1) : turn + 1 == kPer) {
+        const bool shares = S::kOverlap && turn == 0 && (warp >> 2) == (unit & 1 ? 0 : kShare - 1), last = turn + 1 == kPer;
+        if (shares || last) {
           tensor_fence_before();
           __syncwarp();
-          if (lane == 0) mbarrier_arrive_cluster(drained_at + 8 * (unit & 1));
+          if (lane == 0) {
+            if (shares) mbarrier_arrive_cluster(shared_read_at + 8 * (unit & 1));
+            if (last) mbarrier_arrive_cluster(drained_at + 8 * (unit & 1));
+          }
         }
         if (partial) {
 #pragma unroll
@@ -593,7 +603,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
         // counts from 0 to parts - 1 and back to 0
         if (lane == 0) before = atomicInc(a.arrivals + (u.cut * 2 + rank) * kReaders + warp, a.parts - 1);
         before = __shfl_sync(0xffffffffu, before, 0);
-        if (before + 1 == a.parts) {  // all parts are there: add them in their order, this one's from tensor memory
+        if (before + 1 == a.parts) {  // all parts are there: add them in their order, this one's from tensor memory (it is the pair's last unit)
           __threadfence();
           asm volatile("fence.proxy.async;" ::: "memory");
           const uint32_t others = a.parts - 1, batch = S::kSlots / others, slots = base + warp * S::kSlots * 4096, bar = joined + 8 * warp;
