@@ -533,7 +533,14 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const Group<L>&
     Pair sum[2] = {both(0.0f), both(0.0f)}, along[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) {
-      xhat[i] = mul2(add2(xhat[i], both(-mean)), both(rstd));  // columns that do not exist: dy = 0, so this counts nowhere
+      xhat[i] = mul2(add2(xhat[i], both(-mean)), both(rstd));
+      // Zero in columns that do not exist: their x and dy are 0, but -mean rstd may pass the largest float where the row's own
+      // xhat do not (a constant row of 2^120), and 0 times infinity would be NaN in the row's sum.  (Masked here: before the
+      // multiplication, or in a branch for such rows alone, the fp32 kernels spill 180 bytes more.)
+      if (!FULL) {
+        const float2 f = split(xhat[i]);
+        xhat[i] = pair_of(own.has(2 * i) ? f.x : 0.0f, own.has(2 * i + 1) ? f.y : 0.0f);
+      }
       if (SUMS) {
         dbeta[i % kSums] = add2(dbeta[i % kSums], h[i]);
         dgamma[i % kSums] = fma2(h[i], xhat[i], dgamma[i % kSums]);
