@@ -40,3 +40,45 @@ def test_sums_are_read_before_the_unit_after_next_takes_their_place(A, n, k, dty
         first = d if first is None else first
         assert torch.equal(first.view(torch.uint8), d.view(torch.uint8))
     assert A.accept_last_device_status(ws) == 0
+
+
+# ---- tiles cut along k, and fp32 sums in chunks ---------------------------------------------------------------------------
+
+# m, n, k, type of d, bias, accumulate, extra values between rows of d; then what the sizes are chosen for: tiles that are cut,
+# their parts, their columns (0: none is cut)
+CUTS = [
+    (1280, 1100, 9000, BF16, True, False, 0, 25, 2, 256), (2560, 2560, 5000, F32, False, True, 0, 26, 2, 256),
+    (1280, 1000, 6000, F16, True, False, 1, 20, 3, 256), (2048, 3000, 4000, F32, True, False, 1, 22, 3, 256),
+    (1810, 300, 10000, BF16, False, True, 0, 24, 3, 128), (1810, 300, 10000, F32, True, True, 0, 24, 3, 128),
+    (700, 1100, 12000, F32, True, False, 0, 15, 4, 256), (2560, 2100, 4000, BF16, False, True, 3, 16, 4, 256),
+    (1570, 300, 10000, F32, False, False, 0, 14, 5, 256), (2590, 1800, 3500, BF16, True, False, 8, 14, 5, 256),
+    (700, 1000, 8300, F16, False, True, 0, 12, 6, 256), (500, 700, 20000, F32, True, True, 1, 12, 6, 128),
+    (500, 700, 20000, BF16, True, False, 0, 12, 6, 128),
+    # whole tiles whose sums are taken over two and three chunks of k, with and without cut ones beside them
+    (2304, 2100, 8300, F32, True, False, 0, 7, 6, 256), (2304, 2100, 8300, F32, True, True, 0, 7, 6, 256), (2304, 2100, 8300, F32, True, True, 1, 7, 6, 256),
+    (2304, 2100, 8300, F32, False, False, 1, 7, 6, 256), (1280, 2000, 8300, F32, True, True, 0, 0, 1, 256),
+    (1280, 2000, 8300, F32, True, False, 1, 0, 1, 256), (1280, 1100, 8300, F32, False, True, 0, 0, 1, 128), (2560, 2560, 16500, F32, True, True, 0, 0, 1, 256),
+]
+
+
+def bytes_of_parts(case):
+    _, _, _, _, _, _, _, cut, parts, columns = case
+    return cut * parts * 256 * columns * 4
+
+
+@pytest.mark.parametrize("case", CUTS, ids=str)
+def test_product_of_cut_tiles_and_chunks(A, case):
+    m, n, k, dtype, bias, accumulate, pad = case[:7]
+    # the workspace holds the parts' sums and what counts them: the sizes are dealt as this test means them to be
+    beside = A.accept_matmul_workspace_size(A.MatmulParams(m, n, k, dtype_d=ops.code_of(A, dtype), accumulate=accumulate, ldd=n + pad)) - bytes_of_parts(case)
+    assert 16 < beside < 32768 if case[7] else beside == 16
+    ops.check_product(A, m, n, k, "e5m2" if accumulate else "e4m3", "e4m3", dtype, bias, accumulate, pad)
+
+
+def test_cut_tiles_stay_inside_their_buffers(A):
+    from tests import gpu_util
+    with gpu_util.library_variant("bounds"):
+        assert A.accept_bounds_check_report()[:2] == (0, 0)
+        for case in CUTS:
+            ops.check_product(A, *case[:3], "e4m3", "e4m3", *case[3:7])
+        assert A.accept_bounds_check_report()[:2] == (0, 0)
