@@ -269,8 +269,9 @@ accept_status accept_mbq_decompress(const accept_mbq_params* p, const void* d_st
  * Layer norm forward and backward, quantisation to 8-bit floating point with one power-of-two scale
  * for each block of 128 values, and the matrix product of operands in that form (the linear layer's
  * forward product and both of its gradients).  They follow the rules of the entry points above:
- * asynchronous on the stream, nothing allocated, buffers and workspace owned by the caller.  The
- * paper has no counterpart of them.
+ * asynchronous on the stream, nothing allocated, buffers and workspace owned by the caller.  Of a workspace
+ * only the status word (word 0) has a meaning from one call to the next; these entry points may share one,
+ * for any sizes, as long as one call at a time uses it.  The paper has no counterpart of them.
  */
 typedef enum { ACCEPT_DTYPE_F32 = 0, ACCEPT_DTYPE_BF16 = 1, ACCEPT_DTYPE_F16 = 2 } accept_dtype;
 /* 8-bit formats: E4M3 without infinities (largest value 448) and E5M2 (largest finite value 57344). */
@@ -367,8 +368,8 @@ typedef struct {
 
 accept_status accept_matmul_check_params(const accept_matmul_params* p);
 size_t accept_matmul_workspace_size(const accept_matmul_params* p);
-/* bias: n fp32 values, or NULL.  d_ws: 16-byte aligned; zero before its first use by this entry point and after a call
- * whose status word is not zero (calls leave it ready for the next, of any sizes).  The status word gets ACCEPT_DEV_COPY_TIMEOUT if a wait inside the kernel ran out. */
+/* bias: n fp32 values, or NULL.  d_ws: 16-byte aligned.  The status word gets ACCEPT_DEV_COPY_TIMEOUT if a wait inside the
+ * kernel ran out: then d is unspecified, and the whole workspace is to be zeroed before a captured graph repeats that call. */
 accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b,
                                   const void* d_b_scale, const float* d_bias, void* d_d, void* d_ws, size_t ws_bytes,
                                   void* cuda_stream);

@@ -1,4 +1,6 @@
 // Host side of the block-scaled matrix product (accept_block_matmul): argument checks, tensor maps, launches.
+#include <chrono>
+
 #include "accept_host.cuh"
 #include "accept_matmul.cuh"
 
@@ -65,9 +67,26 @@ bool result_map(CUtensorMap* map, void* d, int32_t dtype, uint64_t m, uint64_t n
 }
 
 // ---- large products: pairs of SMs ----
-// Arrival counts at the start of the workspace, for 73 cut tiles of 16 warps at most: a fixed place, so that calls of
-// different sizes can share a workspace.
-constexpr size_t kArrivalBytes = 74 * 64;
+// Arrival counts at the start of the workspace, for 73 cut tiles of 16 warps at most.  What they hold before a call does not
+// matter: a call counts from its own number on (see accept::arrive), so a workspace can serve other calls and other entry
+// points in between, without a launch that clears it.
+constexpr size_t kArrivalBytes = 74 * 16 * sizeof(unsigned long long);
+
+// A number for a call, a multiple of 8 and not 0: 61 bits that no other call of this process has and that what happens to lie
+// in memory does not look like (a counter and the process' start, mixed one to one).
+unsigned long long call_number() {
+  static const uint64_t start = (uint64_t)std::chrono::system_clock::now().time_since_epoch().count() ^ (uint64_t)(uintptr_t)&start;
+  static std::atomic<uint64_t> calls{0};
+  constexpr uint64_t kMask = (1ull << 61) - 1;
+  for (;;) {
+    uint64_t v = (start + calls.fetch_add(1, std::memory_order_relaxed)) & kMask;
+    v = v * 0x9e3779b97f4a7c15ull & kMask;  // odd factors and shifts to the right: one to one on 61 bits
+    v ^= v >> 31;
+    v = v * 0xd6e8feb86659fd93ull & kMask;
+    v ^= v >> 29;
+    if (v != 0) return v << 3;
+  }
+}
 
 // How a product is dealt to the pairs of SMs: see matmul_pair_kernel.
 struct PairPlan { unsigned nt; uint64_t tiles; unsigned pairs; uint32_t whole, parts, chunks; };
@@ -147,7 +166,8 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
   a.bias = base.bias;
   a.d = base.d;
   a.status = base.status;
-  a.arrivals = reinterpret_cast<uint32_t*>(d_ws + 16);
+  a.arrivals = reinterpret_cast<unsigned long long*>(d_ws + 16);
+  a.call = plan.parts > 1 ? call_number() : 0;
   a.partials = reinterpret_cast<float*>(d_ws + 16 + kArrivalBytes);
   a.ldd = base.ldd;
   a.dtype_d = base.dtype_d;

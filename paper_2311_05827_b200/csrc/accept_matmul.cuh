@@ -289,7 +289,8 @@ struct PairArgs {
   void* d;
   uint32_t* status;
   float* partials;     // parts of cut tiles: (tile, part) x 256 x NT values
-  uint32_t* arrivals;  // one for each reading warp of both blocks and each cut tile; zero, and zero again after the call
+  unsigned long long* arrivals;  // one for each reading warp of both blocks and each cut tile, see arrive()
+  unsigned long long call;       // this call's number: a multiple of 8, never 0, another for each call
   uint64_t ldd;
   uint32_t m, n, blocks;
   uint32_t atoms_a, atoms_b;
@@ -310,6 +311,24 @@ struct Unit {
   uint32_t cut;    // index of the cut tile, or ~0
   uint32_t part;
 };
+
+// One arrival of `parts` (8 at most) at a count in the workspace: how many of this call came before it.  A count holds the
+// call's number plus its arrivals; whatever else is there, left by anyone who used the workspace before, stands for none.  The
+// last one leaves zero, which is what the first one of the next call expects.  At most parts + 1 turns: past the second, each
+// turn follows another part's arrival.
+__device__ __forceinline__ uint32_t arrive(unsigned long long* count, unsigned long long call, uint32_t parts) {
+  unsigned long long held = 0;
+  for (;;) {
+    const uint32_t before = held - call < 8 ? (uint32_t)(held - call) : 0;
+    if (before + 1 == parts) {
+      *reinterpret_cast<volatile unsigned long long*>(count) = 0;  // all others have been here
+      return before;
+    }
+    const unsigned long long found = atomicCAS(count, held, call + before + 1);
+    if (found == held) return before;
+    held = found;
+  }
+}
 
 // The i-th unit of a pair; false if it has no more.  Tiles are taken in the order eight tiles of rows, then the next tile
 // of columns: the tiles in flight at a time form a block that shares its operands in L2.
@@ -600,8 +619,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
         __threadfence();
         __syncwarp();
         uint32_t before = 0;
-        // counts from 0 to parts - 1 and back to 0
-        if (lane == 0) before = atomicInc(a.arrivals + (u.cut * 2 + rank) * kReaders + warp, a.parts - 1);
+        if (lane == 0) before = arrive(a.arrivals + (u.cut * 2 + rank) * kReaders + warp, a.call, a.parts);
         before = __shfl_sync(0xffffffffu, before, 0);
         if (before + 1 == a.parts) {  // all parts are there: add them in their order, this one's from tensor memory (it is the pair's last unit)
           __threadfence();

@@ -1,0 +1,77 @@
+"""Buffers that calls share: one workspace for several entry points and sizes."""
+import pytest
+
+from tests import test_gpu_operators as ops
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def A():
+    import paper_2311_05827_b200 as pkg
+    return pkg
+
+
+def test_one_workspace_serves_all_operators_by_turns(A):
+    """A buffer that held anything before, used by products of different cuts (2, 3 and 6 parts), layer norms' backward
+    passes and the quantiser in turn: every result is the one that a fresh workspace gives, bit for bit."""
+    sizes = [(700, 1000, 8300, BF16), (1810, 300, 10000, F32), (1280, 1100, 9000, BF16), (700, 1000, 8300, BF16)]
+    products = []
+    for i, (m, n, k, dtype) in enumerate(sizes):
+        p = A.MatmulParams(m, n, k, dtype_d=ops.code_of(A, dtype))
+        assert A.accept_matmul_workspace_size(p) > 4096
+        operands = ops.coded(2 * i, m, k, "e4m3") + ops.coded(2 * i + 1, n, k, "e4m3")
+        want = torch.empty(m, n, dtype=dtype, device="cuda")
+        A.accept_block_matmul(p, *operands, None, want, A.new_workspace(p))
+        products.append((p, operands, want))
+    norm, q = A.LayerNormParams(900, 1500), A.QuantizeParams(900, 1500)
+    x, dy = ops.random(20, 900, 1500), ops.random(21, 900, 1500)
+    y, mean, rstd = torch.empty_like(x), torch.empty(900, device="cuda"), torch.empty(900, device="cuda")
+    A.accept_layer_norm_forward(norm, x, None, None, y, mean, rstd)
+
+    def backward(ws):
+        out = torch.empty_like(x), torch.empty(1500, device="cuda"), torch.empty(1500, device="cuda")
+        A.accept_layer_norm_backward(norm, dy, x, None, mean, rstd, *out, ws)
+        return out
+
+    def quantize(ws):
+        out = [torch.empty(size(q, side), dtype=torch.uint8, device="cuda") for side in (False, True) for size in (A.accept_block_data_size, A.accept_block_scale_size)]
+        A.accept_block_quantize(q, x, *out, ws)
+        return out
+
+    grads, codes = backward(A.new_workspace(norm)), quantize(A.new_workspace(q))
+    size = max([A.accept_matmul_workspace_size(p) for p, _, _ in products] + [A.accept_layer_norm_workspace_size(norm)])
+    for fill in (0, 1, 0x33, 0xFF):
+        ws = torch.full((size,), fill, dtype=torch.uint8, device="cuda")
+        ws[:4] = 0  # the status word is the caller's
+        for p, operands, want in products:
+            d = torch.full_like(want, float("nan"))
+            A.accept_block_matmul(p, *operands, None, d, ws)
+            assert torch.equal(d, want)
+            for a, b in zip(grads, backward(ws)):
+                assert torch.equal(a, b)
+            for a, b in zip(codes, quantize(ws)):
+                assert torch.equal(a, b)
+        assert A.accept_last_device_status(ws) == 0
+
+
+def test_a_captured_product_of_cut_tiles_repeats(A):
+    """A CUDA graph repeats one call: the same result each time, whatever else the workspace served in between."""
+    m, n, k = 700, 1000, 8300
+    p = A.MatmulParams(m, n, k)
+    operands = ops.coded(1, m, k, "e4m3") + ops.coded(2, n, k, "e4m3")
+    want, d, ws = torch.empty(m, n, dtype=BF16, device="cuda"), torch.empty(m, n, dtype=BF16, device="cuda"), A.new_workspace(p)
+    A.accept_block_matmul(p, *operands, None, want, ws)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.accept_block_matmul(p, *operands, None, d, ws)
+    for fill in (None, None, 1, -1, 0x33333333):
+        if fill is not None:
+            ws[1:] = fill
+        d.fill_(float("nan"))
+        graph.replay()
+        assert torch.equal(d, want)
