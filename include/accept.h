@@ -291,7 +291,8 @@ typedef enum { ACCEPT_BLOCK_ROW = 0, ACCEPT_BLOCK_SQUARE = 1 } accept_block;
  *   dtype_x     type of x and dx;  dtype_y: of y and dy;  dtype_w: of gamma and beta.  Statistics and the
  *               gradients of gamma and beta are fp32, as is everything computed on the way.
  * Pointers need the alignment of their values; rows that start on 16-byte boundaries are read in 16-byte
- * pieces.  A row that holds a NaN or an infinity comes out as NaN; other rows do not notice.
+ * pieces.  y may be x, and dx may be x or dy (the whole matrix, where type and row stride are the same); no
+ * other output may overlap anything.  A row that holds a NaN or an infinity comes out as NaN; other rows do not notice.
  */
 typedef struct {
   uint64_t rows, cols;

@@ -274,8 +274,9 @@ accept_status accept_layer_norm_backward(const accept_layer_norm_params* p, cons
     const Kernels k = select_kernels(p, shape, true, starts);
     const unsigned columns = p->cols % 4 == 0 && starts == RowStarts::kWhole ? 128 : 32;  // a block of the sums
     const bool apart = shape.path != NormPath::kRegisters;
-    if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
+    // the column sums first: dx may take the place of x or dy
     if (apart && weights) ACCEPT_LAUNCH(launch_overlapped(k.sums, dim3((a.cols + columns - 1) / columns, a.n_partials), 256, s, a));
+    if (!apart || d_dx) ACCEPT_LAUNCH(launch_norm(k.rows, shape, a, s));
   }
   const bool summed = shape.joins || (shape.path != NormPath::kRegisters && p->rows != 0 && a.n_partials == 1);
   if (weights && !summed) ACCEPT_LAUNCH(launch_overlapped(accept::norm_join_kernel, dim3((unsigned)((2ull * a.cols + 31) / 32)), 32 * accept::kJoinWarps, s, a));

@@ -1,4 +1,4 @@
-"""Buffers that calls share: one workspace for several entry points and sizes."""
+"""Buffers that calls share: one workspace for several entry points and sizes, and results in the place of inputs."""
 import pytest
 
 from tests import test_gpu_operators as ops
@@ -75,3 +75,29 @@ def test_a_captured_product_of_cut_tiles_repeats(A):
         d.fill_(float("nan"))
         graph.replay()
         assert torch.equal(d, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("rows,cols,pad", [(70, 64, 0), (300, 1024, 0), (1200, 1037, 0), (40, 8192, 8), (600, 8200, 0), (1100, 9001, 0), (33, 16384, 0), (70, 20000, 1), (5, 20001, 0)])
+def test_norm_results_may_take_the_place_of_inputs(A, rows, cols, pad, dtype):
+    """y in the place of x, and dx in the place of x or of dy, give the bits that they give apart."""
+    p = A.LayerNormParams(rows, cols, 1e-5, ops.code_of(A, dtype), ops.code_of(A, dtype), A.DTYPE_F32, cols + pad, cols + pad)
+    place = lambda v: ops.matrix(rows, cols, cols + pad, dtype, v)[1]  # noqa: E731
+    x, dy = place(ops.random(1, rows, cols) + 0.5), place(ops.random(2, rows, cols, scale=0.1))
+    gamma, beta = 1 + 0.2 * ops.random(3, cols), 0.2 * ops.random(4, cols)
+    y, mean, rstd = place(None), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    A.accept_layer_norm_forward(p, x, gamma, beta, y, mean, rstd)
+    over = place(x)
+    A.accept_layer_norm_forward(p, over, gamma, beta, over)
+    assert torch.equal(over, y)
+
+    def backward(dy_, x_, dx):
+        dgamma, dbeta = torch.empty(cols, device="cuda"), torch.empty(cols, device="cuda")
+        A.accept_layer_norm_backward(p, dy_, x_, gamma, mean, rstd, dx, dgamma, dbeta, A.new_workspace(p))
+        return dx, dgamma, dbeta
+
+    want = backward(dy, x, place(None))
+    over_x, over_dy = place(x), place(dy)
+    for got in (backward(dy, over_x, over_x), backward(over_dy, x, over_dy)):
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
