@@ -27,10 +27,12 @@ bool word_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p,
 enum class NormPath { kRegisters, kApart, kLong };
 struct NormShape { NormPath path; int own, lanes; unsigned warps, groups, blocks; bool joins; size_t shared; };
 
-// Rows of a group in shared memory: up to 192 KB for the block.
+// Rows of a group in shared memory: up to 192 KB for the block, and 16 bytes more for each row of a warp (of eight lanes where
+// those share it) and stage where rows are not aligned: 8 KB at most, for 64 rows of eight lanes, two tensors and four stages.
+constexpr int kRing = 196608, kMostShared = kRing + 64 * 16 * 2 * 4;
 constexpr int stages_for(bool backward, int own, int size_x, int size_y) {
   const int row = 512 * own * (size_x + (backward ? size_y : 0));
-  return 196608 / row < 4 ? 196608 / row : 4;
+  return kRing / row < 4 ? kRing / row : 4;
 }
 int stages_of(const accept_layer_norm_params* p, bool backward, int own) {
   return stages_for(backward, own, p->dtype_x == ACCEPT_DTYPE_F32 ? 4 : 2, p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 2);
@@ -137,7 +139,9 @@ cudaError_t launch_norm(KernelFn fn, const NormShape& shape, NormArgs& a, cudaSt
   a.warps = shape.warps;
   const unsigned threads = shape.path == NormPath::kLong ? 1024 : shape.lanes * shape.warps * shape.groups;
   if (shape.shared > 32 * 1024) {  // with the static part, more than a kernel gets without asking
-    const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shape.shared);
+    // the kernel's limit is the process': always the same, so that another thread's call of other sizes cannot lower it before
+    // this one's launch
+    const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared);
     if (err != cudaSuccess) return err;
   }
   if (!shape.joins) return accept::launch_overlapped_shared(fn, dim3(shape.blocks), threads, shape.shared, s, a);

@@ -1,6 +1,11 @@
-"""Buffers that calls share: one workspace for several entry points and sizes, and results in the place of inputs."""
+"""What calls share: one workspace for several entry points and sizes, results in the place of inputs, and kernels that several
+host threads launch."""
+import ctypes
+import threading
+
 import pytest
 
+from tests import operators_plain as plain
 from tests import test_gpu_operators as ops
 
 pytestmark = pytest.mark.gpu
@@ -101,3 +106,43 @@ def test_norm_results_may_take_the_place_of_inputs(A, rows, cols, pad, dtype):
     for got in (backward(dy, over_x, over_x), backward(over_dy, x, over_dy)):
         for a, b in zip(got, want):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+def test_norms_of_different_shapes_from_four_threads(A, backward):
+    """Four host threads with streams and buffers of their own, whose calls run the same kernel with different amounts of
+    shared memory: every call is accepted, and right."""
+    from paper_2311_05827_b200 import binding
+    lib = binding.lib()
+    shapes = [(2048, 1024), (40, 4096), (300, 513), (2048, 4096)]
+    refused, calls = [0] * len(shapes), []
+    for i, (rows, cols) in enumerate(shapes):
+        p, stream = A.LayerNormParams(rows, cols), torch.cuda.Stream()
+        x, out, mean, rstd = ops.random(i, rows, cols), torch.empty(rows, cols, device="cuda"), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        ws = A.new_workspace(p)
+        A.accept_layer_norm_forward(p, x, None, None, out, mean, rstd)
+        handle, c, size = stream.cuda_stream, ctypes.byref(p.c()), 4 * ws.numel()
+        if backward:
+            call = (lib.accept_layer_norm_backward, (c, x.data_ptr(), x.data_ptr(), None, mean.data_ptr(), rstd.data_ptr(), out.data_ptr(), None, None, ws.data_ptr(), size, handle))
+        else:
+            call = (lib.accept_layer_norm_forward, (c, x.data_ptr(), None, None, out.data_ptr(), None, None, handle))
+        calls.append((call, stream, x, mean, rstd, out, p, ws))
+    torch.cuda.synchronize()
+
+    def work(i):
+        (f, args), stream = calls[i][:2]
+        for turn in range(10000):
+            refused[i] += f(*args) != 0
+            if turn % 500 == 0:
+                stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(shapes))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert refused == [0] * len(shapes)
+    for _, _, x, mean, rstd, out, _, _ in calls:
+        want = plain.norm_grad(x, x, None, mean, rstd)[0] if backward else plain.norm(x, None, None, 1e-5)[0]
+        assert float((out.double() - want).abs().max()) < 1e-4
