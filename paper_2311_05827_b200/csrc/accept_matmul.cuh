@@ -24,6 +24,10 @@ struct MatmulArgs {
   int wide_stores;            // four neighbours of d are stored at once (aligned rows, nothing to add)
 };
 
+// How long the warps that read the sums may wait for those over `blocks` blocks of k: the limit of one copy and 2 us for each
+// block (200 to 700 cycles, measured), so that long sums are not taken for lost ones.
+__device__ __forceinline__ unsigned long long sums_wait_ns(uint32_t blocks) { return kCopyWaitNs + 2000ull * blocks; }
+
 __device__ __forceinline__ float load_value(const void* d, int dtype, uint64_t at) {
   if (dtype == kF32) return ld_c(static_cast<const float*>(d) + at);
   if (dtype == kBf16) return __bfloat162float(ld_c(static_cast<const __nv_bfloat16*>(d) + at));
@@ -201,7 +205,7 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
   // The block's sums go through shared memory as fp32, a row of d (a row of a) in 128 floats.
   float* tile = reinterpret_cast<float*>(raw_shared + (base - smem_address(raw_shared)));
   if (warp < kSmallReaders) {
-    const bool ok = mbarrier_wait_warp(done, 0);
+    const bool ok = mbarrier_wait_warp(done, 0, sums_wait_ns(last - first));
     if (!ok) atomicExch(&failed, 1u);
     tensor_fence_after();
     if (ok) {
@@ -582,7 +586,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
         for (uint32_t c = lane; c < NT; c += 32) bias_tile[c] = col0 + c < a.n ? ld_c(a.bias + col0 + c) : 0.0f;
         __syncwarp();
       }
-      if (!mbarrier_wait(done + 8 * (unit & 1), (unit >> 1) & 1)) { atomicExch(&failed, 1u); break; }
+      // by the whole warp: the reads of tensor memory that follow want all of its lanes, also where the wait runs out for some
+      if (!mbarrier_wait_warp(done + 8 * (unit & 1), (unit >> 1) & 1, sums_wait_ns(u.last - u.first))) {
+        if (lane == 0) atomicExch(&failed, 1u);
+        break;
+      }
       tensor_fence_after();
       const uint32_t from = sums + (unit & 1 ? S::kSecond : 0) + (((warp & 3) * 32) << 16);
       // a cut tile: this warp's 32 x NT values of each part, four neighbours of each lane's row side by side

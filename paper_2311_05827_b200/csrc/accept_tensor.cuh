@@ -14,8 +14,8 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
   return r != 0;
 }
-// mbarrier_wait by a whole warp, with one result for all lanes.
-__device__ __forceinline__ bool mbarrier_wait_warp(uint32_t bar, uint32_t parity) {
+// mbarrier_wait by a whole warp, with one result for all lanes; gives up after `limit_ns`.
+__device__ __forceinline__ bool mbarrier_wait_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns = kCopyWaitNs) {
   unsigned long long t0 = 0;
   for (uint32_t it = 0;; ++it) {
     uint32_t done;
@@ -29,7 +29,7 @@ __device__ __forceinline__ bool mbarrier_wait_warp(uint32_t bar, uint32_t parity
       unsigned long long now;
       asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
       if (t0 == 0) t0 = now;
-      else if (__any_sync(0xffffffffu, now - t0 > kCopyWaitNs)) return false;
+      else if (__any_sync(0xffffffffu, now - t0 > limit_ns)) return false;
     }
   }
 }

@@ -82,3 +82,21 @@ def test_cut_tiles_stay_inside_their_buffers(A):
         for case in CUTS:
             ops.check_product(A, *case[:3], "e4m3", "e4m3", *case[3:7])
         assert A.accept_bounds_check_report()[:2] == (0, 0)
+
+
+# ---- long sums --------------------------------------------------------------------------------------------------------------
+
+def test_product_of_the_longest_rows(A):
+    """k = 2^31 - 1, the largest that the header allows: sums that take longer (416 ms, measured) than
+    a copy may (200 ms), and offsets past 31 bits."""
+    k = 2 ** 31 - 1
+    at = [0, 5, 2 ** 30 + 129, k - 1]
+    a, b = torch.zeros(2 ** 31, dtype=torch.uint8, device="cuda"), torch.zeros(2 ** 31, dtype=torch.uint8, device="cuda")
+    for i, c in enumerate(at):
+        a[c], b[c] = 0x38, 0x38 + 8 * i  # 1 times 2^i
+    p = A.MatmulParams(1, 1, k)
+    scales = torch.full((A.accept_block_scale_size(A.QuantizeParams(1, k)),), 127, dtype=torch.uint8, device="cuda")
+    d, ws = torch.zeros(1, 1, dtype=BF16, device="cuda"), A.new_workspace(p)
+    A.accept_block_matmul(p, a, scales, b, scales, None, d, ws)
+    assert A.accept_last_device_status(ws) == 0
+    assert float(d) == 15.0
