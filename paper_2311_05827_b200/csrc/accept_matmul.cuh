@@ -28,6 +28,19 @@ struct MatmulArgs {
 // block (200 to 700 cycles, measured), so that long sums are not taken for lost ones.
 __device__ __forceinline__ unsigned long long sums_wait_ns(uint32_t blocks) { return kCopyWaitNs + 2000ull * blocks; }
 
+// After a wait that ran out in this block (one warp): waits until the products have read the `issued` copies, stage after stage
+// (one that was never filled passes), or none has come for the limit of a wait.  So no copy and no product is under way when the
+// block frees its tensor memory and leaves, also where the other warps went on after one had given up.  (Without such a wait
+// the reading warps' own wait for the last sums says as much; asking every stage there too took 4 x 4096 x 4096 from 5.2 to 5.6 us.)
+template <int STAGES>
+__device__ __noinline__ void settle(uint32_t empty, uint32_t issued) {
+  uint32_t stage = issued % STAGES, parity = 1 ^ (issued / STAGES & 1);
+  for (int i = 0; i < STAGES; ++i) {
+    if (!mbarrier_wait_warp(empty + 8 * stage, parity)) return;
+    if (++stage == STAGES) { stage = 0; parity ^= 1; }
+  }
+}
+
 __device__ __forceinline__ float load_value(const void* d, int dtype, uint64_t at) {
   if (dtype == kF32) return ld_c(static_cast<const float*>(d) + at);
   if (dtype == kBf16) return __bfloat162float(ld_c(static_cast<const __nv_bfloat16*>(d) + at));
@@ -223,19 +236,17 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
   }
   if (parts > 1) cluster_sync();
   else __syncthreads();
+  const bool failure = *reinterpret_cast<volatile uint32_t*>(&failed) != 0;
   if (warp == 0) {
+    if (failure) {
+      if (lane == 0) atomicOr(a.status, kDevCopyTimeout);
+      settle<kStages>(empty, issued);
+    }
     tensor_fence_after();
     tensor_free(sums, kColumns);
   }
 
-  const bool failure = *reinterpret_cast<volatile uint32_t*>(&failed) != 0;
-  if (failure) {
-    if (threadIdx.x == 0) {
-      atomicOr(a.status, kDevCopyTimeout);
-      // no copy of this block may still be on its way when it leaves
-      for (uint32_t i = 0; i < issued && i < kStages; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kStages) & 1);
-    }
-  } else {
+  if (!failure) {
     // wide: a lane has four neighbours of a row; otherwise four columns 32 apart, so that a row leaves in runs
     const bool wide = a.wide_stores && row_a + kTileA <= a.n;
     const uint32_t at = smem_address(tile);
@@ -682,11 +693,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
   }
   __syncwarp();
   __syncthreads();
-  if (threadIdx.x == 0 && *reinterpret_cast<volatile uint32_t*>(&failed)) {
-    atomicOr(a.status, kDevCopyTimeout);
-    // no copy may still be on its way when a block of the pair leaves
-    if (rank == 0)
-      for (uint32_t i = 0; i < issued && i < kStages; ++i) mbarrier_wait(full + 8 * i, ((issued - 1 - i) / kStages) & 1);
+  if (warp == 0 && *reinterpret_cast<volatile uint32_t*>(&failed)) {
+    if (lane == 0) atomicOr(a.status, kDevCopyTimeout);
+    settle<kStages>(empty, issued);
   }
   tensor_fence_before();
   cluster_sync();

@@ -84,6 +84,29 @@ def test_cut_tiles_stay_inside_their_buffers(A):
         assert A.accept_bounds_check_report()[:2] == (0, 0)
 
 
+# ---- waits that run out --------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("m,n,k,dtype", [(4, 300, 64, BF16), (64, 9600, 4096, F32), (300, 300, 100, F32), (2304, 2304, 64, BF16), (8192, 4160, 1024, BF16),
+                                         (700, 1000, 8300, BF16), (2304, 2100, 8300, F32)], ids=str)
+def test_products_whose_copies_do_not_arrive_end_and_leave_the_gpu_usable(A, m, n, k, dtype):
+    """Fewer copies than stages and more of them, many units a pair, cut tiles, chunks of k: the call reports the wait that ran
+    out, and the next call is right."""
+    from tests import gpu_util
+    a, sa = ops.coded(1, m, k, "e4m3")
+    b, sb = ops.coded(2, n, k, "e4m3")
+    p = A.MatmulParams(m, n, k, dtype_d=ops.code_of(A, dtype))
+    d, want, ws = torch.zeros(m, n, dtype=dtype, device="cuda"), torch.zeros(m, n, dtype=dtype, device="cuda"), A.new_workspace(p)
+    A.accept_block_matmul(p, a, sa, b, sb, None, want, ws)
+    assert A.accept_last_device_status(ws) == 0
+    with gpu_util.library_variant("stall"):
+        A.accept_block_matmul(p, a, sa, b, sb, None, d, ws)
+        assert A.accept_last_device_status(ws) == A.DEV_COPY_TIMEOUT
+    ws[0] = 0
+    A.accept_block_matmul(p, a, sa, b, sb, None, d, ws)
+    assert A.accept_last_device_status(ws) == 0
+    assert torch.equal(d, want)
+
+
 # ---- long sums --------------------------------------------------------------------------------------------------------------
 
 def test_product_of_the_longest_rows(A):
