@@ -199,7 +199,9 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
 
 template <int NT>
 cudaError_t launch_small(const CUtensorMap& map_a, const CUtensorMap& map_b, const MatmulArgs& a, unsigned tiles, unsigned parts, cudaStream_t s) {
-  auto fn = accept::matmul_small_kernel<NT>;
+  // 16-bit results are rounded by 2^-9 or 2^-12 in the end: one run does for them
+  const bool chunks = a.dtype_d == ACCEPT_DTYPE_F32 && (a.blocks + parts - 1) / parts > accept::kChunk;
+  auto fn = chunks ? accept::matmul_small_kernel<NT, true> : accept::matmul_small_kernel<NT, false>;
   const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, accept::kSmallShared);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};

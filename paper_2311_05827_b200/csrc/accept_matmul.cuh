@@ -55,12 +55,19 @@ __device__ __forceinline__ uint32_t two_values(int dtype, float x, float y) {  /
   return dtype == kBf16 ? pair_to_word<__nv_bfloat16>(pair_of(x, y)) : pair_to_word<__half>(pair_of(x, y));
 }
 
+// Blocks of k that fp32 results are summed over in one run of the tensor cores (see the pairs of SMs).
+constexpr uint32_t kChunk = 64;
+
 // ---- small products: single tokens, small batches, few tiles ---------------------------------------------------------
 //
 // Bound by the bytes of b, or by the time of a launch.  b's rows take the 128 lanes of the instruction's M side and a's rows
 // its N side (NT = 16 to 128), so nothing is loaded or multiplied for rows that are not there.  Where there are few tiles
 // the blocks of a cluster share k, up to eight ways, and add their sums through each other's shared memory in the order of
 // their ranks.  Every block asks for as much of its share at once as shared memory holds.
+//
+// fp32 results of shares of more than kChunk blocks of k (CHUNKS) are summed as those of pairs are, a chunk at a time: the
+// reading warps hold the sums so far in registers (64 at NT = 128) and add each chunk's, the next chunk's products start once
+// they have read it: 0 to 4 % (16 x 9600 x 32768 73.8 -> 75.8 us, 128 x 9600 x 32768 85.5 -> 86.0).
 constexpr int kTileA = 128;
 constexpr int kSmallReaders = 8;  // warps that read the sums: two share 32 lanes
 constexpr int kSmallThreads = 32 * (kSmallReaders + 2);
@@ -125,7 +132,7 @@ __device__ __forceinline__ void small_store(const MatmulArgs& a, uint32_t tile, 
   }
 }
 
-template <int NT>
+template <int NT, bool CHUNKS>
 __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                  const MatmulArgs a) {
   constexpr int kStage = small_stage_bytes(NT), kStages = small_stages(NT);
@@ -134,18 +141,21 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
   constexpr uint32_t kColumns = NT <= 32 ? 64 : NT <= 64 ? 128 : 256;  // NT sums and the scales, a power of two
   constexpr uint32_t kScaleColumn = kColumns - 8 * kWords;
   extern __shared__ uint8_t raw_shared[];
-  __shared__ __align__(8) uint64_t barriers[2 * kStages + 1];
+  __shared__ __align__(8) uint64_t barriers[2 * kStages + 2];
   __shared__ uint32_t tensor_base, failed, issued;
   const uint32_t base = (smem_address(raw_shared) + 1023) & ~1023u;  // 128-byte swizzle repeats every 1024 bytes
-  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages;
+  const uint32_t full = smem_address(barriers), empty = full + 8 * kStages, done = empty + 8 * kStages, drained = done + 8;
   const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t parts = gridDim.y, rank = blockIdx.y;
   const uint32_t first = (uint32_t)((uint64_t)a.blocks * rank / parts), last = (uint32_t)((uint64_t)a.blocks * (rank + 1) / parts);
   const uint32_t tile_b = blockIdx.x / a.tiles, tile_a = blockIdx.x - tile_b * a.tiles;
   const uint32_t row_a = tile_a * kTileA, row_b = tile_b * NT, rows = min(a.m - row_b, (uint32_t)NT);
+  const uint32_t chunks = CHUNKS ? (last - first + kChunk - 1) / kChunk : 1;
+  const auto chunk_start = [&](uint32_t chunk) { return first + (uint32_t)((uint64_t)(last - first) * chunk / chunks); };
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2 * kStages + 1; ++i) mbarrier_init(full + 8 * i, 1);
+    mbarrier_init(drained, kSmallReaders);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     failed = issued = 0;
     prefetch_map(&map_a);
@@ -184,8 +194,17 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
   } else if (warp == kSmallReaders + 1) {  // matrix instructions
     const bool leader = elect_one();
     const uint32_t tensor = __shfl_sync(0xffffffffu, sums, 0);
-    uint32_t stage = 0, parity = 0, word = kWords - 1, b = first;
+    uint32_t stage = 0, parity = 0, word = kWords - 1, b = first, chunk = 0, from = first;
+    uint32_t stop = CHUNKS ? chunk_start(1) : last;
     for (; b < last; ++b) {
+      if (CHUNKS && b == stop) {
+        if (leader) mma_commit(done);
+        if (!mbarrier_wait_warp(drained, chunk & 1)) break;
+        tensor_fence_after();
+        ++chunk;
+        from = b;
+        stop = chunk_start(chunk + 1);
+      }
       if (!mbarrier_wait_warp(full + 8 * stage, parity)) break;
       tensor_fence_after();
       // A word of scales serves four blocks of k and comes round again after three others, thirteen blocks after the last
@@ -203,7 +222,7 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
         }
 #pragma unroll
         for (uint32_t k = 0; k < 4; ++k)  // 32 values of k: 32 bytes further in the swizzled rows
-          scaled_mma(tensor, da + 2 * k, db + 2 * k, instruction, scale_a, scale_a + 4, b > first || k > 0);
+          scaled_mma(tensor, da + 2 * k, db + 2 * k, instruction, scale_a, scale_a + 4, b > from || k > 0);
         mma_commit(empty + 8 * stage);
       }
       if (++stage == kStages) { stage = 0; parity ^= 1; }
@@ -217,12 +236,47 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
 
   // The block's sums go through shared memory as fp32, a row of d (a row of a) in 128 floats.
   float* tile = reinterpret_cast<float*>(raw_shared + (base - smem_address(raw_shared)));
-  if (warp < kSmallReaders) {
+  constexpr int kPiece = NT < 32 ? 16 : 32;
+  if (CHUNKS && warp < kSmallReaders) {
+    constexpr int kPieces = NT > 2 * kPiece ? NT / (2 * kPiece) : 1;
+    float total[kPieces][kPiece];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+      for (int j = 0; j < kPiece; ++j) total[i][j] = 0.0f;
+    bool ok = true;
+    for (uint32_t chunk = 0; chunk < chunks && ok; ++chunk) {
+      ok = mbarrier_wait_warp(done, chunk & 1, sums_wait_ns(kChunk));
+      if (!ok) break;
+      tensor_fence_after();
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const uint32_t c = kPiece * ((warp >> 2) + 2 * i);
+        if (c < rows) {
+          float v[kPiece];
+          tensor_read(sums + (((warp & 3) * 32) << 16) + c, v);
+          tensor_read_wait();
+#pragma unroll
+          for (int j = 0; j < kPiece; ++j) total[i][j] += v[j];
+        }
+      }
+      tensor_fence_before();
+      __syncwarp();
+      if (lane == 0) mbarrier_arrive(drained);
+    }
+    if (!ok && lane == 0) atomicExch(&failed, 1u);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const uint32_t c = kPiece * ((warp >> 2) + 2 * i);
+      if (ok && c < rows)
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) tile[(c + j) * kTileA + (warp & 3) * 32 + lane] = total[i][j];
+    }
+  } else if (warp < kSmallReaders) {
     const bool ok = mbarrier_wait_warp(done, 0, sums_wait_ns(last - first));
     if (!ok) atomicExch(&failed, 1u);
     tensor_fence_after();
     if (ok) {
-      constexpr int kPiece = NT < 32 ? 16 : 32;
 #pragma unroll 1
       for (uint32_t c = kPiece * (warp >> 2); c < rows; c += 2 * kPiece) {
         float v[kPiece];
@@ -277,9 +331,9 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
 // into the shared memory that the operands have left and adds all parts in their order.  No block waits for another pair.
 //
 // Sums that go out in fp32 are taken over at most kChunk blocks of k at a time and the chunks added one after the other
-// (in d): the tensor cores' own sums over 16384 values of k are off by 1.1e-6 of the result's norm, over 8192 by 0.8e-6.
+// (in d): the tensor cores' own sums are off by what grows with their length, 0.5e-6 of the result's norm over 8192 values of k,
+// 1.5e-6 over 20001, 3.0e-6 over 32768.  In chunks of 8192 it is 0.5e-6 for any k (fp32 library sums: 0.1e-6 to 0.2e-6).
 constexpr uint32_t kPairRows = 256;
-constexpr uint32_t kChunk = 64;
 
 template <int NT>
 struct PairShape {

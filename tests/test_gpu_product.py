@@ -81,6 +81,8 @@ def test_cut_tiles_stay_inside_their_buffers(A):
         assert A.accept_bounds_check_report()[:2] == (0, 0)
         for case in CUTS:
             ops.check_product(A, *case[:3], "e4m3", "e4m3", *case[3:7])
+        for m in (7, 32, 60, 128):  # long shares of few rows
+            ops.check_product(A, m, 2100, 35000, "e4m3", "e4m3", F32, True, False, 1)
         assert A.accept_bounds_check_report()[:2] == (0, 0)
 
 
@@ -108,6 +110,35 @@ def test_products_whose_copies_do_not_arrive_end_and_leave_the_gpu_usable(A, m, 
 
 
 # ---- long sums --------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("m", [5, 17, 64, 100, 128])
+@pytest.mark.parametrize("n,k,bias,accumulate,pad", [(9600, 32768, False, False, 0), (9601, 20001, True, True, 0), (2000, 70000, True, False, 1), (300, 131072, False, True, 0)])
+def test_few_rows_of_long_sums_are_single_precision(A, m, n, k, bias, accumulate, pad):
+    """fp32 results of few rows, shares of up to 256 blocks of k.  The tensor cores' sums over 8192 values are off by less than
+    10^-6 of their norm, so the sum of chunks of that length is too, whatever k is.  In one run, 20001 values are off by
+    1.5e-6 and 32768 by 3.0e-6."""
+    a, sa = ops.coded(1, m, k, "e4m3", spread=0)
+    b, sb = ops.coded(2, n, k, "e4m3", spread=0)
+    offset = ops.random(3, n) if bias else None
+    start = ops.random(4, m, n)
+    gd, d = ops.matrix(m, n, n + pad, F32, start)
+    p = A.MatmulParams(m, n, k, dtype_d=A.DTYPE_F32, accumulate=accumulate, ldd=n + pad)
+    A.accept_block_matmul(p, a, sa, b, sb, offset, d, A.new_workspace(p))
+    gd.check("d")
+    columns = 256  # of the result, the first ones: their scales are the first 128-row groups'
+    whole = b.shape[0]
+    r, at = torch.arange(columns, device="cuda")[:, None], torch.arange(-(-k // 128), device="cuda")[None]
+    e = sb[plain.place(r, at, whole)].double() - 127
+    vb = b[:columns, :k].contiguous().view(torch.float8_e4m3fn).double() * torch.ldexp(torch.ones_like(e), e.int()).repeat_interleave(128, 1)[:, :k]
+    want = plain.decode(a, sa, "e4m3", k) @ vb.t()
+    norm = want.norm()
+    if bias:
+        want += offset[:columns].double()
+    if accumulate:
+        want += start[:, :columns].double()
+    assert float((d[:, :columns].double() - want).norm() / norm) < 1e-6
+    assert bool(torch.isfinite(d).all())
+
 
 def test_product_of_the_longest_rows(A):
     """k = 2^31 - 1, the largest that the header allows: sums that take longer (416 ms, measured) than
