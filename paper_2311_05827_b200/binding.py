@@ -259,8 +259,10 @@ def _stream_handle(stream=None) -> int:
     if _raw_stream is None:
         import torch
         torch.cuda.init()
-        # the current stream's handle itself: building a torch.cuda.Stream object takes as long as a launch
-        _raw_stream = (torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice)
+        # the current stream's handle itself: building a torch.cuda.Stream object takes as long as a launch.  The functions are
+        # private to torch; without them it is the object
+        raw, device = (getattr(torch._C, name, None) for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+        _raw_stream = (raw, device) if raw and device else (lambda _: torch.cuda.current_stream().cuda_stream, lambda: None)
     return _raw_stream[0](_raw_stream[1]())
 
 
