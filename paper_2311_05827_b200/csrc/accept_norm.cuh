@@ -112,7 +112,7 @@ __device__ __forceinline__ void start_units(uint32_t to, const T* from, const Ow
   if constexpr (I + 1 < OWN / V) start_units<T, V, FULL, OWN, L, I + 1>(to, from, own);
 }
 template <typename T, int V, bool FULL, int OWN, int L>
-__device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, uint32_t threads, const Own<V, FULL, OWN, L>& own,
+__device__ __forceinline__ void start_row(uint32_t dst, const T* row, uint32_t cols, uint32_t t, const Own<V, FULL, OWN, L>& own,
                                           const T* begin, const T* end) {
   if constexpr (V > 2) {
     const uint32_t first = column_of<V, OWN, L>(t, 0), to = dst + first * (uint32_t)sizeof(T);
@@ -401,7 +401,7 @@ extern __shared__ __align__(16) uint8_t norm_shared[];
 // costs no digits.  FULL: all columns of this warp exist (the warps of a group meet at the same barriers either way).
 template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES>
 __device__ __forceinline__ void forward_rows(const NormArgs& a, const Group<L>& g, float (&slots)[2][16], uint32_t shared, uint32_t space, uint64_t first, uint32_t step) {
-  const uint32_t t = g.t, threads = g.threads, shared_end = shared + STAGES * space;
+  const uint32_t t = g.t, shared_end = shared + STAGES * space;
   const Own<V, FULL, OWN, L> own(t, a.cols);
   bool ends_inside = false;
 #pragma unroll
@@ -413,7 +413,7 @@ __device__ __forceinline__ void forward_rows(const NormArgs& a, const Group<L>& 
   const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) {
-    if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL, OWN, L>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end);
+    if (first + (uint64_t)s * step < a.rows) start_row<TX, V, FULL, OWN, L>(shared + s * space, row + s * stride_x, a.cols, t, own, x, end);
     copy_commit();
   }
   Pair gamma[OWN / 2], beta[OWN / 2];
@@ -424,7 +424,7 @@ __device__ __forceinline__ void forward_rows(const NormArgs& a, const Group<L>& 
   float* mean_out = a.mean_out && t == 0 ? a.mean_out + first : nullptr;
   float* rstd_out = a.rstd_out && t == 0 ? a.rstd_out + first : nullptr;
   for (;;) {
-    if (left > STAGES - 1) start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end);
+    if (left > STAGES - 1) start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, own, x, end);
     copy_commit();
     copy_wait<STAGES - 1>();
     if (V <= 2) __syncwarp(g.mask);  // other lanes of the warp have copied for this one
@@ -492,7 +492,7 @@ template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES
 __device__ __forceinline__ void backward_rows(const NormArgs& a, const Group<L>& g, float (&slots)[2][32], uint32_t shared, uint32_t space, uint32_t space_x,
                                               uint64_t first, uint32_t step, Pair (&dgamma)[SUMS ? OWN / 2 : 1], Pair (&dbeta)[SUMS ? OWN / 2 : 1]) {
   constexpr int kSums = SUMS ? OWN / 2 : 1;
-  const uint32_t t = g.t, threads = g.threads, shared_end = shared + STAGES * space;
+  const uint32_t t = g.t, shared_end = shared + STAGES * space;
   const Own<V, FULL, OWN, L> own(t, a.cols);
   const TX* x = static_cast<const TX*>(a.x);
   const TY* dy = static_cast<const TY*>(a.dy);
@@ -506,8 +506,8 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const Group<L>&
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) {
     if (first + (uint64_t)s * step < a.rows) {
-      start_row<TX, V, FULL, OWN, L>(shared + s * space, row + s * stride_x, a.cols, t, threads, own, x, end_x);
-      start_row<TY, V, FULL, OWN, L>(shared + s * space + space_x, drow + s * stride_y, a.cols, t, threads, own, dy, end_y);
+      start_row<TX, V, FULL, OWN, L>(shared + s * space, row + s * stride_x, a.cols, t, own, x, end_x);
+      start_row<TY, V, FULL, OWN, L>(shared + s * space + space_x, drow + s * stride_y, a.cols, t, own, dy, end_y);
     }
     copy_commit();
   }
@@ -519,8 +519,8 @@ __device__ __forceinline__ void backward_rows(const NormArgs& a, const Group<L>&
   float mean_next = ld_c(means), rstd_next = ld_c(rstds);
   for (;;) {
     if (left > STAGES - 1) {
-      start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, threads, own, x, end_x);
-      start_row<TY, V, FULL, OWN, L>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, threads, own, dy, end_y);
+      start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, own, x, end_x);
+      start_row<TY, V, FULL, OWN, L>(ahead + space_x, drow + (STAGES - 1) * stride_y, a.cols, t, own, dy, end_y);
     }
     copy_commit();
     const float mean = mean_next, rstd = rstd_next;

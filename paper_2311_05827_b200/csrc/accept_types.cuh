@@ -1,4 +1,4 @@
-// Values of the three floating types the operators beside the codec read and write, eight at a time.
+// Values of the three floating types the operators beside the codec read and write.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -90,79 +90,6 @@ __device__ __forceinline__ Pack<T> ld_pack(const T* p) {
                  : "=r"(v.w[i].x), "=r"(v.w[i].y), "=r"(v.w[i].z), "=r"(v.w[i].w) : "l"(reinterpret_cast<const uint4*>(p) + i));
   }
   return v;
-}
-template <typename T>
-__device__ __forceinline__ void st_pack(T* p, const Pack<T>& v) {
-#pragma unroll
-  for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
-    uint4* q = reinterpret_cast<uint4*>(p) + i;
-    if (!bounds_ok(q, 16, true)) continue;
-    asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(q), "r"(v.w[i].x), "r"(v.w[i].y), "r"(v.w[i].z), "r"(v.w[i].w) : "memory");
-  }
-}
-
-__device__ __forceinline__ void unpack(const Pack<float>& p, float (&v)[8]) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    v[4 * i] = __uint_as_float(p.w[i].x); v[4 * i + 1] = __uint_as_float(p.w[i].y);
-    v[4 * i + 2] = __uint_as_float(p.w[i].z); v[4 * i + 3] = __uint_as_float(p.w[i].w);
-  }
-}
-__device__ __forceinline__ void unpack(const Pack<__nv_bfloat16>& p, float (&v)[8]) {
-  const uint32_t w[4] = {p.w[0].x, p.w[0].y, p.w[0].z, p.w[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {  // bf16 is the upper half of an fp32
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void unpack(const Pack<__half>& p, float (&v)[8]) {
-  const uint32_t w[4] = {p.w[0].x, p.w[0].y, p.w[0].z, p.w[0].w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    __half2 h;
-    memcpy(&h, &w[i], 4);
-    const float2 f = __half22float2(h);
-    v[2 * i] = f.x;
-    v[2 * i + 1] = f.y;
-  }
-}
-
-__device__ __forceinline__ void pack(const float (&v)[8], Pack<float>& p) {
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-    p.w[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-}
-__device__ __forceinline__ void pack(const float (&v)[8], Pack<__nv_bfloat16>& p) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-    memcpy(&w[i], &h, 4);
-  }
-  p.w[0] = make_uint4(w[0], w[1], w[2], w[3]);
-}
-__device__ __forceinline__ void pack(const float (&v)[8], Pack<__half>& p) {
-  uint32_t w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-    memcpy(&w[i], &h, 4);
-  }
-  p.w[0] = make_uint4(w[0], w[1], w[2], w[3]);
-}
-
-// Eight values at p, of which only the first n (0 to 8) exist; the others are zero.
-template <typename T>
-__device__ __forceinline__ void ld_some(const T* p, int n, float (&v)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = j < n ? to_float(ld_c(p + j)) : 0.0f;
-}
-template <typename T>
-__device__ __forceinline__ void st_some(T* p, int n, const float (&v)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < n) st_c(p + j, from_float<T>(v[j]));
 }
 
 }  // namespace accept
