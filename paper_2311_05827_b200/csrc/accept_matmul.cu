@@ -184,13 +184,18 @@ accept_status launch_pairs(const accept_matmul_params* p, const void* d_a, const
   a.chunks = plan.chunks;
   a.instruction = accept::scaled_instruction((uint32_t)p->format_a, (uint32_t)p->format_b, 256, plan.nt);
   const bool single = p->dtype_d == ACCEPT_DTYPE_F32;
-  a.tile_stores = is_aligned(a.d, 16) && a.ldd * value_size(p->dtype_d) % 16 == 0 && (single || !a.accumulate);
+  // Tile stores: 16-byte aligned rows, nothing to add but in fp32.  A tile store ends at a multiple of 16 bytes: where d's rows
+  // do not, its last unit would go over what lies behind the row's n values, so the piece (64 bytes of a row) that holds the end of
+  // the row is stored value by value.
+  const uint64_t size = value_size(p->dtype_d);
+  if (is_aligned(a.d, 16) && a.ldd * size % 16 == 0 && (single || !a.accumulate))
+    a.tile_columns = (uint32_t)(p->n * size % 16 == 0 ? p->n : p->n / (64 / size) * (64 / size));
   a.word_stores = is_aligned(a.d, 4) && a.ldd % 2 == 0;
   const uint64_t groups = (a.blocks + 3) / 4;
   CUtensorMap map_a, map_b, map_sa, map_sb, map_d{};
   if (!operand_map(&map_a, d_a, p->m, p->k, 128) || !operand_map(&map_b, d_b, p->n, p->k, plan.nt / 2) ||
       !scale_map(&map_sa, d_a_scale, groups * a.atoms_a, 1) || !scale_map(&map_sb, d_b_scale, groups * a.atoms_b, plan.nt / 128) ||
-      (a.tile_stores && !result_map(&map_d, a.d, p->dtype_d, p->m, p->n, a.ldd)))
+      (a.tile_columns && !result_map(&map_d, a.d, p->dtype_d, p->m, p->n, a.ldd)))
     return ACCEPT_ERR_CUDA;
   if (plan.nt == 256) ACCEPT_LAUNCH(launch_pair_kernel<256>(single, plan.pairs, s, map_a, map_b, map_sa, map_sb, map_d, a));
   else ACCEPT_LAUNCH(launch_pair_kernel<128>(single, plan.pairs, s, map_a, map_b, map_sa, map_sb, map_d, a));

@@ -369,7 +369,7 @@ struct PairArgs {
   uint32_t chunks;     // of a whole tile, one after the other
   uint32_t instruction;
   int dtype_d, accumulate;
-  int tile_stores;     // d is stored through its tensor map (16-byte aligned rows, nothing to add but in fp32)
+  uint32_t tile_columns;  // columns of d below this one are stored through its tensor map, piece by piece
   int word_stores;     // rows of a 16-bit d start on 4-byte boundaries
 };
 
@@ -431,16 +431,30 @@ __device__ __forceinline__ bool pair_unit(const PairArgs& a, uint32_t pair, uint
   return true;
 }
 
+// For the checking build: what a tile store of a warp's 32 rows may write, 64 bytes of each row or up to the end of d's rows in
+// units of 16 bytes, lies inside the call's buffers.
+template <typename T>
+__device__ __forceinline__ bool tile_inside(const PairArgs& a, uint32_t row, uint32_t col) {
+#ifdef ACCEPT_BOUNDS_CHECK
+  const uint32_t bytes = min(((a.n - col) * (uint32_t)sizeof(T) + 15) & ~15u, 64u);
+  return __all_sync(0xffffffffu, row >= a.m || bounds_ok(static_cast<const T*>(a.d) + row * a.ldd + col, bytes, true));
+#else
+  return true;
+#endif
+}
+
 // 32 columns of a warp's 32 rows to d, through the warp's 2 KB of shared memory (`piece`): 32 rows of 64 bytes, 16-byte units
 // permuted as the tensor map's swizzle has them.
 template <bool SINGLE>
 __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap* map_d, uint8_t* piece, uint32_t piece_address, uint32_t lane,
                                            uint32_t row0, uint32_t col, bool add, float (&v)[32]) {
-  const uint32_t rows = row0 < a.m ? min(a.m - row0, 32u) : 0;
+  if (row0 >= a.m || col >= a.n) return;
+  const uint32_t rows = min(a.m - row0, 32u);
   uint8_t* mine = piece + lane * 64;
   const uint32_t swap = (lane >> 1) & 3;
   if (!SINGLE && !add) {
-    if (a.tile_stores) {
+    const bool by_tile = col < a.tile_columns;
+    if (a.tile_columns) {  // the piece's last tile store has read it
       if (lane == 0) store_wait_read<0>();
       __syncwarp();
     }
@@ -451,11 +465,12 @@ __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap*
       for (uint32_t j = 0; j < 4; ++j) w[j] = two_values(a.dtype_d, v[8 * u + 2 * j], v[8 * u + 2 * j + 1]);
       *reinterpret_cast<uint4*>(mine + 16 * (u ^ swap)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    if (a.tile_stores) {
+    if (by_tile) {
       shared_to_async();
       __syncwarp();
+      const bool inside = tile_inside<uint16_t>(a, row0 + lane, col);
       if (lane == 0) {
-        if (rows && col < a.n) tile_store(map_d, col, row0, piece_address);
+        if (inside) tile_store(map_d, col, row0, piece_address);
         store_commit();
       }
       return;
@@ -484,21 +499,22 @@ __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap*
   // in fp32, sixteen columns at a time
 #pragma unroll
   for (uint32_t half = 0; half < 32; half += 16) {
-    if (SINGLE && a.tile_stores) {
+    if (col + half >= a.n) return;
+    const bool by_tile = SINGLE && col + half < a.tile_columns;
+    if (SINGLE && a.tile_columns) {
       if (lane == 0) store_wait_read<0>();
       __syncwarp();
     }
 #pragma unroll
     for (uint32_t u = 0; u < 4; ++u)
       *reinterpret_cast<float4*>(mine + 16 * (u ^ swap)) = make_float4(v[half + 4 * u], v[half + 4 * u + 1], v[half + 4 * u + 2], v[half + 4 * u + 3]);
-    if (SINGLE && a.tile_stores) {
+    if (by_tile) {
       shared_to_async();
       __syncwarp();
-      if (lane == 0) {
-        if (rows && col + half < a.n) {
-          if (add) tile_add(map_d, col + half, row0, piece_address);
-          else tile_store(map_d, col + half, row0, piece_address);
-        }
+      const bool inside = tile_inside<float>(a, row0 + lane, col + half);
+      if (lane == 0 && inside) {
+        if (add) tile_add(map_d, col + half, row0, piece_address);
+        else tile_store(map_d, col + half, row0, piece_address);
         store_commit();
       }
       continue;

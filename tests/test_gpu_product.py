@@ -86,6 +86,45 @@ def test_cut_tiles_stay_inside_their_buffers(A):
         assert A.accept_bounds_check_report()[:2] == (0, 0)
 
 
+# ---- rows of d that end inside 16 bytes ------------------------------------------------------------------------------------------
+
+# m, n, k, type of d, bias, accumulate, extra values between rows of d: rows start on 16-byte boundaries and end off them
+ENDS = [
+    (2560, 3980, 176, F16, False, False, 4), (2808, 9967, 1, BF16, True, False, 1), (9570, 4310, 1104, BF16, False, False, 2), (3056, 3444, 1, BF16, False, False, 4),
+    (6168, 4407, 10, F32, True, False, 1), (11265, 138, 1672, F32, False, False, 2), (9600, 130, 128, F32, False, False, 2), (903, 1303, 3387, F32, False, False, 1),
+    (428, 9906, 28, F32, True, False, 2), (2304, 2303, 300, F32, True, True, 1), (2304, 2305, 300, F32, False, True, 7), (2304, 2311, 300, F16, False, True, 1),
+    (2304, 2257, 200, BF16, True, False, 7), (2304, 2271, 200, BF16, True, False, 1), (2304, 2289, 200, F16, True, False, 15), (2304, 2287, 200, F16, True, False, 1),
+    # cut tiles, chunks of k
+    (700, 1002, 8300, F16, True, False, 6), (1280, 1001, 6000, F32, True, False, 3), (1810, 301, 10000, BF16, False, False, 3), (1280, 1999, 8300, F32, True, True, 1),
+    (2304, 2101, 8300, F32, True, False, 3), (2304, 2101, 8300, F32, False, True, 3), (1280, 1102, 8300, F32, False, False, 2),
+]
+
+
+@pytest.mark.parametrize("case", ENDS, ids=str)
+def test_product_writes_nothing_behind_the_end_of_a_row(A, case):
+    m, n, k, dtype, bias, accumulate, pad = case
+    assert n * dtype.itemsize % 16 != 0 and (n + pad) * dtype.itemsize % 16 == 0
+    ops.check_product(A, m, n, k, "e4m3", "e5m2", dtype, bias, accumulate, pad)
+    # d as the first columns of a matrix whose other columns are someone else's
+    a, sa = ops.coded(5, m, k, "e4m3")
+    b, sb = ops.coded(6, n, k, "e4m3")
+    whole = ops.random(7, m, n + pad).to(dtype)
+    others = whole[:, n:].clone()
+    p = A.MatmulParams(m, n, k, dtype_d=ops.code_of(A, dtype), accumulate=accumulate, ldd=n + pad)
+    A.accept_block_matmul(p, a, sa, b, sb, None, whole, A.new_workspace(p))
+    assert torch.equal(whole[:, n:], others)
+
+
+def test_row_ends_stay_inside_their_buffers(A):
+    """The checking build compares a tile store in units of 16 bytes, as it writes them."""
+    from tests import gpu_util
+    with gpu_util.library_variant("bounds"):
+        assert A.accept_bounds_check_report()[:2] == (0, 0)
+        for case in ENDS:
+            ops.check_product(A, *case[:3], "e4m3", "e4m3", *case[3:])
+        assert A.accept_bounds_check_report()[:2] == (0, 0)
+
+
 # ---- waits that run out --------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("m,n,k,dtype", [(4, 300, 64, BF16), (64, 9600, 4096, F32), (300, 300, 100, F32), (2304, 2304, 64, BF16), (8192, 4160, 1024, BF16),
