@@ -20,7 +20,8 @@ bool word_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p,
 
 // Launch shape of a pass.  A row is shared by as many warps as hold it at `own` columns a thread; a block holds as many
 // such groups as fit 512 threads, fewer where there are too few rows for every SM.  16 columns a thread, 32 for rows of more
-// than 8192 (32 everywhere: 16384 x 4096 fp32 to bf16 62 -> 77 us, 8 x 4096 bf16 2.6 -> 3.7 us, for want of registers).  The
+// than 8192 (32 everywhere: 16384 x 4096 fp32 to bf16 62 -> 77 us, 8 x 4096 bf16 2.6 -> 3.7 us, for want of registers: those
+// kernels spill 204 to 424 bytes; 16 columns a thread none in the forward pass, 0 to 20 bytes in the backward pass).  The
 // backward pass over more than 8192 columns has no registers for the sums over the rows and leaves them to a pass of their
 // own (kApart); rows of more than 16384 columns are not held (kLong).  Rows of up to 128 columns take eight lanes each: with
 // a warp each, 14400 x 105 bf16 took 13.4 us.
