@@ -6,11 +6,12 @@ quantize, pack) followed by accept_decompress (unpack, dequantize) of the stream
 The metric is GB/s of fp32 input through that round trip; compress and decompress are also
 reported on their own, each with its achieved fraction of the measured HBM copy bandwidth.
 
-    python bench.py [--gpus N] [--steps K] [--warmup W] [--workload NAME] [--sweep]
+    python bench.py [--gpus N] [--steps K] [--warmup W] [--workload NAME] [--sweep] [--whole-line]
     python bench.py --impl reference ...      # the CPU oracle on the host cores
 
 The headline (`value`) is the round trip on --workload (cfg4_hidden by default): the median over --repeats
-blocks of exactly K back-to-back steps each.  On one GPU the line also carries, under "workloads", one
+blocks of exactly K back-to-back steps each.  On one GPU a second JSON line, on stderr so that the first stays short
+(about 2 KB; 20 KB with it, for which --whole-line asks), carries under "workloads" one
 row per tensor of 100 MB or more in its headline modes (cfg3 forward and backward, cfg4, the 256 MB and
 1 GB points of the size sweep) with both kernels timed inside the step and in loops of their own, and under
 "small" the tensors of 16 MB and less replayed from CUDA graphs next to an empty kernel launched the same way.
@@ -680,7 +681,15 @@ def run_gpu(args):
         dist.barrier()
         dist.destroy_process_group()
     if rank == 0:
-        print(json.dumps(out))
+        print_line(out, args.whole_line)
+
+
+def print_line(out: dict, whole: bool) -> None:
+    """The result as one line; the rows of the other workloads with it (`whole`) or as a line of their own on stderr."""
+    details = {} if whole else {key: out.pop(key) for key in ("workloads", "small") if key in out}
+    if details:
+        print(json.dumps(details), file=sys.stderr)
+    print(json.dumps(out))
 
 
 def sweep(A, torch, peak, args):
@@ -897,6 +906,7 @@ def main():
     ap.add_argument("--gpus", type=int, default=1)
     ap.add_argument("--steps", type=int, default=50)
     ap.add_argument("--repeats", type=int, default=10, help="blocks of --steps steps; the headline is their median")
+    ap.add_argument("--whole-line", action="store_true", help="the rows of the other workloads in the line itself, not on stderr")
     ap.add_argument("--headline-only", action="store_true", help="skip the rows of the other workloads")
     ap.add_argument("--warmup", type=int, default=5)
     ap.add_argument("--impl", default="ours", choices=["ours", "reference"])
