@@ -382,13 +382,13 @@ def _plan(state):
     elif op == "store4":
         rounding = A.ROUND_STOCHASTIC if c["stochastic"] else A.ROUND_NEAREST
         r, k = (c["rows"], c["cols"]) if c["side"] == "rows" else (c["cols"], c["rows"])
-        p = [A.Mx4Params(c["rows"], c["cols"], types[c["x"]], rounding, A.BLOCK_SQUARE if c["square"] else A.BLOCK_ROW, seed, c["offset"]),
-             A.Mx4Params(r, k, types[c["x"]])]
+        p = [A.MicroParams(c["rows"], c["cols"], types[c["x"]], rounding, A.BLOCK_SQUARE if c["square"] else A.BLOCK_ROW, seed, c["offset"]),
+             A.MicroParams(r, k, types[c["x"]])]
     elif op == "linear4":
-        p = [A.Mx4Params(c["m"], c["k"], types[c["x"]]), A.Mx4MatmulParams(c["m"], c["n"], c["k"], types[c["d"]])]
+        p = [A.MicroParams(c["m"], c["k"], types[c["x"]]), A.MicroMatmulParams(c["m"], c["n"], c["k"], types[c["d"]])]
     else:
-        p = [A.Mx4Params(c["m"], c["n"], types[c["x"]], A.ROUND_STOCHASTIC, A.BLOCK_ROW, seed, c["offset"]),
-             A.Mx4MatmulParams(c["m"], c["k"], c["n"], types[c["x"]]), A.Mx4MatmulParams(c["n"], c["k"], c["m"], A.DTYPE_F32)]
+        p = [A.MicroParams(c["m"], c["n"], types[c["x"]], A.ROUND_STOCHASTIC, A.BLOCK_ROW, seed, c["offset"]),
+             A.MicroMatmulParams(c["m"], c["k"], c["n"], types[c["x"]]), A.MicroMatmulParams(c["n"], c["k"], c["m"], A.DTYPE_F32)]
     return A, p, [A.new_workspace(each) for each in p]
 
 
@@ -410,16 +410,16 @@ def _own(state):
         return {k: s[k] for k in (("dx", "dgamma", "dbranch") if c["branch"] else ("dx", "dgamma"))}
     if op == "store4":
         sides = (s["q"], s["scale"], None, None) if c["side"] == "rows" else (None, None, s["q"], s["scale"])
-        A.accept_mx4_quantize(p[0], s["x"], *sides, ws[0])
-        A.accept_mx4_dequantize(p[1], s["q"], s["scale"], s["back"])
+        A.accept_micro_quantize(p[0], s["x"], *sides, ws[0])
+        A.accept_micro_dequantize(p[1], s["q"], s["scale"], s["back"])
         return {"back": s["back"]}
     if op == "linear4":
-        A.accept_mx4_quantize(p[0], s["x"], s["q"], s["scale"], None, None, ws[0])
-        A.accept_mx4_matmul(p[1], s["q"], s["scale"], s["w"], s["w_scale"], s["bias"], s["d"], ws[1])
+        A.accept_micro_quantize(p[0], s["x"], s["q"], s["scale"], None, None, ws[0])
+        A.accept_micro_matmul(p[1], s["q"], s["scale"], s["w"], s["w_scale"], s["bias"], s["d"], ws[1])
         return {"d": s["d"]}
-    A.accept_mx4_quantize(p[0], s["dy"], s["q"], s["scale"], s["qt"], s["scale_t"], ws[0])
-    A.accept_mx4_matmul(p[1], s["q"], s["scale"], s["wt"], s["wt_scale"], None, s["dx"], ws[1])
-    A.accept_mx4_matmul(p[2], s["qt"], s["scale_t"], s["xt"], s["xt_scale"], None, s["dw"], ws[2])
+    A.accept_micro_quantize(p[0], s["dy"], s["q"], s["scale"], s["qt"], s["scale_t"], ws[0])
+    A.accept_micro_matmul(p[1], s["q"], s["scale"], s["wt"], s["wt_scale"], None, s["dx"], ws[1])
+    A.accept_micro_matmul(p[2], s["qt"], s["scale_t"], s["xt"], s["xt_scale"], None, s["dw"], ws[2])
     return {"dx": s["dx"], "dw": s["dw"]}
 
 
