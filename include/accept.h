@@ -375,6 +375,141 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
                                   const void* d_b_scale, const float* d_bias, void* d_d, void* d_ws, size_t ws_bytes,
                                   void* cuda_stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators of a residual stage: dropout, the root-mean-square norm of a residual stream and its gradient, and the linear
+ * layer in 4 bits.  The rules are those of the operators above.  The paper has no counterpart.
+ */
+
+/*
+ * Dropout: y[i][j] = residual[i][j] + (U >= p ? x[i][j] / (1 - p) : 0), U the number of counter rng_offset + i cols + j (mod 2^64) under
+ * `seed`, drawn as at accept_params.seed.  No mask is stored: the backward pass is the same call with dy in the place of x and no
+ * residual (the residual's gradient is dy itself).  Advance rng_offset by rows * cols between calls to draw fresh numbers.
+ *   p            0 (nothing is dropped) to 1 (everything is); 1 / (1 - p) is rounded to fp32 once, product and sum are fp32
+ *                operations, y is rounded once.  What is dropped is 0, also where x is a NaN or an infinity.
+ *   rows, cols   >= 0;  ld_x, ld_y: values between the starts of two rows of x, and of residual and y (>= cols).
+ *   dtype_x      type of x;  dtype_y: of residual and y.
+ * residual may be NULL (0).  Pointers need the alignment of their values.  y may be x or residual (the whole matrix, where type and
+ * row stride are the same); otherwise it overlaps neither.
+ */
+typedef struct {
+  uint64_t rows, cols;
+  uint64_t ld_x, ld_y;
+  uint64_t seed, rng_offset;
+  float p;
+  int32_t dtype_x; /* accept_dtype */
+  int32_t dtype_y;
+  int32_t reserved; /* 0 */
+} accept_dropout_params;
+
+accept_status accept_dropout_check_params(const accept_dropout_params* p);
+accept_status accept_dropout(const accept_dropout_params* p, const void* d_x, const void* d_residual, void* d_y, void* cuda_stream);
+
+/*
+ * Root-mean-square norm over the rows of a residual stream, to which a branch is added first.
+ *   forward   s = x + drop(branch), rounded to dtype_x;  rstd = 1 / sqrt(sum s^2 / cols + eps);  y = s rstd gamma
+ *   backward  xhat = s rstd,  h = dy gamma,  dx = rstd (h - xhat mean(h xhat)) + dsum,  dbranch = drop'(dx),
+ *             dgamma = sum_rows dy xhat
+ * drop() is accept_dropout's with the same p, seed, rng_offset and cols (p = 0: the branch as it is), drop'() its gradient, taken of dx
+ * before dx is rounded.  dsum is the gradient that reaches s by the stream itself.
+ *   outputs of the forward pass, each of which may be NULL (one at least is not):  sum: s;  y;  q and scale: y in 8 bits, codes and scales
+ *             as accept_block_quantize writes them for BLOCK_ROW and `format` (y is not rounded before; ACCEPT_DEV_NONFINITE as there);
+ *             rstd: rows fp32 values for the backward pass.
+ *   rows, cols  rows >= 0 (below 2^31 with q), 1 <= cols < 2^31.  No rows: the forward pass does nothing, the backward pass writes zero dgamma.
+ *   ld_x, ld_y  values between the starts of two rows (>= cols) of x, sum, s, dsum and dx, and of branch, y, dy and dbranch.
+ *   dtype_x     type of x, sum, s, dsum and dx;  dtype_y: of branch, y, dy and dbranch;  dtype_w: of gamma.  Statistics, dgamma and everything
+ *               computed on the way are fp32.
+ * Squares that leave the range of fp32 are taken again with scaled values; rstd itself is an fp32 value (with eps = 0 a row whose root mean
+ * square is below 2^-127 comes out as infinities, a row of zeros as NaN).  A NaN makes its row NaN; an infinity makes the finite
+ * values of its row 0 and itself NaN.  Pointers need the alignment of their values (q, scale and the backward pass's workspace: 16 bytes); rows that
+ * start on 16-byte boundaries are read in 16-byte pieces.  sum may be x, y may be branch, dx may be s or dsum, and dbranch may be dy (the whole
+ * matrix); no other output may overlap anything.
+ */
+typedef struct {
+  uint64_t rows, cols;
+  uint64_t ld_x, ld_y;
+  uint64_t seed, rng_offset;
+  float eps;       /* >= 0 */
+  float p;         /* 0 to 1 */
+  int32_t dtype_x; /* accept_dtype */
+  int32_t dtype_y;
+  int32_t dtype_w;
+  int32_t format;  /* accept_format of q */
+} accept_rms_norm_params;
+
+accept_status accept_rms_norm_check_params(const accept_rms_norm_params* p);
+size_t accept_rms_norm_workspace_size(const accept_rms_norm_params* p); /* of the backward pass; 0 if p is invalid */
+/* branch and gamma may be NULL (0 and 1).  d_ws: the status word, 16 bytes, 4-byte aligned; may be NULL without q. */
+accept_status accept_rms_norm_forward(const accept_rms_norm_params* p, const void* d_x, const void* d_branch, const void* d_gamma,
+                                      void* d_sum, void* d_y, void* d_q, void* d_scale, float* d_rstd, void* d_ws, size_t ws_bytes,
+                                      void* cuda_stream);
+/* gamma and dsum may be NULL (1 and 0); dx, dbranch and dgamma may each be NULL (not written), not all.  dgamma is summed in an order
+ * that depends on the sizes alone. */
+accept_status accept_rms_norm_backward(const accept_rms_norm_params* p, const void* d_dy, const void* d_s, const void* d_gamma,
+                                       const float* d_rstd, const void* d_dsum, void* d_dx, void* d_dbranch, float* d_dgamma,
+                                       void* d_ws, size_t ws_bytes, void* cuda_stream);
+
+/*
+ * 4-bit floating point (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) with one power-of-two scale for each 32 values.
+ *   block  ROW: 32 consecutive values of a row (the last block of a row may be shorter);  SQUARE: 32 x 32
+ *   scale  a = the largest |x| of the block; e = the least integer with a 2^-e <= 6, held to -127 and above; 0 where a = 0.  Scale byte
+ *          e + 127.  A block that holds a NaN or an infinity has scale byte 255 (NaN) and zero codes, and ACCEPT_DEV_NONFINITE
+ *          is set in the status word.
+ *   code   t = |x| 2^-e (exact) between two neighbours g < h of the list:  NEAREST: the nearer, a tie to the one with an even place in the
+ *          list;  STOCHASTIC: h where U < (t - g) / (h - g), else g, U the number of counter rng_offset + i cols + j (mod 2^64) for x[i][j]
+ *          under `seed`, drawn as at accept_params.seed; the comparison is exact.  Bits 0 to 2 are the place in the list, bit 3 the sign.
+ * One read of x gives either or both of
+ *   rows     q (rows x cols): blocks run along the columns;
+ *   columns  q_t (cols x rows): the transpose, blocks run along the rows.
+ * An element has the same U in both, and a square block the same scale.  Layout of a coded R x C matrix (R = rows or cols):
+ *   codes    two to a byte, the even column in the lower half; R rows of C rounded up to 32 values, those past C zero codes
+ *            (accept_micro_data_size bytes, 16-byte aligned);
+ *   scales   as for 8-bit codes, with blocks of 32: the byte of row r and block b is at
+ *            ((b / 4) ceil(R / 128) + r / 128) 512 + (r % 32) 16 + (r / 32 % 4) 4 + b % 4
+ *            (accept_micro_scale_size bytes, 16-byte aligned; rows and blocks of the padding hold 127).
+ *   rows, cols  >= 0, below 2^31;  ld: values between the starts of two rows of x (>= cols)
+ */
+typedef struct {
+  uint64_t rows, cols;
+  uint64_t ld;
+  uint64_t seed, rng_offset; /* STOCHASTIC only */
+  int32_t dtype;    /* accept_dtype of x */
+  int32_t round;    /* accept_round */
+  int32_t block;    /* accept_block */
+  int32_t reserved; /* 0 */
+} accept_micro_params;
+
+accept_status accept_micro_check_params(const accept_micro_params* p);
+/* Bytes of the codes and of the scales, of q (transposed = 0) or q_t (1); 0 if p is invalid. */
+size_t accept_micro_data_size(const accept_micro_params* p, int transposed);
+size_t accept_micro_scale_size(const accept_micro_params* p, int transposed);
+size_t accept_micro_workspace_size(const accept_micro_params* p);
+/* q and its scales, or q_t and its scales, may be NULL; not both.  x may have any alignment of its values. */
+accept_status accept_micro_quantize(const accept_micro_params* p, const void* d_x, void* d_q, void* d_scale, void* d_qt, void* d_scale_t,
+                                  void* d_ws, size_t ws_bytes, void* cuda_stream);
+/* The values that codes by rows stand for: x[i][j] = code 2^(scale byte - 127) (byte 255: NaN), rounded to dtype once (exact but for the range of
+ * fp16).  p gives rows, cols, ld and dtype of x; its round, block, seed and rng_offset are not used.  Codes of a transpose are those
+ * of a cols x rows matrix. */
+accept_status accept_micro_dequantize(const accept_micro_params* p, const void* d_q, const void* d_scale, void* d_x, void* cuda_stream);
+
+/*
+ * d = a b^T (+ bias) (+ d) for a (m x k) and b (n x k) as accept_micro_quantize writes them, as accept_block_matmul: products are exact, sums are
+ * fp32 in an order that depends on the sizes alone, d is rounded once.  A scale byte of 255 makes every sum that it
+ * enters NaN.
+ *   m, n, k >= 0, below 2^31 (k = 0: the sum is empty);  ldd: values between the starts of two rows of d (>= n)
+ */
+typedef struct {
+  uint64_t m, n, k;
+  uint64_t ldd;
+  int32_t dtype_d;    /* accept_dtype */
+  int32_t accumulate; /* 0 or 1: add to what d holds */
+} accept_micro_matmul_params;
+
+accept_status accept_micro_matmul_check_params(const accept_micro_matmul_params* p);
+size_t accept_micro_matmul_workspace_size(const accept_micro_matmul_params* p);
+/* bias: n fp32 values, or NULL.  d_ws: 16-byte aligned; ACCEPT_DEV_COPY_TIMEOUT as for accept_block_matmul. */
+accept_status accept_micro_matmul(const accept_micro_matmul_params* p, const void* d_a, const void* d_a_scale, const void* d_b,
+                                const void* d_b_scale, const float* d_bias, void* d_d, void* d_ws, size_t ws_bytes, void* cuda_stream);
+
 /*
  * Synchronises cuda_stream, copies the status word to the host and returns it in *status_bits
  * (ACCEPT_DEV_* bits).  Returns ACCEPT_ERR_CUDA if the stream reports an error.

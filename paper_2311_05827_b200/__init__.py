@@ -14,4 +14,8 @@ from .binding import (  # noqa: F401
     QuantizeParams, accept_block_check_params, accept_block_data_size, accept_block_matmul, accept_block_quantize,
     accept_block_scale_size, accept_block_workspace_size, accept_layer_norm_backward, accept_layer_norm_check_params,
     accept_layer_norm_forward, accept_layer_norm_workspace_size, accept_matmul_check_params, accept_matmul_workspace_size,
+    DropoutParams, MicroMatmulParams, MicroParams, RmsNormParams, accept_dropout, accept_dropout_check_params, accept_micro_check_params,
+    accept_micro_data_size, accept_micro_dequantize, accept_micro_matmul, accept_micro_matmul_check_params, accept_micro_matmul_workspace_size,
+    accept_micro_quantize, accept_micro_scale_size, accept_micro_workspace_size, accept_rms_norm_backward, accept_rms_norm_check_params,
+    accept_rms_norm_forward, accept_rms_norm_workspace_size,
 )

@@ -42,6 +42,10 @@ EXPORTS = [
     "accept_layer_norm_backward", "accept_block_check_params", "accept_block_data_size", "accept_block_scale_size",
     "accept_block_workspace_size", "accept_block_quantize", "accept_matmul_check_params", "accept_matmul_workspace_size",
     "accept_block_matmul",
+    "accept_dropout_check_params", "accept_dropout", "accept_rms_norm_check_params", "accept_rms_norm_workspace_size",
+    "accept_rms_norm_forward", "accept_rms_norm_backward", "accept_micro_check_params", "accept_micro_data_size",
+    "accept_micro_scale_size", "accept_micro_workspace_size", "accept_micro_quantize", "accept_micro_dequantize",
+    "accept_micro_matmul_check_params", "accept_micro_matmul_workspace_size", "accept_micro_matmul",
 ]
 
 
@@ -111,6 +115,29 @@ class CMatmulParams(ctypes.Structure):
                 ("accumulate", ctypes.c_int32)]
 
 
+class CDropoutParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("ld_x", ctypes.c_uint64), ("ld_y", ctypes.c_uint64),
+                ("seed", ctypes.c_uint64), ("rng_offset", ctypes.c_uint64), ("p", ctypes.c_float), ("dtype_x", ctypes.c_int32),
+                ("dtype_y", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class CRmsNormParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("ld_x", ctypes.c_uint64), ("ld_y", ctypes.c_uint64),
+                ("seed", ctypes.c_uint64), ("rng_offset", ctypes.c_uint64), ("eps", ctypes.c_float), ("p", ctypes.c_float),
+                ("dtype_x", ctypes.c_int32), ("dtype_y", ctypes.c_int32), ("dtype_w", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class CMicroParams(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("ld", ctypes.c_uint64), ("seed", ctypes.c_uint64),
+                ("rng_offset", ctypes.c_uint64), ("dtype", ctypes.c_int32), ("round", ctypes.c_int32), ("block", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class CMicroMatmulParams(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_uint64), ("n", ctypes.c_uint64), ("k", ctypes.c_uint64), ("ldd", ctypes.c_uint64),
+                ("dtype_d", ctypes.c_int32), ("accumulate", ctypes.c_int32)]
+
+
 @dataclass(frozen=True)
 class LayerNormParams:
     """Layer norm over the rows of a rows x cols matrix; ld_x / ld_y 0: rows are cols values apart."""
@@ -165,6 +192,90 @@ class MatmulParams:
                                                      self.dtype_d, int(self.accumulate)))
 
     def c(self) -> CMatmulParams:
+        return self._c
+
+
+@dataclass(frozen=True)
+class DropoutParams:
+    """Dropout of a rows x cols matrix at rate p; ld_x / ld_y 0: rows are cols values apart."""
+    rows: int
+    cols: int
+    p: float
+    dtype_x: int = DTYPE_F32
+    dtype_y: int = DTYPE_F32
+    seed: int = 0
+    rng_offset: int = 0
+    ld_x: int = 0
+    ld_y: int = 0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", CDropoutParams(self.rows, self.cols, self.ld_x or self.cols, self.ld_y or self.cols, self.seed & (2**64 - 1),
+                                                      self.rng_offset & (2**64 - 1), self.p, self.dtype_x, self.dtype_y, 0))
+
+    def c(self) -> CDropoutParams:
+        return self._c
+
+
+@dataclass(frozen=True)
+class RmsNormParams:
+    """Root-mean-square norm over the rows of a rows x cols stream (dtype_x) and its branch (dtype_y), dropped at rate p; ld_x / ld_y 0:
+    rows are cols values apart."""
+    rows: int
+    cols: int
+    eps: float = 1e-5
+    dtype_x: int = DTYPE_F32
+    dtype_y: int = DTYPE_F32
+    dtype_w: int = DTYPE_F32
+    p: float = 0.0
+    seed: int = 0
+    rng_offset: int = 0
+    format: int = FORMAT_E4M3
+    ld_x: int = 0
+    ld_y: int = 0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", CRmsNormParams(self.rows, self.cols, self.ld_x or self.cols, self.ld_y or self.cols, self.seed & (2**64 - 1),
+                                                      self.rng_offset & (2**64 - 1), self.eps, self.p, self.dtype_x, self.dtype_y, self.dtype_w,
+                                                      self.format))
+
+    def c(self) -> CRmsNormParams:
+        return self._c
+
+
+@dataclass(frozen=True)
+class MicroParams:
+    """Quantisation of a rows x cols matrix to 4 bits in blocks of 32; ld 0: rows are cols values apart."""
+    rows: int
+    cols: int
+    dtype: int = DTYPE_F32
+    round: int = ROUND_NEAREST
+    block: int = BLOCK_ROW
+    seed: int = 0
+    rng_offset: int = 0
+    ld: int = 0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", CMicroParams(self.rows, self.cols, self.ld or self.cols, self.seed & (2**64 - 1), self.rng_offset & (2**64 - 1),
+                                                  self.dtype, self.round, self.block, 0))
+
+    def c(self) -> CMicroParams:
+        return self._c
+
+
+@dataclass(frozen=True)
+class MicroMatmulParams:
+    """d (m x n) = a (m x k) b (n x k)^T of 4-bit operands; ldd 0: rows of d are n values apart."""
+    m: int
+    n: int
+    k: int
+    dtype_d: int = DTYPE_BF16
+    accumulate: bool = False
+    ldd: int = 0
+
+    def __post_init__(self):
+        object.__setattr__(self, "_c", CMicroMatmulParams(self.m, self.n, self.k, self.ldd or self.n, self.dtype_d, int(self.accumulate)))
+
+    def c(self) -> CMicroMatmulParams:
         return self._c
 
 
@@ -235,6 +346,28 @@ def load(path: str) -> ctypes.CDLL:
     L.accept_block_quantize.argtypes = [QP, vp, vp, vp, vp, vp, vp, sz, vp]
     L.accept_block_matmul.restype = ctypes.c_int
     L.accept_block_matmul.argtypes = [TP, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    DP, RP, FP, GP = (ctypes.POINTER(c) for c in (CDropoutParams, CRmsNormParams, CMicroParams, CMicroMatmulParams))
+    for name, params in (("accept_dropout", DP), ("accept_rms_norm", RP), ("accept_micro", FP), ("accept_micro_matmul", GP)):
+        getattr(L, name + "_check_params").restype = ctypes.c_int
+        getattr(L, name + "_check_params").argtypes = [params]
+        if name != "accept_dropout":
+            getattr(L, name + "_workspace_size").restype = sz
+            getattr(L, name + "_workspace_size").argtypes = [params]
+    for name in ("accept_micro_data_size", "accept_micro_scale_size"):
+        getattr(L, name).restype = sz
+        getattr(L, name).argtypes = [FP, ctypes.c_int]
+    L.accept_dropout.restype = ctypes.c_int
+    L.accept_dropout.argtypes = [DP, vp, vp, vp, vp]
+    L.accept_rms_norm_forward.restype = ctypes.c_int
+    L.accept_rms_norm_forward.argtypes = [RP] + [vp] * 9 + [sz, vp]
+    L.accept_rms_norm_backward.restype = ctypes.c_int
+    L.accept_rms_norm_backward.argtypes = [RP] + [vp] * 9 + [sz, vp]
+    L.accept_micro_quantize.restype = ctypes.c_int
+    L.accept_micro_quantize.argtypes = [FP, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.accept_micro_dequantize.restype = ctypes.c_int
+    L.accept_micro_dequantize.argtypes = [FP, vp, vp, vp, vp]
+    L.accept_micro_matmul.restype = ctypes.c_int
+    L.accept_micro_matmul.argtypes = [GP, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.accept_launch_count.restype = u64
     L.accept_launch_count.argtypes = []
     L.accept_launch_null.restype = ctypes.c_int
@@ -461,6 +594,83 @@ def accept_block_matmul(p: MatmulParams, d_a, d_a_scale, d_b, d_b_scale, d_bias,
            "accept_block_matmul")
 
 
+# ---- operators of a residual stage: dropout, root-mean-square norm, the linear layer in 4 bits ------
+
+def accept_dropout_check_params(p: DropoutParams) -> int:
+    return int(lib().accept_dropout_check_params(ctypes.byref(p.c())))
+
+
+def accept_dropout(p: DropoutParams, d_x, d_residual, d_y, stream=None) -> None:
+    """d_residual may be None.  The backward pass is the same call with dy in the place of x and no residual."""
+    _check(lib().accept_dropout(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_residual), d_y.data_ptr(), _stream_handle(stream)), "accept_dropout")
+
+
+def accept_rms_norm_check_params(p: RmsNormParams) -> int:
+    return int(lib().accept_rms_norm_check_params(ctypes.byref(p.c())))
+
+
+def accept_rms_norm_workspace_size(p: RmsNormParams) -> int:
+    return int(lib().accept_rms_norm_workspace_size(ctypes.byref(p.c())))
+
+
+def accept_rms_norm_forward(p: RmsNormParams, d_x, d_branch, d_gamma, d_sum, d_y, d_q=None, d_scale=None, d_rstd=None, d_ws=None, stream=None) -> None:
+    """d_branch and d_gamma may be None; so may the outputs: d_sum, d_y, d_q with d_scale (uint8, as accept_block_quantize writes them; with d_ws) and
+    d_rstd (float32, p.rows elements, kept for the backward pass)."""
+    _check(lib().accept_rms_norm_forward(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_branch), _ptr(d_gamma), _ptr(d_sum), _ptr(d_y), _ptr(d_q),
+                                         _ptr(d_scale), _ptr(d_rstd), _ptr(d_ws), 0 if d_ws is None else _nbytes(d_ws), _stream_handle(stream)),
+           "accept_rms_norm_forward")
+
+
+def accept_rms_norm_backward(p: RmsNormParams, d_dy, d_s, d_gamma, d_rstd, d_dsum, d_dx, d_dbranch, d_dgamma, d_ws, stream=None) -> None:
+    """d_gamma and d_dsum may be None; so may the outputs d_dx, d_dbranch and d_dgamma (float32, p.cols elements): not computed."""
+    _check(lib().accept_rms_norm_backward(ctypes.byref(p.c()), d_dy.data_ptr(), d_s.data_ptr(), _ptr(d_gamma), d_rstd.data_ptr(), _ptr(d_dsum),
+                                          _ptr(d_dx), _ptr(d_dbranch), _ptr(d_dgamma), d_ws.data_ptr(), _nbytes(d_ws), _stream_handle(stream)),
+           "accept_rms_norm_backward")
+
+
+def accept_micro_check_params(p: MicroParams) -> int:
+    return int(lib().accept_micro_check_params(ctypes.byref(p.c())))
+
+
+def accept_micro_data_size(p: MicroParams, transposed: bool = False) -> int:
+    return int(lib().accept_micro_data_size(ctypes.byref(p.c()), int(transposed)))
+
+
+def accept_micro_scale_size(p: MicroParams, transposed: bool = False) -> int:
+    return int(lib().accept_micro_scale_size(ctypes.byref(p.c()), int(transposed)))
+
+
+def accept_micro_workspace_size(p: MicroParams) -> int:
+    return int(lib().accept_micro_workspace_size(ctypes.byref(p.c())))
+
+
+def accept_micro_quantize(p: MicroParams, d_x, d_q, d_scale, d_qt, d_scale_t, d_ws, stream=None) -> None:
+    """d_q / d_scale (codes along the columns) or d_qt / d_scale_t (the transpose, codes along the rows) may be None:
+    uint8 CUDA tensors of accept_micro_data_size and accept_micro_scale_size bytes."""
+    _check(lib().accept_micro_quantize(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_q), _ptr(d_scale), _ptr(d_qt), _ptr(d_scale_t), d_ws.data_ptr(),
+                                     _nbytes(d_ws), _stream_handle(stream)), "accept_micro_quantize")
+
+
+def accept_micro_dequantize(p: MicroParams, d_q, d_scale, d_x, stream=None) -> None:
+    """The values of a p.rows x p.cols matrix in d_x (p.dtype, p.ld) from its codes by rows and their scales."""
+    _check(lib().accept_micro_dequantize(ctypes.byref(p.c()), d_q.data_ptr(), d_scale.data_ptr(), d_x.data_ptr(), _stream_handle(stream)),
+           "accept_micro_dequantize")
+
+
+def accept_micro_matmul_check_params(p: MicroMatmulParams) -> int:
+    return int(lib().accept_micro_matmul_check_params(ctypes.byref(p.c())))
+
+
+def accept_micro_matmul_workspace_size(p: MicroMatmulParams) -> int:
+    return int(lib().accept_micro_matmul_workspace_size(ctypes.byref(p.c())))
+
+
+def accept_micro_matmul(p: MicroMatmulParams, d_a, d_a_scale, d_b, d_b_scale, d_bias, d_d, d_ws, stream=None) -> None:
+    """d_bias: float32 CUDA tensor of p.n elements, or None."""
+    _check(lib().accept_micro_matmul(ctypes.byref(p.c()), d_a.data_ptr(), d_a_scale.data_ptr(), d_b.data_ptr(), d_b_scale.data_ptr(), _ptr(d_bias),
+                                   d_d.data_ptr(), d_ws.data_ptr(), _nbytes(d_ws), _stream_handle(stream)), "accept_micro_matmul")
+
+
 # ---- small conveniences for callers (allocation only) -----------------------------------------
 
 def new_stream_buffer(p, device="cuda"):
@@ -472,6 +682,7 @@ def new_stream_buffer(p, device="cuda"):
 def new_workspace(p, device="cuda"):
     import torch
     query = {MbqParams: accept_mbq_workspace_size, LayerNormParams: accept_layer_norm_workspace_size,
-             QuantizeParams: accept_block_workspace_size, MatmulParams: accept_matmul_workspace_size}
+             QuantizeParams: accept_block_workspace_size, MatmulParams: accept_matmul_workspace_size,
+             RmsNormParams: accept_rms_norm_workspace_size, MicroParams: accept_micro_workspace_size, MicroMatmulParams: accept_micro_matmul_workspace_size}
     size = query.get(type(p), accept_workspace_size)(p)
     return torch.zeros((size + 3) // 4, dtype=torch.int32, device=device)

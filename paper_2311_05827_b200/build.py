@@ -20,7 +20,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJECTS = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libaccept.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("accept_api.cu", "accept_norm.cu", "accept_block.cu", "accept_matmul.cu")]
+SOURCES = [os.path.join(CSRC, f) for f in ("accept_api.cu", "accept_norm.cu", "accept_block.cu", "accept_matmul.cu", "accept_dropout.cu",
+                                              "accept_rms_forward.cu", "accept_rms_backward.cu", "accept_micro.cu", "accept_micro_matmul.cu")]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -725,7 +725,10 @@ accept_status accept_bounds_check_report(void* cuda_stream, uint32_t* violations
   *violations = 0;
   if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return ACCEPT_ERR_CUDA;
   if (!accept::collect_bounds(violations, first) || !accept::collect_norm_bounds(violations, first) ||
-      !accept::collect_block_bounds(violations, first) || !accept::collect_matmul_bounds(violations, first))
+      !accept::collect_block_bounds(violations, first) || !accept::collect_matmul_bounds(violations, first) ||
+      !accept::collect_dropout_bounds(violations, first) || !accept::collect_rms_forward_bounds(violations, first) ||
+      !accept::collect_rms_backward_bounds(violations, first) || !accept::collect_micro_bounds(violations, first) ||
+      !accept::collect_micro_matmul_bounds(violations, first))
     return ACCEPT_ERR_CUDA;
   if (first_address) *first_address = first[0];
   if (first_size_and_kind) *first_size_and_kind = first[1];

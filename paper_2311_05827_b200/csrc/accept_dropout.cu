@@ -1,0 +1,89 @@
+// Host side of dropout (accept_dropout): argument checks, launches.
+#include "accept_dropout.cuh"
+#include "accept_drop_host.cuh"
+
+namespace {
+
+using accept::DropoutArgs;
+using accept::is_aligned;
+
+size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
+bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF16 || d == ACCEPT_DTYPE_F16; }
+
+using KernelFn = void (*)(const DropoutArgs);
+constexpr int kUnits = 2;
+
+template <typename TX, typename TY>
+KernelFn select_units(bool whole) { return whole ? accept::dropout_kernel<TX, TY, true, kUnits> : accept::dropout_kernel<TX, TY, false, kUnits>; }
+template <typename TX>
+KernelFn select_y(int32_t dtype_y, bool whole) {
+  switch (dtype_y) {
+    case ACCEPT_DTYPE_F32: return select_units<TX, float>(whole);
+    case ACCEPT_DTYPE_BF16: return select_units<TX, __nv_bfloat16>(whole);
+    default: return select_units<TX, __half>(whole);
+  }
+}
+KernelFn select_kernel(int32_t dtype_x, int32_t dtype_y, bool whole) {
+  switch (dtype_x) {
+    case ACCEPT_DTYPE_F32: return select_y<float>(dtype_y, whole);
+    case ACCEPT_DTYPE_BF16: return select_y<__nv_bfloat16>(dtype_y, whole);
+    default: return select_y<__half>(dtype_y, whole);
+  }
+}
+
+}  // namespace
+
+#ifdef ACCEPT_BOUNDS_CHECK
+bool accept::collect_dropout_bounds(uint32_t* violations, unsigned long long (&first)[2]) { return collect_bounds(violations, first); }
+#endif
+
+extern "C" {
+
+accept_status accept_dropout_check_params(const accept_dropout_params* p) {
+  if (!p) return ACCEPT_ERR_NULL;
+  // every offset of a value must be a 63-bit number of bytes
+  if (p->ld_x < p->cols || p->ld_y < p->cols || p->rows > (1ull << 40) || p->cols > (1ull << 40) || p->ld_x > (1ull << 40) || p->ld_y > (1ull << 40) ||
+      (p->rows && (p->ld_x > (1ull << 60) / p->rows || p->ld_y > (1ull << 60) / p->rows)))
+    return ACCEPT_ERR_BAD_SIZE;
+  if (p->rows * ((p->cols + 7) / 8) / (kUnits * accept::kDropThreads) >= 0x7fffffffull) return ACCEPT_ERR_BAD_SIZE;  // blocks of a grid
+  if (!is_dtype(p->dtype_x) || !is_dtype(p->dtype_y) || p->reserved != 0) return ACCEPT_ERR_BAD_ENUM;
+  if (!accept::is_drop_rate(p->p)) return ACCEPT_ERR_BAD_SIZE;
+  return ACCEPT_OK;
+}
+
+accept_status accept_dropout(const accept_dropout_params* p, const void* d_x, const void* d_residual, void* d_y, void* cuda_stream) {
+  if (!p) return ACCEPT_ERR_NULL;
+  const accept_status st = accept_dropout_check_params(p);
+  if (st != ACCEPT_OK) return st;
+  if (p->rows == 0 || p->cols == 0) return ACCEPT_OK;
+  if (!d_x || !d_y) return ACCEPT_ERR_NULL;
+  const size_t size_x = value_size(p->dtype_x), size_y = value_size(p->dtype_y);
+  if (!is_aligned(d_x, size_x) || !is_aligned(d_residual, size_y) || !is_aligned(d_y, size_y)) return ACCEPT_ERR_MISALIGNED;
+  cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
+  DropoutArgs a{};
+  a.x = d_x;
+  a.residual = d_residual;
+  a.y = d_y;
+  a.rows = p->rows;
+  a.cols = p->cols;
+  a.ld_x = p->ld_x;
+  a.ld_y = p->ld_y;
+  a.drop = accept::drop_of(p->p, p->seed, p->rng_offset);
+  ACCEPT_BOUNDS(s, bounds_list.add(d_x, ((p->rows - 1) * p->ld_x + p->cols) * size_x, false);
+                bounds_list.add(d_residual, ((p->rows - 1) * p->ld_y + p->cols) * size_y, false);
+                bounds_list.add(d_y, ((p->rows - 1) * p->ld_y + p->cols) * size_y, true));
+  bool whole = is_aligned(d_x, 16) && is_aligned(d_residual, 16) && is_aligned(d_y, 16);
+  if (p->rows == 1 || (p->ld_x == p->cols && p->ld_y == p->cols)) {  // no gaps: one row
+    a.cols = p->rows * p->cols;
+    a.rows = 1;
+  } else {
+    whole = whole && p->ld_x * size_x % 16 == 0 && p->ld_y * size_y % 16 == 0;
+  }
+  a.per_row = (a.cols + 7) / 8;
+  a.units = a.rows * a.per_row;
+  const uint64_t blocks = (a.units + kUnits * accept::kDropThreads - 1) / (kUnits * accept::kDropThreads);
+  ACCEPT_LAUNCH(accept::launch_overlapped(select_kernel(p->dtype_x, p->dtype_y, whole), dim3((unsigned)blocks), accept::kDropThreads, s, a));
+  return ACCEPT_OK;
+}
+
+}  // extern "C"

@@ -95,6 +95,11 @@ inline bool collect_bounds(uint32_t* violations, unsigned long long (&first)[2])
 bool collect_norm_bounds(uint32_t* violations, unsigned long long (&first)[2]);
 bool collect_block_bounds(uint32_t* violations, unsigned long long (&first)[2]);
 bool collect_matmul_bounds(uint32_t* violations, unsigned long long (&first)[2]);
+bool collect_dropout_bounds(uint32_t* violations, unsigned long long (&first)[2]);
+bool collect_rms_forward_bounds(uint32_t* violations, unsigned long long (&first)[2]);
+bool collect_rms_backward_bounds(uint32_t* violations, unsigned long long (&first)[2]);
+bool collect_micro_bounds(uint32_t* violations, unsigned long long (&first)[2]);
+bool collect_micro_matmul_bounds(uint32_t* violations, unsigned long long (&first)[2]);
 #define ACCEPT_BOUNDS(stream, ...)                                              \
   do {                                                                          \
     accept::BoundsList bounds_list;                                                     \

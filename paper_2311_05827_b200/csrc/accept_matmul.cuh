@@ -1,4 +1,5 @@
-// Matrix product of 8-bit operands with a power-of-two scale for each row and block of 128 values of k (sm_100a).
+// Matrix product of 8-bit operands with a power-of-two scale for each row and 128 values of k, and of 4-bit operands with one for
+// each 32 (sm_100a).
 //
 // The tensor cores apply such scales themselves: the scale bytes go to tensor memory next to the sums, the sums stay
 // there in fp32 over all of k, and a scale costs no instruction of its own.
@@ -8,6 +9,39 @@
 
 namespace accept {
 
+// What the operands are.  A block of k is 128 bytes of each row; scales lie in groups of 512 bytes, 128 rows and four scales of each.
+struct EightBit {
+  static constexpr uint32_t kValues = 128;  // of a block
+  static constexpr uint32_t kServes = 4;    // blocks that a group of scales serves
+  static constexpr uint32_t kGroups = 1;    // groups of a block
+  static constexpr uint32_t instruction(uint32_t format_a, uint32_t format_b, uint32_t m, uint32_t n) { return scaled_instruction(format_a, format_b, m, n); }
+};
+struct FourBit {
+  static constexpr uint32_t kValues = 256;
+  static constexpr uint32_t kServes = 1;
+  static constexpr uint32_t kGroups = 2;
+  static constexpr uint32_t instruction(uint32_t, uint32_t, uint32_t m, uint32_t n) { return scaled4_instruction(m, n); }
+};
+// The first group of block b, and whether its scales come with it (they do for the first block of a sum too).
+template <typename Op> __device__ __forceinline__ uint32_t first_group(uint32_t b) { return b * Op::kGroups / Op::kServes; }
+template <typename Op> __device__ __forceinline__ bool brings_scales(uint32_t b) { return b % Op::kServes == 0; }
+// The products of the 128 bytes of k at da and db, 32 bytes at a time (that much further in the swizzled rows); a group's scales of a
+// lie in tensor memory at scale_a, those of b four columns on, the next group `stride` columns on.
+template <typename Op, bool PAIR>
+__device__ __forceinline__ void block_mma(uint32_t into, uint64_t da, uint64_t db, uint32_t instruction, uint32_t b, uint32_t scale_a, uint32_t stride, bool add) {
+#pragma unroll
+  for (uint32_t k = 0; k < 4; ++k) {
+    if constexpr (Op::kGroups == 1) {
+      if (PAIR) pair_scaled_mma(into, da + 2 * k, db + 2 * k, with_scale_byte(instruction, b & 3), scale_a, scale_a + 4, add || k > 0);
+      else scaled_mma(into, da + 2 * k, db + 2 * k, with_scale_byte(instruction, b & 3), scale_a, scale_a + 4, add || k > 0);
+    } else {
+      const uint32_t at = scale_a + k / 2 * stride, with = with_scale_byte(instruction, k % 2 * 2);
+      if (PAIR) pair_scaled4_mma(into, da + 2 * k, db + 2 * k, with, at, at + 4, add || k > 0);
+      else scaled4_mma(into, da + 2 * k, db + 2 * k, with, at, at + 4, add || k > 0);
+    }
+  }
+}
+
 struct MatmulArgs {
   const uint8_t* scale_a;  // of the operand on the instruction's M side: b's rows, the columns of d
   const uint8_t* scale_b;  // of a
@@ -16,7 +50,8 @@ struct MatmulArgs {
   uint32_t* status;
   uint64_t ldd;
   uint32_t m, n;
-  uint32_t blocks;            // ceil(k / 128)
+  uint32_t blocks;            // of k
+  uint32_t groups;            // of scales along k
   uint32_t atoms_a, atoms_b;  // groups of 128 rows in the scales
   uint32_t tiles;             // along n
   uint32_t instruction;
@@ -55,8 +90,8 @@ __device__ __forceinline__ uint32_t two_values(int dtype, float x, float y) {  /
   return dtype == kBf16 ? pair_to_word<__nv_bfloat16>(pair_of(x, y)) : pair_to_word<__half>(pair_of(x, y));
 }
 
-// Blocks of k that fp32 results are summed over in one run of the tensor cores (see the pairs of SMs).
-constexpr uint32_t kChunk = 64;
+// Blocks of k that fp32 results are summed over in one run of the tensor cores (see the pairs of SMs): 8192 values.
+template <typename Op> constexpr uint32_t kChunk = 8192 / Op::kValues;
 
 // ---- small products: single tokens, small batches, few tiles ---------------------------------------------------------
 //
@@ -72,8 +107,8 @@ constexpr int kTileA = 128;
 constexpr int kSmallReaders = 8;  // warps that read the sums: two share 32 lanes
 constexpr int kSmallThreads = 32 * (kSmallReaders + 2);
 constexpr int kSmallShared = 224 * 1024;
-__host__ __device__ constexpr int small_stage_bytes(int nt) { return (kTileA + nt) * 128 + 1024; }  // both tiles and 1 KB of scales
-__host__ __device__ constexpr int small_stages(int nt) { return (kSmallShared - 1024) / small_stage_bytes(nt); }
+template <typename Op> __host__ __device__ constexpr int small_stage_bytes(int nt) { return (kTileA + nt) * 128 + 1024 * (int)Op::kGroups; }  // both tiles and 1 KB of scales a group
+template <typename Op> __host__ __device__ constexpr int small_stages(int nt) { return (kSmallShared - 1024) / small_stage_bytes<Op>(nt); }
 
 // The finished rows to d, dealt over the cluster's blocks and their warps; several rows' reads are on their way at once.
 template <bool WIDE, uint32_t PARTS>
@@ -132,14 +167,17 @@ __device__ __forceinline__ void small_store(const MatmulArgs& a, uint32_t tile, 
   }
 }
 
-template <int NT, bool CHUNKS>
+template <typename Op, int NT, bool CHUNKS>
 __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                  const MatmulArgs a) {
-  constexpr int kStage = small_stage_bytes(NT), kStages = small_stages(NT);
+  constexpr int kStage = small_stage_bytes<Op>(NT), kStages = small_stages<Op>(NT);
   constexpr int kWords = 4;  // of scales in tensor memory, used in turn
-  static_assert(kStages <= 13, "a word comes round again thirteen blocks on, when the stage says that its products are done");
-  constexpr uint32_t kColumns = NT <= 32 ? 64 : NT <= 64 ? 128 : 256;  // NT sums and the scales, a power of two
-  constexpr uint32_t kScaleColumn = kColumns - 8 * kWords;
+  constexpr uint32_t kWordColumns = 8 * Op::kGroups;
+  static_assert(Op::kServes == 1 || kStages <= 13, "a word comes round again thirteen blocks on, when the stage says that its products are done");
+  static_assert(Op::kServes != 1 || kStages > kWords, "the products of the last use of a word belong to another stage");
+  constexpr uint32_t kNeeded = NT + kWordColumns * kWords;  // the sums and the scales
+  constexpr uint32_t kColumns = kNeeded <= 64 ? 64 : kNeeded <= 128 ? 128 : 256;
+  constexpr uint32_t kScaleColumn = kColumns - kWordColumns * kWords;
   extern __shared__ uint8_t raw_shared[];
   __shared__ __align__(8) uint64_t barriers[2 * kStages + 2];
   __shared__ uint32_t tensor_base, failed, issued;
@@ -150,7 +188,7 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
   const uint32_t first = (uint32_t)((uint64_t)a.blocks * rank / parts), last = (uint32_t)((uint64_t)a.blocks * (rank + 1) / parts);
   const uint32_t tile_b = blockIdx.x / a.tiles, tile_a = blockIdx.x - tile_b * a.tiles;
   const uint32_t row_a = tile_a * kTileA, row_b = tile_b * NT, rows = min(a.m - row_b, (uint32_t)NT);
-  const uint32_t chunks = CHUNKS ? (last - first + kChunk - 1) / kChunk : 1;
+  const uint32_t chunks = CHUNKS ? (last - first + kChunk<Op> - 1) / kChunk<Op> : 1;
   const auto chunk_start = [&](uint32_t chunk) { return first + (uint32_t)((uint64_t)(last - first) * chunk / chunks); };
 
   if (threadIdx.x == 0) {
@@ -176,13 +214,19 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
       if (!mbarrier_wait_warp(empty + 8 * stage, parity)) break;
       if (leader) {
         const uint32_t at = base + stage * kStage, bar = full + 8 * stage;
-        const bool scales = b == first || (b & 3) == 0;  // a word of scales serves four blocks of k
-        mbarrier_expect_bytes(bar, (kTileA + NT) * 128 + (scales ? 1024 : 0) + kCopyAnnounceExtra);
+        // k may end before a block's second group: the group before it comes a second time, its codes there are zeros
+        const uint32_t group = first_group<Op>(b), more = Op::kGroups > 1 && group + 1 < a.groups ? 1 : 0;
+        const bool scales = b == first || brings_scales<Op>(b);
+        mbarrier_expect_bytes(bar, (kTileA + NT) * 128 + (scales ? 1024 * Op::kGroups : 0) + kCopyAnnounceExtra);
         tile_load(at, &map_a, b * 128, row_a, bar);
         tile_load(at + kTileA * 128, &map_b, b * 128, row_b, bar);
         if (scales) {
-          bulk_copy_to_shared(at + (kTileA + NT) * 128, a.scale_a + ((uint64_t)(b >> 2) * a.atoms_a + tile_a) * 512, 512, bar);
-          bulk_copy_to_shared(at + (kTileA + NT) * 128 + 512, a.scale_b + ((uint64_t)(b >> 2) * a.atoms_b + tile_b) * 512, 512, bar);  // NT < 128: one tile
+#pragma unroll
+          for (uint32_t g = 0; g < Op::kGroups; ++g) {
+            const uint32_t to = at + (kTileA + NT) * 128 + 1024 * g, of = group + (g ? more : 0);
+            bulk_copy_to_shared(to, a.scale_a + ((uint64_t)of * a.atoms_a + tile_a) * 512, 512, bar);
+            bulk_copy_to_shared(to + 512, a.scale_b + ((uint64_t)of * a.atoms_b + tile_b) * 512, 512, bar);  // NT < 128: one tile
+          }
         }
       }
       if (++stage == kStages) { stage = 0; parity ^= 1; }
@@ -210,19 +254,23 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
       // A word of scales serves four blocks of k and comes round again after three others, thirteen blocks after the last
       // that used it (only a share's first and last word serve fewer); this stage was filled again, so the products of
       // kStages blocks back are done.
-      const bool fresh = b == first || (b & 3) == 0;
+      const bool fresh = b == first || brings_scales<Op>(b);
       if (fresh) word = word + 1 == kWords ? 0 : word + 1;
-      const uint32_t at = base + stage * kStage, scale_a = tensor + kScaleColumn + 8 * word;
-      const uint32_t instruction = with_scale_byte(a.instruction, b & 3);
+      if (Op::kServes == 1 && b - first >= kWords) {  // a word of one block: wait for the products that used it last
+        const uint32_t before = b - first - kWords;
+        if (!mbarrier_wait_warp(empty + 8 * (before % kStages), before / kStages & 1)) break;
+      }
+      const uint32_t at = base + stage * kStage, scale_a = tensor + kScaleColumn + kWordColumns * word;
       const uint64_t da = operand_descriptor(at), db = operand_descriptor(at + kTileA * 128), ds = scale_descriptor(at + (kTileA + NT) * 128);
       if (leader) {
         if (fresh) {
-          scale_copy(scale_a, ds);
-          scale_copy(scale_a + 4, ds + 32);
-        }
 #pragma unroll
-        for (uint32_t k = 0; k < 4; ++k)  // 32 values of k: 32 bytes further in the swizzled rows
-          scaled_mma(tensor, da + 2 * k, db + 2 * k, instruction, scale_a, scale_a + 4, b > from || k > 0);
+          for (uint32_t g = 0; g < Op::kGroups; ++g) {
+            scale_copy(scale_a + 8 * g, ds + 64 * g);
+            scale_copy(scale_a + 8 * g + 4, ds + 64 * g + 32);
+          }
+        }
+        block_mma<Op, false>(tensor, da, db, a.instruction, b, scale_a, 8, b > from);
         mma_commit(empty + 8 * stage);
       }
       if (++stage == kStages) { stage = 0; parity ^= 1; }
@@ -246,7 +294,7 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
       for (int j = 0; j < kPiece; ++j) total[i][j] = 0.0f;
     bool ok = true;
     for (uint32_t chunk = 0; chunk < chunks && ok; ++chunk) {
-      ok = mbarrier_wait_warp(done, chunk & 1, sums_wait_ns(kChunk));
+      ok = mbarrier_wait_warp(done, chunk & 1, sums_wait_ns(kChunk<Op>));
       if (!ok) break;
       tensor_fence_after();
 #pragma unroll
@@ -318,7 +366,7 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
 // block loads its own 128 rows of a and half of b, so an operand byte in shared memory feeds twice the products it would
 // feed for one SM alone.  Each pair keeps taking units of work; the sums of the next one are formed while the last one's
 // are read.  NT = 256 for large products; two tiles of sums (2 x 256 columns) and the scales do not fit 512 columns side by
-// side, so the two overlap by 24 columns: those are read first, and the next unit's products start once they are.
+// side, so the two overlap by 24 columns (48 with 4-bit operands): those are read first, and the next unit's products start once they are.
 // NT = 128 where tiles of 256 would leave pairs without work.
 // The products of unit i so wait twice: for the last read of unit i - 2, whose columns they take over (`drained`: all reading
 // warps of both blocks), and, where the two tiles overlap, for the first reads of unit i - 1 by the warps that hold the shared
@@ -335,19 +383,22 @@ __global__ void __launch_bounds__(kSmallThreads) matmul_small_kernel(const __gri
 // 1.5e-6 over 20001, 3.0e-6 over 32768.  In chunks of 8192 it is 0.5e-6 for any k (fp32 library sums: 0.1e-6 to 0.2e-6).
 constexpr uint32_t kPairRows = 256;
 
-template <int NT>
+template <typename Op, int NT>
 struct PairShape {
   static constexpr int kReaders = 8;                                     // warps that read sums: two share 32 rows
   static constexpr int kThreads = 32 * (kReaders + 2);
-  static constexpr int kStages = NT == 256 ? 6 : 8;
+  static constexpr int kStages = (NT == 256 ? 6 : 8) - (Op::kGroups - 1);
   static constexpr int kOperandBytes = (128 + NT / 2) * 128;             // a block's rows of a and of b, 128 bytes each
-  static constexpr int kScaleBytes = 512 + 4 * NT;                       // scales of 128 rows of a, of NT of b, four blocks of k
+  static constexpr int kGroupBytes = 512 + 4 * NT;                       // a group of scales: of 128 rows of a, of NT of b
+  static constexpr int kScaleBytes = Op::kGroups * kGroupBytes;
   static constexpr int kStaging = kReaders * 2048;                       // a piece of the result for each of those warps: 32 rows of 64 bytes
   static constexpr int kSharedBytes = 1024 + kStages * (kOperandBytes + kScaleBytes) + kStaging + kReaders * 4 * NT;  // and each warp's copy of the bias
-  static constexpr uint32_t kWordColumns = 4 + NT / 32;                  // a word of scales in tensor memory: of a, of b
+  static constexpr uint32_t kGroupColumns = 4 + NT / 32;                 // a group of scales in tensor memory: of a, of b
+  static constexpr uint32_t kWordColumns = Op::kGroups * kGroupColumns;  // a block's
   static constexpr uint32_t kScaleColumn = 512 - 2 * kWordColumns;       // two words in turn
   static constexpr uint32_t kSecond = kScaleColumn - NT < (uint32_t)NT ? kScaleColumn - NT : NT;  // the second tile of sums
   static constexpr bool kOverlap = kSecond < (uint32_t)NT;
+  static constexpr uint32_t kOverlapPieces = (NT - kSecond + 31) / 32;   // pieces of 32 columns that hold shared ones
   static_assert(kStages * kScaleBytes % 1024 == 0, "the pieces lie on the boundaries that the tensor map's swizzle counts from");
   // pieces of other parts' sums (32 rows x 32 columns, 4 KB) that a reading warp can have in shared memory at the end
   static constexpr uint32_t kSlots = kStages * kOperandBytes / kReaders / 4096;
@@ -544,12 +595,12 @@ __device__ __forceinline__ void pair_store(const PairArgs& a, const CUtensorMap*
   }
 }
 
-template <int NT, bool SINGLE>  // SINGLE: d is fp32
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThreads)
+template <typename Op, int NT, bool SINGLE>  // SINGLE: d is fp32
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<Op, NT>::kThreads)
     matmul_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                        const __grid_constant__ CUtensorMap map_sa, const __grid_constant__ CUtensorMap map_sb,
                        const __grid_constant__ CUtensorMap map_d, const PairArgs a) {
-  using S = PairShape<NT>;
+  using S = PairShape<Op, NT>;
   constexpr int kStages = S::kStages, kReaders = S::kReaders, kShare = kReaders / 4, kPer = NT / 32 / kShare;  // warps that share 32 rows, pieces of 32 columns for each
   extern __shared__ uint8_t raw_shared[];
   __shared__ __align__(8) uint64_t barriers[2 * kStages + 6 + kReaders];
@@ -593,14 +644,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
       for (uint32_t b = u.first; b < u.last; ++b, ++i) {
         if (!mbarrier_wait_warp(empty + 8 * stage, parity)) { ok = false; break; }
         if (leader) {
-          const bool with_scales = b == u.first || (b & 3) == 0;
+          const bool with_scales = b == u.first || brings_scales<Op>(b);
           const uint32_t at = base + stage * S::kOperandBytes, at_scales = scales + stage * S::kScaleBytes, bar = full_cluster + 8 * stage;
           if (rank == 0) mbarrier_expect_bytes(full + 8 * stage, 2 * (S::kOperandBytes + (with_scales ? S::kScaleBytes : 0)) + kCopyAnnounceExtra);
           pair_tile_load(at, &map_a, b * 128, row_a, bar);
           pair_tile_load(at + 128 * 128, &map_b, b * 128, row_b, bar);
           if (with_scales) {
-            pair_tile_load(at_scales, &map_sa, 0, (b >> 2) * a.atoms_a + u.tile_m * 2 + rank, bar);
-            pair_tile_load(at_scales + 512, &map_sb, 0, (b >> 2) * a.atoms_b + u.tile_n * (NT / 128), bar);
+#pragma unroll
+            for (uint32_t g = 0; g < Op::kGroups; ++g) {  // past the last group of k: zeros, and so are the codes there
+              const uint32_t group = first_group<Op>(b) + g;
+              pair_tile_load(at_scales + g * S::kGroupBytes, &map_sa, 0, group * a.atoms_a + u.tile_m * 2 + rank, bar);
+              pair_tile_load(at_scales + g * S::kGroupBytes + 512, &map_sb, 0, group * a.atoms_b + u.tile_n * (NT / 128), bar);
+            }
           }
         }
         if (++stage == kStages) { stage = 0; parity ^= 1; }
@@ -625,7 +680,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
       for (uint32_t b = u.first; b < u.last; ++b) {
         if (!mbarrier_wait_warp(full + 8 * stage, parity)) { ok = false; break; }
         tensor_fence_after();
-        const bool fresh = b == u.first || (b & 3) == 0;  // a word of scales serves four blocks of k
+        const bool fresh = b == u.first || brings_scales<Op>(b);
         if (fresh) {
           // the products that used this word before must be done (at most five blocks back: that phase is the latest)
           word ^= 1;
@@ -636,16 +691,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
         if (word) used[1] = i;
         else used[0] = i;
         const uint32_t at = base + stage * S::kOperandBytes, scale_a = tensor + S::kScaleColumn + S::kWordColumns * word;
-        const uint32_t instruction = with_scale_byte(a.instruction, b & 3);
         const uint64_t da = operand_descriptor(at), db = operand_descriptor(at + 128 * 128), ds = scale_descriptor(scales + stage * S::kScaleBytes);
         if (leader) {
           if (fresh) {
-            pair_scale_copy(scale_a, ds);
-            pair_scale_copy(scale_a + 4, ds + 32);
-            if (NT == 256) pair_scale_copy(scale_a + 8, ds + 64);
-          }
 #pragma unroll
-          for (uint32_t k = 0; k < 4; ++k) pair_scaled_mma(into, da + 2 * k, db + 2 * k, instruction, scale_a, scale_a + 4, b > u.first || k > 0);
+            for (uint32_t g = 0; g < Op::kGroups; ++g) {
+              const uint32_t to = scale_a + g * S::kGroupColumns;
+              const uint64_t from = ds + g * (S::kGroupBytes / 16);
+              pair_scale_copy(to, from);
+              pair_scale_copy(to + 4, from + 32);
+              if (NT == 256) pair_scale_copy(to + 8, from + 64);
+            }
+          }
+          block_mma<Op, true>(into, da, db, a.instruction, b, scale_a, S::kGroupColumns, b > u.first);
           pair_mma_commit(empty + 8 * stage);
         }
         if (++stage == kStages) { stage = 0; parity ^= 1; }
@@ -684,7 +742,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
         float v[32];
         tensor_read(from + c, v);
         tensor_read_wait();
-        const bool shares = S::kOverlap && turn == 0 && (warp >> 2) == (unit & 1 ? 0 : kShare - 1), last = turn + 1 == kPer;
+        const bool shares = S::kOverlap && turn + 1 == S::kOverlapPieces && (warp >> 2) == (unit & 1 ? 0 : kShare - 1), last = turn + 1 == kPer;
         if (shares || last) {
           tensor_fence_before();
           __syncwarp();
@@ -774,9 +832,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<NT>::kThre
 }
 
 // k = 0: the sum is empty.
-__global__ void __launch_bounds__(256) matmul_empty_kernel(const MatmulArgs a) {
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) matmul_empty_kernel(const MatmulArgs a) {
   grid_dependency_handshake();
-  const uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = i / a.n, col = i % a.n;
+  const uint64_t i = (uint64_t)blockIdx.x * THREADS + threadIdx.x, row = i / a.n, col = i % a.n;
   if (row < a.m) {
     const float v = a.bias ? ld_c(a.bias + col) : 0.0f;
     store_value(a.d, a.dtype_d, row * a.ldd + col, a.accumulate ? v + load_value(a.d, a.dtype_d, row * a.ldd + col) : v);

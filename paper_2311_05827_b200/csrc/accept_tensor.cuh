@@ -104,6 +104,16 @@ __device__ __forceinline__ void scaled_mma(uint32_t d, uint64_t a, uint64_t b, u
       "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"((uint32_t)add) : "memory");
 }
+// 4-bit operands (E2M1, two to a byte) with a scale for each 32 values of k: formats 1, and which pair of a scale word's bytes (0 or 2) in
+// the place of the byte above.
+__host__ __device__ constexpr uint32_t scaled4_instruction(uint32_t m, uint32_t n) { return scaled_instruction(1, 1, m, n); }
+// d (+)= a b^T over 64 values of k.
+__device__ __forceinline__ void scaled4_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t scale_a, uint32_t scale_b, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"((uint32_t)add) : "memory");
+}
 // The barrier is arrived at once all matrix instructions issued so far by this thread are done.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -131,6 +141,12 @@ __device__ __forceinline__ void pair_scaled_mma(uint32_t d, uint64_t a, uint64_t
   asm volatile(
       "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
       "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+      ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void pair_scaled4_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t instruction, uint32_t scale_a, uint32_t scale_b, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
       ::"r"(d), "l"(a), "l"(b), "r"(instruction), "r"(scale_a), "r"(scale_b), "r"((uint32_t)add) : "memory");
 }
 // The barrier at this place in both blocks is arrived at once the matrix instructions issued so far are done.
