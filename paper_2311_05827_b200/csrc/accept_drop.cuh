@@ -17,15 +17,22 @@ struct Drop {
 // Random word of any counter.
 static __device__ __noinline__ uint32_t drop_word_far(uint32_t seed_lo, uint32_t seed_hi, uint64_t ctr) { return Rng{seed_lo, seed_hi}.word(ctr); }
 
-// The counters from `first` on, `span` of them at most.
+// What counters share while the upper 30 bits of the counter stay.
+struct DropKey {
+  uint32_t high, key;
+  __device__ __forceinline__ DropKey(const Rng& rng, uint64_t first) : high((uint32_t)(first >> 34)), key(rng.key(high)) {}
+};
+
+// The counters from `first` on, `span` of them at most; `known`: the key of counters near by.
 struct DropRow {
   uint64_t first;
   uint32_t quad, key, phase;
   bool wraps;  // the low word of the quad index wraps inside: every element by itself
-  __device__ __forceinline__ DropRow(const Rng& rng, uint64_t first_, uint32_t span) : first(first_) {
+  __device__ __forceinline__ DropRow(const Rng& rng, uint64_t first_, uint32_t span, const DropKey& known) : first(first_) {
     const uint64_t q = first >> 2;
     quad = (uint32_t)q;
-    key = rng.key((uint32_t)(q >> 32));
+    key = known.key;
+    if ((uint32_t)(q >> 32) != known.high) key = rng.key((uint32_t)(q >> 32));
     phase = (uint32_t)first & 3;
     wraps = quad > 0xffffffffu - (span / 4 + 2);
   }
@@ -36,47 +43,59 @@ struct DropRow {
   }
 };
 
-// Random words of N neighbours from column `col` on (both multiples of four).  A hash serves four counters; where the row's
-// counters do not start on a multiple of four, four columns take theirs from two hashes, split at the same place in the whole
-// row.
-template <int N>
-__device__ __forceinline__ void number_unit(const Rng& rng, const DropRow& r, uint32_t col, uint32_t (&w)[N]) {
-  if (r.wraps) {
+// Random words of the N counters (or their complements, NOT: ~(h M) = -h M - 1 costs nothing more) from a multiple of four on: a hash
+// serves four.
+template <int N, bool NOT>
+__device__ __forceinline__ void number_quads(uint32_t quad, uint32_t key, uint32_t (&w)[N]) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) w[e] = drop_word_far(rng.seed_lo, rng.seed_hi, r.first + col + e);
-  } else if (r.phase == 0) {
+  for (int i = 0; i < N; i += 4) {
+    uint32_t h = Rng::quad_hash(quad + i / 4, key);
+    if (NOT) h = 0u - h;
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const uint32_t h = Rng::quad_hash(r.quad + (col + i) / 4, r.key);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[i + e] = lane_word(h, e);
-    }
-  } else {
-    uint32_t times[4], h = Rng::quad_hash(r.quad + col / 4, r.key);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t m = (r.phase + e) & 3;
-      times[e] = m == 0 ? 1u : m == 1 ? 0x9E3779B1u : m == 2 ? 0x85EBCA77u : 0xC2B2AE3Du;
-    }
-#pragma unroll
-    for (int i = 0; i < N; i += 4) {
-      const uint32_t next = Rng::quad_hash(r.quad + (col + i) / 4 + 1, r.key);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[i + e] = (r.phase + e >= 4 ? next : h) * times[e];
-      h = next;
-    }
+    for (int e = 0; e < 4; ++e) w[i + e] = h * (e == 0 ? 1u : e == 1 ? 0x9E3779B1u : e == 2 ? 0x85EBCA77u : 0xC2B2AE3Du) + (NOT ? 0xffffffffu : 0u);
   }
 }
-// N neighbours from column `col` on: v / (1 - p) where kept, else 0.
+
+// Those of N neighbours from column `col` on (both multiples of four).  Where the row's counters do not start on a multiple of four,
+// four columns take theirs from two hashes, split at the same place in the whole row.
+template <int N, bool NOT = false>
+__device__ __forceinline__ void number_unit(const Rng& rng, const DropRow& r, uint32_t col, uint32_t (&w)[N]) {
+  constexpr uint32_t kAdd = NOT ? 0xffffffffu : 0u;
+  if (r.wraps) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) w[e] = drop_word_far(rng.seed_lo, rng.seed_hi, r.first + col + e) ^ kAdd;
+    return;
+  }
+  if (r.phase == 0) return number_quads<N, NOT>(r.quad + col / 4, r.key, w);
+  uint32_t h[N / 4 + 1];
+#pragma unroll
+  for (int i = 0; i <= N / 4; ++i) {
+    h[i] = Rng::quad_hash(r.quad + col / 4 + i, r.key);
+    if (NOT) h[i] = 0u - h[i];
+  }
+  uint32_t times[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t m = (r.phase + e) & 3;
+    times[e] = m == 0 ? 1u : m == 1 ? 0x9E3779B1u : m == 2 ? 0x85EBCA77u : 0xC2B2AE3Du;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) w[i] = (r.phase + i % 4 >= 4 ? h[i / 4 + 1] : h[i / 4]) * times[i % 4] + kAdd;
+}
+// v / (1 - p) where kept, else 0.
 template <int N>
-__device__ __forceinline__ void drop_unit(const Drop& d, const DropRow& r, uint32_t col, Pair* v) {
-  uint32_t w[N];
-  number_unit<N>(d.rng, r, col, w);
+__device__ __forceinline__ void drop_values(const Drop& d, const uint32_t (&w)[N], Pair* v) {
 #pragma unroll
   for (int i = 0; i < N / 2; ++i) {
     const float2 f = split(mul2(v[i], both(d.scale)));
     v[i] = pair_of(w[2 * i] > d.limit ? f.x : 0.0f, w[2 * i + 1] > d.limit ? f.y : 0.0f);
   }
+}
+template <int N>  // N neighbours from column `col` on
+__device__ __forceinline__ void drop_unit(const Drop& d, const DropRow& r, uint32_t col, Pair* v) {
+  uint32_t w[N];
+  number_unit<N>(d.rng, r, col, w);
+  drop_values<N>(d, w, v);
 }
 
 }  // namespace accept

@@ -11,23 +11,27 @@ size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
 bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF16 || d == ACCEPT_DTYPE_F16; }
 
 using KernelFn = void (*)(const DropoutArgs);
-constexpr int kUnits = 2;
+constexpr int kUnits = 2, kFlatUnits = 4;
+enum class Rows { kFlat, kWhole, kLoose };  // no gaps, every row on a 16-byte boundary, neither
 
 template <typename TX, typename TY>
-KernelFn select_units(bool whole) { return whole ? accept::dropout_kernel<TX, TY, true, kUnits> : accept::dropout_kernel<TX, TY, false, kUnits>; }
+KernelFn select_rows(Rows rows) {
+  return rows == Rows::kFlat    ? accept::dropout_flat_kernel<TX, TY, kFlatUnits>
+         : rows == Rows::kWhole ? accept::dropout_kernel<TX, TY, true, kUnits> : accept::dropout_kernel<TX, TY, false, kUnits>;
+}
 template <typename TX>
-KernelFn select_y(int32_t dtype_y, bool whole) {
+KernelFn select_y(int32_t dtype_y, Rows rows) {
   switch (dtype_y) {
-    case ACCEPT_DTYPE_F32: return select_units<TX, float>(whole);
-    case ACCEPT_DTYPE_BF16: return select_units<TX, __nv_bfloat16>(whole);
-    default: return select_units<TX, __half>(whole);
+    case ACCEPT_DTYPE_F32: return select_rows<TX, float>(rows);
+    case ACCEPT_DTYPE_BF16: return select_rows<TX, __nv_bfloat16>(rows);
+    default: return select_rows<TX, __half>(rows);
   }
 }
-KernelFn select_kernel(int32_t dtype_x, int32_t dtype_y, bool whole) {
+KernelFn select_kernel(int32_t dtype_x, int32_t dtype_y, Rows rows) {
   switch (dtype_x) {
-    case ACCEPT_DTYPE_F32: return select_y<float>(dtype_y, whole);
-    case ACCEPT_DTYPE_BF16: return select_y<__nv_bfloat16>(dtype_y, whole);
-    default: return select_y<__half>(dtype_y, whole);
+    case ACCEPT_DTYPE_F32: return select_y<float>(dtype_y, rows);
+    case ACCEPT_DTYPE_BF16: return select_y<__nv_bfloat16>(dtype_y, rows);
+    default: return select_y<__half>(dtype_y, rows);
   }
 }
 
@@ -72,17 +76,17 @@ accept_status accept_dropout(const accept_dropout_params* p, const void* d_x, co
   ACCEPT_BOUNDS(s, bounds_list.add(d_x, ((p->rows - 1) * p->ld_x + p->cols) * size_x, false);
                 bounds_list.add(d_residual, ((p->rows - 1) * p->ld_y + p->cols) * size_y, false);
                 bounds_list.add(d_y, ((p->rows - 1) * p->ld_y + p->cols) * size_y, true));
-  bool whole = is_aligned(d_x, 16) && is_aligned(d_residual, 16) && is_aligned(d_y, 16);
-  if (p->rows == 1 || (p->ld_x == p->cols && p->ld_y == p->cols)) {  // no gaps: one row
+  const bool starts = is_aligned(d_x, 16) && is_aligned(d_residual, 16) && is_aligned(d_y, 16);
+  Rows rows = starts && p->ld_x * size_x % 16 == 0 && p->ld_y * size_y % 16 == 0 ? Rows::kWhole : Rows::kLoose;
+  if (p->rows == 1 || (p->ld_x == p->cols && p->ld_y == p->cols)) {
     a.cols = p->rows * p->cols;
     a.rows = 1;
-  } else {
-    whole = whole && p->ld_x * size_x % 16 == 0 && p->ld_y * size_y % 16 == 0;
+    rows = starts ? Rows::kFlat : Rows::kLoose;
   }
   a.per_row = (a.cols + 7) / 8;
   a.units = a.rows * a.per_row;
-  const uint64_t blocks = (a.units + kUnits * accept::kDropThreads - 1) / (kUnits * accept::kDropThreads);
-  ACCEPT_LAUNCH(accept::launch_overlapped(select_kernel(p->dtype_x, p->dtype_y, whole), dim3((unsigned)blocks), accept::kDropThreads, s, a));
+  const uint64_t block = (rows == Rows::kFlat ? kFlatUnits : kUnits) * accept::kDropThreads;
+  ACCEPT_LAUNCH(accept::launch_overlapped(select_kernel(p->dtype_x, p->dtype_y, rows), dim3((unsigned)((a.units + block - 1) / block)), accept::kDropThreads, s, a));
   return ACCEPT_OK;
 }
 

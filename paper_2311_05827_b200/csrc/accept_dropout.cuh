@@ -56,9 +56,54 @@ __device__ __forceinline__ void store_eight(T* p, int n, const Pair (&v)[4]) {
   }
 }
 
-// The units of eight neighbours of all rows in turn; a thread takes UNITS of them, a block's width apart, all loads first.  A
-// matrix without gaps is one row (the counters run on from row to row anyway), others cost a division for each unit.
 constexpr int kDropThreads = 256;
+
+// A matrix without gaps is one row (the counters run on from row to row): a thread takes UNITS units of eight neighbours, a block's
+// width apart, all loads first.
+template <typename TX, typename TY, int UNITS>
+__global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(const DropoutArgs a) {
+  grid_dependency_handshake();
+  constexpr uint32_t kStride = 8 * kDropThreads;
+  const uint64_t c0 = ((uint64_t)blockIdx.x * (UNITS * kDropThreads) + threadIdx.x) * 8;
+  const TX* x = static_cast<const TX*>(a.x) + c0;
+  const TY* residual = static_cast<const TY*>(a.residual) + c0;
+  TY* y = static_cast<TY*>(a.y) + c0;
+  const uint64_t first = a.drop.offset + c0;
+  const DropRow row(a.drop.rng, first, UNITS * kStride, DropKey(a.drop.rng, first));
+  const auto take = [&](int i, Pair (&v)[4], const Pair (&add)[4]) {
+    if (a.drop.on) drop_unit<8>(a.drop, row, i * kStride, v);
+    if (a.residual)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[j] = add2(v[j], add[j]);
+  };
+  if (c0 + (UNITS - 1) * kStride + 8 <= a.cols) {
+    Pair v[UNITS][4], add[UNITS][4];
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) load_eight<TX, true>(x + i * kStride, 8, v[i]);
+    if (a.residual)
+#pragma unroll
+      for (int i = 0; i < UNITS; ++i) load_eight<TY, true>(residual + i * kStride, 8, add[i]);
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) {
+      take(i, v[i], add[i]);
+      store_eight<TY, true>(y + i * kStride, 8, v[i]);
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < UNITS; ++i) {
+      const uint64_t c = c0 + i * kStride;
+      const int n = c < a.cols ? (int)min(a.cols - c, (uint64_t)8) : 0;
+      if (n == 0) break;
+      Pair v[4], add[4];
+      load_eight<TX, true>(x + i * kStride, n, v);
+      if (a.residual) load_eight<TY, true>(residual + i * kStride, n, add);
+      take(i, v, add);
+      store_eight<TY, true>(y + i * kStride, n, v);
+    }
+  }
+}
+
+// Other matrices: the units of all rows in turn, a division for each.
 template <typename TX, typename TY, bool VEC, int UNITS>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs a) {
   grid_dependency_handshake();
@@ -69,7 +114,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
 #pragma unroll
   for (int i = 0; i < UNITS; ++i) {
     const uint64_t u = first + i * kDropThreads;
-    row[i] = a.rows == 1 ? 0 : a.units <= 0xffffffffu ? (uint32_t)u / (uint32_t)a.per_row : u / a.per_row;
+    row[i] = a.units <= 0xffffffffu ? (uint32_t)u / (uint32_t)a.per_row : u / a.per_row;
     col[i] = (u - row[i] * a.per_row) * 8;
     n[i] = u < a.units ? (int)min(a.cols - col[i], (uint64_t)8) : 0;
     if (n[i] == 0) continue;
@@ -79,7 +124,10 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
 #pragma unroll
   for (int i = 0; i < UNITS; ++i) {
     if (n[i] == 0) continue;
-    if (a.drop.on) drop_unit<8>(a.drop, DropRow(a.drop.rng, a.drop.offset + row[i] * a.cols + col[i], 8), 0, v[i]);
+    if (a.drop.on) {
+      const uint64_t at = a.drop.offset + row[i] * a.cols + col[i];
+      drop_unit<8>(a.drop, DropRow(a.drop.rng, at, 8, DropKey(a.drop.rng, at)), 0, v[i]);
+    }
     if (a.residual)
 #pragma unroll
       for (int j = 0; j < 4; ++j) v[i][j] = add2(v[i][j], add[i][j]);

@@ -13,16 +13,21 @@ size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
 uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
 using KernelFn = void (*)(const MicroArgs);
+using accept::MicroRound;
+template <typename T, MicroRound ROUND>
+KernelFn select_rows(bool whole) { return whole ? accept::micro_quantize_kernel<T, ROUND, true> : accept::micro_quantize_kernel<T, ROUND, false>; }
 template <typename T>
-KernelFn select_round(int32_t round, bool whole) {
-  if (round == ACCEPT_ROUND_STOCHASTIC) return whole ? accept::micro_quantize_kernel<T, true, true> : accept::micro_quantize_kernel<T, true, false>;
-  return whole ? accept::micro_quantize_kernel<T, false, true> : accept::micro_quantize_kernel<T, false, false>;
+KernelFn select_round(MicroRound round, bool whole) {
+  return round == MicroRound::kNearest ? select_rows<T, MicroRound::kNearest>(whole)
+         : round == MicroRound::kQuads ? select_rows<T, MicroRound::kQuads>(whole) : select_rows<T, MicroRound::kAnywhere>(whole);
 }
 KernelFn select_kernel(const accept_micro_params* p, bool whole) {
+  const MicroRound round = p->round == ACCEPT_ROUND_NEAREST ? MicroRound::kNearest
+                           : p->cols % 4 == 0 && p->rng_offset % 4 == 0 ? MicroRound::kQuads : MicroRound::kAnywhere;
   switch (p->dtype) {
-    case ACCEPT_DTYPE_F32: return select_round<float>(p->round, whole);
-    case ACCEPT_DTYPE_BF16: return select_round<__nv_bfloat16>(p->round, whole);
-    default: return select_round<__half>(p->round, whole);
+    case ACCEPT_DTYPE_F32: return select_round<float>(round, whole);
+    case ACCEPT_DTYPE_BF16: return select_round<__nv_bfloat16>(round, whole);
+    default: return select_round<__half>(round, whole);
   }
 }
 
@@ -117,11 +122,11 @@ accept_status accept_micro_dequantize(const accept_micro_params* p, const void* 
   a.cols = (uint32_t)p->cols;
   a.ldq = (uint32_t)(up(p->cols, 32) / 2);
   a.atoms = (uint32_t)(up(p->rows, 128) / 128);
-  a.per_row = (p->cols + 7) / 8;
+  const bool whole = is_aligned(d_x, 16) && p->ld * value_size(p->dtype) % 16 == 0;
+  a.per_row = (p->cols + (whole ? 0 : 16 / value_size(p->dtype) - 1) + 7) / 8;  // units start on 16-byte boundaries: one more where a row does not
   a.units = p->rows * a.per_row;
   ACCEPT_BOUNDS(s, bounds_list.add(d_q, accept_micro_data_size(p, 0), false); bounds_list.add(d_scale, accept_micro_scale_size(p, 0), false);
                 bounds_list.add(d_x, ((p->rows - 1) * p->ld + p->cols) * value_size(p->dtype), true));
-  const bool whole = is_aligned(d_x, 16) && p->ld * value_size(p->dtype) % 16 == 0;
   const ValueFn fn = p->dtype == ACCEPT_DTYPE_F32 ? select_values<float>(whole) : p->dtype == ACCEPT_DTYPE_BF16 ? select_values<__nv_bfloat16>(whole) : select_values<__half>(whole);
   const uint64_t blocks = (a.units + kUnits * accept::kValueThreads - 1) / (kUnits * accept::kValueThreads);
   if (blocks > 0x7fffffffull) return ACCEPT_ERR_BAD_SIZE;

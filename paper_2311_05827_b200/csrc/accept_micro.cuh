@@ -47,38 +47,50 @@ __device__ __forceinline__ uint32_t micro_encode(const float (&v)[8]) {
       : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
   return r;
 }
-// One value (|v| <= 6) with stochastic rounding, in exact fixed point: F = the value's place in the list of codes times 2^24,
-// rounded up, so that (F + 2^24 - 1 - r) >> 24 is the upper neighbour where r 2^-24 is below the value's share of the step.  From
-// 1 on the list is that of fp32's own upper bits; below, steps are 0.5.  `less`: 2^24 - 1 - r.  The code is in the top four
-// bits, its sign above it.
-__device__ __forceinline__ uint32_t micro_stochastic(float v, uint32_t less) {
-  const float size = fabsf(v);
-  const uint32_t f = size < 1.0f ? __float2uint_ru(__fmul_rn(size, 0x1p+25f)) : (__float_as_uint(size) << 2) - ((0x3f800000u << 2) - (2u << 24));
-  return ((f + less) << 4) | (__float_as_uint(v) & 0x80000000u);
+// One value (|v| <= 6, v25 = v 2^25) to a code with stochastic rounding, in exact fixed point: F = the value's place in the list of
+// codes times 2^24, rounded up, so that F + 2^24 - 1 - r carries into the next place where r 2^-24 is below the value's share of the
+// step.  From 1 on the list is that of fp32's own upper bits; below, steps are 0.5.  `less`: the upper 28 bits of the random word's
+// complement, 2^24 - 1 - r over four bits that change nothing beside a multiple of 16.  The code is in the top four bits, its sign
+// first.  Additions run as multiply-adds beside the logic instructions, which bound this.
+__device__ __forceinline__ uint32_t micro_stochastic(float v, float v25, uint32_t less) {
+  uint32_t r;
+  asm("{\n\t.reg .pred p;\n\t.reg .f32 s, t;\n\t.reg .b32 f;\n\t"
+      "abs.f32 s, %1;\n\t"
+      "setp.ge.f32 p, s, 0f3F800000;\n\t"
+      "abs.f32 t, %2;\n\t"
+      "cvt.rpi.u32.f32 f, t;\n\t"
+      "@p mad.lo.u32 f, %4, 4, %5;\n\t"
+      "mad.lo.u32 f, f, 16, %3;\n\t"
+      "lop3.b32 %0, f, %4, 0x80000000, 0xF8;\n\t}"  // f | (v & sign)
+      : "=r"(r) : "f"(v), "f"(v25), "r"(less), "r"(__float_as_uint(v)), "r"((2u << 24) - (0x3f800000u << 2)));
+  return r;
 }
-// Eight such results to eight codes (each in its top four bits).
-__device__ __forceinline__ uint32_t micro_pack(const uint32_t (&w)[8]) {
-  uint32_t r = w[7] & 0xf0000000u;
+// Eight codes from the top four bits of words, the first in the lowest bits.
+__device__ __forceinline__ uint32_t micro_join(const uint32_t (&w)[8]) {
+  uint32_t r = w[7] >> 28;
 #pragma unroll
-  for (int i = 0; i < 7; ++i) r |= (w[i] >> 28) << 4 * i;
+  for (int i = 6; i >= 0; --i) r = __funnelshift_l(w[i], r, 4);
   return r;
 }
 
-// What a thread's 8 x 8 values need of the generator: word e of row i as `less` above.
-struct MicroNumbers {
-  uint32_t less[8][8];
-};
-
-// Thread t holds columns 8 (t % 16) .. + 7 of rows 8 (t / 16) .. + 7 of the tile.
-template <typename T, bool STOCHASTIC, bool WHOLE>
-__global__ void __launch_bounds__(256, 2) micro_quantize_kernel(const MicroArgs a) {
+// Thread (warp w, lane l) holds columns 64 (w % 2) + 8 (l % 8) .. + 7 of rows 32 (w / 2) + 8 (l / 8) .. + 7 of the tile: a warp has 32 rows
+// of two blocks of columns, so the largest values of all blocks, both ways, are found within it.
+//
+// Measured on 16384 x 4096 bf16, nearest: see the launch.  Stochastic rounding is bound by instruction issue: some 30 a value for
+// both outputs.
+// ROUND: nearest, or stochastic where all rows' counters start on a multiple of four (kQuads) or not (kAnywhere).
+enum class MicroRound { kNearest, kQuads, kAnywhere };
+template <typename T, MicroRound ROUND, bool WHOLE>
+__global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T) == 4 ? 2 : 3) micro_quantize_kernel(const MicroArgs a) {
+  constexpr bool STOCHASTIC = ROUND != MicroRound::kNearest;
   __shared__ __align__(16) uint8_t turned[kTile * (kTile / 2)];
-  __shared__ __align__(16) float column_most[8][kTile];
-  __shared__ __align__(16) float column_scale[4][kTile];
+  __shared__ __align__(16) uint8_t bytes_t[kTile][4];
+  constexpr bool kKept = sizeof(T) == 2;  // the numbers of all values stay in registers; beside fp32 values they are drawn twice
   grid_dependency_handshake();
   const uint32_t tile_r = blockIdx.x / a.tiles_c, tile_c = blockIdx.x - tile_r * a.tiles_c;
-  const uint32_t t = threadIdx.x, lane = t & 31, warp = t >> 5, part = t & 15;
-  const uint32_t r0 = tile_r * kTile + 8 * (t >> 4), c0 = tile_c * kTile + 8 * part;
+  const uint32_t t = threadIdx.x, lane = t & 31, warp = t >> 5, part = lane & 7, down = lane >> 3;
+  const uint32_t r_in = 32 * (warp >> 1) + 8 * down, c_in = 64 * (warp & 1) + 8 * part;
+  const uint32_t r0 = tile_r * kTile + r_in, c0 = tile_c * kTile + c_in;
 
   Held<T> h;
   {
@@ -98,32 +110,32 @@ __global__ void __launch_bounds__(256, 2) micro_quantize_kernel(const MicroArgs 
   for (int i = 0; i < 8; ++i) bad |= !is_finite_bits(row_most[i]);
   if (bad) atomicOr(a.status, kDevNonFinite);
 
-  MicroNumbers numbers;
-  if (STOCHASTIC) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const DropRow row(a.rng, a.offset + (uint64_t)(r0 + i) * a.cols + c0, 8);
-      uint32_t w[8];
-      number_unit<8>(a.rng, row, 0, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) numbers.less[i][j] = ~w[j] >> 8;
-    }
-  }
-
   uint32_t square_byte = 0;  // of the 32 x 32 block that this thread's values lie in
   if (a.square) {
     float most = row_most[0];
 #pragma unroll
     for (int i = 1; i < 8; ++i) most = max_nan(most, row_most[i]);
 #pragma unroll
-    for (int d = 1; d <= 2; d <<= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
-    most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, 16));
-    if (lane < 16 && !(lane & 3)) column_most[warp][lane >> 2] = most;
-    __syncthreads();
-    most = max_nan(column_most[warp & ~1u][part >> 2], column_most[warp | 1u][part >> 2]);
+    for (int d = 1; d <= 16; d <<= 1)
+      if (d != 4) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
     square_byte = micro_scale_byte(most);
-    __syncthreads();
   }
+
+  const uint64_t first = a.offset + (uint64_t)r0 * a.cols + c0;
+  const DropKey key(a.rng, first);
+  const uint32_t quad = (uint32_t)(first >> 2);
+  const bool together = (uint32_t)((first + 7ull * a.cols + 8) >> 34) == key.high;  // one key for all values of the thread
+  const auto draw_row = [&](int i, uint32_t (&less)[8]) {
+    uint32_t w[8];
+    if (ROUND == MicroRound::kQuads && together) number_quads<8, true>(quad + i * (a.cols / 4), key.key, w);
+    else number_unit<8, true>(a.rng, DropRow(a.rng, first + (uint64_t)i * a.cols, 8, key), 0, w);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) less[j] = w[j] >> 4;
+  };
+  uint32_t numbers[STOCHASTIC && kKept ? 8 : 1][8];
+  if (STOCHASTIC && kKept)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) draw_row(i, numbers[i % (STOCHASTIC && kKept ? 8 : 1)]);
 
   if (a.q) {
     // four lanes hold eight rows of a block: each exchange halves the rows that a lane looks after, until it has two
@@ -138,19 +150,15 @@ __global__ void __launch_bounds__(256, 2) micro_quantize_kernel(const MicroArgs 
       const float away = part & 1 ? m[k] : m[k + 2], keep = part & 1 ? m[k + 2] : m[k];
       m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 1));
     }
-    uint32_t byte[2];
     float inverse[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {  // rows 2 (part % 4) + k of the eight
-      byte[k] = a.square ? square_byte : micro_scale_byte(m[k]);
-      inverse[k] = micro_inverse(byte[k]);
-      // rows and blocks that do not exist hold zeros: 127 from micro_scale_byte, also beside a square block that ends inside
-      const bool there = r0 + 2 * (part & 3) + k < a.rows && (c0 & ~31u) < a.cols;
-      uint32_t word = (there ? byte[k] : 127u) << 8 * (part >> 2);
-      word |= __shfl_xor_sync(0xffffffffu, word, 4);
-      word |= __shfl_xor_sync(0xffffffffu, word, 8);
       const uint32_t row = r0 + 2 * (part & 3) + k;
-      if (part < 4) st_c(reinterpret_cast<uint32_t*>(a.scale + scale_offset(row, 4 * tile_c, a.tiles_r)), word);
+      uint32_t byte = a.square ? square_byte : micro_scale_byte(m[k]);
+      inverse[k] = micro_inverse(byte);
+      if (row >= a.rows || (c0 & ~31u) >= a.cols) byte = 127u;  // rows and blocks that do not exist, beside a square block that ends inside
+      const uint32_t next = __shfl_xor_sync(0xffffffffu, byte, 4);
+      if (part < 4) st_c(reinterpret_cast<uint16_t*>(a.scale + scale_offset(row, 4 * tile_c + 2 * (warp & 1), a.tiles_r)), (uint16_t)(byte | next << 8));
     }
     uint8_t* q = a.q + (uint64_t)r0 * a.ldq + c0 / 2;
 #pragma unroll
@@ -164,11 +172,16 @@ __global__ void __launch_bounds__(256, 2) micro_quantize_kernel(const MicroArgs 
         v[2 * j + 1] = f.y;
       }
       uint32_t code;
-      if (STOCHASTIC) {
-        uint32_t w[8];
+      if constexpr (STOCHASTIC) {
+        uint32_t w[8], drawn[8];
+        if (!kKept) draw_row(i, drawn);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = micro_stochastic(v[j], numbers.less[i][j]);
-        code = micro_pack(w);
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = split(mul2(pair_of(v[2 * j], v[2 * j + 1]), both(0x1p+25f)));
+          w[2 * j] = micro_stochastic(v[2 * j], f.x, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j] : drawn[2 * j]);
+          w[2 * j + 1] = micro_stochastic(v[2 * j + 1], f.y, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j + 1] : drawn[2 * j + 1]);
+        }
+        code = micro_join(w);
       } else {
         code = micro_encode(v);
       }
@@ -178,69 +191,68 @@ __global__ void __launch_bounds__(256, 2) micro_quantize_kernel(const MicroArgs 
   }
 
   if (a.qt) {
-    // the largest of 32 rows: four threads down, in two warps
-    if (!a.square) {
-      float m[4];  // of the lower or the upper four columns
+    // four lanes hold eight columns of a block, 32 rows: as above
+    float m[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float away = lane & 16 ? col_most[k] : col_most[k + 4], keep = lane & 16 ? col_most[k + 4] : col_most[k];
-        m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 16));
-      }
-      *reinterpret_cast<float4*>(&column_most[warp][8 * part + (lane & 16 ? 4 : 0)]) = make_float4(m[0], m[1], m[2], m[3]);
-    } else if (lane < 16) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) column_most[warp][8 * part + k] = __uint_as_float(square_byte);
+    for (int k = 0; k < 4; ++k) {
+      const float away = lane & 16 ? col_most[k] : col_most[k + 4], keep = lane & 16 ? col_most[k + 4] : col_most[k];
+      m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 16));
     }
-    __syncthreads();
-    if (t < kTile) {
-      uint32_t word = 0;
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float lower = column_most[2 * g][t], upper = column_most[2 * g + 1][t];
-        uint32_t byte = a.square ? __float_as_uint(lower) : micro_scale_byte(max_nan(lower, upper));
-        column_scale[g][t] = micro_inverse(byte);
-        if (tile_c * kTile + t >= a.cols || tile_r * kTile + 32 * g >= a.rows) byte = 127u;
-        word |= byte << 8 * g;
-      }
-      st_c(reinterpret_cast<uint32_t*>(a.scale_t + scale_offset(tile_c * kTile + t, 4 * tile_r, a.tiles_c)), word);
+    for (int k = 0; k < 2; ++k) {
+      const float away = lane & 8 ? m[k] : m[k + 2], keep = lane & 8 ? m[k + 2] : m[k];
+      m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 8));
     }
-    __syncthreads();
-    const float4 lo = *reinterpret_cast<const float4*>(&column_scale[warp >> 1][8 * part]), hi = *reinterpret_cast<const float4*>(&column_scale[warp >> 1][8 * part + 4]);
-    const float scale[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-    // Column c of the tile is 16 words (the eight rows of one thread each), word g at place g ^ (c / 8): the sixteen threads that
-    // write one word of different columns meet sixteen different places.
-    uint8_t* word = turned + 8 * part * (kTile / 2) + 4 * ((t >> 4) ^ part);
+    float inverse[2];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      float v[8];
+    for (int k = 0; k < 2; ++k) {  // columns 2 down + k of the eight
+      uint32_t byte = a.square ? square_byte : micro_scale_byte(m[k]);
+      inverse[k] = micro_inverse(byte);
+      if (c0 + 2 * down + k >= a.cols || (r0 & ~31u) >= a.rows) byte = 127u;
+      bytes_t[c_in + 2 * down + k][warp >> 1] = (uint8_t)byte;
+    }
+    // Column c of the tile is 16 words (eight rows each), those of 32 rows side by side, u-th four at place u ^ (c / 8 % 4): the lanes
+    // that write the words of different columns meet different places.
+    uint8_t* word = turned + c_in * (kTile / 2) + 16 * ((warp >> 1) ^ (part & 3)) + 4 * down;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float s0 = __shfl_sync(0xffffffffu, inverse[0], part | j << 3), s1 = __shfl_sync(0xffffffffu, inverse[1], part | j << 3);
+      const Pair scale = pair_of(s0, s1);
+      float left[8], right[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float2 f = split(held_pair(h, i, j / 2));
-        v[i] = __fmul_rn(j % 2 ? f.y : f.x, scale[j]);
+        const float2 f = split(mul2(held_pair(h, i, j), scale));
+        left[i] = f.x;
+        right[i] = f.y;
       }
-      uint32_t code;
-      if (STOCHASTIC) {
-        uint32_t w[8];
+      uint32_t code[2];
+      if constexpr (STOCHASTIC) {
+        uint32_t w[2][8], drawn[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = micro_stochastic(v[i], numbers.less[i][j]);
-        code = micro_pack(w);
+        for (int i = 0; i < 8; ++i) {
+          if (!kKept) draw_row(i, drawn);  // what this pair of columns does not need falls away
+          const float2 f = split(mul2(pair_of(left[i], right[i]), both(0x1p+25f)));
+          w[0][i] = micro_stochastic(left[i], f.x, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j] : drawn[2 * j]);
+          w[1][i] = micro_stochastic(right[i], f.y, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j + 1] : drawn[2 * j + 1]);
+        }
+        code[0] = micro_join(w[0]);
+        code[1] = micro_join(w[1]);
       } else {
-        code = micro_encode(v);
+        code[0] = micro_encode(left);
+        code[1] = micro_encode(right);
       }
-      *reinterpret_cast<uint32_t*>(word + j * (kTile / 2)) = scale[j] == 0.0f ? 0u : code;
+      *reinterpret_cast<uint32_t*>(word + 2 * j * (kTile / 2)) = s0 == 0.0f ? 0u : code[0];
+      *reinterpret_cast<uint32_t*>(word + (2 * j + 1) * (kTile / 2)) = s1 == 0.0f ? 0u : code[1];
     }
     __syncthreads();
+    if (t < kTile)
+      st_c(reinterpret_cast<uint32_t*>(a.scale_t + scale_offset(tile_c * kTile + t, 4 * tile_r, a.tiles_c)), *reinterpret_cast<const uint32_t*>(bytes_t[t]));
 #pragma unroll
     for (int k = 0; k < 2; ++k) {  // four threads a column, 16 bytes each
-      const uint32_t c = (t >> 2) + 64 * k, u = t & 3, turn = c >> 3;
-      const uint4 w = *reinterpret_cast<const uint4*>(turned + c * (kTile / 2) + 16 * (u ^ (turn >> 2)));
-      const uint32_t in[4] = {w.x, w.y, w.z, w.w};
-      uint32_t out[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) out[i] = (turn & 1 ? (turn & 2 ? in[i ^ 3] : in[i ^ 1]) : (turn & 2 ? in[i ^ 2] : in[i]));
+      const uint32_t c = (t >> 2) + 64 * k, u = t & 3;
+      const uint4 w = *reinterpret_cast<const uint4*>(turned + c * (kTile / 2) + 16 * (u ^ (c >> 3 & 3)));
       const uint32_t byte = tile_r * (kTile / 2) + 16 * u;
-      if (tile_c * kTile + c < a.cols && byte < a.ldqt)
-        st_c(reinterpret_cast<uint4*>(a.qt + (uint64_t)(tile_c * kTile + c) * a.ldqt + byte), make_uint4(out[0], out[1], out[2], out[3]));
+      if (tile_c * kTile + c < a.cols && byte < a.ldqt) st_c(reinterpret_cast<uint4*>(a.qt + (uint64_t)(tile_c * kTile + c) * a.ldqt + byte), w);
     }
   }
 }
@@ -255,41 +267,71 @@ struct MicroValueArgs {
   uint32_t cols, ldq, atoms;
 };
 
-// Eight codes as fp32 pairs.  As fp32 bits a code's two exponent and one fraction bits are its value
-// times 2^-126 (the smallest, 0.5, a subnormal), so one exact product gives the value and another one applies the scale.
-__device__ __forceinline__ void micro_decode(uint32_t codes, float scale, Pair (&v)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const uint32_t lo = codes >> 8 * j, hi = codes >> (8 * j + 4);
-    const Pair raw = pair_of(__uint_as_float((lo << 28 & 0x80000000u) | (lo << 22 & 0x01c00000u)),
-                             __uint_as_float((hi << 28 & 0x80000000u) | (hi << 22 & 0x01c00000u)));
-    v[j] = mul2(mul2(raw, both(0x1p+126f)), both(scale));
-  }
+// Eight codes as fp32 pairs.  As fp32 bits a code's two exponent and one fraction bits are its value times 2^-126 (the smallest,
+// 0.5, a subnormal), so one exact product gives the value and another one applies the scale (of the pair's first and second).
+__device__ __forceinline__ Pair micro_value(uint32_t codes, int j, Pair scale) {
+  const uint32_t lo = codes >> 8 * j, hi = codes >> (8 * j + 4);
+  const Pair raw = pair_of(__uint_as_float((lo << 28 & 0x80000000u) | (lo << 22 & 0x01c00000u)),
+                           __uint_as_float((hi << 28 & 0x80000000u) | (hi << 22 & 0x01c00000u)));
+  return mul2(mul2(raw, both(0x1p+126f)), scale);
 }
+__device__ __forceinline__ float micro_scale(uint32_t byte) { return __uint_as_float(byte == 255u ? 0x7fffffffu : byte ? byte << 23 : 1u << 22); }
 
+// A unit is eight neighbours of a row that start on a 16-byte boundary of x.  Where rows do not (WHOLE false), a unit's codes are
+// shifted out of two words and may have two scales; the ends of a row are written value by value.  (One value a store:
+// 4096 x 1001 fp32 27.7 us.)
 constexpr int kValueThreads = 256;
-template <typename T, bool VEC, int UNITS>
+template <typename T, bool WHOLE, int UNITS>
 __global__ void __launch_bounds__(kValueThreads) micro_dequantize_kernel(const MicroValueArgs a) {
   grid_dependency_handshake();
   const uint64_t first = (uint64_t)blockIdx.x * (UNITS * kValueThreads) + threadIdx.x;
-  uint32_t codes[UNITS], byte[UNITS], row[UNITS], col[UNITS];
-  int n[UNITS];
+  constexpr int kEach = 16 / (int)sizeof(T);
+  uint32_t codes[UNITS], byte[UNITS], next[UNITS], row[UNITS];
+  int col[UNITS], n[UNITS];  // of a unit: its first column (below 0 where the row starts inside it), how many exist
 #pragma unroll
   for (int i = 0; i < UNITS; ++i) {
     const uint64_t u = first + i * kValueThreads;
     row[i] = a.units <= 0xffffffffu ? (uint32_t)u / (uint32_t)a.per_row : (uint32_t)(u / a.per_row);
-    col[i] = (uint32_t)(u - row[i] * a.per_row) * 8;
-    n[i] = u < a.units ? (int)min(a.cols - col[i], 8u) : 0;
+    uint32_t c = (uint32_t)(u - row[i] * a.per_row) * 8;
+    uint32_t before = 0;  // values between the 16-byte boundary and the row's start
+    if (!WHOLE) before = (uint32_t)(((uint64_t)reinterpret_cast<uintptr_t>(a.x) / sizeof(T) + row[i] * a.ld) % kEach);
+    col[i] = (int)(c - before);
+    n[i] = u < a.units && c < a.cols + before ? 1 : 0;
     if (n[i] == 0) continue;
-    codes[i] = ldg_c(reinterpret_cast<const uint32_t*>(a.q + (uint64_t)row[i] * a.ldq + col[i] / 2));
-    byte[i] = ldg_c(a.scale + scale_offset(row[i], col[i] / 32, a.atoms));
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + (uint64_t)row[i] * a.ldq);
+    const uint32_t start = WHOLE ? c : col[i] < 0 ? 0u : (uint32_t)col[i];
+    codes[i] = ldg_c(q + start / 8);
+    byte[i] = next[i] = ldg_c(a.scale + scale_offset(row[i], start / 32, a.atoms));
+    if (!WHOLE) {
+      const uint32_t end = min((uint32_t)(col[i] + 7), a.cols - 1);
+      uint32_t more = codes[i];
+      if (end / 8 != start / 8) more = ldg_c(q + end / 8);
+      if (end / 32 != start / 32) next[i] = ldg_c(a.scale + scale_offset(row[i], end / 32, a.atoms));
+      codes[i] = col[i] < 0 ? codes[i] << 4 * (uint32_t)-col[i] : __funnelshift_r(codes[i], more, 4 * (start % 8));
+    }
   }
 #pragma unroll
   for (int i = 0; i < UNITS; ++i) {
     if (n[i] == 0) continue;
     Pair v[4];
-    micro_decode(codes[i], __uint_as_float(byte[i] == 255u ? 0x7fffffffu : byte[i] ? byte[i] << 23 : 1u << 22), v);
-    store_eight<T, VEC>(static_cast<T*>(a.x) + (uint64_t)row[i] * a.ld + col[i], n[i], v);
+    const float s = micro_scale(byte[i]), s2 = WHOLE ? s : micro_scale(next[i]);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int lo = (col[i] + 2 * j) & 31, hi = (col[i] + 2 * j + 1) & 31;  // the second scale from the first boundary on
+      const bool second_lo = !WHOLE && col[i] >= 0 && lo < (col[i] & 31), second_hi = !WHOLE && col[i] >= 0 && hi < (col[i] & 31);
+      v[j] = micro_value(codes[i], j, pair_of(second_lo ? s2 : s, second_hi ? s2 : s));
+    }
+    T* x = static_cast<T*>(a.x) + (uint64_t)row[i] * a.ld;
+    if (WHOLE || (col[i] >= 0 && (uint32_t)col[i] + 8 <= a.cols)) {
+      store_eight<T, true>(x + col[i], WHOLE ? (int)min(a.cols - (uint32_t)col[i], 8u) : 8, v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float2 f = split(v[j / 2]);
+        const int c = col[i] + j;
+        if (c >= 0 && (uint32_t)c < a.cols) st_c(x + c, from_float<T>(j % 2 ? f.y : f.x));
+      }
+    }
   }
 }
 

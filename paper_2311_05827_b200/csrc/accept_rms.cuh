@@ -164,6 +164,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
   load_weights<V, FULL, OWN, L>(a, a.gamma, own, 1.0f, t, gamma);
   uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;  // where this row lies, and where the one to start goes
   uint64_t r = first;
+  const DropKey key(a.drop.rng, a.drop.offset + r * a.cols);
   for (;;) {
     if (r + (STAGES - 1) * (uint64_t)step < a.rows) {
       start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, own, x, end_x);
@@ -177,7 +178,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
     if (branch) {
       Pair b[OWN / 2];
       take_row<TY, V, FULL, OWN, L>(here + space_x, brow, t, own, b);
-      if (a.drop.on) drop_row<V, FULL, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, a.cols), t, b);
+      if (a.drop.on) drop_row<V, FULL, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key), t, b);
 #pragma unroll
       for (int i = 0; i < OWN / 2; ++i) v[i] = rounded<TX>(add2(v[i], b[i]));
     }
@@ -276,6 +277,7 @@ __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<
   uint32_t here = shared, ahead = shared + (STAGES - 1) * space, turn = 0;
   uint64_t r = first;
   float rstd_next = ld_c(a.rstd + r);
+  const DropKey key(a.drop.rng, a.drop.offset + r * a.cols);
   for (;;) {
     if (r + (STAGES - 1) * (uint64_t)step < a.rows) start(ahead, at_x + (STAGES - 1) * stride_x, at_y + (STAGES - 1) * stride_y);
     copy_commit();
@@ -306,7 +308,7 @@ __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<
       }
       if (a.dx) store_row<TX, V, FULL, OWN, L>(static_cast<TX*>(a.dx) + at_x, t, own, h);
       if (a.dbranch) {
-        if (a.drop.on) drop_row<V, FULL, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, a.cols), t, h);
+        if (a.drop.on) drop_row<V, FULL, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key), t, h);
         store_row<TY, V, FULL, OWN, L>(static_cast<TY*>(a.dbranch) + at_y, t, own, h);
       }
     }
@@ -478,11 +480,12 @@ __global__ void __launch_bounds__(kWideThreads) rms_forward_wide_kernel(const Rm
   grid_dependency_handshake();
   if (a.q) pad_scales(a);
   uint32_t turn = 0;
+  const DropKey key(a.drop.rng, a.drop.offset + blockIdx.x * (uint64_t)a.cols);
   for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
     const TX* row = static_cast<const TX*>(a.x) + r * a.ld_x;
     const TY* branch = a.branch ? static_cast<const TY*>(a.branch) + r * a.ld_y : nullptr;
     TX* kept = a.sum ? static_cast<TX*>(a.sum) + r * a.ld_x : nullptr;
-    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, a.cols);
+    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key);
     const auto sum_of_eight = [&](uint32_t c, int n, Pair (&v)[4]) {
       load_eight<TX, VEC>(row + c, n, v);
       if (branch) {
@@ -551,6 +554,7 @@ __global__ void __launch_bounds__(kWideThreads) rms_backward_wide_kernel(const R
   __shared__ float slots[2][32];
   grid_dependency_handshake();
   uint32_t turn = 0;
+  const DropKey key(a.drop.rng, a.drop.offset + blockIdx.x * (uint64_t)a.cols);
   for (uint64_t r = blockIdx.x; r < a.rows; r += gridDim.x, turn ^= 1) {
     const TX* row = static_cast<const TX*>(a.x) + r * a.ld_x;
     const TY* drow = static_cast<const TY*>(a.dy) + r * a.ld_y;
@@ -574,7 +578,7 @@ __global__ void __launch_bounds__(kWideThreads) rms_backward_wide_kernel(const R
       for (int j = 0; j < 4; ++j) along = fma2(h[j], xhat[j], along);
     }
     const Pair slope = both(-rms_block_sum(sum_of(along), slots[turn]) * a.inv_cols);
-    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, a.cols);
+    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key);
     for (uint32_t c = 8 * threadIdx.x; c < a.cols; c += 8 * kWideThreads) {
       const int n = (int)min(a.cols - c, 8u);
       Pair xhat[4], h[4];
