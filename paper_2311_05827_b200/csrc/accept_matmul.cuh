@@ -398,7 +398,10 @@ struct PairShape {
   static constexpr uint32_t kScaleColumn = 512 - 2 * kWordColumns;       // two words in turn
   static constexpr uint32_t kSecond = kScaleColumn - NT < (uint32_t)NT ? kScaleColumn - NT : NT;  // the second tile of sums
   static constexpr bool kOverlap = kSecond < (uint32_t)NT;
-  static constexpr uint32_t kOverlapPieces = (NT - kSecond + 31) / 32;   // pieces of 32 columns that hold shared ones
+  // Two pieces of 32 columns hold shared ones (48, with 4-bit operands): the two warps that share 32 rows read one each first, so
+  // that the next unit waits for one read (16384 x 4096 x 4096: 112 -> 106 us).
+  static constexpr bool kDealt = NT - kSecond > 32;
+  static_assert(NT - kSecond <= 64, "one piece for each of two warps");
   static_assert(kStages * kScaleBytes % 1024 == 0, "the pieces lie on the boundaries that the tensor map's swizzle counts from");
   // pieces of other parts' sums (32 rows x 32 columns, 4 KB) that a reading warp can have in shared memory at the end
   static constexpr uint32_t kSlots = kStages * kOperandBytes / kReaders / 4096;
@@ -615,7 +618,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<Op, NT>::k
     for (int i = 0; i < 2 * kStages + 2; ++i) mbarrier_init(full + 8 * i, 1);
     for (int i = 0; i < 2; ++i) {  // warps of both blocks
       mbarrier_init(drained + 8 * i, 2 * kReaders);
-      mbarrier_init(shared_read + 8 * i, 2 * 4);
+      mbarrier_init(shared_read + 8 * i, S::kDealt ? 2 * kReaders : 2 * 4);
     }
     for (int i = 0; i < kReaders; ++i) mbarrier_init(joined + 8 * i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -716,6 +719,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<Op, NT>::k
     uint8_t* piece = raw_shared + (piece_address - smem_address(raw_shared));
     float* bias_tile = reinterpret_cast<float*>(raw_shared + (staging + S::kStaging - smem_address(raw_shared))) + warp * NT;
     const uint32_t drained_at = address_in(drained, 0), shared_read_at = address_in(shared_read, 0);
+    // the i-th piece of 32 columns that a warp reads: of its half, or, where two pieces hold shared columns, of every kShare-th
+    constexpr bool kDealt = S::kDealt;
+    const auto piece_at = [&](uint32_t i) { return kDealt ? i * kShare + (warp >> 2) : (warp >> 2) * kPer + i; };
     Unit u;
     for (uint32_t unit = 0; pair_unit(a, pair, pairs, unit, u); ++unit) {
       const uint32_t row0 = u.tile_m * kPairRows + rank * 128 + (warp & 3) * 32, col0 = u.tile_n * NT;
@@ -738,11 +744,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<Op, NT>::k
       if (u.chunk > 0 && lane == 0) store_wait();  // the chunk before must lie in d
 #pragma unroll 1
       for (uint32_t turn = 0; turn < kPer; ++turn) {  // 32 columns at a time, those shared with the next unit's sums first
-        const uint32_t c = 32 * ((warp >> 2) * kPer + (unit & 1 || !S::kOverlap ? turn : kPer - 1 - turn));
+        const uint32_t c = 32 * piece_at(unit & 1 || !S::kOverlap ? turn : kPer - 1 - turn);
         float v[32];
         tensor_read(from + c, v);
         tensor_read_wait();
-        const bool shares = S::kOverlap && turn + 1 == S::kOverlapPieces && (warp >> 2) == (unit & 1 ? 0 : kShare - 1), last = turn + 1 == kPer;
+        const bool shares = S::kOverlap && turn == 0 && (kDealt || (warp >> 2) == (unit & 1 ? 0 : kShare - 1)), last = turn + 1 == kPer;
         if (shares || last) {
           tensor_fence_before();
           __syncwarp();
@@ -780,11 +786,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<Op, NT>::k
               mbarrier_expect_bytes(bar, (stop - start) * others * 4096 + kCopyAnnounceExtra);
               for (uint32_t i = start; i < stop; ++i)
                 for (uint32_t o = 0; o < others; ++o)
-                  bulk_copy_to_shared(slots + ((i - start) * others + o) * 4096, partial + (o + (o >= u.part)) * part_stride + 8 * ((warp >> 2) * kPer + i) * 32, 4096, bar);
+                  bulk_copy_to_shared(slots + ((i - start) * others + o) * 4096, partial + (o + (o >= u.part)) * part_stride + 8 * piece_at(i) * 32, 4096, bar);
             }
             landed = mbarrier_wait_warp(bar, phase);
             for (uint32_t i = start; i < stop && landed; ++i) {
-              const uint32_t c = 32 * ((warp >> 2) * kPer + i);
+              const uint32_t c = 32 * piece_at(i);
               float own[32], v[32];
               tensor_read(from + c, own);
               tensor_read_wait();
