@@ -56,31 +56,47 @@ __device__ __forceinline__ void number_quads(uint32_t quad, uint32_t key, uint32
   }
 }
 
-// Those of N neighbours from column `col` on (both multiples of four).  Where the row's counters do not start on a multiple of four,
-// four columns take theirs from two hashes, split at the same place in the whole row.
-template <int N, bool NOT = false>
-__device__ __forceinline__ void number_unit(const Rng& rng, const DropRow& r, uint32_t col, uint32_t (&w)[N]) {
+// Those of UNITS units of N neighbours, the first from column `col` on and `step` columns apart (multiples of four), for take(unit, words).
+// Where the row's counters do not start on a multiple of four, four columns take theirs from two hashes, split at the same place in
+// the whole row.
+template <int N, bool NOT, int UNITS, typename Take>
+__device__ __forceinline__ void number_units(const Rng& rng, const DropRow& r, uint32_t col, uint32_t step, const Take& take) {
   constexpr uint32_t kAdd = NOT ? 0xffffffffu : 0u;
   if (r.wraps) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) w[e] = drop_word_far(rng.seed_lo, rng.seed_hi, r.first + col + e) ^ kAdd;
-    return;
-  }
-  if (r.phase == 0) return number_quads<N, NOT>(r.quad + col / 4, r.key, w);
-  uint32_t h[N / 4 + 1];
+    for (int u = 0; u < UNITS; ++u) {
+      uint32_t w[N];
 #pragma unroll
-  for (int i = 0; i <= N / 4; ++i) {
-    h[i] = Rng::quad_hash(r.quad + col / 4 + i, r.key);
-    if (NOT) h[i] = 0u - h[i];
-  }
-  uint32_t times[4];
+      for (int e = 0; e < N; ++e) w[e] = drop_word_far(rng.seed_lo, rng.seed_hi, r.first + col + u * step + e) ^ kAdd;
+      take(u, w);
+    }
+  } else if (r.phase == 0) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t m = (r.phase + e) & 3;
-    times[e] = m == 0 ? 1u : m == 1 ? 0x9E3779B1u : m == 2 ? 0x85EBCA77u : 0xC2B2AE3Du;
-  }
+    for (int u = 0; u < UNITS; ++u) {
+      uint32_t w[N];
+      number_quads<N, NOT>(r.quad + (col + u * step) / 4, r.key, w);
+      take(u, w);
+    }
+  } else {
+    uint32_t times[4];
 #pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = (r.phase + i % 4 >= 4 ? h[i / 4 + 1] : h[i / 4]) * times[i % 4] + kAdd;
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t m = (r.phase + e) & 3;
+      times[e] = m == 0 ? 1u : m == 1 ? 0x9E3779B1u : m == 2 ? 0x85EBCA77u : 0xC2B2AE3Du;
+    }
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      uint32_t w[N], h[N / 4 + 1];
+#pragma unroll
+      for (int i = 0; i <= N / 4; ++i) {
+        h[i] = Rng::quad_hash(r.quad + (col + u * step) / 4 + i, r.key);
+        if (NOT) h[i] = 0u - h[i];
+      }
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = (r.phase + i % 4 >= 4 ? h[i / 4 + 1] : h[i / 4]) * times[i % 4] + kAdd;
+      take(u, w);
+    }
+  }
 }
 // v / (1 - p) where kept, else 0.
 template <int N>
@@ -91,11 +107,10 @@ __device__ __forceinline__ void drop_values(const Drop& d, const uint32_t (&w)[N
     v[i] = pair_of(w[2 * i] > d.limit ? f.x : 0.0f, w[2 * i + 1] > d.limit ? f.y : 0.0f);
   }
 }
-template <int N>  // N neighbours from column `col` on
-__device__ __forceinline__ void drop_unit(const Drop& d, const DropRow& r, uint32_t col, Pair* v) {
-  uint32_t w[N];
-  number_unit<N>(d.rng, r, col, w);
-  drop_values<N>(d, w, v);
+// UNITS units of N values each, as above.
+template <int N, int UNITS>
+__device__ __forceinline__ void drop_units(const Drop& d, const DropRow& r, uint32_t col, uint32_t step, Pair* v) {
+  number_units<N, false, UNITS>(d.rng, r, col, step, [&](int u, const uint32_t (&w)[N]) { drop_values<N>(d, w, v + u * (N / 2)); });
 }
 
 }  // namespace accept

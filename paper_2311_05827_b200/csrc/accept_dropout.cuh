@@ -70,12 +70,6 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(const Dropou
   TY* y = static_cast<TY*>(a.y) + c0;
   const uint64_t first = a.drop.offset + c0;
   const DropRow row(a.drop.rng, first, UNITS * kStride, DropKey(a.drop.rng, first));
-  const auto take = [&](int i, Pair (&v)[4], const Pair (&add)[4]) {
-    if (a.drop.on) drop_unit<8>(a.drop, row, i * kStride, v);
-    if (a.residual)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = add2(v[j], add[j]);
-  };
   if (c0 + (UNITS - 1) * kStride + 8 <= a.cols) {
     Pair v[UNITS][4], add[UNITS][4];
 #pragma unroll
@@ -83,9 +77,12 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(const Dropou
     if (a.residual)
 #pragma unroll
       for (int i = 0; i < UNITS; ++i) load_eight<TY, true>(residual + i * kStride, 8, add[i]);
+    if (a.drop.on) drop_units<8, UNITS>(a.drop, row, 0, kStride, &v[0][0]);
 #pragma unroll
     for (int i = 0; i < UNITS; ++i) {
-      take(i, v[i], add[i]);
+      if (a.residual)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = add2(v[i][j], add[i][j]);
       store_eight<TY, true>(y + i * kStride, 8, v[i]);
     }
   } else {
@@ -97,7 +94,10 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(const Dropou
       Pair v[4], add[4];
       load_eight<TX, true>(x + i * kStride, n, v);
       if (a.residual) load_eight<TY, true>(residual + i * kStride, n, add);
-      take(i, v, add);
+      if (a.drop.on) drop_units<8, 1>(a.drop, row, i * kStride, 0, v);
+      if (a.residual)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = add2(v[j], add[j]);
       store_eight<TY, true>(y + i * kStride, n, v);
     }
   }
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
     if (n[i] == 0) continue;
     if (a.drop.on) {
       const uint64_t at = a.drop.offset + row[i] * a.cols + col[i];
-      drop_unit<8>(a.drop, DropRow(a.drop.rng, at, 8, DropKey(a.drop.rng, at)), 0, v[i]);
+      drop_units<8, 1>(a.drop, DropRow(a.drop.rng, at, 8, DropKey(a.drop.rng, at)), 0, 0, v[i]);
     }
     if (a.residual)
 #pragma unroll

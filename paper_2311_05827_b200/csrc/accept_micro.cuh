@@ -128,7 +128,10 @@ __global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T
   const auto draw_row = [&](int i, uint32_t (&less)[8]) {
     uint32_t w[8];
     if (ROUND == MicroRound::kQuads && together) number_quads<8, true>(quad + i * (a.cols / 4), key.key, w);
-    else number_unit<8, true>(a.rng, DropRow(a.rng, first + (uint64_t)i * a.cols, 8, key), 0, w);
+    else number_units<8, true, 1>(a.rng, DropRow(a.rng, first + (uint64_t)i * a.cols, 8, key), 0, 0, [&](int, const uint32_t (&drawn)[8]) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = drawn[j];
+    });
 #pragma unroll
     for (int j = 0; j < 8; ++j) less[j] = w[j] >> 4;
   };

@@ -55,8 +55,7 @@ __device__ __forceinline__ float rms_rstd(const RmsArgs& a, float squares, const
 template <int V, bool FULL, int OWN, int L>
 __device__ __forceinline__ void drop_row(const Drop& d, const DropRow& r, uint32_t t, Pair (&v)[OWN / 2]) {
   if constexpr (V > 2) {
-#pragma unroll
-    for (int i = 0; i < OWN / V; ++i) drop_unit<V>(d, r, column_of<V, OWN, L>(t, V * i), v + V * i / 2);
+    drop_units<V, OWN / V>(d, r, column_of<V, OWN, L>(t, 0), L * V, v);
   } else {
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) {
@@ -73,63 +72,88 @@ __device__ __forceinline__ Pair rounded(Pair v) {
   else return word_to_pair<T>(pair_to_word<T>(v));
 }
 
+// The largest magnitude of the lanes that share a block, kLanes neighbours; a NaN or an infinity comes out on top.
+template <int LANES>
+__device__ __forceinline__ float largest_of(float most, uint32_t mask) {
+  if constexpr (LANES == 32) {
+    float r;
+    asm("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(most));
+    return r;
+  }
+#pragma unroll
+  for (int d = LANES / 2; d >= 1; d >>= 1) most = max_nan(most, __shfl_xor_sync(mask, most, d));
+  return most;
+}
+
 // The row's values as 8-bit codes with a scale for each 128 columns (accept_block.cuh): a block's columns lie with kLanes lanes
-// of a warp, kUnits units of each.
+// of a warp, kUnits units of each.  The lanes' columns are the four blocks (or the one) of a word of scales.
 template <int FORMAT, int V, int OWN, int L>
 __device__ __forceinline__ void store_codes(const RmsArgs& a, uint64_t row, uint32_t t, uint32_t mask, Pair (&v)[OWN / 2]) {
-  constexpr int kUnits = 128 / (L * V) > 0 ? 128 / (L * V) : 1, kLanes = 128 / (V * kUnits);
-  static_assert(kLanes <= L && OWN / V % kUnits == 0, "a block lies within a warp");
-  uint8_t* q = a.q + row * a.ldq;
+  constexpr int kUnits = 128 / (L * V) > 0 ? 128 / (L * V) : 1, kLanes = 128 / (V * kUnits), kBlocks = OWN / V / kUnits, kPairs = kUnits * V / 2;
+  static_assert(kLanes <= L && OWN / V % kUnits == 0 && L * OWN == (L == 32 ? 512 : 128), "a block lies within a warp, a word of scales is one");
+  float most[kBlocks];
+  bool bad = false;
 #pragma unroll
-  for (int b = 0; b < OWN / V / kUnits; ++b) {
-    constexpr int kPairs = kUnits * V / 2;
-    float most = 0.0f;
+  for (int b = 0; b < kBlocks; ++b) {
+    most[b] = 0.0f;
 #pragma unroll
     for (int j = 0; j < kPairs; ++j) {
       const float2 f = split(v[b * kPairs + j]);
-      most = max3_nan(most, fabsf(f.x), fabsf(f.y));
+      most[b] = max3_nan(most[b], fabsf(f.x), fabsf(f.y));
     }
+    most[b] = largest_of<kLanes>(most[b], mask);
+    bad |= !is_finite_bits(most[b]);
+  }
+  if (__any_sync(mask, bad)) {  // rare: scales are those of the finite values, the others become NaN
+    bad = false;
 #pragma unroll
-    for (int d = kLanes / 2; d >= 1; d >>= 1) most = max_nan(most, __shfl_xor_sync(mask, most, d));
-    if (__any_sync(mask, !is_finite_bits(most))) {  // rare: the scale is that of the finite values, the others become NaN
-      bool bad = false;
-      most = 0.0f;
+    for (int b = 0; b < kBlocks; ++b) {
+      most[b] = 0.0f;
 #pragma unroll
       for (int j = 0; j < kPairs; ++j) {
         const float2 f = split(v[b * kPairs + j]);
         const bool x = is_finite_bits(f.x), y = is_finite_bits(f.y);
         bad |= !x || !y;
-        most = fmaxf(most, fmaxf(x ? fabsf(f.x) : 0.0f, y ? fabsf(f.y) : 0.0f));
+        most[b] = fmaxf(most[b], fmaxf(x ? fabsf(f.x) : 0.0f, y ? fabsf(f.y) : 0.0f));
         v[b * kPairs + j] = pair_of(x ? f.x : __uint_as_float(0x7fffffffu), y ? f.y : __uint_as_float(0x7fffffffu));
       }
-#pragma unroll
-      for (int d = kLanes / 2; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor_sync(mask, most, d));
-      if (bad) atomicOr(a.status, kDevNonFinite);
+      most[b] = largest_of<kLanes>(most[b], mask);
     }
-    const int e = scale_exponent<FORMAT>(most);
-    const Pair inverse = both(power_of_two(-e));
-    const uint32_t block = column_of<V, OWN, L>(t, b * kUnits * V) / 128;
-    if ((t & (kLanes - 1)) == 0 && block < a.blocks) store_scale(a.scale, (uint32_t)row, block, a.blocks, a.atoms, e);
+    if (bad) atomicOr(a.status, kDevNonFinite);
+  }
+  uint32_t word = L < 32 ? 0x7f7f7f00u : 0u;
+  Pair inverse[kBlocks];
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      const uint32_t c = column_of<V, OWN, L>(t, (b * kUnits + u) * V);
-      if (c >= a.ldq) continue;
-      uint32_t code[V > 2 ? V / 2 : 1];
-      if constexpr (V > 1) {
+  for (int b = 0; b < kBlocks; ++b) {
+    const int e = scale_exponent<FORMAT>(most[b]);
+    inverse[b] = both(power_of_two(-e));
+    word |= (uint32_t)(e + 127) << (kLanes == 16 ? 16 * b : 8 * b);
+  }
+  if (kLanes == 16) word |= __shfl_xor_sync(mask, word, 16) << 8;  // lane 0: blocks 0 and 2 its own, 1 and 3 of the upper lanes
+  if (t % L == 0) {
+    const uint32_t r = (uint32_t)row;
+    st_c(reinterpret_cast<uint32_t*>(a.scale + ((uint64_t)(t / L) * a.atoms + (r >> 7)) * 512 + (r & 31) * 16 + ((r >> 5) & 3) * 4), word);
+  }
+  uint8_t* q = a.q + row * a.ldq + column_of<V, OWN, L>(t, 0);
 #pragma unroll
-        for (int j = 0; j < V / 2; ++j) {
-          const float2 f = split(mul2(v[(b * kUnits + u) * V / 2 + j], inverse));
-          code[j] = encode_two<FORMAT>(f.x, f.y);
-        }
-      } else {
-        const float2 f = split(mul2(v[(b * kUnits + u) / 2], inverse));
-        code[0] = encode_two<FORMAT>((b * kUnits + u) % 2 ? f.y : f.x, 0.0f);
+  for (int u = 0; u < OWN / V; ++u) {
+    if (column_of<V, OWN, L>(t, u * V) >= a.ldq) continue;
+    uint32_t code[V > 2 ? V / 2 : 1];
+    if constexpr (V > 1) {
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) {
+        const float2 f = split(mul2(v[u * V / 2 + j], inverse[u / kUnits]));
+        code[j] = encode_two<FORMAT>(f.x, f.y);
       }
-      if constexpr (V == 8) st_c(reinterpret_cast<uint2*>(q + c), make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16));
-      else if constexpr (V == 4) st_c(reinterpret_cast<uint32_t*>(q + c), code[0] | code[1] << 16);
-      else if constexpr (V == 2) st_c(reinterpret_cast<uint16_t*>(q + c), (uint16_t)code[0]);
-      else st_c(q + c, (uint8_t)code[0]);
+    } else {
+      const float2 f = split(mul2(v[u / 2], inverse[u / kUnits]));
+      code[0] = encode_two<FORMAT>(u % 2 ? f.y : f.x, 0.0f);
     }
+    uint8_t* to = q + u * (L * V);
+    if constexpr (V == 8) st_c(reinterpret_cast<uint2*>(to), make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16));
+    else if constexpr (V == 4) st_c(reinterpret_cast<uint32_t*>(to), code[0] | code[1] << 16);
+    else if constexpr (V == 2) st_c(reinterpret_cast<uint16_t*>(to), (uint16_t)code[0]);
+    else st_c(to, (uint8_t)code[0]);
   }
 }
 
@@ -491,7 +515,7 @@ __global__ void __launch_bounds__(kWideThreads) rms_forward_wide_kernel(const Rm
       if (branch) {
         Pair b[4];
         load_eight<TY, VEC>(branch + c, n, b);
-        if (a.drop.on) drop_unit<8>(a.drop, numbers, c, b);
+        if (a.drop.on) drop_units<8, 1>(a.drop, numbers, c, 0, b);
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = rounded<TX>(add2(v[j], b[j]));
       }
@@ -592,7 +616,7 @@ __global__ void __launch_bounds__(kWideThreads) rms_backward_wide_kernel(const R
       }
       if (a.dx) store_eight<TX, VEC>(static_cast<TX*>(a.dx) + r * a.ld_x + c, n, h);
       if (a.dbranch) {
-        if (a.drop.on) drop_unit<8>(a.drop, numbers, c, h);
+        if (a.drop.on) drop_units<8, 1>(a.drop, numbers, c, 0, h);
         store_eight<TY, VEC>(static_cast<TY*>(a.dbranch) + r * a.ld_y + c, n, h);
       }
     }
