@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(const Dropou
   const TY* residual = static_cast<const TY*>(a.residual) + c0;
   TY* y = static_cast<TY*>(a.y) + c0;
   const uint64_t first = a.drop.offset + c0;
-  const DropRow row(a.drop.rng, first, UNITS * kStride, DropKey(a.drop.rng, first));
+  const DropRow row(a.drop.rng, first, DropKey(a.drop.rng, first));
   if (c0 + (UNITS - 1) * kStride + 8 <= a.cols) {
     Pair v[UNITS][4], add[UNITS][4];
 #pragma unroll
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
     if (n[i] == 0) continue;
     if (a.drop.on) {
       const uint64_t at = a.drop.offset + row[i] * a.cols + col[i];
-      drop_units<8, 1>(a.drop, DropRow(a.drop.rng, at, 8, DropKey(a.drop.rng, at)), 0, 0, v[i]);
+      drop_units<8, 1>(a.drop, DropRow(a.drop.rng, at, DropKey(a.drop.rng, at)), 0, 0, v[i]);
     }
     if (a.residual)
 #pragma unroll

@@ -123,17 +123,15 @@ __global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T
 
   const uint64_t first = a.offset + (uint64_t)r0 * a.cols + c0;
   const DropKey key(a.rng, first);
-  const uint32_t quad = (uint32_t)(first >> 2);
-  const bool together = (uint32_t)((first + 7ull * a.cols + 8) >> 34) == key.high;  // one key for all values of the thread
+  DropRow quads(a.rng, first, key);
+  if (ROUND == MicroRound::kQuads) quads.phase = 0;  // known here: the other way of counting falls away
   const auto draw_row = [&](int i, uint32_t (&less)[8]) {
-    uint32_t w[8];
-    if (ROUND == MicroRound::kQuads && together) number_quads<8, true>(quad + i * (a.cols / 4), key.key, w);
-    else number_units<8, true, 1>(a.rng, DropRow(a.rng, first + (uint64_t)i * a.cols, 8, key), 0, 0, [&](int, const uint32_t (&drawn)[8]) {
+    const auto keep = [&](int, const uint32_t (&w)[8]) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = drawn[j];
-    });
-#pragma unroll
-    for (int j = 0; j < 8; ++j) less[j] = w[j] >> 4;
+      for (int j = 0; j < 8; ++j) less[j] = w[j] >> 4;
+    };
+    if (ROUND == MicroRound::kQuads) number_units<8, true, 1>(quads, i * (a.cols & ~3u), 0, keep);
+    else number_units<8, true, 1>(DropRow(a.rng, first + (uint64_t)i * a.cols, key), 0, 0, keep);
   };
   uint32_t numbers[STOCHASTIC && kKept ? 8 : 1][8];
   if (STOCHASTIC && kKept)

@@ -52,17 +52,151 @@ __device__ __forceinline__ float rms_rstd(const RmsArgs& a, float squares, const
 }
 
 // The branch's elements after dropout: pairs as column_of deals them.
-template <int V, bool FULL, int OWN, int L>
+template <int V, int OWN, int L>
 __device__ __forceinline__ void drop_row(const Drop& d, const DropRow& r, uint32_t t, Pair (&v)[OWN / 2]) {
-  if constexpr (V > 2) {
-    drop_units<V, OWN / V>(d, r, column_of<V, OWN, L>(t, 0), L * V, v);
-  } else {
+  drop_units<V, OWN / V>(d, r, column_of<V, OWN, L>(t, 0), L * V, v);
+}
+
+// ---- rows that start anywhere (LOOSE) ----
+// The row lies in shared memory as the 16-byte pieces that hold it, and in the registers of its threads as any other; what is read
+// from there, and what is written to a row, is shifted by what the row's start is off: the same for the whole row.  So all loads
+// and stores are whole units, but for the two ends of a warp's columns.
+// (One or two values a load and store, as layer norm has it: 16384 x 4095 bf16 with a dropped branch 280 us forward.)
+
+// Words `by` bytes (a multiple of 2, the same for the whole warp) into `c`, of which there are N + M.
+template <int N, int M>
+__device__ __forceinline__ void shifted_words(const uint32_t (&c)[N + M], uint32_t by, uint32_t (&out)[N]) {
+  uint32_t w[N + M];
 #pragma unroll
-    for (int i = 0; i < OWN / 2; ++i) {
-      const float2 f = split(mul2(v[i], both(d.scale)));
-      v[i] = pair_of(r.word(d, column_of<V, OWN, L>(t, 2 * i)) > d.limit ? f.x : 0.0f, r.word(d, column_of<V, OWN, L>(t, 2 * i + 1)) > d.limit ? f.y : 0.0f);
+  for (int i = 0; i < N + M; ++i) w[i] = c[i];
+#pragma unroll
+  for (int step = M / 2; step >= 1; step /= 2)  // by / 4 is below M, a power of two
+#pragma unroll
+    for (int i = 0; i + step < N + M; ++i) w[i] = by & 4 * step ? w[i + step] : w[i];
+  const uint32_t pick = by & 2 ? 0x5432u : 0x3210u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = __byte_perm(w[i], w[i + 1], pick);
+}
+
+template <typename T, int V, int OWN, int L>
+__device__ __forceinline__ void take_loose(uint32_t src, const T* row, uint32_t t, Pair (&v)[OWN / 2]) {
+  constexpr int kUnit = V * (int)sizeof(T), kWords = kUnit / 4;  // a unit is 16 bytes, or 8
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15);
+  const uint32_t from = src + t / L * (L * OWN * (uint32_t)sizeof(T) + 16) + t % L * kUnit + (off & ~(uint32_t)(kUnit - 1));
+#pragma unroll
+  for (int i = 0; i < OWN / V; ++i) {
+    uint32_t c[2 * kWords], w[kWords];
+    if constexpr (kWords == 4) {
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]) : "r"(from + i * L * kUnit));
+      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[4]), "=r"(c[5]), "=r"(c[6]), "=r"(c[7]) : "r"(from + i * L * kUnit + 16));
+    } else {
+      asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(from + i * L * kUnit));
+      asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(c[2]), "=r"(c[3]) : "r"(from + i * L * kUnit + 8));
+    }
+    shifted_words<kWords, kWords>(c, off & (kUnit - 1), w);
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      if constexpr (sizeof(T) == 4) v[i * V / 2 + j] = pair_of(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+      else v[i * V / 2 + j] = word_to_pair<T>(w[j]);
     }
   }
+}
+
+// A unit that starts at a boundary takes its first values from the lane before, which had them at the end of its own.  The two
+// ends of the warp's columns, less than a unit each, are written value by value: the first by the first V lanes, the last by the next V
+// (where L lanes are fewer, by the first V again).
+template <typename T, int V, bool FULL, int OWN, int L>
+__device__ __forceinline__ void store_loose(T* row, uint32_t cols, uint32_t t, uint32_t mask, const Pair (&v)[OWN / 2]) {
+  constexpr int kUnit = V * (int)sizeof(T), kWords = kUnit / 4, kUnits = OWN / V;
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row) & (kUnit - 1)), back = off / (uint32_t)sizeof(T), lane = t % L;
+  const uint32_t low = t / L * (L * OWN), high = FULL ? low + L * OWN : min(low + L * OWN, cols);  // the warp's columns that exist
+  const uint32_t here = threadIdx.x & 31 & ~(uint32_t)(L - 1), lane_before = here | ((lane + L - 1) & (L - 1));
+  uint32_t mine[kUnits][kWords];
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i)
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) {
+      if constexpr (sizeof(T) == 4) mine[i][j] = __float_as_uint(j % 2 ? split(v[(i * V + j) / 2]).y : split(v[(i * V + j) / 2]).x);
+      else mine[i][j] = pair_to_word<T>(v[i * V / 2 + j]);
+    }
+  T* first = row + (int)(low + lane * V - back);
+  const auto store_unit = [&](T* p, const uint32_t (&w)[kWords]) {
+    if constexpr (kWords == 4) {
+      if (bounds_ok(p, 16, true)) __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+    } else {
+      if (bounds_ok(p, 8, true)) __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
+    }
+  };
+  const auto store_value = [&](T* p, uint32_t w, uint32_t e) {
+    if constexpr (sizeof(T) == 4) st_c(reinterpret_cast<uint32_t*>(p), w);
+    else st_c(reinterpret_cast<uint16_t*>(p), (uint16_t)(e & 1 ? w >> 16 : w));
+  };
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) {
+    uint32_t w[kWords];
+    if (off == 0) {
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) w[j] = mine[i][j];
+    } else {
+      uint32_t c[2 * kWords];
+#pragma unroll
+      for (int j = 0; j < kWords; ++j) {  // the first lane's come from the last lane's unit before this
+        c[j] = __shfl_sync(mask, i > 0 && lane == L - 1 ? mine[i > 0 ? i - 1 : 0][j] : mine[i][j], lane_before);
+        c[kWords + j] = mine[i][j];
+      }
+      shifted_words<kWords, kWords>(c, kUnit - off, w);
+    }
+    const int start = (int)(low + (i * L + lane) * V - back);
+    if ((FULL || start + V <= (int)high) && (i > 0 || lane > 0 || off == 0)) {
+      store_unit(first + i * (L * V), w);
+    } else if (!FULL && (i > 0 || lane > 0 || off == 0)) {  // the row ends inside this unit, or before it
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (start + e < (int)high) store_value(first + i * (L * V) + e, w[e * (int)sizeof(T) / 4], e);
+    }
+  }
+  if (off == 0) return;
+  // lanes 0 .. V - 1: value `lane` of the first lane's first unit; lanes V .. 2 V - 1: of the last lane's last unit
+  constexpr bool kOnce = L >= 2 * V;
+#pragma unroll
+  for (int end = 0; end < (kOnce ? 1 : 2); ++end) {
+    const bool last = kOnce ? lane >= V : end == 1;
+    uint32_t w[kWords];
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) w[j] = __shfl_sync(mask, lane == 0 && (kOnce || end == 0) ? mine[0][j] : mine[kUnits - 1][j], here | (last ? L - 1 : 0));
+    const uint32_t e = lane % V, at = e * (uint32_t)sizeof(T) / 4;
+    uint32_t word = w[0];
+#pragma unroll
+    for (int j = 1; j < kWords; ++j) word = at == (uint32_t)j ? w[j] : word;
+    const uint32_t col = last ? low + L * OWN - V + e : low + e;
+    if (lane < (kOnce ? 2 * V : V) && col < high && (last ? e >= V - back : e < V - back)) store_value(row + col, word, e);
+  }
+}
+
+// A row's copies, a row that has landed, and a row's values to memory, for rows that start on 16-byte boundaries or anywhere.
+template <typename T, int V, bool FULL, int OWN, int L, bool LOOSE>
+__device__ __forceinline__ void start_any(uint32_t dst, const T* row, uint32_t cols, uint32_t t, const Own<V, FULL, OWN, L>& own, const T* begin, const T* end) {
+  if constexpr (LOOSE) start_row<T, 2, FULL, OWN, L>(dst, row, cols, t, Own<2, FULL, OWN, L>(t, cols), begin, end);
+  else start_row<T, V, FULL, OWN, L>(dst, row, cols, t, own, begin, end);
+}
+template <typename T, int V, bool FULL, int OWN, int L, bool LOOSE>
+__device__ __forceinline__ void take_any(uint32_t src, const T* row, uint32_t t, const Own<V, FULL, OWN, L>& own, Pair (&v)[OWN / 2]) {
+  if constexpr (LOOSE) {
+    take_loose<T, V, OWN, L>(src, row, t, v);
+    if (!FULL)  // what lies behind the row's end is dropped
+#pragma unroll
+      for (int i = 0; i < OWN / 2; ++i) {
+        const float2 f = split(v[i]);
+        v[i] = pair_of(own.has(2 * i) ? f.x : 0.0f, own.has(2 * i + 1) ? f.y : 0.0f);
+      }
+  } else {
+    take_row<T, V, FULL, OWN, L>(src, row, t, own, v);
+  }
+}
+template <typename T, int V, bool FULL, int OWN, int L, bool LOOSE>
+__device__ __forceinline__ void store_any(T* row, uint32_t cols, uint32_t t, uint32_t mask, const Own<V, FULL, OWN, L>& own, const Pair (&v)[OWN / 2]) {
+  if constexpr (LOOSE) store_loose<T, V, FULL, OWN, L>(row, cols, t, mask, v);
+  else store_row<T, V, FULL, OWN, L>(row, t, own, v);
 }
 
 // v rounded to T, as it is kept.
@@ -138,22 +272,15 @@ __device__ __forceinline__ void store_codes(const RmsArgs& a, uint64_t row, uint
 #pragma unroll
   for (int u = 0; u < OWN / V; ++u) {
     if (column_of<V, OWN, L>(t, u * V) >= a.ldq) continue;
-    uint32_t code[V > 2 ? V / 2 : 1];
-    if constexpr (V > 1) {
+    uint32_t code[V / 2];
 #pragma unroll
-      for (int j = 0; j < V / 2; ++j) {
-        const float2 f = split(mul2(v[u * V / 2 + j], inverse[u / kUnits]));
-        code[j] = encode_two<FORMAT>(f.x, f.y);
-      }
-    } else {
-      const float2 f = split(mul2(v[u / 2], inverse[u / kUnits]));
-      code[0] = encode_two<FORMAT>(u % 2 ? f.y : f.x, 0.0f);
+    for (int j = 0; j < V / 2; ++j) {
+      const float2 f = split(mul2(v[u * V / 2 + j], inverse[u / kUnits]));
+      code[j] = encode_two<FORMAT>(f.x, f.y);
     }
     uint8_t* to = q + u * (L * V);
     if constexpr (V == 8) st_c(reinterpret_cast<uint2*>(to), make_uint2(code[0] | code[1] << 16, code[2] | code[3] << 16));
-    else if constexpr (V == 4) st_c(reinterpret_cast<uint32_t*>(to), code[0] | code[1] << 16);
-    else if constexpr (V == 2) st_c(reinterpret_cast<uint16_t*>(to), (uint16_t)code[0]);
-    else st_c(to, (uint8_t)code[0]);
+    else st_c(reinterpret_cast<uint32_t*>(to), code[0] | code[1] << 16);
   }
 }
 
@@ -164,7 +291,7 @@ __device__ __forceinline__ void pad_scales(const RmsArgs& a) {
     st_c(reinterpret_cast<uint32_t*>(a.scale + scale_offset((uint32_t)a.rows + i / words, i % words * 4, a.atoms)), 0x7f7f7f7fu);
 }
 
-template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES>
+template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES, bool LOOSE>
 __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L>& g, float (&slots)[3][16], uint32_t shared, uint32_t space, uint32_t space_x,
                                                  uint64_t first, uint32_t step) {
   const uint32_t t = g.t, shared_end = shared + STAGES * space;
@@ -179,8 +306,8 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) {
     if (first + (uint64_t)s * step < a.rows) {
-      start_row<TX, V, FULL, OWN, L>(shared + s * space, row + s * stride_x, a.cols, t, own, x, end_x);
-      if (branch) start_row<TY, V, FULL, OWN, L>(shared + s * space + space_x, brow + s * stride_y, a.cols, t, own, branch, end_y);
+      start_any<TX, V, FULL, OWN, L, LOOSE>(shared + s * space, row + s * stride_x, a.cols, t, own, x, end_x);
+      if (branch) start_any<TY, V, FULL, OWN, L, LOOSE>(shared + s * space + space_x, brow + s * stride_y, a.cols, t, own, branch, end_y);
     }
     copy_commit();
   }
@@ -191,22 +318,22 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
   const DropKey key(a.drop.rng, a.drop.offset + r * a.cols);
   for (;;) {
     if (r + (STAGES - 1) * (uint64_t)step < a.rows) {
-      start_row<TX, V, FULL, OWN, L>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, own, x, end_x);
-      if (branch) start_row<TY, V, FULL, OWN, L>(ahead + space_x, brow + (STAGES - 1) * stride_y, a.cols, t, own, branch, end_y);
+      start_any<TX, V, FULL, OWN, L, LOOSE>(ahead, row + (STAGES - 1) * stride_x, a.cols, t, own, x, end_x);
+      if (branch) start_any<TY, V, FULL, OWN, L, LOOSE>(ahead + space_x, brow + (STAGES - 1) * stride_y, a.cols, t, own, branch, end_y);
     }
     copy_commit();
     copy_wait<STAGES - 1>();
-    if (V <= 2) __syncwarp(g.mask);  // other lanes of the warp have copied for this one
+    if (LOOSE) __syncwarp(g.mask);  // other lanes of the warp have copied for this one
     Pair v[OWN / 2];
-    take_row<TX, V, FULL, OWN, L>(here, row, t, own, v);
+    take_any<TX, V, FULL, OWN, L, LOOSE>(here, row, t, own, v);
     if (branch) {
       Pair b[OWN / 2];
-      take_row<TY, V, FULL, OWN, L>(here + space_x, brow, t, own, b);
-      if (a.drop.on) drop_row<V, FULL, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key), t, b);
+      take_any<TY, V, FULL, OWN, L, LOOSE>(here + space_x, brow, t, own, b);
+      if (a.drop.on) drop_row<V, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, key), t, b);
 #pragma unroll
       for (int i = 0; i < OWN / 2; ++i) v[i] = rounded<TX>(add2(v[i], b[i]));
     }
-    if (a.sum) store_row<TX, V, FULL, OWN, L>(static_cast<TX*>(a.sum) + r * a.ld_x, t, own, v);
+    if (a.sum) store_any<TX, V, FULL, OWN, L, LOOSE>(static_cast<TX*>(a.sum) + r * a.ld_x, a.cols, t, g.mask, own, v);
     Pair squares[2] = {mul2(v[0], v[0]), mul2(v[1], v[1])};
 #pragma unroll
     for (int i = 2; i < OWN / 2; ++i) squares[i % 2] = fma2(v[i], v[i], squares[i % 2]);
@@ -222,7 +349,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
     turn ^= 1;
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) v[i] = mul2(mul2(v[i], both(rstd)), gamma[i]);
-    if (a.y) store_row<TY, V, FULL, OWN, L>(static_cast<TY*>(a.y) + r * a.ld_y, t, own, v);
+    if (a.y) store_any<TY, V, FULL, OWN, L, LOOSE>(static_cast<TY*>(a.y) + r * a.ld_y, a.cols, t, g.mask, own, v);
     if (a.q) {
       if (!FULL)  // zero bytes behind the row's end, whatever its rstd is
 #pragma unroll
@@ -243,12 +370,12 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
   }
 }
 
-template <typename TX, typename TY, int V, int OWN, int L, int STAGES>
+template <typename TX, typename TY, int V, int OWN, int L, int STAGES, bool LOOSE>
 __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   __shared__ __align__(16) float slots[kMostGroups][3][16];
   const Group<L> g(a.warps);
   const uint32_t groups = blockDim.x / g.threads;
-  const uint32_t space_x = row_space<TX>(V, OWN, L, a.warps), space = space_x + (a.branch ? row_space<TY>(V, OWN, L, a.warps) : 0);
+  const uint32_t space_x = row_space<TX>(LOOSE ? 2 : V, OWN, L, a.warps), space = space_x + (a.branch ? row_space<TY>(LOOSE ? 2 : V, OWN, L, a.warps) : 0);
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(rms_shared) + g.index * STAGES * space;
   const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
   const uint32_t step = gridDim.x * groups;
@@ -256,8 +383,8 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   if (!full) {
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) {
-      clear_row<TX, V, OWN, L>(shared + i * space, g.t, a.cols);
-      if (a.branch) clear_row<TY, V, OWN, L>(shared + i * space + space_x, g.t, a.cols);
+      clear_row<TX, LOOSE ? 2 : V, OWN, L>(shared + i * space, g.t, a.cols);
+      if (a.branch) clear_row<TY, LOOSE ? 2 : V, OWN, L>(shared + i * space + space_x, g.t, a.cols);
     }
   }
   if (L == 32 && a.warps > 1) {
@@ -268,13 +395,13 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   grid_dependency_handshake();
   if (a.q) pad_scales(a);
   if (first >= a.rows) return;
-  if (full) rms_forward_rows<TX, TY, V, true, OWN, L, STAGES>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
-  else rms_forward_rows<TX, TY, V, false, OWN, L, STAGES>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
+  if (full) rms_forward_rows<TX, TY, V, true, OWN, L, STAGES, LOOSE>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
+  else rms_forward_rows<TX, TY, V, false, OWN, L, STAGES, LOOSE>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
 }
 
 // Backward: dx = rstd (h - xhat mean(h xhat)) + dsum, h = dy gamma, xhat = x rstd; the sum over the rows (dgamma) is held in registers over
 // all rows of a group, added up over the block's groups and joined by rms_join_kernel.
-template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES>
+template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES, bool LOOSE>
 __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<L>& g, float (&slots)[2][16], uint32_t shared, uint32_t space, uint32_t space_x,
                                                   uint32_t space_y, uint64_t first, uint32_t step, Pair (&dgamma)[OWN / 2]) {
   const uint32_t t = g.t, shared_end = shared + STAGES * space;
@@ -287,9 +414,9 @@ __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<
   uint64_t at_x = first * a.ld_x, at_y = first * a.ld_y;
   const uint64_t stride_x = step * a.ld_x, stride_y = step * a.ld_y;
   const auto start = [&](uint32_t to, uint64_t from_x, uint64_t from_y) {
-    start_row<TX, V, FULL, OWN, L>(to, x + from_x, a.cols, t, own, x, x + last);
-    start_row<TY, V, FULL, OWN, L>(to + space_x, dy + from_y, a.cols, t, own, dy, end_y);
-    if (dsum) start_row<TX, V, FULL, OWN, L>(to + space_x + space_y, dsum + from_x, a.cols, t, own, dsum, dsum + last);
+    start_any<TX, V, FULL, OWN, L, LOOSE>(to, x + from_x, a.cols, t, own, x, x + last);
+    start_any<TY, V, FULL, OWN, L, LOOSE>(to + space_x, dy + from_y, a.cols, t, own, dy, end_y);
+    if (dsum) start_any<TX, V, FULL, OWN, L, LOOSE>(to + space_x + space_y, dsum + from_x, a.cols, t, own, dsum, dsum + last);
   };
 #pragma unroll
   for (int s = 0; s + 1 < STAGES; ++s) {
@@ -308,10 +435,10 @@ __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<
     const float rstd = rstd_next;
     if (r + step < a.rows) rstd_next = ld_c(a.rstd + r + step);
     copy_wait<STAGES - 1>();
-    if (V <= 2) __syncwarp(g.mask);  // other lanes of the warp have copied for this one
+    if (LOOSE) __syncwarp(g.mask);  // other lanes of the warp have copied for this one
     Pair xhat[OWN / 2], h[OWN / 2];
-    take_row<TX, V, FULL, OWN, L>(here, x + at_x, t, own, xhat);
-    take_row<TY, V, FULL, OWN, L>(here + space_x, dy + at_y, t, own, h);
+    take_any<TX, V, FULL, OWN, L, LOOSE>(here, x + at_x, t, own, xhat);
+    take_any<TY, V, FULL, OWN, L, LOOSE>(here + space_x, dy + at_y, t, own, h);
     Pair along[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) {
@@ -326,17 +453,17 @@ __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<
 #pragma unroll
       for (int i = 0; i < OWN / 2; ++i) h[i] = mul2(fma2(xhat[i], slope, h[i]), both(rstd));
       if (dsum) {
-        take_row<TX, V, FULL, OWN, L>(here + space_x + space_y, dsum + at_x, t, own, xhat);
+        take_any<TX, V, FULL, OWN, L, LOOSE>(here + space_x + space_y, dsum + at_x, t, own, xhat);
 #pragma unroll
         for (int i = 0; i < OWN / 2; ++i) h[i] = add2(h[i], xhat[i]);
       }
-      if (a.dx) store_row<TX, V, FULL, OWN, L>(static_cast<TX*>(a.dx) + at_x, t, own, h);
+      if (a.dx) store_any<TX, V, FULL, OWN, L, LOOSE>(static_cast<TX*>(a.dx) + at_x, a.cols, t, g.mask, own, h);
       if (a.dbranch) {
-        if (a.drop.on) drop_row<V, FULL, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key), t, h);
-        store_row<TY, V, FULL, OWN, L>(static_cast<TY*>(a.dbranch) + at_y, t, own, h);
+        if (a.drop.on) drop_row<V, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, key), t, h);
+        store_any<TY, V, FULL, OWN, L, LOOSE>(static_cast<TY*>(a.dbranch) + at_y, a.cols, t, g.mask, own, h);
       }
     }
-    if (V <= 2) __syncwarp(g.mask);  // the row has been read: its place is free
+    if (LOOSE) __syncwarp(g.mask);  // the row has been read: its place is free
     r += step;
     if (r >= a.rows) break;
     at_x += stride_x;
@@ -346,12 +473,12 @@ __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<
   }
 }
 
-template <typename TX, typename TY, int V, int OWN, int L, int STAGES>
+template <typename TX, typename TY, int V, int OWN, int L, int STAGES, bool LOOSE>
 __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsArgs a) {
   __shared__ __align__(16) float slots[kMostGroups][2][16];
   const Group<L> g(a.warps);
   const uint32_t groups = blockDim.x / g.threads, t = g.t, threads = g.threads;
-  const uint32_t space_x = row_space<TX>(V, OWN, L, a.warps), space_y = row_space<TY>(V, OWN, L, a.warps), space = space_x + space_y + (a.dsum ? space_x : 0);
+  const uint32_t space_x = row_space<TX>(LOOSE ? 2 : V, OWN, L, a.warps), space_y = row_space<TY>(LOOSE ? 2 : V, OWN, L, a.warps), space = space_x + space_y + (a.dsum ? space_x : 0);
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(rms_shared) + g.index * STAGES * space;
   const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
   const uint32_t step = gridDim.x * groups;
@@ -359,9 +486,9 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsArgs a) {
   if (!full) {
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) {
-      clear_row<TX, V, OWN, L>(shared + i * space, t, a.cols);
-      clear_row<TY, V, OWN, L>(shared + i * space + space_x, t, a.cols);
-      if (a.dsum) clear_row<TX, V, OWN, L>(shared + i * space + space_x + space_y, t, a.cols);
+      clear_row<TX, LOOSE ? 2 : V, OWN, L>(shared + i * space, t, a.cols);
+      clear_row<TY, LOOSE ? 2 : V, OWN, L>(shared + i * space + space_x, t, a.cols);
+      if (a.dsum) clear_row<TX, LOOSE ? 2 : V, OWN, L>(shared + i * space + space_x + space_y, t, a.cols);
     }
   }
   if (L == 32 && a.warps > 1) {
@@ -374,23 +501,23 @@ __global__ void __launch_bounds__(512) rms_backward_kernel(const RmsArgs a) {
 #pragma unroll
   for (int i = 0; i < OWN / 2; ++i) dgamma[i] = both(0.0f);
   if (first < a.rows) {
-    if (full) rms_backward_rows<TX, TY, V, true, OWN, L, STAGES>(a, g, slots[g.index % kMostGroups], shared, space, space_x, space_y, first, step, dgamma);
-    else rms_backward_rows<TX, TY, V, false, OWN, L, STAGES>(a, g, slots[g.index % kMostGroups], shared, space, space_x, space_y, first, step, dgamma);
+    if (full) rms_backward_rows<TX, TY, V, true, OWN, L, STAGES, LOOSE>(a, g, slots[g.index % kMostGroups], shared, space, space_x, space_y, first, step, dgamma);
+    else rms_backward_rows<TX, TY, V, false, OWN, L, STAGES, LOOSE>(a, g, slots[g.index % kMostGroups], shared, space, space_x, space_y, first, step, dgamma);
   }
   if (!a.dgamma) return;
   float* out = a.partials + (uint64_t)blockIdx.x * a.cols;
   if (groups == 1 && !a.joins) {
-    const bool quads = V > 2 && a.cols % 4 == 0;
+    const bool quads = a.cols % 4 == 0;
 #pragma unroll
-    for (int i = 0; i < OWN; i += V > 2 ? 4 : 2) {
+    for (int i = 0; i < OWN; i += 4) {
       const uint32_t c = column_of<V, OWN, L>(t, i);
-      const float2 d0 = split(dgamma[i / 2]), d1 = split(dgamma[(i / 2 + 1) % (OWN / 2)]);
+      const float2 d0 = split(dgamma[i / 2]), d1 = split(dgamma[i / 2 + 1]);
       if (quads) {
         if (c < a.cols) st_c(reinterpret_cast<float4*>(out + c), make_float4(d0.x, d0.y, d1.x, d1.y));
       } else {
         const float d[4] = {d0.x, d0.y, d1.x, d1.y};
 #pragma unroll
-        for (int j = 0; j < (V > 2 ? 4 : 2); ++j) {
+        for (int j = 0; j < 4; ++j) {
           const uint32_t cj = column_of<V, OWN, L>(t, i + j);
           if (cj < a.cols) st_c(out + cj, d[j]);
         }
@@ -509,7 +636,7 @@ __global__ void __launch_bounds__(kWideThreads) rms_forward_wide_kernel(const Rm
     const TX* row = static_cast<const TX*>(a.x) + r * a.ld_x;
     const TY* branch = a.branch ? static_cast<const TY*>(a.branch) + r * a.ld_y : nullptr;
     TX* kept = a.sum ? static_cast<TX*>(a.sum) + r * a.ld_x : nullptr;
-    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key);
+    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, key);
     const auto sum_of_eight = [&](uint32_t c, int n, Pair (&v)[4]) {
       load_eight<TX, VEC>(row + c, n, v);
       if (branch) {
@@ -602,7 +729,7 @@ __global__ void __launch_bounds__(kWideThreads) rms_backward_wide_kernel(const R
       for (int j = 0; j < 4; ++j) along = fma2(h[j], xhat[j], along);
     }
     const Pair slope = both(-rms_block_sum(sum_of(along), slots[turn]) * a.inv_cols);
-    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, a.cols, key);
+    const DropRow numbers(a.drop.rng, a.drop.offset + r * a.cols, key);
     for (uint32_t c = 8 * threadIdx.x; c < a.cols; c += 8 * kWideThreads) {
       const int n = (int)min(a.cols - c, 8u);
       Pair xhat[4], h[4];

@@ -8,12 +8,12 @@ using namespace accept;
 template <typename TX, typename TY>
 struct Backward {
   static constexpr int kStages = rms_stages_for((int)(2 * sizeof(TX) + sizeof(TY)));
-  template <int V, int L> static RmsKernel held() { return rms_backward_kernel<TX, TY, V, kRmsOwn, L, kStages>; }
+  template <int V, int L, bool LOOSE> static RmsKernel held() { return rms_backward_kernel<TX, TY, V, kRmsOwn, L, kStages, LOOSE>; }
   template <bool VEC> static RmsKernel wide() { return rms_backward_wide_kernel<TX, TY, VEC>; }
 };
 template <typename TX, typename TY>
 struct ColumnSums {  // of wide rows only
-  template <int V, int L> static RmsKernel held() { return nullptr; }
+  template <int V, int L, bool LOOSE> static RmsKernel held() { return nullptr; }
   template <bool VEC> static RmsKernel wide() { return rms_column_sums_kernel<TX, TY, VEC>; }
 };
 
@@ -41,8 +41,8 @@ extern "C" accept_status accept_rms_norm_backward(const accept_rms_norm_params* 
     return rows(d_s, p->ld_x, p->dtype_x) && rows(d_dsum, p->ld_x, p->dtype_x) && rows(d_dx, p->ld_x, p->dtype_x) && rows(d_dy, p->ld_y, p->dtype_y) &&
            rows(d_dbranch, p->ld_y, p->dtype_y);
   };
-  const RmsRows rows = all(rms_whole_rows) ? RmsRows::kWhole : all(rms_word_rows) ? RmsRows::kWords : RmsRows::kLoose;
-  const RmsShape shape = rms_shape(p, true, rms_unit(p, rows), d_dsum ? 2 : 1, 1);
+  const bool whole = all(rms_whole_rows);
+  const RmsShape shape = rms_shape(p, true, whole, d_dsum ? 2 : 1, 1);
   RmsArgs a = rms_args(p, d_gamma);
   a.x = d_s;
   a.dy = d_dy;
@@ -63,8 +63,8 @@ extern "C" accept_status accept_rms_norm_backward(const accept_rms_norm_params* 
   if (p->rows != 0) {
     // the column sums of wide rows first: dx may take the place of the sum, dbranch that of dy
     if (shape.wide && d_dgamma)
-      ACCEPT_LAUNCH(launch_overlapped(rms_kernel<ColumnSums>(p, shape, rows), dim3((a.cols + 255) / 256, a.n_partials), 256, s, a));
-    if (!shape.wide || d_dx || d_dbranch) ACCEPT_LAUNCH(launch_rms(rms_kernel<Backward>(p, shape, rows), shape, a, s));
+      ACCEPT_LAUNCH(launch_overlapped(rms_kernel<ColumnSums>(p, shape, whole), dim3((a.cols + 255) / 256, a.n_partials), 256, s, a));
+    if (!shape.wide || d_dx || d_dbranch) ACCEPT_LAUNCH(launch_rms(rms_kernel<Backward>(p, shape, whole), shape, a, s));
   }
   const bool summed = p->rows != 0 && (shape.joins || (shape.wide && a.n_partials == 1));
   if (d_dgamma && !summed)

@@ -11,7 +11,7 @@ uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 template <typename TX, typename TY>
 struct Forward {
   static constexpr int kStages = rms_stages_for((int)(sizeof(TX) + sizeof(TY)));
-  template <int V, int L> static RmsKernel held() { return rms_forward_kernel<TX, TY, V, kRmsOwn, L, kStages>; }
+  template <int V, int L, bool LOOSE> static RmsKernel held() { return rms_forward_kernel<TX, TY, V, kRmsOwn, L, kStages, LOOSE>; }
   template <bool VEC> static RmsKernel wide() { return rms_forward_wide_kernel<TX, TY, VEC>; }
 };
 
@@ -38,7 +38,7 @@ accept_status accept_rms_norm_check_params(const accept_rms_norm_params* p) {
 
 size_t accept_rms_norm_workspace_size(const accept_rms_norm_params* p) {
   if (accept_rms_norm_check_params(p) != ACCEPT_OK) return 0;
-  const RmsShape s = rms_shape(p, true, 4, 2, 1);  // the partials depend on the rows and columns alone
+  const RmsShape s = rms_shape(p, true, true, 2, 1);  // the partials depend on the rows and columns alone
   return 16 + (size_t)(rms_partials(p, s) * 4 * p->cols);
 }
 
@@ -84,9 +84,9 @@ accept_status accept_rms_norm_forward(const accept_rms_norm_params* p, const voi
   const auto all = [&](auto rows) {
     return rows(d_x, p->ld_x, p->dtype_x) && rows(d_sum, p->ld_x, p->dtype_x) && rows(d_branch, p->ld_y, p->dtype_y) && rows(d_y, p->ld_y, p->dtype_y);
   };
-  const RmsRows rows = all(rms_whole_rows) ? RmsRows::kWhole : all(rms_word_rows) ? RmsRows::kWords : RmsRows::kLoose;
-  const RmsShape shape = rms_shape(p, false, rms_unit(p, rows), 1, d_branch ? 1 : 0);
-  ACCEPT_LAUNCH(launch_rms(rms_kernel<Forward>(p, shape, rows), shape, a, s));
+  const bool whole = all(rms_whole_rows);
+  const RmsShape shape = rms_shape(p, false, whole, 1, d_branch ? 1 : 0);
+  ACCEPT_LAUNCH(launch_rms(rms_kernel<Forward>(p, shape, whole), shape, a, s));
   return ACCEPT_OK;
 }
 

@@ -8,9 +8,8 @@ namespace accept {
 constexpr unsigned kRmsSms = 148;
 
 inline size_t rms_value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
-// rows that all start on 16-byte boundaries, or on 4-byte ones
+// rows that all start on 16-byte boundaries
 inline bool rms_whole_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p, 16) && (!p || ld * rms_value_size(dtype) % 16 == 0); }
-inline bool rms_word_rows(const void* p, uint64_t ld, int32_t dtype) { return is_aligned(p, 4) && (!p || ld * rms_value_size(dtype) % 4 == 0); }
 
 // Launch shape of a pass, as layer norm's: a row is shared by as many warps as hold it at 16 columns a thread, a block holds
 // as many such groups as fit 512 threads, fewer where there are too few rows for every SM.  Rows of up to 128 columns take
@@ -28,8 +27,8 @@ inline int rms_column_bytes(const accept_rms_norm_params* p, bool backward) {
   return (int)((backward ? 2 : 1) * rms_value_size(p->dtype_x) + rms_value_size(p->dtype_y));
 }
 
-// v: columns that a thread takes side by side; streams_x, streams_y: tensors of each type that the pass reads.
-inline RmsShape rms_shape(const accept_rms_norm_params* p, bool backward, int v, int streams_x, int streams_y) {
+// whole: rows start on 16-byte boundaries; streams_x, streams_y: tensors of each type that the pass reads.
+inline RmsShape rms_shape(const accept_rms_norm_params* p, bool backward, bool whole, int streams_x, int streams_y) {
   RmsShape s{};
   s.wide = p->cols > 8192;
   if (s.wide) {
@@ -44,6 +43,7 @@ inline RmsShape rms_shape(const accept_rms_norm_params* p, bool backward, int v,
   const uint64_t over = s.joins ? 8 : kRmsSms, spread = (p->rows + over - 1) / over;
   s.groups = (unsigned)(spread < most ? (spread ? spread : 1) : most);
   if (s.lanes < 32) s.groups = (s.groups + 3) / 4 * 4;  // whole warps
+  const int v = whole ? 4 : 2;  // as row_space has it
   const auto space = [&](int32_t dtype) {
     return (size_t)(dtype == ACCEPT_DTYPE_F32 ? row_space<float>(v, kRmsOwn, s.lanes, s.warps) : row_space<uint16_t>(v, kRmsOwn, s.lanes, s.warps));
   };
@@ -62,40 +62,32 @@ inline uint64_t rms_partials(const accept_rms_norm_params* p, const RmsShape& s)
   return slabs < 32 ? slabs : 32;
 }
 
-// How rows lie: all tensors' on 16-byte boundaries, or the 16-bit tensors' on 4-byte boundaries, or neither.
-enum class RmsRows { kWhole, kWords, kLoose };
-inline int rms_unit(const accept_rms_norm_params* p, RmsRows rows) {
-  if (rows != RmsRows::kWhole) return rows == RmsRows::kWords ? 2 : 1;
-  return p->dtype_x == ACCEPT_DTYPE_F32 || p->dtype_y == ACCEPT_DTYPE_F32 ? 4 : 8;
-}
-
 using RmsKernel = void (*)(const RmsArgs);
 
-// The kernel of the pass that Pass<TX, TY> has for these types, rows and widths.
+// The kernel of the pass that Pass<TX, TY> has for these types, rows and widths.  A thread takes eight columns side by side, four
+// where a tensor is fp32 (16 bytes at most).
 template <template <typename, typename> class Pass, typename TX, typename TY>
-RmsKernel rms_kernel_of(const RmsShape& s, RmsRows rows) {
+RmsKernel rms_kernel_of(const RmsShape& s, bool whole) {
   using P = Pass<TX, TY>;
-  if (s.wide) return rows == RmsRows::kWhole ? P::template wide<true>() : P::template wide<false>();
   constexpr int kUnit = sizeof(TX) == 2 && sizeof(TY) == 2 ? 8 : 4;
-  if (rows == RmsRows::kWhole) return s.lanes == 32 ? P::template held<kUnit, 32>() : P::template held<kUnit, 8>();
-  if (rows == RmsRows::kWords) return s.lanes == 32 ? P::template held<2, 32>() : P::template held<2, 8>();
-  if constexpr (sizeof(TX) + sizeof(TY) < 8) return s.lanes == 32 ? P::template held<1, 32>() : P::template held<1, 8>();
-  else return nullptr;  // fp32 values start on 4-byte boundaries
+  if (s.wide) return whole ? P::template wide<true>() : P::template wide<false>();
+  if (whole) return s.lanes == 32 ? P::template held<kUnit, 32, false>() : P::template held<kUnit, 8, false>();
+  return s.lanes == 32 ? P::template held<kUnit, 32, true>() : P::template held<kUnit, 8, true>();
 }
 template <template <typename, typename> class Pass, typename TX>
-RmsKernel rms_kernel_y(const accept_rms_norm_params* p, const RmsShape& s, RmsRows rows) {
+RmsKernel rms_kernel_y(const accept_rms_norm_params* p, const RmsShape& s, bool whole) {
   switch (p->dtype_y) {
-    case ACCEPT_DTYPE_F32: return rms_kernel_of<Pass, TX, float>(s, rows);
-    case ACCEPT_DTYPE_BF16: return rms_kernel_of<Pass, TX, __nv_bfloat16>(s, rows);
-    default: return rms_kernel_of<Pass, TX, __half>(s, rows);
+    case ACCEPT_DTYPE_F32: return rms_kernel_of<Pass, TX, float>(s, whole);
+    case ACCEPT_DTYPE_BF16: return rms_kernel_of<Pass, TX, __nv_bfloat16>(s, whole);
+    default: return rms_kernel_of<Pass, TX, __half>(s, whole);
   }
 }
 template <template <typename, typename> class Pass>
-RmsKernel rms_kernel(const accept_rms_norm_params* p, const RmsShape& s, RmsRows rows) {
+RmsKernel rms_kernel(const accept_rms_norm_params* p, const RmsShape& s, bool whole) {
   switch (p->dtype_x) {
-    case ACCEPT_DTYPE_F32: return rms_kernel_y<Pass, float>(p, s, rows);
-    case ACCEPT_DTYPE_BF16: return rms_kernel_y<Pass, __nv_bfloat16>(p, s, rows);
-    default: return rms_kernel_y<Pass, __half>(p, s, rows);
+    case ACCEPT_DTYPE_F32: return rms_kernel_y<Pass, float>(p, s, whole);
+    case ACCEPT_DTYPE_BF16: return rms_kernel_y<Pass, __nv_bfloat16>(p, s, whole);
+    default: return rms_kernel_y<Pass, __half>(p, s, whole);
   }
 }
 
