@@ -2,6 +2,7 @@
 // out from the counters.
 #pragma once
 #include "accept_drop.cuh"
+#include "accept_shift.cuh"
 
 namespace accept {
 
@@ -10,8 +11,8 @@ struct DropoutArgs {
   const void* residual;  // may be null
   void* y;
   uint64_t rows, cols, ld_x, ld_y;
-  uint64_t per_row, units;  // units of eight neighbours
   Drop drop;
+  int log_units;  // see dropout_kernel
 };
 
 // Eight neighbours at p, of which the first n exist.
@@ -103,35 +104,87 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(const Dropou
   }
 }
 
-// Other matrices: the units of all rows in turn, a division for each.
-template <typename TX, typename TY, bool VEC, int UNITS>
+// Other matrices: a block takes 2^log_units units of eight neighbours of ROWS times as many rows as that leaves threads for.  Units
+// start on y's 16-byte boundaries; what is read there is shifted, and the ends of a row leave value by value.
+template <typename TX, typename TY, int ROWS>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs a) {
   grid_dependency_handshake();
-  const uint64_t first = (uint64_t)blockIdx.x * (UNITS * kDropThreads) + threadIdx.x;
-  Pair v[UNITS][4], add[UNITS][4];
-  uint64_t row[UNITS], col[UNITS];
-  int n[UNITS];
+  constexpr uint32_t kEach = 16 / (uint32_t)sizeof(TY);
+  const uint32_t rows_at_once = kDropThreads >> a.log_units;
+  const uint64_t unit = ((uint64_t)blockIdx.x << a.log_units) + (threadIdx.x & ((1u << a.log_units) - 1));
+  const uint64_t groups = (a.rows + rows_at_once * ROWS - 1) / (rows_at_once * ROWS);
+  const DropKey key(a.drop.rng, a.drop.offset + blockIdx.y * (uint64_t)(rows_at_once * ROWS) * a.cols);
+  for (uint64_t group = blockIdx.y; group < groups; group += gridDim.y) {
+    const uint64_t r0 = group * (rows_at_once * ROWS) + (threadIdx.x >> a.log_units);
+    Pair v[ROWS][4], add[ROWS][4];
+    int64_t col[ROWS];
+    int lo[ROWS], hi[ROWS];
+    const TX* x[ROWS];
+    const TY* residual[ROWS];
+    // all eight exist and the row is not the first or the last, beside which nothing may be read (told by the columns too, the test
+    // itself costs more than those rows: 16384 x 4095 bf16 with gaps 103 -> 128 us)
+    bool inner = true;
 #pragma unroll
-  for (int i = 0; i < UNITS; ++i) {
-    const uint64_t u = first + i * kDropThreads;
-    row[i] = a.units <= 0xffffffffu ? (uint32_t)u / (uint32_t)a.per_row : u / a.per_row;
-    col[i] = (u - row[i] * a.per_row) * 8;
-    n[i] = u < a.units ? (int)min(a.cols - col[i], (uint64_t)8) : 0;
-    if (n[i] == 0) continue;
-    load_eight<TX, VEC>(static_cast<const TX*>(a.x) + row[i] * a.ld_x + col[i], n[i], v[i]);
-    if (a.residual) load_eight<TY, VEC>(static_cast<const TY*>(a.residual) + row[i] * a.ld_y + col[i], n[i], add[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < UNITS; ++i) {
-    if (n[i] == 0) continue;
-    if (a.drop.on) {
-      const uint64_t at = a.drop.offset + row[i] * a.cols + col[i];
-      drop_units<8, 1>(a.drop, DropRow(a.drop.rng, at, DropKey(a.drop.rng, at)), 0, 0, v[i]);
+    for (int i = 0; i < ROWS; ++i) {
+      const uint64_t r = r0 + i * rows_at_once;
+      const uint32_t before = (uint32_t)((reinterpret_cast<uintptr_t>(a.y) / sizeof(TY) + r * a.ld_y) % kEach);  // values between the boundary and the row
+      col[i] = (int64_t)(unit * 8) - before;
+      lo[i] = col[i] < 0 ? (int)-col[i] : 0;
+      hi[i] = r < a.rows ? (int)min(max((int64_t)a.cols - col[i], (int64_t)0), (int64_t)8) : 0;
+      x[i] = static_cast<const TX*>(a.x) + (int64_t)(r * a.ld_x) + col[i];
+      residual[i] = static_cast<const TY*>(a.residual) + (int64_t)(r * a.ld_y) + col[i];
+      inner = inner && lo[i] == 0 && hi[i] == 8 && r > 0 && r + 1 < a.rows;
     }
-    if (a.residual)
+    if (inner) {
+      RawEight<TX> raw_x[ROWS];
+      RawEight<TY> raw_r[ROWS];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[i][j] = add2(v[i][j], add[i][j]);
-    store_eight<TY, VEC>(static_cast<TY*>(a.y) + row[i] * a.ld_y + col[i], n[i], v[i]);
+      for (int i = 0; i < ROWS; ++i) {
+        load_raw<TX>(x[i], raw_x[i]);
+        if (a.residual) load_raw<TY>(residual[i], raw_r[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        uint32_t w[2 * sizeof(TX)], u[2 * sizeof(TY)];
+        words_of<TX>(raw_x[i], x[i], w);
+        pairs_of<TX>(w, v[i]);
+        if (a.residual) {
+          words_of<TY>(raw_r[i], residual[i], u);
+          pairs_of<TY>(u, add[i]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        uint32_t w[2 * sizeof(TX)], u[2 * sizeof(TY)];
+        load_some<TX>(x[i], lo[i], hi[i], w);
+        pairs_of<TX>(w, v[i]);
+        if (a.residual) {
+          load_some<TY>(residual[i], lo[i], hi[i], u);
+          pairs_of<TY>(u, add[i]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+      if (hi[i] <= lo[i]) continue;
+      const uint64_t r = r0 + i * rows_at_once;
+      // (counters before the row's first are drawn and dropped where it starts inside the unit)
+      if (a.drop.on) drop_units<8, 1>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols + (uint64_t)col[i], key), 0, 0, v[i]);
+      if (a.residual)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = add2(v[i][j], add[i][j]);
+      TY* y = static_cast<TY*>(a.y) + (int64_t)(r * a.ld_y) + col[i];
+      if (lo[i] == 0 && hi[i] == 8) {
+        store_eight<TY, true>(y, 8, v[i]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 f = split(v[i][e / 2]);
+          if (e >= lo[i] && e < hi[i]) st_c(y + e, from_float<TY>(e % 2 ? f.y : f.x));
+        }
+      }
+    }
   }
 }
 

@@ -96,11 +96,24 @@ __global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T
   {
     const T* p = static_cast<const T*>(a.x) + (uint64_t)r0 * a.ld + c0;
     const int n = c0 < a.cols ? (int)min(a.cols - c0, 8u) : 0;
+    if (!WHOLE && sizeof(T) == 2 && n == 8 && (r0 > 0 || c0 > 0) && (r0 + 8 < a.rows || (r0 + 8 == a.rows && c0 + 8 < a.cols))) {
+      RawEight<T> raw[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const bool there = r0 + i < a.rows;
-      hold_row(h, i, p, WHOLE && there && n == 8, there ? n : 0);
-      p += a.ld;
+      for (int i = 0; i < 8; ++i) load_raw<T>(p + i * a.ld, raw[i]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        uint32_t w[2 * sizeof(T)];
+        words_of<T>(raw[i], p + i * a.ld, w);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h.w[i][j] = w[j];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool there = r0 + i < a.rows;
+        hold_row(h, i, p, WHOLE && there && n == 8, there ? n : 0);
+        p += a.ld;
+      }
     }
   }
   float row_most[8], col_most[8];

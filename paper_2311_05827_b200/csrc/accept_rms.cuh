@@ -8,6 +8,7 @@
 #include "accept_drop.cuh"
 #include "accept_dropout.cuh"
 #include "accept_rows.cuh"
+#include "accept_shift.cuh"
 
 namespace accept {
 
@@ -63,21 +64,6 @@ __device__ __forceinline__ void drop_row(const Drop& d, const DropRow& r, uint32
 // and stores are whole units, but for the two ends of a warp's columns.
 // (One or two values a load and store, as layer norm has it: 16384 x 4095 bf16 with a dropped branch 280 us forward.)
 
-// Words `by` bytes (a multiple of 2, the same for the whole warp) into `c`, of which there are N + M.
-template <int N, int M>
-__device__ __forceinline__ void shifted_words(const uint32_t (&c)[N + M], uint32_t by, uint32_t (&out)[N]) {
-  uint32_t w[N + M];
-#pragma unroll
-  for (int i = 0; i < N + M; ++i) w[i] = c[i];
-#pragma unroll
-  for (int step = M / 2; step >= 1; step /= 2)  // by / 4 is below M, a power of two
-#pragma unroll
-    for (int i = 0; i + step < N + M; ++i) w[i] = by & 4 * step ? w[i + step] : w[i];
-  const uint32_t pick = by & 2 ? 0x5432u : 0x3210u;
-#pragma unroll
-  for (int i = 0; i < N; ++i) out[i] = __byte_perm(w[i], w[i + 1], pick);
-}
-
 template <typename T, int V, int OWN, int L>
 __device__ __forceinline__ void take_loose(uint32_t src, const T* row, uint32_t t, Pair (&v)[OWN / 2]) {
   constexpr int kUnit = V * (int)sizeof(T), kWords = kUnit / 4;  // a unit is 16 bytes, or 8
@@ -102,15 +88,15 @@ __device__ __forceinline__ void take_loose(uint32_t src, const T* row, uint32_t 
   }
 }
 
-// A unit that starts at a boundary takes its first values from the lane before, which had them at the end of its own.  The two
-// ends of the warp's columns, less than a unit each, are written value by value: the first by the first V lanes, the last by the next V
-// (where L lanes are fewer, by the first V again).
+// To a row by way of `place`, the warp's part of a row of this type in shared memory that has been read: laid down as the threads hold
+// them, fetched again as units that start on the row's boundaries.  The ends of the warp's columns, less than a unit each, leave value
+// by value, the lower one from the first V lanes, the upper one from the next.
 template <typename T, int V, bool FULL, int OWN, int L>
-__device__ __forceinline__ void store_loose(T* row, uint32_t cols, uint32_t t, uint32_t mask, const Pair (&v)[OWN / 2]) {
+__device__ __forceinline__ void store_loose(T* row, uint32_t place, uint32_t cols, uint32_t t, uint32_t mask, const Pair (&v)[OWN / 2]) {
   constexpr int kUnit = V * (int)sizeof(T), kWords = kUnit / 4, kUnits = OWN / V;
-  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row) & (kUnit - 1)), back = off / (uint32_t)sizeof(T), lane = t % L;
-  const uint32_t low = t / L * (L * OWN), high = FULL ? low + L * OWN : min(low + L * OWN, cols);  // the warp's columns that exist
-  const uint32_t here = threadIdx.x & 31 & ~(uint32_t)(L - 1), lane_before = here | ((lane + L - 1) & (L - 1));
+  const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(row) & (kUnit - 1)), lane = t % L;
+  const uint32_t low = t / L * (L * OWN), have = FULL ? L * OWN : min((uint32_t)(L * OWN), cols - min(low, cols));  // of the warp's columns
+  place += t / L * (L * OWN * (uint32_t)sizeof(T) + 16);
   uint32_t mine[kUnits][kWords];
 #pragma unroll
   for (int i = 0; i < kUnits; ++i)
@@ -119,57 +105,56 @@ __device__ __forceinline__ void store_loose(T* row, uint32_t cols, uint32_t t, u
       if constexpr (sizeof(T) == 4) mine[i][j] = __float_as_uint(j % 2 ? split(v[(i * V + j) / 2]).y : split(v[(i * V + j) / 2]).x);
       else mine[i][j] = pair_to_word<T>(v[i * V / 2 + j]);
     }
-  T* first = row + (int)(low + lane * V - back);
-  const auto store_unit = [&](T* p, const uint32_t (&w)[kWords]) {
-    if constexpr (kWords == 4) {
-      if (bounds_ok(p, 16, true)) __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
-    } else {
-      if (bounds_ok(p, 8, true)) __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
-    }
-  };
-  const auto store_value = [&](T* p, uint32_t w, uint32_t e) {
-    if constexpr (sizeof(T) == 4) st_c(reinterpret_cast<uint32_t*>(p), w);
-    else st_c(reinterpret_cast<uint16_t*>(p), (uint16_t)(e & 1 ? w >> 16 : w));
-  };
+  const uint32_t own_place = place + lane * kUnit;
+  __syncwarp(mask);  // all lanes have read what lay there
 #pragma unroll
   for (int i = 0; i < kUnits; ++i) {
-    uint32_t w[kWords];
-    if (off == 0) {
+    if constexpr (kWords == 4) asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(own_place + i * L * kUnit), "r"(mine[i][0]), "r"(mine[i][1]), "r"(mine[i][2]), "r"(mine[i][3]) : "memory");
+    else asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(own_place + i * L * kUnit), "r"(mine[i][0]), "r"(mine[i][1]) : "memory");
+  }
+  __syncwarp(mask);
+  T* to = row + low;
+  const uint32_t ahead = (kUnit - off) & (kUnit - 1);  // bytes before the first boundary
+  const uint32_t bytes = have * (uint32_t)sizeof(T), inner = bytes > ahead ? (bytes - ahead) / kUnit : 0;  // units between the boundaries
 #pragma unroll
-      for (int j = 0; j < kWords; ++j) w[j] = mine[i][j];
-    } else {
-      uint32_t c[2 * kWords];
-#pragma unroll
-      for (int j = 0; j < kWords; ++j) {  // the first lane's come from the last lane's unit before this
-        c[j] = __shfl_sync(mask, i > 0 && lane == L - 1 ? mine[i > 0 ? i - 1 : 0][j] : mine[i][j], lane_before);
-        c[kWords + j] = mine[i][j];
+  for (int i = 0; i < kUnits; ++i) {
+    if (lane + i * L < inner) {
+      uint32_t c[2 * kWords], w[kWords];
+      const uint32_t from = own_place + i * L * kUnit;  // and the unit behind it: the space of a warp is 16 bytes longer
+      if constexpr (kWords == 4) {
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]) : "r"(from) : "memory");
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(c[4]), "=r"(c[5]), "=r"(c[6]), "=r"(c[7]) : "r"(from + 16) : "memory");
+      } else {
+        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(c[0]), "=r"(c[1]) : "r"(from) : "memory");
+        asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(c[2]), "=r"(c[3]) : "r"(from + 8) : "memory");
       }
-      shifted_words<kWords, kWords>(c, kUnit - off, w);
-    }
-    const int start = (int)(low + (i * L + lane) * V - back);
-    if ((FULL || start + V <= (int)high) && (i > 0 || lane > 0 || off == 0)) {
-      store_unit(first + i * (L * V), w);
-    } else if (!FULL && (i > 0 || lane > 0 || off == 0)) {  // the row ends inside this unit, or before it
-#pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (start + e < (int)high) store_value(first + i * (L * V) + e, w[e * (int)sizeof(T) / 4], e);
+      shifted_words<kWords, kWords>(c, ahead, w);
+      uint8_t* p = reinterpret_cast<uint8_t*>(to) + ahead + (lane + i * L) * kUnit;
+      if constexpr (kWords == 4) {
+        if (bounds_ok(p, 16, true)) __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
+      } else {
+        if (bounds_ok(p, 8, true)) __stcs(reinterpret_cast<uint2*>(p), make_uint2(w[0], w[1]));
+      }
     }
   }
-  if (off == 0) return;
-  // lanes 0 .. V - 1: value `lane` of the first lane's first unit; lanes V .. 2 V - 1: of the last lane's last unit
+  // below the first boundary (or the end, where that comes first), and behind the last one
   constexpr bool kOnce = L >= 2 * V;
+  const uint32_t head = min(ahead / (uint32_t)sizeof(T), have), tail = bytes > ahead ? (ahead + inner * kUnit) / (uint32_t)sizeof(T) : have;
 #pragma unroll
   for (int end = 0; end < (kOnce ? 1 : 2); ++end) {
     const bool last = kOnce ? lane >= V : end == 1;
-    uint32_t w[kWords];
-#pragma unroll
-    for (int j = 0; j < kWords; ++j) w[j] = __shfl_sync(mask, lane == 0 && (kOnce || end == 0) ? mine[0][j] : mine[kUnits - 1][j], here | (last ? L - 1 : 0));
-    const uint32_t e = lane % V, at = e * (uint32_t)sizeof(T) / 4;
-    uint32_t word = w[0];
-#pragma unroll
-    for (int j = 1; j < kWords; ++j) word = at == (uint32_t)j ? w[j] : word;
-    const uint32_t col = last ? low + L * OWN - V + e : low + e;
-    if (lane < (kOnce ? 2 * V : V) && col < high && (last ? e >= V - back : e < V - back)) store_value(row + col, word, e);
+    const uint32_t c = (last ? tail : 0) + lane % V;
+    if (lane < (kOnce ? 2 * V : V) && c < (last ? have : head)) {
+      if constexpr (sizeof(T) == 4) {
+        uint32_t w;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(place + 4 * c) : "memory");
+        st_c(reinterpret_cast<uint32_t*>(to + c), w);
+      } else {
+        uint16_t w;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(place + 2 * c) : "memory");
+        st_c(reinterpret_cast<uint16_t*>(to + c), w);
+      }
+    }
   }
 }
 
@@ -185,17 +170,21 @@ __device__ __forceinline__ void take_any(uint32_t src, const T* row, uint32_t t,
     take_loose<T, V, OWN, L>(src, row, t, v);
     if (!FULL)  // what lies behind the row's end is dropped
 #pragma unroll
-      for (int i = 0; i < OWN / 2; ++i) {
-        const float2 f = split(v[i]);
-        v[i] = pair_of(own.has(2 * i) ? f.x : 0.0f, own.has(2 * i + 1) ? f.y : 0.0f);
+      for (int i = 0; i < OWN / V; ++i) {
+        if (own.of(i) == V) continue;
+#pragma unroll
+        for (int j = i * V / 2; j < (i + 1) * V / 2; ++j) {
+          const float2 f = split(v[j]);
+          v[j] = pair_of(own.has(2 * j) ? f.x : 0.0f, own.has(2 * j + 1) ? f.y : 0.0f);
+        }
       }
   } else {
     take_row<T, V, FULL, OWN, L>(src, row, t, own, v);
   }
 }
 template <typename T, int V, bool FULL, int OWN, int L, bool LOOSE>
-__device__ __forceinline__ void store_any(T* row, uint32_t cols, uint32_t t, uint32_t mask, const Own<V, FULL, OWN, L>& own, const Pair (&v)[OWN / 2]) {
-  if constexpr (LOOSE) store_loose<T, V, FULL, OWN, L>(row, cols, t, mask, v);
+__device__ __forceinline__ void store_any(T* row, uint32_t place, uint32_t cols, uint32_t t, uint32_t mask, const Own<V, FULL, OWN, L>& own, const Pair (&v)[OWN / 2]) {
+  if constexpr (LOOSE) store_loose<T, V, FULL, OWN, L>(row, place, cols, t, mask, v);
   else store_row<T, V, FULL, OWN, L>(row, t, own, v);
 }
 
@@ -333,7 +322,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
 #pragma unroll
       for (int i = 0; i < OWN / 2; ++i) v[i] = rounded<TX>(add2(v[i], b[i]));
     }
-    if (a.sum) store_any<TX, V, FULL, OWN, L, LOOSE>(static_cast<TX*>(a.sum) + r * a.ld_x, a.cols, t, g.mask, own, v);
+    if (a.sum) store_any<TX, V, FULL, OWN, L, LOOSE>(static_cast<TX*>(a.sum) + r * a.ld_x, here, a.cols, t, g.mask, own, v);
     Pair squares[2] = {mul2(v[0], v[0]), mul2(v[1], v[1])};
 #pragma unroll
     for (int i = 2; i < OWN / 2; ++i) squares[i % 2] = fma2(v[i], v[i], squares[i % 2]);
@@ -349,7 +338,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
     turn ^= 1;
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) v[i] = mul2(mul2(v[i], both(rstd)), gamma[i]);
-    if (a.y) store_any<TY, V, FULL, OWN, L, LOOSE>(static_cast<TY*>(a.y) + r * a.ld_y, a.cols, t, g.mask, own, v);
+    if (a.y) store_any<TY, V, FULL, OWN, L, LOOSE>(static_cast<TY*>(a.y) + r * a.ld_y, here + space_x, a.cols, t, g.mask, own, v);
     if (a.q) {
       if (!FULL)  // zero bytes behind the row's end, whatever its rstd is
 #pragma unroll
@@ -361,6 +350,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
       else store_codes<kE5m2, V, OWN, L>(a, r, t, g.mask, v);
     }
     if (a.rstd_out && t == 0) st_c(a.rstd_out + r, rstd);
+    if (LOOSE) __syncwarp(g.mask);  // the row's place, through which it left, is free
     r += step;
     if (r >= a.rows) break;
     row += stride_x;
@@ -375,7 +365,7 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   __shared__ __align__(16) float slots[kMostGroups][3][16];
   const Group<L> g(a.warps);
   const uint32_t groups = blockDim.x / g.threads;
-  const uint32_t space_x = row_space<TX>(LOOSE ? 2 : V, OWN, L, a.warps), space = space_x + (a.branch ? row_space<TY>(LOOSE ? 2 : V, OWN, L, a.warps) : 0);
+  const uint32_t space_x = row_space<TX>(LOOSE ? 2 : V, OWN, L, a.warps), space = space_x + (a.branch || LOOSE ? row_space<TY>(LOOSE ? 2 : V, OWN, L, a.warps) : 0);
   const uint32_t shared = (uint32_t)__cvta_generic_to_shared(rms_shared) + g.index * STAGES * space;
   const uint64_t first = (uint64_t)blockIdx.x * groups + g.index;
   const uint32_t step = gridDim.x * groups;
@@ -457,10 +447,10 @@ __device__ __forceinline__ void rms_backward_rows(const RmsArgs& a, const Group<
 #pragma unroll
         for (int i = 0; i < OWN / 2; ++i) h[i] = add2(h[i], xhat[i]);
       }
-      if (a.dx) store_any<TX, V, FULL, OWN, L, LOOSE>(static_cast<TX*>(a.dx) + at_x, a.cols, t, g.mask, own, h);
+      if (a.dx) store_any<TX, V, FULL, OWN, L, LOOSE>(static_cast<TX*>(a.dx) + at_x, here, a.cols, t, g.mask, own, h);
       if (a.dbranch) {
         if (a.drop.on) drop_row<V, OWN, L>(a.drop, DropRow(a.drop.rng, a.drop.offset + r * a.cols, key), t, h);
-        store_any<TY, V, FULL, OWN, L, LOOSE>(static_cast<TY*>(a.dbranch) + at_y, a.cols, t, g.mask, own, h);
+        store_any<TY, V, FULL, OWN, L, LOOSE>(static_cast<TY*>(a.dbranch) + at_y, here + space_x, a.cols, t, g.mask, own, h);
       }
     }
     if (LOOSE) __syncwarp(g.mask);  // the row has been read: its place is free
@@ -774,8 +764,10 @@ __global__ void __launch_bounds__(256) rms_column_sums_kernel(const RmsArgs a) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) u[j][k] = v[j][k] = both(0.0f);
         if (row < a.rows) {
-          load_eight<TY, VEC>(static_cast<const TY*>(a.dy) + row * a.ld_y + c, n, u[j]);
-          load_eight<TX, VEC>(static_cast<const TX*>(a.x) + row * a.ld_x + c, n, v[j]);
+          const TY* drow = static_cast<const TY*>(a.dy) + row * a.ld_y;
+          const TX* xrow = static_cast<const TX*>(a.x) + row * a.ld_x;
+          load_eight<TY, VEC>(drow + c, n, u[j]);
+          load_eight<TX, VEC>(xrow + c, n, v[j]);
           rstd[j] = ld_c(a.rstd + row);
         }
       }

@@ -85,7 +85,7 @@ accept_status accept_rms_norm_forward(const accept_rms_norm_params* p, const voi
     return rows(d_x, p->ld_x, p->dtype_x) && rows(d_sum, p->ld_x, p->dtype_x) && rows(d_branch, p->ld_y, p->dtype_y) && rows(d_y, p->ld_y, p->dtype_y);
   };
   const bool whole = all(rms_whole_rows);
-  const RmsShape shape = rms_shape(p, false, whole, 1, d_branch ? 1 : 0);
+  const RmsShape shape = rms_shape(p, false, whole, 1, d_branch || !whole ? 1 : 0);
   ACCEPT_LAUNCH(launch_rms(rms_kernel<Forward>(p, shape, whole), shape, a, s));
   return ACCEPT_OK;
 }
