@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, fields
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libaccept.so")
@@ -195,8 +195,15 @@ class MatmulParams:
         return self._c
 
 
+class _Held:
+    """Parameters that hold their C struct and a reference to it: copies and pickles are made of the fields alone."""
+
+    def __reduce__(self):
+        return type(self), tuple(getattr(self, f.name) for f in fields(self))
+
+
 @dataclass(frozen=True)
-class DropoutParams:
+class DropoutParams(_Held):
     """Dropout of a rows x cols matrix at rate p; ld_x / ld_y 0: rows are cols values apart."""
     rows: int
     cols: int
@@ -211,13 +218,14 @@ class DropoutParams:
     def __post_init__(self):
         object.__setattr__(self, "_c", CDropoutParams(self.rows, self.cols, self.ld_x or self.cols, self.ld_y or self.cols, self.seed & (2**64 - 1),
                                                       self.rng_offset & (2**64 - 1), self.p, self.dtype_x, self.dtype_y, 0))
+        object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
     def c(self) -> CDropoutParams:
         return self._c
 
 
 @dataclass(frozen=True)
-class RmsNormParams:
+class RmsNormParams(_Held):
     """Root-mean-square norm over the rows of a rows x cols stream (dtype_x) and its branch (dtype_y), dropped at rate p; ld_x / ld_y 0:
     rows are cols values apart."""
     rows: int
@@ -237,13 +245,14 @@ class RmsNormParams:
         object.__setattr__(self, "_c", CRmsNormParams(self.rows, self.cols, self.ld_x or self.cols, self.ld_y or self.cols, self.seed & (2**64 - 1),
                                                       self.rng_offset & (2**64 - 1), self.eps, self.p, self.dtype_x, self.dtype_y, self.dtype_w,
                                                       self.format))
+        object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
     def c(self) -> CRmsNormParams:
         return self._c
 
 
 @dataclass(frozen=True)
-class MicroParams:
+class MicroParams(_Held):
     """Quantisation of a rows x cols matrix to 4 bits in blocks of 32; ld 0: rows are cols values apart."""
     rows: int
     cols: int
@@ -257,13 +266,14 @@ class MicroParams:
     def __post_init__(self):
         object.__setattr__(self, "_c", CMicroParams(self.rows, self.cols, self.ld or self.cols, self.seed & (2**64 - 1), self.rng_offset & (2**64 - 1),
                                                   self.dtype, self.round, self.block, 0))
+        object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
     def c(self) -> CMicroParams:
         return self._c
 
 
 @dataclass(frozen=True)
-class MicroMatmulParams:
+class MicroMatmulParams(_Held):
     """d (m x n) = a (m x k) b (n x k)^T of 4-bit operands; ldd 0: rows of d are n values apart."""
     m: int
     n: int
@@ -274,6 +284,7 @@ class MicroMatmulParams:
 
     def __post_init__(self):
         object.__setattr__(self, "_c", CMicroMatmulParams(self.m, self.n, self.k, self.ldd or self.n, self.dtype_d, int(self.accumulate)))
+        object.__setattr__(self, "_ref", ctypes.byref(self._c))
 
     def c(self) -> CMicroMatmulParams:
         return self._c
@@ -595,80 +606,101 @@ def accept_block_matmul(p: MatmulParams, d_a, d_a_scale, d_b, d_b_scale, d_bias,
 
 
 # ---- operators of a residual stage: dropout, root-mean-square norm, the linear layer in 4 bits ------
+#
+# Small calls are bound by the host, so these keep to one Python frame: parameters hold a reference to their struct, pointers are
+# asked for in place.
 
 def accept_dropout_check_params(p: DropoutParams) -> int:
-    return int(lib().accept_dropout_check_params(ctypes.byref(p.c())))
+    return int(lib().accept_dropout_check_params(p._ref))
 
 
 def accept_dropout(p: DropoutParams, d_x, d_residual, d_y, stream=None) -> None:
     """d_residual may be None.  The backward pass is the same call with dy in the place of x and no residual."""
-    _check(lib().accept_dropout(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_residual), d_y.data_ptr(), _stream_handle(stream)), "accept_dropout")
+    code = lib().accept_dropout(p._ref, d_x.data_ptr(), None if d_residual is None else d_residual.data_ptr(), d_y.data_ptr(), _stream_handle(stream))
+    if code:
+        raise AcceptError(code, "accept_dropout")
 
 
 def accept_rms_norm_check_params(p: RmsNormParams) -> int:
-    return int(lib().accept_rms_norm_check_params(ctypes.byref(p.c())))
+    return int(lib().accept_rms_norm_check_params(p._ref))
 
 
 def accept_rms_norm_workspace_size(p: RmsNormParams) -> int:
-    return int(lib().accept_rms_norm_workspace_size(ctypes.byref(p.c())))
+    return int(lib().accept_rms_norm_workspace_size(p._ref))
 
 
 def accept_rms_norm_forward(p: RmsNormParams, d_x, d_branch, d_gamma, d_sum, d_y, d_q=None, d_scale=None, d_rstd=None, d_ws=None, stream=None) -> None:
     """d_branch and d_gamma may be None; so may the outputs: d_sum, d_y, d_q with d_scale (uint8, as accept_block_quantize writes them; with d_ws) and
     d_rstd (float32, p.rows elements, kept for the backward pass)."""
-    _check(lib().accept_rms_norm_forward(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_branch), _ptr(d_gamma), _ptr(d_sum), _ptr(d_y), _ptr(d_q),
-                                         _ptr(d_scale), _ptr(d_rstd), _ptr(d_ws), 0 if d_ws is None else _nbytes(d_ws), _stream_handle(stream)),
-           "accept_rms_norm_forward")
+    code = lib().accept_rms_norm_forward(
+        p._ref, d_x.data_ptr(), None if d_branch is None else d_branch.data_ptr(), None if d_gamma is None else d_gamma.data_ptr(),
+        None if d_sum is None else d_sum.data_ptr(), None if d_y is None else d_y.data_ptr(), None if d_q is None else d_q.data_ptr(),
+        None if d_scale is None else d_scale.data_ptr(), None if d_rstd is None else d_rstd.data_ptr(),
+        None if d_ws is None else d_ws.data_ptr(), 0 if d_ws is None else d_ws.nbytes, _stream_handle(stream))
+    if code:
+        raise AcceptError(code, "accept_rms_norm_forward")
 
 
 def accept_rms_norm_backward(p: RmsNormParams, d_dy, d_s, d_gamma, d_rstd, d_dsum, d_dx, d_dbranch, d_dgamma, d_ws, stream=None) -> None:
     """d_gamma and d_dsum may be None; so may the outputs d_dx, d_dbranch and d_dgamma (float32, p.cols elements): not computed."""
-    _check(lib().accept_rms_norm_backward(ctypes.byref(p.c()), d_dy.data_ptr(), d_s.data_ptr(), _ptr(d_gamma), d_rstd.data_ptr(), _ptr(d_dsum),
-                                          _ptr(d_dx), _ptr(d_dbranch), _ptr(d_dgamma), d_ws.data_ptr(), _nbytes(d_ws), _stream_handle(stream)),
-           "accept_rms_norm_backward")
+    code = lib().accept_rms_norm_backward(
+        p._ref, d_dy.data_ptr(), d_s.data_ptr(), None if d_gamma is None else d_gamma.data_ptr(), d_rstd.data_ptr(),
+        None if d_dsum is None else d_dsum.data_ptr(), None if d_dx is None else d_dx.data_ptr(),
+        None if d_dbranch is None else d_dbranch.data_ptr(), None if d_dgamma is None else d_dgamma.data_ptr(), d_ws.data_ptr(), d_ws.nbytes,
+        _stream_handle(stream))
+    if code:
+        raise AcceptError(code, "accept_rms_norm_backward")
 
 
 def accept_micro_check_params(p: MicroParams) -> int:
-    return int(lib().accept_micro_check_params(ctypes.byref(p.c())))
+    return int(lib().accept_micro_check_params(p._ref))
 
 
 def accept_micro_data_size(p: MicroParams, transposed: bool = False) -> int:
-    return int(lib().accept_micro_data_size(ctypes.byref(p.c()), int(transposed)))
+    return int(lib().accept_micro_data_size(p._ref, int(transposed)))
 
 
 def accept_micro_scale_size(p: MicroParams, transposed: bool = False) -> int:
-    return int(lib().accept_micro_scale_size(ctypes.byref(p.c()), int(transposed)))
+    return int(lib().accept_micro_scale_size(p._ref, int(transposed)))
 
 
 def accept_micro_workspace_size(p: MicroParams) -> int:
-    return int(lib().accept_micro_workspace_size(ctypes.byref(p.c())))
+    return int(lib().accept_micro_workspace_size(p._ref))
 
 
 def accept_micro_quantize(p: MicroParams, d_x, d_q, d_scale, d_qt, d_scale_t, d_ws, stream=None) -> None:
     """d_q / d_scale (codes along the columns) or d_qt / d_scale_t (the transpose, codes along the rows) may be None:
     uint8 CUDA tensors of accept_micro_data_size and accept_micro_scale_size bytes."""
-    _check(lib().accept_micro_quantize(ctypes.byref(p.c()), d_x.data_ptr(), _ptr(d_q), _ptr(d_scale), _ptr(d_qt), _ptr(d_scale_t), d_ws.data_ptr(),
-                                     _nbytes(d_ws), _stream_handle(stream)), "accept_micro_quantize")
+    code = lib().accept_micro_quantize(
+        p._ref, d_x.data_ptr(), None if d_q is None else d_q.data_ptr(), None if d_scale is None else d_scale.data_ptr(),
+        None if d_qt is None else d_qt.data_ptr(), None if d_scale_t is None else d_scale_t.data_ptr(), d_ws.data_ptr(), d_ws.nbytes,
+        _stream_handle(stream))
+    if code:
+        raise AcceptError(code, "accept_micro_quantize")
 
 
 def accept_micro_dequantize(p: MicroParams, d_q, d_scale, d_x, stream=None) -> None:
     """The values of a p.rows x p.cols matrix in d_x (p.dtype, p.ld) from its codes by rows and their scales."""
-    _check(lib().accept_micro_dequantize(ctypes.byref(p.c()), d_q.data_ptr(), d_scale.data_ptr(), d_x.data_ptr(), _stream_handle(stream)),
-           "accept_micro_dequantize")
+    code = lib().accept_micro_dequantize(p._ref, d_q.data_ptr(), d_scale.data_ptr(), d_x.data_ptr(), _stream_handle(stream))
+    if code:
+        raise AcceptError(code, "accept_micro_dequantize")
 
 
 def accept_micro_matmul_check_params(p: MicroMatmulParams) -> int:
-    return int(lib().accept_micro_matmul_check_params(ctypes.byref(p.c())))
+    return int(lib().accept_micro_matmul_check_params(p._ref))
 
 
 def accept_micro_matmul_workspace_size(p: MicroMatmulParams) -> int:
-    return int(lib().accept_micro_matmul_workspace_size(ctypes.byref(p.c())))
+    return int(lib().accept_micro_matmul_workspace_size(p._ref))
 
 
 def accept_micro_matmul(p: MicroMatmulParams, d_a, d_a_scale, d_b, d_b_scale, d_bias, d_d, d_ws, stream=None) -> None:
     """d_bias: float32 CUDA tensor of p.n elements, or None."""
-    _check(lib().accept_micro_matmul(ctypes.byref(p.c()), d_a.data_ptr(), d_a_scale.data_ptr(), d_b.data_ptr(), d_b_scale.data_ptr(), _ptr(d_bias),
-                                   d_d.data_ptr(), d_ws.data_ptr(), _nbytes(d_ws), _stream_handle(stream)), "accept_micro_matmul")
+    code = lib().accept_micro_matmul(
+        p._ref, d_a.data_ptr(), d_a_scale.data_ptr(), d_b.data_ptr(), d_b_scale.data_ptr(), None if d_bias is None else d_bias.data_ptr(),
+        d_d.data_ptr(), d_ws.data_ptr(), d_ws.nbytes, _stream_handle(stream))
+    if code:
+        raise AcceptError(code, "accept_micro_matmul")
 
 
 # ---- small conveniences for callers (allocation only) -----------------------------------------

@@ -31,10 +31,10 @@ KernelFn select_kernel(const accept_micro_params* p, bool whole) {
   }
 }
 
-constexpr int kUnits = 4;
+constexpr int kRows = 4;
 using ValueFn = void (*)(const MicroValueArgs);
 template <typename T>
-ValueFn select_values(bool whole) { return whole ? accept::micro_dequantize_kernel<T, true, kUnits> : accept::micro_dequantize_kernel<T, false, kUnits>; }
+ValueFn select_values(bool whole) { return whole ? accept::micro_dequantize_kernel<T, true, kRows> : accept::micro_dequantize_kernel<T, false, kRows>; }
 
 }  // namespace
 
@@ -119,18 +119,21 @@ accept_status accept_micro_dequantize(const accept_micro_params* p, const void* 
   a.scale = static_cast<const uint8_t*>(d_scale);
   a.x = d_x;
   a.ld = p->ld;
+  a.rows = (uint32_t)p->rows;
   a.cols = (uint32_t)p->cols;
   a.ldq = (uint32_t)(up(p->cols, 32) / 2);
   a.atoms = (uint32_t)(up(p->rows, 128) / 128);
-  const bool whole = is_aligned(d_x, 16) && p->ld * value_size(p->dtype) % 16 == 0;
-  a.per_row = (p->cols + (whole ? 0 : 16 / value_size(p->dtype) - 1) + 7) / 8;  // units start on 16-byte boundaries: one more where a row does not
-  a.units = p->rows * a.per_row;
   ACCEPT_BOUNDS(s, bounds_list.add(d_q, accept_micro_data_size(p, 0), false); bounds_list.add(d_scale, accept_micro_scale_size(p, 0), false);
                 bounds_list.add(d_x, ((p->rows - 1) * p->ld + p->cols) * value_size(p->dtype), true));
+  const bool whole = is_aligned(d_x, 16) && p->ld * value_size(p->dtype) % 16 == 0;
   const ValueFn fn = p->dtype == ACCEPT_DTYPE_F32 ? select_values<float>(whole) : p->dtype == ACCEPT_DTYPE_BF16 ? select_values<__nv_bfloat16>(whole) : select_values<__half>(whole);
-  const uint64_t blocks = (a.units + kUnits * accept::kValueThreads - 1) / (kUnits * accept::kValueThreads);
-  if (blocks > 0x7fffffffull) return ACCEPT_ERR_BAD_SIZE;
-  ACCEPT_LAUNCH(launch_overlapped(fn, dim3((unsigned)blocks), accept::kValueThreads, s, a));
+  // Units start on x's 16-byte boundaries: one more than the columns fill where a row does not.  A warp takes neighbours of one row
+  // where there are so many; a few blocks for each SM take groups of rows in turn.
+  const uint64_t per_row = (p->cols + (whole ? 0 : 16 / value_size(p->dtype) - 1) + 7) / 8;
+  while (a.log_units < 5 && (1u << a.log_units) < per_row) ++a.log_units;
+  const uint64_t wide = (per_row + (1u << a.log_units) - 1) >> a.log_units, each = (uint64_t)kRows * (accept::kValueThreads >> a.log_units);
+  const uint64_t high = (p->rows + each - 1) / each, most = wide < 16 * 148 ? 16 * 148 / wide : 1;
+  ACCEPT_LAUNCH(launch_overlapped(fn, dim3((unsigned)wide, (unsigned)(high < most ? high : most)), accept::kValueThreads, s, a));
   return ACCEPT_OK;
 }
 

@@ -277,8 +277,9 @@ struct MicroValueArgs {
   const uint8_t* q;
   const uint8_t* scale;
   void* x;
-  uint64_t ld, per_row, units;  // units of eight neighbours
-  uint32_t cols, ldq, atoms;
+  uint64_t ld;
+  uint32_t rows, cols, ldq, atoms;
+  int log_units;  // see micro_dequantize_kernel
 };
 
 // Eight codes as fp32 pairs.  As fp32 bits a code's two exponent and one fraction bits are its value times 2^-126 (the smallest,
@@ -293,57 +294,61 @@ __device__ __forceinline__ float micro_scale(uint32_t byte) { return __uint_as_f
 
 // A unit is eight neighbours of a row that start on a 16-byte boundary of x.  Where rows do not (WHOLE false), a unit's codes are
 // shifted out of two words and may have two scales; the ends of a row are written value by value.  (One value a store:
-// 4096 x 1001 fp32 27.7 us.)
+// 4096 x 1001 fp32 27.7 us.)  A block takes 2^log_units units of ROWS times as many rows as that leaves threads for, in turn.
 constexpr int kValueThreads = 256;
-template <typename T, bool WHOLE, int UNITS>
+template <typename T, bool WHOLE, int ROWS>
 __global__ void __launch_bounds__(kValueThreads) micro_dequantize_kernel(const MicroValueArgs a) {
   grid_dependency_handshake();
-  const uint64_t first = (uint64_t)blockIdx.x * (UNITS * kValueThreads) + threadIdx.x;
-  constexpr int kEach = 16 / (int)sizeof(T);
-  uint32_t codes[UNITS], byte[UNITS], next[UNITS], row[UNITS];
-  int col[UNITS], n[UNITS];  // of a unit: its first column (below 0 where the row starts inside it), how many exist
+  constexpr uint32_t kEach = 16 / (uint32_t)sizeof(T);
+  const uint32_t at_once = kValueThreads >> a.log_units, c = ((blockIdx.x << a.log_units) + (threadIdx.x & ((1u << a.log_units) - 1))) * 8;
+  const uint32_t groups = (a.rows + at_once * ROWS - 1) / (at_once * ROWS);
+  for (uint32_t group = blockIdx.y; group < groups; group += gridDim.y) {
+    const uint32_t r0 = group * (at_once * ROWS) + (threadIdx.x >> a.log_units);
+    uint32_t codes[ROWS], byte[ROWS], next[ROWS];
+    int col[ROWS];  // of a unit: its first column, below 0 where the row starts inside it
+    bool some[ROWS];
 #pragma unroll
-  for (int i = 0; i < UNITS; ++i) {
-    const uint64_t u = first + i * kValueThreads;
-    row[i] = a.units <= 0xffffffffu ? (uint32_t)u / (uint32_t)a.per_row : (uint32_t)(u / a.per_row);
-    uint32_t c = (uint32_t)(u - row[i] * a.per_row) * 8;
-    uint32_t before = 0;  // values between the 16-byte boundary and the row's start
-    if (!WHOLE) before = (uint32_t)(((uint64_t)reinterpret_cast<uintptr_t>(a.x) / sizeof(T) + row[i] * a.ld) % kEach);
-    col[i] = (int)(c - before);
-    n[i] = u < a.units && c < a.cols + before ? 1 : 0;
-    if (n[i] == 0) continue;
-    const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + (uint64_t)row[i] * a.ldq);
-    const uint32_t start = WHOLE ? c : col[i] < 0 ? 0u : (uint32_t)col[i];
-    codes[i] = ldg_c(q + start / 8);
-    byte[i] = next[i] = ldg_c(a.scale + scale_offset(row[i], start / 32, a.atoms));
-    if (!WHOLE) {
-      const uint32_t end = min((uint32_t)(col[i] + 7), a.cols - 1);
-      uint32_t more = codes[i];
-      if (end / 8 != start / 8) more = ldg_c(q + end / 8);
-      if (end / 32 != start / 32) next[i] = ldg_c(a.scale + scale_offset(row[i], end / 32, a.atoms));
-      codes[i] = col[i] < 0 ? codes[i] << 4 * (uint32_t)-col[i] : __funnelshift_r(codes[i], more, 4 * (start % 8));
+    for (int i = 0; i < ROWS; ++i) {
+      const uint32_t row = r0 + i * at_once;
+      uint32_t before = 0;  // values between the 16-byte boundary and the row's start
+      if (!WHOLE) before = (uint32_t)((reinterpret_cast<uintptr_t>(a.x) / sizeof(T) + row * a.ld) % kEach);
+      col[i] = (int)(c - before);
+      some[i] = row < a.rows && row >= r0 && c < a.cols + before;
+      codes[i] = byte[i] = next[i] = 0;
+      if (!some[i]) continue;
+      const uint32_t* q = reinterpret_cast<const uint32_t*>(a.q + (uint64_t)row * a.ldq);
+      const uint32_t start = WHOLE ? c : col[i] < 0 ? 0u : (uint32_t)col[i];
+      codes[i] = ldg_c(q + start / 8);
+      byte[i] = next[i] = ldg_c(a.scale + scale_offset(row, start / 32, a.atoms));
+      if (!WHOLE) {
+        const uint32_t end = min((uint32_t)(col[i] + 7), a.cols - 1);
+        uint32_t more = codes[i];
+        if (end / 8 != start / 8) more = ldg_c(q + end / 8);
+        if (end / 32 != start / 32) next[i] = ldg_c(a.scale + scale_offset(row, end / 32, a.atoms));
+        codes[i] = col[i] < 0 ? codes[i] << 4 * (uint32_t)-col[i] : __funnelshift_r(codes[i], more, 4 * (start % 8));
+      }
     }
-  }
 #pragma unroll
-  for (int i = 0; i < UNITS; ++i) {
-    if (n[i] == 0) continue;
-    Pair v[4];
-    const float s = micro_scale(byte[i]), s2 = WHOLE ? s : micro_scale(next[i]);
+    for (int i = 0; i < ROWS; ++i) {
+      if (!some[i]) continue;
+      Pair v[4];
+      const float s = micro_scale(byte[i]), s2 = WHOLE ? s : micro_scale(next[i]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int lo = (col[i] + 2 * j) & 31, hi = (col[i] + 2 * j + 1) & 31;  // the second scale from the first boundary on
-      const bool second_lo = !WHOLE && col[i] >= 0 && lo < (col[i] & 31), second_hi = !WHOLE && col[i] >= 0 && hi < (col[i] & 31);
-      v[j] = micro_value(codes[i], j, pair_of(second_lo ? s2 : s, second_hi ? s2 : s));
-    }
-    T* x = static_cast<T*>(a.x) + (uint64_t)row[i] * a.ld;
-    if (WHOLE || (col[i] >= 0 && (uint32_t)col[i] + 8 <= a.cols)) {
-      store_eight<T, true>(x + col[i], WHOLE ? (int)min(a.cols - (uint32_t)col[i], 8u) : 8, v);
-    } else {
+      for (int j = 0; j < 4; ++j) {
+        const int lo = (col[i] + 2 * j) & 31, hi = (col[i] + 2 * j + 1) & 31;  // the second scale from the first boundary on
+        const bool second_lo = !WHOLE && col[i] >= 0 && lo < (col[i] & 31), second_hi = !WHOLE && col[i] >= 0 && hi < (col[i] & 31);
+        v[j] = micro_value(codes[i], j, pair_of(second_lo ? s2 : s, second_hi ? s2 : s));
+      }
+      T* x = static_cast<T*>(a.x) + (uint64_t)(r0 + i * at_once) * a.ld;
+      if (WHOLE || (col[i] >= 0 && (uint32_t)col[i] + 8 <= a.cols)) {
+        store_eight<T, true>(x + col[i], WHOLE ? (int)min(a.cols - (uint32_t)col[i], 8u) : 8, v);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float2 f = split(v[j / 2]);
-        const int c = col[i] + j;
-        if (c >= 0 && (uint32_t)c < a.cols) st_c(x + c, from_float<T>(j % 2 ? f.y : f.x));
+        for (int j = 0; j < 8; ++j) {
+          const float2 f = split(v[j / 2]);
+          const int at = col[i] + j;
+          if (at >= 0 && (uint32_t)at < a.cols) st_c(x + at, from_float<T>(j % 2 ? f.y : f.x));
+        }
       }
     }
   }

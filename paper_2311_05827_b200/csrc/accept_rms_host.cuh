@@ -17,11 +17,14 @@ inline bool rms_whole_rows(const void* p, uint64_t ld, int32_t dtype) { return i
 constexpr int kRmsOwn = 16;
 struct RmsShape { bool wide; int lanes; unsigned warps, groups, blocks; bool joins; size_t shared; };
 
-// Rows of a group in shared memory: up to 192 KB for the block, and 16 bytes more for each row of a warp (of eight lanes where
+// Rows of a group in shared memory: up to 144 KB for the block, and 16 bytes more for each row of a warp (of eight lanes where
 // those share it), tensor and stage where rows are not aligned: 64 rows of eight lanes, three tensors, four stages at most.
-constexpr int kRmsRing = 196608, kRmsMostShared = kRmsRing + 64 * 16 * 3 * 4;
+constexpr int kRmsRing = 147456, kRmsMostShared = kRmsRing + 64 * 16 * 3 * 4;
+// Rows ahead of the one in work, and it.  Up to three of less than 64 KB; of longer ones (for 8192 columns) that one alone, while
+// the block's other group computes: 16384 x 4096, fp32 both, forward 181 us with two, 166 with one; fp32 and bf16, backward 177 and
+// 168; fp32 and bf16 to codes, forward 123 with two, 113 with three or four.
 constexpr int rms_stages_for(int bytes) {  // of a column in all tensors that a pass reads
-  return kRmsRing / (512 * kRmsOwn * bytes) < 4 ? kRmsRing / (512 * kRmsOwn * bytes) : 4;
+  return 512 * kRmsOwn * bytes >= 65536 ? 1 : kRmsRing / (512 * kRmsOwn * bytes) < 4 ? kRmsRing / (512 * kRmsOwn * bytes) : 4;
 }
 inline int rms_column_bytes(const accept_rms_norm_params* p, bool backward) {
   return (int)((backward ? 2 : 1) * rms_value_size(p->dtype_x) + rms_value_size(p->dtype_y));
