@@ -12,22 +12,26 @@ bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF1
 
 using KernelFn = void (*)(const DropoutArgs);
 constexpr int kRows = 2, kFlatUnits = 4;
+enum class Rows { kFlat, kFew, kMany };  // no gaps; others
 
 template <typename TX, typename TY>
-KernelFn select_rows(bool flat) { return flat ? accept::dropout_flat_kernel<TX, TY, kFlatUnits> : accept::dropout_kernel<TX, TY, kRows>; }
+KernelFn select_rows(Rows rows) {
+  return rows == Rows::kFlat  ? accept::dropout_flat_kernel<TX, TY, kFlatUnits>
+         : rows == Rows::kFew ? accept::dropout_kernel<TX, TY, kRows, true> : accept::dropout_kernel<TX, TY, kRows, false>;
+}
 template <typename TX>
-KernelFn select_y(int32_t dtype_y, bool flat) {
+KernelFn select_y(int32_t dtype_y, Rows rows) {
   switch (dtype_y) {
-    case ACCEPT_DTYPE_F32: return select_rows<TX, float>(flat);
-    case ACCEPT_DTYPE_BF16: return select_rows<TX, __nv_bfloat16>(flat);
-    default: return select_rows<TX, __half>(flat);
+    case ACCEPT_DTYPE_F32: return select_rows<TX, float>(rows);
+    case ACCEPT_DTYPE_BF16: return select_rows<TX, __nv_bfloat16>(rows);
+    default: return select_rows<TX, __half>(rows);
   }
 }
-KernelFn select_kernel(int32_t dtype_x, int32_t dtype_y, bool flat) {
+KernelFn select_kernel(int32_t dtype_x, int32_t dtype_y, Rows rows) {
   switch (dtype_x) {
-    case ACCEPT_DTYPE_F32: return select_y<float>(dtype_y, flat);
-    case ACCEPT_DTYPE_BF16: return select_y<__nv_bfloat16>(dtype_y, flat);
-    default: return select_y<__half>(dtype_y, flat);
+    case ACCEPT_DTYPE_F32: return select_y<float>(dtype_y, rows);
+    case ACCEPT_DTYPE_BF16: return select_y<__nv_bfloat16>(dtype_y, rows);
+    default: return select_y<__half>(dtype_y, rows);
   }
 }
 
@@ -45,7 +49,7 @@ accept_status accept_dropout_check_params(const accept_dropout_params* p) {
   if (p->ld_x < p->cols || p->ld_y < p->cols || p->rows > (1ull << 40) || p->cols > (1ull << 40) || p->ld_x > (1ull << 40) || p->ld_y > (1ull << 40) ||
       (p->rows && (p->ld_x > (1ull << 60) / p->rows || p->ld_y > (1ull << 60) / p->rows)))
     return ACCEPT_ERR_BAD_SIZE;
-  if (p->rows * ((p->cols + 14) / 8) / accept::kDropThreads >= 0x7fffffffull) return ACCEPT_ERR_BAD_SIZE;  // blocks of a grid
+  if (p->rows * ((p->cols + 14) / 8) / 32 >= 0x7fffffffull) return ACCEPT_ERR_BAD_SIZE;  // blocks of a grid
   if (!is_dtype(p->dtype_x) || !is_dtype(p->dtype_y) || p->reserved != 0) return ACCEPT_ERR_BAD_ENUM;
   if (!accept::is_drop_rate(p->p)) return ACCEPT_ERR_BAD_SIZE;
   return ACCEPT_OK;
@@ -78,17 +82,17 @@ accept_status accept_dropout(const accept_dropout_params* p, const void* d_x, co
     a.rows = 1;
     flat = is_aligned(d_x, 16) && is_aligned(d_residual, 16) && is_aligned(d_y, 16);
   }
-  const KernelFn fn = select_kernel(p->dtype_x, p->dtype_y, flat);
+  const KernelFn fn = select_kernel(p->dtype_x, p->dtype_y, flat ? Rows::kFlat : a.rows < 32 ? Rows::kFew : Rows::kMany);
   if (flat) {
     const uint64_t block = 8 * kFlatUnits * accept::kDropThreads;
     ACCEPT_LAUNCH(accept::launch_overlapped(fn, dim3((unsigned)((a.cols + block - 1) / block)), accept::kDropThreads, s, a));
     return ACCEPT_OK;
   }
   // Units start on y's 16-byte boundaries: one more than the columns fill where a row does not.  A warp takes neighbours of one row
-  // where there are so many.
+  // where there are so many, more of a block where there are few rows.
   const bool on_boundaries = is_aligned(d_y, 16) && a.ld_y * size_y % 16 == 0;
   const uint64_t per_row = (a.cols + (on_boundaries ? 0 : 16 / size_y - 1) + 7) / 8;
-  while (a.log_units < 5 && (1u << a.log_units) < per_row) ++a.log_units;
+  while (a.log_units < 8 && (1u << a.log_units) < per_row && (a.log_units < 5 || (uint64_t)kRows * (accept::kDropThreads >> a.log_units) > a.rows)) ++a.log_units;
   const uint64_t wide = (per_row + (1u << a.log_units) - 1) >> a.log_units, each = (uint64_t)kRows * (accept::kDropThreads >> a.log_units);
   // a few blocks for each SM, which take groups of rows in turn: what they work out once serves all of them
   const uint64_t high = (a.rows + each - 1) / each, most = wide < 8 * 148 ? 8 * 148 / wide : 1;

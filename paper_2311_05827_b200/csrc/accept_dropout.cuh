@@ -113,12 +113,15 @@ __global__ void __launch_bounds__(kDropThreads) dropout_flat_kernel(const Dropou
 
 // Other matrices: a block takes 2^log_units units of eight neighbours of ROWS times as many rows as that leaves threads for.  Units
 // start on y's 16-byte boundaries; what is read there is shifted, and the ends of a row leave value by value.
-template <typename TX, typename TY, int ROWS>
+// FEW: so few rows that the first and the last count, beside which nothing may be read: there only the units at the very ends are read
+// value by value (1 x 30000001 bf16 off a boundary 439 -> 84 us).
+template <typename TX, typename TY, int ROWS, bool FEW>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs a) {
   grid_dependency_handshake();
   constexpr uint32_t kEach = 16 / (uint32_t)sizeof(TY);
   const uint32_t rows_at_once = kDropThreads >> a.log_units;
   const uint64_t unit = ((uint64_t)blockIdx.x << a.log_units) + (threadIdx.x & ((1u << a.log_units) - 1));
+  const bool behind_start = unit > 0, before_end = unit * 8 + 8 < a.cols;
   const uint64_t groups = (a.rows + rows_at_once * ROWS - 1) / (rows_at_once * ROWS);
   const DropKey key(a.drop.rng, a.drop.offset + blockIdx.y * (uint64_t)(rows_at_once * ROWS) * a.cols);
   for (uint64_t group = blockIdx.y; group < groups; group += gridDim.y) {
@@ -128,9 +131,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
     int lo[ROWS], hi[ROWS];
     const TX* x[ROWS];
     const TY* residual[ROWS];
-    // all eight exist and the row is not the first or the last, beside which nothing may be read (told by the columns too, the test
-    // itself costs more than those rows: 16384 x 4095 bf16 with gaps 103 -> 128 us)
-    bool inner = true;
+    bool inner = true;  // all eight exist, and the value on either side lies in the matrix
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       const uint64_t r = r0 + i * rows_at_once;
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
       hi[i] = r < a.rows ? (int)min(max((int64_t)a.cols - col[i], (int64_t)0), (int64_t)8) : 0;
       x[i] = static_cast<const TX*>(a.x) + (int64_t)(r * a.ld_x) + col[i];
       residual[i] = static_cast<const TY*>(a.residual) + (int64_t)(r * a.ld_y) + col[i];
-      inner = inner && lo[i] == 0 && hi[i] == 8 && r > 0 && r + 1 < a.rows;
+      inner = inner && lo[i] == 0 && hi[i] == 8 && ((FEW && behind_start) || r > 0) && ((FEW && before_end) || r + 1 < a.rows);
     }
     if (inner) {
       RawEight<TX> raw_x[ROWS];

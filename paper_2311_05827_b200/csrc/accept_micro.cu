@@ -13,15 +13,18 @@ size_t value_size(int32_t dtype) { return dtype == ACCEPT_DTYPE_F32 ? 4 : 2; }
 uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
 using KernelFn = void (*)(const MicroArgs);
+struct Kernel { KernelFn fn; unsigned threads; };
 using accept::MicroRound;
 template <typename T, MicroRound ROUND>
-KernelFn select_rows(bool whole) { return whole ? accept::micro_quantize_kernel<T, ROUND, true> : accept::micro_quantize_kernel<T, ROUND, false>; }
+Kernel select_rows(bool whole) {
+  return {whole ? accept::micro_quantize_kernel<T, ROUND, true> : accept::micro_quantize_kernel<T, ROUND, false>, (unsigned)accept::kMicroThreads<T, ROUND>};
+}
 template <typename T>
-KernelFn select_round(MicroRound round, bool whole) {
+Kernel select_round(MicroRound round, bool whole) {
   return round == MicroRound::kNearest ? select_rows<T, MicroRound::kNearest>(whole)
          : round == MicroRound::kQuads ? select_rows<T, MicroRound::kQuads>(whole) : select_rows<T, MicroRound::kAnywhere>(whole);
 }
-KernelFn select_kernel(const accept_micro_params* p, bool whole) {
+Kernel select_kernel(const accept_micro_params* p, bool whole) {
   const MicroRound round = p->round == ACCEPT_ROUND_NEAREST ? MicroRound::kNearest
                            : p->cols % 4 == 0 && p->rng_offset % 4 == 0 ? MicroRound::kQuads : MicroRound::kAnywhere;
   switch (p->dtype) {
@@ -102,7 +105,8 @@ accept_status accept_micro_quantize(const accept_micro_params* p, const void* d_
                 bounds_list.add(d_qt, accept_micro_data_size(p, 1), true); bounds_list.add(d_scale_t, accept_micro_scale_size(p, 1), true);
                 bounds_list.add(d_ws, 16, true));
   const bool whole = is_aligned(d_x, 16) && p->ld * value_size(p->dtype) % 16 == 0;
-  ACCEPT_LAUNCH(launch_overlapped(select_kernel(p, whole), dim3(a.tiles_r * a.tiles_c), 256, s, a));
+  const Kernel kernel = select_kernel(p, whole);
+  ACCEPT_LAUNCH(launch_overlapped(kernel.fn, dim3(a.tiles_r * a.tiles_c), kernel.threads, s, a));
   return ACCEPT_OK;
 }
 

@@ -35,16 +35,26 @@ __device__ __forceinline__ uint32_t micro_scale_byte(float a) {
 // 2^(127 - byte); 0 for 255, which makes every code of the block zero.
 __device__ __forceinline__ float micro_inverse(uint32_t byte) { return __uint_as_float(byte == 255u ? 0u : (254u - byte) << 23); }
 
-// Eight values to eight codes, the first in the lowest bits; ties to even.
-__device__ __forceinline__ uint32_t micro_encode(const float (&v)[8]) {
+// N values (4 or 8) to codes, the first in the lowest bits; ties to even.
+template <int N>
+__device__ __forceinline__ uint32_t micro_encode(const float (&v)[N]) {
   uint32_t r;
-  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-      "mov.b32 %0, {a, b, c, d};\n\t}"
-      : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  if constexpr (N == 8) {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+  } else {
+    asm("{\n\t.reg .b8 a, b;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "mov.b32 %0, {a, b, a, b};\n\t}"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]));
+    r &= 0xffffu;
+  }
   return r;
 }
 // One value (|v| <= 6, v25 = v 2^25) to a code with stochastic rounding, in exact fixed point: F = the value's place in the list of
@@ -65,43 +75,97 @@ __device__ __forceinline__ uint32_t micro_stochastic(float v, float v25, uint32_
       : "=r"(r) : "f"(v), "f"(v25), "r"(less), "r"(__float_as_uint(v)), "r"((2u << 24) - (0x3f800000u << 2)));
   return r;
 }
-// Eight codes from the top four bits of words, the first in the lowest bits.
-__device__ __forceinline__ uint32_t micro_join(const uint32_t (&w)[8]) {
-  uint32_t r = w[7] >> 28;
+// N codes from the top four bits of words, the first in the lowest bits.
+template <int N>
+__device__ __forceinline__ uint32_t micro_join(const uint32_t (&w)[N]) {
+  uint32_t r = w[N - 1] >> 28;
 #pragma unroll
-  for (int i = 6; i >= 0; --i) r = __funnelshift_l(w[i], r, 4);
+  for (int i = N - 2; i >= 0; --i) r = __funnelshift_l(w[i], r, 4);
   return r;
 }
 
-// Thread (warp w, lane l) holds columns 64 (w % 2) + 8 (l % 8) .. + 7 of rows 32 (w / 2) + 8 (l / 8) .. + 7 of the tile: a warp has 32 rows
-// of two blocks of columns, so the largest values of all blocks, both ways, are found within it.
-//
-// Measured on 16384 x 4096 bf16, nearest: see the launch.  Stochastic rounding is bound by instruction issue: some 30 a value for
-// both outputs.
+// The largest magnitude of each of the first ROWS rows, and of each column over them; a NaN or an infinity comes out on top.
+template <int ROWS, typename T>
+__device__ __forceinline__ void micro_largest(const Held<T>& h, float (&row)[ROWS], float (&col)[8]) {
+  uint32_t down[4];
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i) {
+    uint32_t m[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = h.w[i][j] & 0x7fff7fffu;
+      down[j] = i ? max_words(down[j], m[j], T()) : m[j];
+    }
+    const float2 f = split(word_to_pair<T>(max_words(max_words(m[0], m[1], T()), max_words(m[2], m[3], T()), T())));
+    row[i] = max_nan(f.x, f.y);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 f = split(word_to_pair<T>(down[j]));
+    col[2 * j] = f.x;
+    col[2 * j + 1] = f.y;
+  }
+}
+template <int ROWS>
+__device__ __forceinline__ void micro_largest(const Held<float>& h, float (&row)[ROWS], float (&col)[8]) {
+#pragma unroll
+  for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float2 f = split(h.w[i][j]);
+      const float x = fabsf(f.x), y = fabsf(f.y);
+      row[i] = j ? max3_nan(row[i], x, y) : max_nan(x, y);
+      col[2 * j] = i ? max_nan(col[2 * j], x) : x;
+      col[2 * j + 1] = i ? max_nan(col[2 * j + 1], y) : y;
+    }
+}
+
+// Each exchange over lane bit BIT halves the values that a lane looks after: N of them to N / 2, the upper half where the bit is set.
+template <int N>
+__device__ __forceinline__ void halve_most(const float (&m)[N], bool upper, int bit, float (&out)[N / 2]) {
+#pragma unroll
+  for (int k = 0; k < N / 2; ++k) {
+    const float away = upper ? m[k] : m[k + N / 2], keep = upper ? m[k + N / 2] : m[k];
+    out[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, bit));
+  }
+}
+
 // ROUND: nearest, or stochastic where all rows' counters start on a multiple of four (kQuads) or not (kAnywhere).
 enum class MicroRound { kNearest, kQuads, kAnywhere };
+
+// A tile is 8 or 16 warps of 32 rows by 64 or 32 columns, a thread has ROWS rows of eight neighbours.  A warp has whole blocks both ways,
+// so their largest values are found within it.  Eight rows; four for stochastic rounding of fp32, whose values and random numbers would
+// else not fit the registers (16384 x 4096 both ways 151 -> 138 us; no gain for bf16, 97 us).
+// Measured on 16384 x 4096 bf16: rows 28.5 us (0.91 of the copy rate), both ways 41 (0.77); stochastic rounding is bound by the logic
+// pipe (75 % busy): some 40 instructions a value both ways, 97 us.
+template <typename T, MicroRound ROUND> constexpr int kMicroRows = ROUND != MicroRound::kNearest && sizeof(T) == 4 ? 4 : 8;
+template <typename T, MicroRound ROUND> constexpr int kMicroThreads = kTile * kTile / 8 / kMicroRows<T, ROUND>;
 template <typename T, MicroRound ROUND, bool WHOLE>
-__global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T) == 4 ? 2 : 3) micro_quantize_kernel(const MicroArgs a) {
+__global__ void __launch_bounds__(kMicroThreads<T, ROUND>, kMicroRows<T, ROUND> == 4 ? 1 : ROUND != MicroRound::kNearest || sizeof(T) == 4 ? 2 : 3)
+    micro_quantize_kernel(const MicroArgs a) {
   constexpr bool STOCHASTIC = ROUND != MicroRound::kNearest;
+  constexpr int ROWS = kMicroRows<T, ROUND>, kAcross = ROWS, kDown = 32 / kAcross;  // lanes side by side, and one below the other
+  constexpr int kRowsEach = ROWS / 4, kColsEach = 8 / kDown;                        // that a lane looks after in the end
+  constexpr int kWarpsAcross = kTile / (8 * kAcross);
   __shared__ __align__(16) uint8_t turned[kTile * (kTile / 2)];
-  __shared__ __align__(16) uint8_t bytes_t[kTile][4];
-  constexpr bool kKept = sizeof(T) == 2;  // the numbers of all values stay in registers; beside fp32 values they are drawn twice
+  __shared__ __align__(16) uint8_t bytes_r[kTile][4], bytes_t[kTile][4];
   grid_dependency_handshake();
   const uint32_t tile_r = blockIdx.x / a.tiles_c, tile_c = blockIdx.x - tile_r * a.tiles_c;
-  const uint32_t t = threadIdx.x, lane = t & 31, warp = t >> 5, part = lane & 7, down = lane >> 3;
-  const uint32_t r_in = 32 * (warp >> 1) + 8 * down, c_in = 64 * (warp & 1) + 8 * part;
+  const uint32_t t = threadIdx.x, lane = t & 31, warp = t >> 5, part = lane % kAcross, down = lane / kAcross;
+  const uint32_t warp_r = warp / kWarpsAcross, warp_c = warp % kWarpsAcross;
+  const uint32_t r_in = 32 * warp_r + ROWS * down, c_in = 8 * (kAcross * warp_c + part);
   const uint32_t r0 = tile_r * kTile + r_in, c0 = tile_c * kTile + c_in;
 
   Held<T> h;
   {
     const T* p = static_cast<const T*>(a.x) + (uint64_t)r0 * a.ld + c0;
     const int n = c0 < a.cols ? (int)min(a.cols - c0, 8u) : 0;
-    if (!WHOLE && sizeof(T) == 2 && n == 8 && (r0 > 0 || c0 > 0) && (r0 + 8 < a.rows || (r0 + 8 == a.rows && c0 + 8 < a.cols))) {
-      RawEight<T> raw[8];
+    if (!WHOLE && sizeof(T) == 2 && n == 8 && (r0 > 0 || c0 > 0) && (r0 + ROWS < a.rows || (r0 + ROWS == a.rows && c0 + 8 < a.cols))) {
+      RawEight<T> raw[ROWS];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) load_raw<T>(p + i * a.ld, raw[i]);
+      for (int i = 0; i < ROWS; ++i) load_raw<T>(p + i * a.ld, raw[i]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < ROWS; ++i) {
         uint32_t w[2 * sizeof(T)];
         words_of<T>(raw[i], p + i * a.ld, w);
 #pragma unroll
@@ -109,28 +173,28 @@ __global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < ROWS; ++i) {
         const bool there = r0 + i < a.rows;
         hold_row(h, i, p, WHOLE && there && n == 8, there ? n : 0);
         p += a.ld;
       }
     }
   }
-  float row_most[8], col_most[8];
-  largest(h, row_most, col_most);  // a NaN or an infinity comes out on top
+  float row_most[ROWS], col_most[8];
+  micro_largest<ROWS>(h, row_most, col_most);
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) bad |= !is_finite_bits(row_most[i]);
+  for (int i = 0; i < ROWS; ++i) bad |= !is_finite_bits(row_most[i]);
   if (bad) atomicOr(a.status, kDevNonFinite);
 
   uint32_t square_byte = 0;  // of the 32 x 32 block that this thread's values lie in
   if (a.square) {
     float most = row_most[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) most = max_nan(most, row_most[i]);
+    for (int i = 1; i < ROWS; ++i) most = max_nan(most, row_most[i]);
 #pragma unroll
     for (int d = 1; d <= 16; d <<= 1)
-      if (d != 4) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));
+      if (kAcross == 4 || d != 4) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, d));  // eight lanes across are two blocks
     square_byte = micro_scale_byte(most);
   }
 
@@ -138,46 +202,36 @@ __global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T
   const DropKey key(a.rng, first);
   DropRow quads(a.rng, first, key);
   if (ROUND == MicroRound::kQuads) quads.phase = 0;  // known here: the other way of counting falls away
-  const auto draw_row = [&](int i, uint32_t (&less)[8]) {
-    const auto keep = [&](int, const uint32_t (&w)[8]) {
+  uint32_t numbers[STOCHASTIC ? ROWS : 1][8];  // the upper 28 bits of the words' complements
+  if constexpr (STOCHASTIC) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) less[j] = w[j] >> 4;
-    };
-    if (ROUND == MicroRound::kQuads) number_units<8, true, 1>(quads, i * (a.cols & ~3u), 0, keep);
-    else number_units<8, true, 1>(DropRow(a.rng, first + (uint64_t)i * a.cols, key), 0, 0, keep);
-  };
-  uint32_t numbers[STOCHASTIC && kKept ? 8 : 1][8];
-  if (STOCHASTIC && kKept)
+    for (int i = 0; i < ROWS; ++i) {
+      const auto keep = [&](int, const uint32_t (&w)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) draw_row(i, numbers[i % (STOCHASTIC && kKept ? 8 : 1)]);
+        for (int j = 0; j < 8; ++j) numbers[i][j] = w[j] >> 4;
+      };
+      if (ROUND == MicroRound::kQuads) number_units<8, true, 1>(quads, i * (a.cols & ~3u), 0, keep);
+      else number_units<8, true, 1>(DropRow(a.rng, first + (uint64_t)i * a.cols, key), 0, 0, keep);
+    }
+  }
 
   if (a.q) {
-    // four lanes hold eight rows of a block: each exchange halves the rows that a lane looks after, until it has two
-    float m[4];
+    float most[kRowsEach], half[ROWS / 2];
+    halve_most<ROWS>(row_most, part & 2, 2, half);
+    halve_most<ROWS / 2>(half, part & 1, 1, most);
+    float inverse[kRowsEach];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float away = part & 2 ? row_most[k] : row_most[k + 4], keep = part & 2 ? row_most[k + 4] : row_most[k];
-      m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 2));
-    }
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float away = part & 1 ? m[k] : m[k + 2], keep = part & 1 ? m[k + 2] : m[k];
-      m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 1));
-    }
-    float inverse[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {  // rows 2 (part % 4) + k of the eight
-      const uint32_t row = r0 + 2 * (part & 3) + k;
-      uint32_t byte = a.square ? square_byte : micro_scale_byte(m[k]);
+    for (int k = 0; k < kRowsEach; ++k) {  // rows kRowsEach (part % 4) + k of the thread's
+      const uint32_t in = kRowsEach * (part & 3) + k;
+      uint32_t byte = a.square ? square_byte : micro_scale_byte(most[k]);
       inverse[k] = micro_inverse(byte);
-      if (row >= a.rows || (c0 & ~31u) >= a.cols) byte = 127u;  // rows and blocks that do not exist, beside a square block that ends inside
-      const uint32_t next = __shfl_xor_sync(0xffffffffu, byte, 4);
-      if (part < 4) st_c(reinterpret_cast<uint16_t*>(a.scale + scale_offset(row, 4 * tile_c + 2 * (warp & 1), a.tiles_r)), (uint16_t)(byte | next << 8));
+      if (r0 + in >= a.rows || (c0 & ~31u) >= a.cols) byte = 127u;  // rows and blocks that do not exist, beside a square block that ends inside
+      bytes_r[r_in + in][c_in / 32] = (uint8_t)byte;
     }
     uint8_t* q = a.q + (uint64_t)r0 * a.ldq + c0 / 2;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float s = __shfl_sync(0xffffffffu, inverse[i & 1], (lane & ~3u) | (i >> 1));
+    for (int i = 0; i < ROWS; ++i) {
+      const float s = __shfl_sync(0xffffffffu, inverse[i % kRowsEach], (lane & ~3u) | (i / kRowsEach));
       float v[8];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -187,17 +241,16 @@ __global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T
       }
       uint32_t code;
       if constexpr (STOCHASTIC) {
-        uint32_t w[8], drawn[8];
-        if (!kKept) draw_row(i, drawn);
+        uint32_t w[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 f = split(mul2(pair_of(v[2 * j], v[2 * j + 1]), both(0x1p+25f)));
-          w[2 * j] = micro_stochastic(v[2 * j], f.x, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j] : drawn[2 * j]);
-          w[2 * j + 1] = micro_stochastic(v[2 * j + 1], f.y, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j + 1] : drawn[2 * j + 1]);
+          w[2 * j] = micro_stochastic(v[2 * j], f.x, numbers[i][2 * j]);
+          w[2 * j + 1] = micro_stochastic(v[2 * j + 1], f.y, numbers[i][2 * j + 1]);
         }
-        code = micro_join(w);
+        code = micro_join<8>(w);
       } else {
-        code = micro_encode(v);
+        code = micro_encode<8>(v);
       }
       if (r0 + i < a.rows && c0 / 2 < a.ldq) st_c(reinterpret_cast<uint32_t*>(q), s == 0.0f ? 0u : code);
       q += a.ldq;
@@ -205,65 +258,70 @@ __global__ void __launch_bounds__(256, ROUND != MicroRound::kNearest || sizeof(T
   }
 
   if (a.qt) {
-    // four lanes hold eight columns of a block, 32 rows: as above
-    float m[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const float away = lane & 16 ? col_most[k] : col_most[k + 4], keep = lane & 16 ? col_most[k + 4] : col_most[k];
-      m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 16));
+    float most[kColsEach];
+    {
+      float half[4], quarter[2];
+      halve_most<8>(col_most, lane & 16, 16, half);
+      halve_most<4>(half, lane & 8, 8, quarter);
+      if constexpr (kColsEach == 1) halve_most<2>(quarter, lane & 4, 4, most);
+      else { most[0] = quarter[0]; most[kColsEach - 1] = quarter[1]; }
     }
+    float inverse[kColsEach];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const float away = lane & 8 ? m[k] : m[k + 2], keep = lane & 8 ? m[k + 2] : m[k];
-      m[k] = max_nan(keep, __shfl_xor_sync(0xffffffffu, away, 8));
-    }
-    float inverse[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {  // columns 2 down + k of the eight
-      uint32_t byte = a.square ? square_byte : micro_scale_byte(m[k]);
+    for (int k = 0; k < kColsEach; ++k) {  // columns kColsEach down + k of the eight
+      const uint32_t in = kColsEach * down + k;
+      uint32_t byte = a.square ? square_byte : micro_scale_byte(most[k]);
       inverse[k] = micro_inverse(byte);
-      if (c0 + 2 * down + k >= a.cols || (r0 & ~31u) >= a.rows) byte = 127u;
-      bytes_t[c_in + 2 * down + k][warp >> 1] = (uint8_t)byte;
+      if (c0 + in >= a.cols || (r0 & ~31u) >= a.rows) byte = 127u;
+      bytes_t[c_in + in][warp_r] = (uint8_t)byte;
     }
-    // Column c of the tile is 16 words (eight rows each), those of 32 rows side by side, u-th four at place u ^ (c / 8 % 4): the lanes
-    // that write the words of different columns meet different places.
-    uint8_t* word = turned + c_in * (kTile / 2) + 16 * ((warp >> 1) ^ (part & 3)) + 4 * down;
+    // Column c of the tile is 64 bytes, ROWS rows of one thread side by side, 32 rows 16 bytes; u-th 16 at place u ^ (c / 8 % 4): the
+    // lanes that write different columns meet different places.
+    uint8_t* place = turned + c_in * (kTile / 2) + 16 * (warp_r ^ (part & 3)) + ROWS / 2 * down;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float s0 = __shfl_sync(0xffffffffu, inverse[0], part | j << 3), s1 = __shfl_sync(0xffffffffu, inverse[1], part | j << 3);
+      const float s0 = __shfl_sync(0xffffffffu, inverse[0], part | (2 * j / kColsEach) * kAcross);
+      const float s1 = __shfl_sync(0xffffffffu, inverse[kColsEach - 1], part | ((2 * j + 1) / kColsEach) * kAcross);
       const Pair scale = pair_of(s0, s1);
-      float left[8], right[8];
+      float left[ROWS], right[ROWS];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < ROWS; ++i) {
         const float2 f = split(mul2(held_pair(h, i, j), scale));
         left[i] = f.x;
         right[i] = f.y;
       }
       uint32_t code[2];
       if constexpr (STOCHASTIC) {
-        uint32_t w[2][8], drawn[8];
+        uint32_t w[2][ROWS];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (!kKept) draw_row(i, drawn);  // what this pair of columns does not need falls away
+        for (int i = 0; i < ROWS; ++i) {
           const float2 f = split(mul2(pair_of(left[i], right[i]), both(0x1p+25f)));
-          w[0][i] = micro_stochastic(left[i], f.x, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j] : drawn[2 * j]);
-          w[1][i] = micro_stochastic(right[i], f.y, kKept ? numbers[i % (kKept ? 8 : 1)][2 * j + 1] : drawn[2 * j + 1]);
+          w[0][i] = micro_stochastic(left[i], f.x, numbers[i][2 * j]);
+          w[1][i] = micro_stochastic(right[i], f.y, numbers[i][2 * j + 1]);
         }
-        code[0] = micro_join(w[0]);
-        code[1] = micro_join(w[1]);
+        code[0] = micro_join<ROWS>(w[0]);
+        code[1] = micro_join<ROWS>(w[1]);
       } else {
-        code[0] = micro_encode(left);
-        code[1] = micro_encode(right);
+        code[0] = micro_encode<ROWS>(left);
+        code[1] = micro_encode<ROWS>(right);
       }
-      *reinterpret_cast<uint32_t*>(word + 2 * j * (kTile / 2)) = s0 == 0.0f ? 0u : code[0];
-      *reinterpret_cast<uint32_t*>(word + (2 * j + 1) * (kTile / 2)) = s1 == 0.0f ? 0u : code[1];
-    }
-    __syncthreads();
-    if (t < kTile)
-      st_c(reinterpret_cast<uint32_t*>(a.scale_t + scale_offset(tile_c * kTile + t, 4 * tile_r, a.tiles_c)), *reinterpret_cast<const uint32_t*>(bytes_t[t]));
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {  // four threads a column, 16 bytes each
-      const uint32_t c = (t >> 2) + 64 * k, u = t & 3;
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t w = (k ? s1 : s0) == 0.0f ? 0u : code[k];
+        if constexpr (ROWS == 8) *reinterpret_cast<uint32_t*>(place + (2 * j + k) * (kTile / 2)) = w;
+        else *reinterpret_cast<uint16_t*>(place + (2 * j + k) * (kTile / 2)) = (uint16_t)w;
+      }
+    }
+  }
+  __syncthreads();
+  if (t < kTile) {
+    if (a.q) st_c(reinterpret_cast<uint32_t*>(a.scale + scale_offset(tile_r * kTile + t, 4 * tile_c, a.tiles_r)), *reinterpret_cast<const uint32_t*>(bytes_r[t]));
+    if (a.qt) st_c(reinterpret_cast<uint32_t*>(a.scale_t + scale_offset(tile_c * kTile + t, 4 * tile_r, a.tiles_c)), *reinterpret_cast<const uint32_t*>(bytes_t[t]));
+  }
+  if (a.qt) {
+#pragma unroll
+    for (int k = 0; k < kTile / (kMicroThreads<T, ROUND> / 4); ++k) {  // four threads a column, 16 bytes each
+      const uint32_t c = (t >> 2) + kMicroThreads<T, ROUND> / 4 * k, u = t & 3;
       const uint4 w = *reinterpret_cast<const uint4*>(turned + c * (kTile / 2) + 16 * (u ^ (c >> 3 & 3)));
       const uint32_t byte = tile_r * (kTile / 2) + 16 * u;
       if (tile_c * kTile + c < a.cols && byte < a.ldqt) st_c(reinterpret_cast<uint4*>(a.qt + (uint64_t)(tile_c * kTile + c) * a.ldqt + byte), w);
