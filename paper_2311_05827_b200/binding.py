@@ -616,7 +616,7 @@ def accept_dropout_check_params(p: DropoutParams) -> int:
 
 def accept_dropout(p: DropoutParams, d_x, d_residual, d_y, stream=None) -> None:
     """d_residual may be None.  The backward pass is the same call with dy in the place of x and no residual."""
-    code = lib().accept_dropout(p._ref, d_x.data_ptr(), None if d_residual is None else d_residual.data_ptr(), d_y.data_ptr(), _stream_handle(stream))
+    code = (_lib or lib()).accept_dropout(p._ref, d_x.data_ptr(), None if d_residual is None else d_residual.data_ptr(), d_y.data_ptr(), _stream_handle(stream))
     if code:
         raise AcceptError(code, "accept_dropout")
 
@@ -632,7 +632,7 @@ def accept_rms_norm_workspace_size(p: RmsNormParams) -> int:
 def accept_rms_norm_forward(p: RmsNormParams, d_x, d_branch, d_gamma, d_sum, d_y, d_q=None, d_scale=None, d_rstd=None, d_ws=None, stream=None) -> None:
     """d_branch and d_gamma may be None; so may the outputs: d_sum, d_y, d_q with d_scale (uint8, as accept_block_quantize writes them; with d_ws) and
     d_rstd (float32, p.rows elements, kept for the backward pass)."""
-    code = lib().accept_rms_norm_forward(
+    code = (_lib or lib()).accept_rms_norm_forward(
         p._ref, d_x.data_ptr(), None if d_branch is None else d_branch.data_ptr(), None if d_gamma is None else d_gamma.data_ptr(),
         None if d_sum is None else d_sum.data_ptr(), None if d_y is None else d_y.data_ptr(), None if d_q is None else d_q.data_ptr(),
         None if d_scale is None else d_scale.data_ptr(), None if d_rstd is None else d_rstd.data_ptr(),
@@ -643,7 +643,7 @@ def accept_rms_norm_forward(p: RmsNormParams, d_x, d_branch, d_gamma, d_sum, d_y
 
 def accept_rms_norm_backward(p: RmsNormParams, d_dy, d_s, d_gamma, d_rstd, d_dsum, d_dx, d_dbranch, d_dgamma, d_ws, stream=None) -> None:
     """d_gamma and d_dsum may be None; so may the outputs d_dx, d_dbranch and d_dgamma (float32, p.cols elements): not computed."""
-    code = lib().accept_rms_norm_backward(
+    code = (_lib or lib()).accept_rms_norm_backward(
         p._ref, d_dy.data_ptr(), d_s.data_ptr(), None if d_gamma is None else d_gamma.data_ptr(), d_rstd.data_ptr(),
         None if d_dsum is None else d_dsum.data_ptr(), None if d_dx is None else d_dx.data_ptr(),
         None if d_dbranch is None else d_dbranch.data_ptr(), None if d_dgamma is None else d_dgamma.data_ptr(), d_ws.data_ptr(), d_ws.nbytes,
@@ -671,7 +671,7 @@ def accept_micro_workspace_size(p: MicroParams) -> int:
 def accept_micro_quantize(p: MicroParams, d_x, d_q, d_scale, d_qt, d_scale_t, d_ws, stream=None) -> None:
     """d_q / d_scale (codes along the columns) or d_qt / d_scale_t (the transpose, codes along the rows) may be None:
     uint8 CUDA tensors of accept_micro_data_size and accept_micro_scale_size bytes."""
-    code = lib().accept_micro_quantize(
+    code = (_lib or lib()).accept_micro_quantize(
         p._ref, d_x.data_ptr(), None if d_q is None else d_q.data_ptr(), None if d_scale is None else d_scale.data_ptr(),
         None if d_qt is None else d_qt.data_ptr(), None if d_scale_t is None else d_scale_t.data_ptr(), d_ws.data_ptr(), d_ws.nbytes,
         _stream_handle(stream))
@@ -681,7 +681,7 @@ def accept_micro_quantize(p: MicroParams, d_x, d_q, d_scale, d_qt, d_scale_t, d_
 
 def accept_micro_dequantize(p: MicroParams, d_q, d_scale, d_x, stream=None) -> None:
     """The values of a p.rows x p.cols matrix in d_x (p.dtype, p.ld) from its codes by rows and their scales."""
-    code = lib().accept_micro_dequantize(p._ref, d_q.data_ptr(), d_scale.data_ptr(), d_x.data_ptr(), _stream_handle(stream))
+    code = (_lib or lib()).accept_micro_dequantize(p._ref, d_q.data_ptr(), d_scale.data_ptr(), d_x.data_ptr(), _stream_handle(stream))
     if code:
         raise AcceptError(code, "accept_micro_dequantize")
 
@@ -696,7 +696,7 @@ def accept_micro_matmul_workspace_size(p: MicroMatmulParams) -> int:
 
 def accept_micro_matmul(p: MicroMatmulParams, d_a, d_a_scale, d_b, d_b_scale, d_bias, d_d, d_ws, stream=None) -> None:
     """d_bias: float32 CUDA tensor of p.n elements, or None."""
-    code = lib().accept_micro_matmul(
+    code = (_lib or lib()).accept_micro_matmul(
         p._ref, d_a.data_ptr(), d_a_scale.data_ptr(), d_b.data_ptr(), d_b_scale.data_ptr(), None if d_bias is None else d_bias.data_ptr(),
         d_d.data_ptr(), d_ws.data_ptr(), d_ws.nbytes, _stream_handle(stream))
     if code:

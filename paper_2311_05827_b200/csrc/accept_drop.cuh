@@ -42,6 +42,8 @@ struct DropRow {
 
 __device__ __forceinline__ uint32_t lane_factor(uint32_t m) { return m == 0 ? 1u : m == 1 ? 0x9E3779B1u : m == 2 ? 0x85EBCA77u : 0xC2B2AE3Du; }
 
+static __constant__ uint32_t kLaneFactors[8] = {1u, 0x9E3779B1u, 0x85EBCA77u, 0xC2B2AE3Du, 1u, 0x9E3779B1u, 0x85EBCA77u, 0xC2B2AE3Du};
+
 // Random words of UNITS units of N neighbours (or their complements, NOT: ~(h M) = -h M - 1 costs nothing more), the first from column
 // `col` on and `step` columns apart (multiples of four), for take(unit, words).  A hash serves four counters; where the row's counters do
 // not start on a multiple of four, four columns take theirs from two hashes, split at the same place in the whole row.
@@ -64,7 +66,7 @@ __device__ __forceinline__ void number_units(const DropRow& r, uint32_t col, uin
   } else {
     uint32_t times[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) times[e] = lane_factor((r.phase + e) & 3);
+    for (int e = 0; e < 4; ++e) times[e] = kLaneFactors[r.phase + e];
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       uint32_t w[N], h[N / 4 + 1];
