@@ -280,7 +280,8 @@ __device__ __forceinline__ void pad_scales(const RmsArgs& a) {
     st_c(reinterpret_cast<uint32_t*>(a.scale + scale_offset((uint32_t)a.rows + i / words, i % words * 4, a.atoms)), 0x7f7f7f7fu);
 }
 
-template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES, bool LOOSE>
+// CODES: with 8-bit codes.  One kernel for both is slower without: 16384 x 4096 bf16 with dropped branch to bf16 97 us against 82.
+template <typename TX, typename TY, int V, bool FULL, int OWN, int L, int STAGES, bool LOOSE, bool CODES>
 __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L>& g, float (&slots)[3][16], uint32_t shared, uint32_t space, uint32_t space_x,
                                                  uint64_t first, uint32_t step) {
   const uint32_t t = g.t, shared_end = shared + STAGES * space;
@@ -339,7 +340,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
 #pragma unroll
     for (int i = 0; i < OWN / 2; ++i) v[i] = mul2(mul2(v[i], both(rstd)), gamma[i]);
     if (a.y) store_any<TY, V, FULL, OWN, L, LOOSE>(static_cast<TY*>(a.y) + r * a.ld_y, here + space_x, a.cols, t, g.mask, own, v);
-    if (a.q) {
+    if (CODES && a.q) {
       if (!FULL)  // zero bytes behind the row's end, whatever its rstd is
 #pragma unroll
         for (int i = 0; i < OWN / 2; ++i) {
@@ -360,7 +361,7 @@ __device__ __forceinline__ void rms_forward_rows(const RmsArgs& a, const Group<L
   }
 }
 
-template <typename TX, typename TY, int V, int OWN, int L, int STAGES, bool LOOSE>
+template <typename TX, typename TY, int V, int OWN, int L, int STAGES, bool LOOSE, bool CODES>
 __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
   __shared__ __align__(16) float slots[kMostGroups][3][16];
   const Group<L> g(a.warps);
@@ -383,10 +384,10 @@ __global__ void __launch_bounds__(512) rms_forward_kernel(const RmsArgs a) {
     g.sync();
   }
   grid_dependency_handshake();
-  if (a.q) pad_scales(a);
+  if (CODES && a.q) pad_scales(a);
   if (first >= a.rows) return;
-  if (full) rms_forward_rows<TX, TY, V, true, OWN, L, STAGES, LOOSE>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
-  else rms_forward_rows<TX, TY, V, false, OWN, L, STAGES, LOOSE>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
+  if (full) rms_forward_rows<TX, TY, V, true, OWN, L, STAGES, LOOSE, CODES>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
+  else rms_forward_rows<TX, TY, V, false, OWN, L, STAGES, LOOSE, CODES>(a, g, slots[g.index % kMostGroups], shared, space, space_x, first, step);
 }
 
 // Backward: dx = rstd (h - xhat mean(h xhat)) + dsum, h = dy gamma, xhat = x rstd; the sum over the rows (dgamma) is held in registers over

@@ -8,12 +8,14 @@ using namespace accept;
 bool is_dtype(int32_t d) { return d == ACCEPT_DTYPE_F32 || d == ACCEPT_DTYPE_BF16 || d == ACCEPT_DTYPE_F16; }
 uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
 
-template <typename TX, typename TY>
-struct Forward {
+template <typename TX, typename TY, bool CODES>
+struct ForwardTo {
   static constexpr int kStages = rms_stages_for((int)(sizeof(TX) + sizeof(TY)));
-  template <int V, int L, bool LOOSE> static RmsKernel held() { return rms_forward_kernel<TX, TY, V, kRmsOwn, L, kStages, LOOSE>; }
+  template <int V, int L, bool LOOSE> static RmsKernel held() { return rms_forward_kernel<TX, TY, V, kRmsOwn, L, kStages, LOOSE, CODES>; }
   template <bool VEC> static RmsKernel wide() { return rms_forward_wide_kernel<TX, TY, VEC>; }
 };
+template <typename TX, typename TY> using Forward = ForwardTo<TX, TY, false>;
+template <typename TX, typename TY> using ForwardToCodes = ForwardTo<TX, TY, true>;
 
 }  // namespace
 
@@ -86,7 +88,7 @@ accept_status accept_rms_norm_forward(const accept_rms_norm_params* p, const voi
   };
   const bool whole = all(rms_whole_rows);
   const RmsShape shape = rms_shape(p, false, whole, 1, d_branch || !whole ? 1 : 0);
-  ACCEPT_LAUNCH(launch_rms(rms_kernel<Forward>(p, shape, whole), shape, a, s));
+  ACCEPT_LAUNCH(launch_rms(d_q ? rms_kernel<ForwardToCodes>(p, shape, whole) : rms_kernel<Forward>(p, shape, whole), shape, a, s));
   return ACCEPT_OK;
 }
 
