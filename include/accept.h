@@ -384,6 +384,7 @@ accept_status accept_block_matmul(const accept_matmul_params* p, const void* d_a
  * Dropout: y[i][j] = residual[i][j] + (U >= p ? x[i][j] / (1 - p) : 0), U the number of counter rng_offset + i cols + j (mod 2^64) under
  * `seed`, drawn as at accept_params.seed.  No mask is stored: the backward pass is the same call with dy in the place of x and no
  * residual (the residual's gradient is dy itself).  Advance rng_offset by rows * cols between calls to draw fresh numbers.
+ * Seed and counter are taken when the call is made: a captured call draws the same numbers at every replay.
  *   p            0 (nothing is dropped) to 1 (everything is); 1 / (1 - p) is rounded to fp32 once, product and sum are fp32
  *                operations, y is rounded once.  What is dropped is 0, also where x is a NaN or an infinity.
  *   rows, cols   >= 0;  ld_x, ld_y: values between the starts of two rows of x, and of residual and y (>= cols).

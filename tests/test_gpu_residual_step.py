@@ -1,5 +1,7 @@
 """The operators of a residual stage together, as the example uses them: its output and gradients against 64-bit formulas on what the
 codes stand for."""
+import threading
+
 import pytest
 
 from tests import operators_plain as plain8
@@ -86,3 +88,70 @@ def test_example_runs():
     from examples import residual_stage as example
     errors = example.run(256, 512, 384, seed=3)
     assert set(errors) == {"y", "dx", "dbranch", "dweight", "dgamma", "answer"} and all(e == e for e in errors.values())
+
+
+def test_two_streams_and_several_host_threads_at_once():
+    """Stages of different sizes, each with buffers and workspaces of its own, stepped by four host threads on their own streams at the same
+    time: the bits of each are those of the same steps made one after the other."""
+    from examples import residual_stage as example
+    sizes = [(300, 520, 200), (64, 4096, 128), (1000, 77, 260), (129, 2048, 1030)]
+
+    def stages():
+        made = []
+        for k, (tokens, width, features) in enumerate(sizes):
+            i = example.inputs(tokens, width, features, k)
+            made.append((i, example.Stage(tokens, width, features, i["weight"], i["bias"], i["gamma"], 0.1, k)))
+        torch.cuda.synchronize()
+        return made
+
+    def steps(i, stage):
+        for number in range(8):
+            stage.forward(i["x"], i["branch"], number)
+            stage.backward(i["dout"], i["dsum"], number)
+
+    results = lambda stage: [stage.sum, stage.normed, stage.out, stage.dnormed, stage.dweight, stage.dx, stage.dbranch, stage.dgamma]  # noqa: E731
+    one, errors = stages(), []
+    for i, stage in one:
+        steps(i, stage)
+    torch.cuda.synchronize()
+    many = stages()
+
+    def work(i, stage):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                steps(i, stage)
+        except Exception as e:  # noqa: BLE001
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=m) for m in many]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for (_, a), (_, b) in zip(one, many):
+        assert b.status() == 0 and all(torch.equal(u, v) for u, v in zip(results(a), results(b)))
+
+
+def test_captured_step_is_replayed():
+    """A whole step in a graph, replayed on new inputs: the bits of the calls themselves, the numbers of the captured counters."""
+    i, stage, _, _, _ = step(200, 328, 264)
+    other = {k: v.clone() for k, v in i.items()}
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        stage.forward(other["x"], other["branch"], 6)
+        stage.backward(other["dout"], other["dsum"], 6)
+    for scale in (1.0, 0.5):
+        for k in ("x", "branch", "dout", "dsum"):
+            other[k].copy_(i[k] * scale)
+        stage.dweight.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (stage.out, stage.dx, stage.dbranch, stage.dgamma, stage.dweight)]
+        stage.dweight.zero_()
+        stage.forward(other["x"], other["branch"], 6)
+        stage.backward(other["dout"], other["dsum"], 6)
+        torch.cuda.synchronize()
+        assert all(torch.equal(u, v) for u, v in zip(got, (stage.out, stage.dx, stage.dbranch, stage.dgamma, stage.dweight)))
