@@ -44,11 +44,12 @@ __device__ __forceinline__ uint32_t lane_factor(uint32_t m) { return m == 0 ? 1u
 
 static __constant__ uint32_t kLaneFactors[8] = {1u, 0x9E3779B1u, 0x85EBCA77u, 0xC2B2AE3Du, 1u, 0x9E3779B1u, 0x85EBCA77u, 0xC2B2AE3Du};
 
-// Random words of UNITS units of N neighbours (or their complements, NOT: ~(h M) = -h M - 1 costs nothing more), the first from column
-// `col` on and `step` columns apart (multiples of four), for take(unit, words).  A hash serves four counters; where the row's counters do
-// not start on a multiple of four, four columns take theirs from two hashes, split at the same place in the whole row.
+// Random words of UNITS units of N neighbours (or their complements, NOT: ~(h M) = -h M - 1 costs nothing more), the first from the
+// quad-th four columns on (columns themselves may pass 32 bits) and `step` columns apart (a multiple of four), for take(unit, words).  A hash
+// serves four counters; where the row's counters do not start on a multiple of four, four columns take theirs from two hashes, split at
+// the same place in the whole row.
 template <int N, bool NOT, int UNITS, typename Take>
-__device__ __forceinline__ void number_units(const DropRow& r, uint32_t col, uint32_t step, const Take& take) {
+__device__ __forceinline__ void number_units(const DropRow& r, uint32_t quad, uint32_t step, const Take& take) {
   constexpr uint32_t kAdd = NOT ? 0xffffffffu : 0u;
   if (r.phase == 0) {
 #pragma unroll
@@ -56,7 +57,7 @@ __device__ __forceinline__ void number_units(const DropRow& r, uint32_t col, uin
       uint32_t w[N];
 #pragma unroll
       for (int i = 0; i < N; i += 4) {
-        uint32_t h = r.hash((col + u * step + i) / 4);
+        uint32_t h = r.hash(quad + u * (step / 4) + i / 4);
         if (NOT) h = 0u - h;
 #pragma unroll
         for (int e = 0; e < 4; ++e) w[i + e] = h * lane_factor(e) + kAdd;
@@ -72,7 +73,7 @@ __device__ __forceinline__ void number_units(const DropRow& r, uint32_t col, uin
       uint32_t w[N], h[N / 4 + 1];
 #pragma unroll
       for (int i = 0; i <= N / 4; ++i) {
-        h[i] = r.hash((col + u * step) / 4 + i);
+        h[i] = r.hash(quad + u * (step / 4) + i);
         if (NOT) h[i] = 0u - h[i];
       }
 #pragma unroll
@@ -90,10 +91,10 @@ __device__ __forceinline__ void drop_values(const Drop& d, const uint32_t (&w)[N
     v[i] = pair_of(w[2 * i] > d.limit ? f.x : 0.0f, w[2 * i + 1] > d.limit ? f.y : 0.0f);
   }
 }
-// UNITS units of N values each, as above.
+// UNITS units of N values each, the first from column `col` on, a multiple of four.
 template <int N, int UNITS>
 __device__ __forceinline__ void drop_units(const Drop& d, const DropRow& r, uint32_t col, uint32_t step, Pair* v) {
-  number_units<N, false, UNITS>(r, col, step, [&](int u, const uint32_t (&w)[N]) { drop_values<N>(d, w, v + u * (N / 2)); });
+  number_units<N, false, UNITS>(r, col / 4, step, [&](int u, const uint32_t (&w)[N]) { drop_values<N>(d, w, v + u * (N / 2)); });
 }
 
 }  // namespace accept

@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kMicroThreads<T, ROUND>, kMicroRows<T, ROUND> 
 #pragma unroll
         for (int j = 0; j < 8; ++j) numbers[i][j] = w[j] >> 4;
       };
-      if (ROUND == MicroRound::kQuads) number_units<8, true, 1>(quads, i * (a.cols & ~3u), 0, keep);
+      if (ROUND == MicroRound::kQuads) number_units<8, true, 1>(quads, i * (a.cols / 4), 0, keep);  // below 2^32: columns would wrap
       else number_units<8, true, 1>(DropRow(a.rng, first + (uint64_t)i * a.cols, key), 0, 0, keep);
     }
   }
