@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
   constexpr uint32_t kEach = 16 / (uint32_t)sizeof(TY);
   const uint32_t rows_at_once = kDropThreads >> a.log_units;
   const uint64_t unit = ((uint64_t)blockIdx.x << a.log_units) + (threadIdx.x & ((1u << a.log_units) - 1));
-  const bool behind_start = unit > 0, before_end = unit * 8 + 8 < a.cols;
+  const bool behind_start = unit > 0, before_end = unit * 8 + 9 < a.cols;
   const uint64_t groups = (a.rows + rows_at_once * ROWS - 1) / (rows_at_once * ROWS);
   const DropKey key(a.drop.rng, a.drop.offset + blockIdx.y * (uint64_t)(rows_at_once * ROWS) * a.cols);
   for (uint64_t group = blockIdx.y; group < groups; group += gridDim.y) {
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(const DropoutArgs
     int lo[ROWS], hi[ROWS];
     const TX* x[ROWS];
     const TY* residual[ROWS];
-    bool inner = true;  // all eight exist, and the value on either side lies in the matrix
+    bool inner = true;  // all eight exist, and the value before and the two behind lie in the matrix
 #pragma unroll
     for (int i = 0; i < ROWS; ++i) {
       const uint64_t r = r0 + i * rows_at_once;

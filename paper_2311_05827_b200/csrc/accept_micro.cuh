@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(kMicroThreads<T, ROUND>, kMicroRows<T, ROUND> 
   {
     const T* p = static_cast<const T*>(a.x) + (uint64_t)r0 * a.ld + c0;
     const int n = c0 < a.cols ? (int)min(a.cols - c0, 8u) : 0;
-    if (!WHOLE && sizeof(T) == 2 && n == 8 && (r0 > 0 || c0 > 0) && (r0 + ROWS < a.rows || (r0 + ROWS == a.rows && c0 + 8 < a.cols))) {
+    if (!WHOLE && sizeof(T) == 2 && n == 8 && (r0 > 0 || c0 > 0) && (r0 + ROWS < a.rows || (r0 + ROWS == a.rows && c0 + 9 < a.cols))) {
       RawEight<T> raw[ROWS];
 #pragma unroll
       for (int i = 0; i < ROWS; ++i) load_raw<T>(p + i * a.ld, raw[i]);

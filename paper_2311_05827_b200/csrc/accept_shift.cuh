@@ -19,8 +19,8 @@ __device__ __forceinline__ void shifted_words(const uint32_t (&c)[N + M], uint32
   for (int i = 0; i < N; ++i) out[i] = __byte_perm(w[i], w[i + 1], pick);
 }
 
-// Eight neighbours at p, a 16-bit type's from the five 4-byte words that hold them (one value before and after may be read).  The words
-// of several units are loaded before the first is used.
+// Eight neighbours at p, a 16-bit type's from five 4-byte words: where p is off a word, the value before and the one behind are read too,
+// else the two behind.  The words of several units are loaded before the first is used.
 template <typename T> struct RawEight { uint32_t c[sizeof(T) == 2 ? 5 : 8]; };
 __device__ __forceinline__ uint32_t ld_word(uintptr_t p) {
   uint32_t w = 0;

@@ -1,15 +1,17 @@
-"""Operators of a residual stage where sizes pass 32 bits, against 64-bit plain forms of parts of the matrix and against the same calls on
-rows side by side."""
+"""Operators of a residual stage at the ends of their matrices and where sizes pass 32 bits, against 64-bit plain forms."""
 import pytest
 
+from tests import gpu_util
 from tests import residual_plain as plain
-from tests.test_gpu_operators import code_of, random
+from tests.test_gpu_micro import check_quantize
+from tests.test_gpu_operators import code_of, matrix, random
+from tests.test_gpu_residual import check_dropout, same
 
 pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-F32, BF16 = torch.float32, torch.bfloat16
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 
 
 @pytest.fixture(scope="module")
@@ -38,3 +40,26 @@ def test_stochastic_codes_of_very_wide_rows(A, dtype, rows, cols, first):
         for c in (0, cols // 64 * 32, cols - part):
             codes, _ = plain.code4(x[r:r + 1, c:c + part], False, plain.draws(1, part, seed, first + r * cols + c))
             assert torch.equal(q[r:r + 1, c // 2:(c + part) // 2], plain.packed4(codes)), (r, c)
+
+
+def test_nothing_is_read_behind_a_matrix_that_ends_one_value_past_a_unit(A):
+    """16-bit values read as words off 16-byte boundaries, the last unit of eight on a 4-byte one: the word behind it holds the last value
+    and one that does not exist.  On the checking build, which compares each access with the bytes of the call's matrices."""
+    with gpu_util.library_variant("bounds"):
+        assert A.accept_bounds_check_report()[:2] == (0, 0)
+        for dtype in (BF16, F16):
+            for rows, cols, pad, offset in ((8, 1001, 1, 0), (16, 1001, 1, 2), (8, 9, 1, 0), (136, 137, 1, 4), (8, 1001, 0, 1)):
+                for stochastic in (False, True):
+                    check_quantize(A, random(rows, rows, cols).to(dtype), pad, offset, False, stochastic)
+            for rows, cols, pad, offset in ((1, 5001, 0, 2), (1, 9, 0, 2), (3, 1001, 7, 2), (31, 25, 7, 4), (1, 5001, 0, 3), (2, 5000, 1, 1)):
+                for to in (dtype, F32):
+                    check_dropout(A, rows, cols, pad, pad, offset, dtype, to, True, 0.1, 5)
+            # the residual off a boundary, beside x and y on one
+            x, r = random(1, 1, 5001).to(dtype), random(2, 1, 5001).to(dtype)
+            for offset in (2, 3, 4):
+                (_, vx), (_, vr), (gy, y) = matrix(1, 5001, 5001, dtype, x), matrix(1, 5001, 5001, dtype, r, offset), matrix(1, 5001, 5001, dtype)
+                A.accept_dropout(A.DropoutParams(1, 5001, 0.1, code_of(A, dtype), code_of(A, dtype), 3, 6), vx, vr, y)
+                assert same(y, (plain.dropped32(x, 0.1, 3, 6) + r.float()).to(dtype))
+                gy.check()
+        code, count, addr, size, write = A.accept_bounds_check_report()
+        assert (code, count) == (0, 0), f"{count} accesses outside, first at {addr:#x} ({size} bytes, write={write})"
