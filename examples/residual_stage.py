@@ -20,6 +20,12 @@ import paper_2311_05827_b200 as A
 
 EPS = 1e-5
 
+# Relative errors that coding explains for inputs() of 256 tokens, 512 values, 384 features, and a sixth (answer: a third) above them.  Coding in
+# 4 bits costs normal values 0.115 in blocks of 32, weights 0.126 in squares, the gradient with stochastic rounding 0.166; the errors of a
+# product's two sides are independent: y 0.17, dweight 0.20, dnormed and so dgamma 0.21, of which dx and dbranch carry half beside dsum,
+# 0.107.  In 8 bits each side costs 0.026, so the answer 0.037.
+LIMITS = {"y": 0.2, "dx": 0.125, "dbranch": 0.125, "dweight": 0.235, "dgamma": 0.25, "answer": 0.05}
+
 
 class Coded:
     """A matrix in 4-bit blocks: codes and scales by rows and by columns."""

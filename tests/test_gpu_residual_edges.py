@@ -63,3 +63,16 @@ def test_nothing_is_read_behind_a_matrix_that_ends_one_value_past_a_unit(A):
                 gy.check()
         code, count, addr, size, write = A.accept_bounds_check_report()
         assert (code, count) == (0, 0), f"{count} accesses outside, first at {addr:#x} ({size} bytes, write={write})"
+
+
+def test_example_is_as_near_as_its_codes(A, monkeypatch):
+    """The example's outputs and gradients against fp32 operations: no further off than coding explains.  Where those draw the mask of
+    other counters, as a wrong mask in the library would look, all that depends on it is."""
+    from examples import residual_stage as example
+    for seed in range(3):
+        errors = example.run(256, 512, 384, seed=seed)
+        assert set(errors) == set(example.LIMITS) and all(errors[k] < limit for k, limit in example.LIMITS.items()), errors
+    params = A.DropoutParams
+    monkeypatch.setattr(example.A, "DropoutParams", lambda *a, rng_offset, **more: params(*a, rng_offset=rng_offset + 4, **more))
+    errors = example.run(256, 512, 384)
+    assert all(errors[k] > example.LIMITS[k] for k in ("y", "dbranch", "dweight")), errors
