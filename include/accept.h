@@ -487,8 +487,10 @@ size_t accept_micro_workspace_size(const accept_micro_params* p);
 /* q and its scales, or q_t and its scales, may be NULL; not both.  x may have any alignment of its values. */
 accept_status accept_micro_quantize(const accept_micro_params* p, const void* d_x, void* d_q, void* d_scale, void* d_qt, void* d_scale_t,
                                   void* d_ws, size_t ws_bytes, void* cuda_stream);
-/* The values that codes by rows stand for: x[i][j] = code 2^(scale byte - 127) (byte 255: NaN), rounded to dtype once (exact but for the range of
- * fp16).  p gives rows, cols, ld and dtype of x; its round, block, seed and rng_offset are not used.  Codes of a transpose are those
+/* The values that codes by rows stand for: x[i][j] = code 2^(scale byte - 127) (byte 255: NaN), rounded to dtype once: exact but where that
+ * leaves dtype's range.  So does 2^128, as which the quantiser may code values of fp32 and bf16 from 1.5 2^127 on (NEAREST: from 1.75 2^127
+ * on), and 2^16 of fp16 likewise: they come back as infinities, without a bit in the status word; to a product they are the factors
+ * 2^128 and 2^16.  p gives rows, cols, ld and dtype of x; its round, block, seed and rng_offset are not used.  Codes of a transpose are those
  * of a cols x rows matrix. */
 accept_status accept_micro_dequantize(const accept_micro_params* p, const void* d_q, const void* d_scale, void* d_x, void* cuda_stream);
 

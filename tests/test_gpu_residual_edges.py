@@ -76,3 +76,27 @@ def test_example_is_as_near_as_its_codes(A, monkeypatch):
     monkeypatch.setattr(example.A, "DropoutParams", lambda *a, rng_offset, **more: params(*a, rng_offset=rng_offset + 4, **more))
     errors = example.run(256, 512, 384)
     assert all(errors[k] > example.LIMITS[k] for k in ("y", "dbranch", "dweight")), errors
+
+
+def test_values_at_the_top_of_the_range_round_up_past_it(A):
+    """From 1.75 2^127 on the nearest code stands for 4 2^126, which neither fp32 nor bf16 has; from 1.75 2^15 on for 2^16, which fp16 has not:
+    infinities, of which the status word says nothing.  As a factor such a code is 2^128."""
+    for dtype, top in ((F32, 127), (BF16, 127), (F16, 15)):
+        x = torch.zeros(4, 32, dtype=dtype, device="cuda")
+        x[0, 3], x[1, 4], x[2, 5], x[3, 6] = 1.75 * 2.0 ** top, -torch.finfo(dtype).max, 1.5 * 2.0 ** top, 1.625 * 2.0 ** top
+        p = A.MicroParams(4, 32, code_of(A, dtype))
+        q, s = (torch.empty(size(p), dtype=torch.uint8, device="cuda") for size in (A.accept_micro_data_size, A.accept_micro_scale_size))
+        ws, back = A.new_workspace(p), torch.empty_like(x)
+        A.accept_micro_quantize(p, x, q, s, None, None, ws)
+        A.accept_micro_dequantize(p, q, s, back)
+        assert A.accept_last_device_status(ws) == 0
+        want = torch.zeros_like(x)
+        want[0, 3], want[1, 4], want[2, 5], want[3, 6] = float("inf"), -float("inf"), 1.5 * 2.0 ** top, 1.5 * 2.0 ** top
+        assert torch.equal(back, want)
+        b = torch.full((16, 32), 2.0 ** -20, device="cuda")
+        pb, d = A.MicroParams(16, 32), torch.empty(4, 16, device="cuda")
+        qb, sb = (torch.empty(size(pb), dtype=torch.uint8, device="cuda") for size in (A.accept_micro_data_size, A.accept_micro_scale_size))
+        A.accept_micro_quantize(pb, b, qb, sb, None, None, A.new_workspace(pb))
+        g = A.MicroMatmulParams(4, 16, 32, A.DTYPE_F32)
+        A.accept_micro_matmul(g, q, s, qb, sb, None, d, A.new_workspace(g))
+        assert torch.equal(d, torch.tensor([2.0, -2.0, 1.5, 1.5], device="cuda")[:, None].expand(4, 16) * 2.0 ** (top - 20))
