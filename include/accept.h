@@ -455,7 +455,7 @@ accept_status accept_rms_norm_backward(const accept_rms_norm_params* p, const vo
  *   scale  a = the largest |x| of the block; e = the least integer with a 2^-e <= 6, held to -127 and above; 0 where a = 0.  Scale byte
  *          e + 127.  A block that holds a NaN or an infinity has scale byte 255 (NaN) and zero codes, and ACCEPT_DEV_NONFINITE
  *          is set in the status word.
- *   code   t = |x| 2^-e (exact) between two neighbours g < h of the list:  NEAREST: the nearer, a tie to the one with an even place in the
+ *   code   t = |x| 2^-e (exact, but that 2^-150 and less is 0) between two neighbours g < h of the list:  NEAREST: the nearer, a tie to the one with an even place in the
  *          list;  STOCHASTIC: h where U < (t - g) / (h - g), else g, U the number of counter rng_offset + i cols + j (mod 2^64) for x[i][j]
  *          under `seed`, drawn as at accept_params.seed; the comparison is exact.  Bits 0 to 2 are the place in the list, bit 3 the sign.
  * One read of x gives either or both of

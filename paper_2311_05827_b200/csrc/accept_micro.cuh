@@ -57,7 +57,8 @@ __device__ __forceinline__ uint32_t micro_encode(const float (&v)[N]) {
   }
   return r;
 }
-// One value (|v| <= 6, v25 = v 2^25) to a code with stochastic rounding, in exact fixed point: F = the value's place in the list of
+// One value (|v| <= 6, v25 = v 2^25; a value 2^-150 of its block's scale and less has come out as v = 0) to a code with stochastic rounding, in
+// exact fixed point: F = the value's place in the list of
 // codes times 2^24, rounded up, so that F + 2^24 - 1 - r carries into the next place where r 2^-24 is below the value's share of the
 // step.  From 1 on the list is that of fp32's own upper bits; below, steps are 0.5.  `less`: the upper 28 bits of the random word's
 // complement, 2^24 - 1 - r over four bits that change nothing beside a multiple of 16.  The code is in the top four bits, its sign

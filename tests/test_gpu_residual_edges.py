@@ -100,3 +100,18 @@ def test_values_at_the_top_of_the_range_round_up_past_it(A):
         g = A.MicroMatmulParams(4, 16, 32, A.DTYPE_F32)
         A.accept_micro_matmul(g, q, s, qb, sb, None, d, A.new_workspace(g))
         assert torch.equal(d, torch.tensor([2.0, -2.0, 1.5, 1.5], device="cuda")[:, None].expand(4, 16) * 2.0 ** (top - 20))
+
+
+def test_stochastic_codes_of_values_far_below_their_block(A):
+    """Where U = 0 any t above 0 is coded 0.5, but for t that fp32 has no value for, 2^-150 and less: those count as 0."""
+    seed, n = 5, 1 << 24
+    first = next(at + int(hit[0]) for at in range(0, 64 * n, n) for hit in [torch.nonzero(plain.draws(1, n, seed, at)[0] == 0)[:, 0]] if len(hit) and at + int(hit[0]) >= 5)
+    for dtype in (F32, BF16):
+        for t, code in ((2.0 ** -100, 1), (2.0 ** -149, 1), (1.5 * 2.0 ** -150, 1), (2.0 ** -150, 0), (2.0 ** -155, 0), (0.0, 0)):
+            for sign in (1, -1):
+                x = torch.zeros(1, 32, dtype=dtype, device="cuda")
+                x[0, 0], x[0, 5] = 2.0 ** 127, sign * t * 2.0 ** 125  # the block's scale is 2^125
+                p = A.MicroParams(1, 32, code_of(A, dtype), A.ROUND_STOCHASTIC, seed=seed, rng_offset=first - 5)
+                q, s = (torch.empty(size(p), dtype=torch.uint8, device="cuda") for size in (A.accept_micro_data_size, A.accept_micro_scale_size))
+                A.accept_micro_quantize(p, x, q, s, None, None, A.new_workspace(p))
+                assert int(s[0]) == 125 + 127 and int(q[2] >> 4) == code + (8 if sign < 0 else 0), (dtype, t, sign)
