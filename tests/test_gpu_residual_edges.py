@@ -115,3 +115,14 @@ def test_stochastic_codes_of_values_far_below_their_block(A):
                 q, s = (torch.empty(size(p), dtype=torch.uint8, device="cuda") for size in (A.accept_micro_data_size, A.accept_micro_scale_size))
                 A.accept_micro_quantize(p, x, q, s, None, None, A.new_workspace(p))
                 assert int(s[0]) == 125 + 127 and int(q[2] >> 4) == code + (8 if sign < 0 else 0), (dtype, t, sign)
+
+
+def test_masks_are_the_codecs_own_numbers(A):
+    """What dropout keeps, against the words of the codec's CPU implementation: U = (word >> 8) 2^-24."""
+    import oracle
+    n = 100_003
+    for seed, first, rate in ((1, 0, 0.1), (0xFEDCBA9876543210, (1 << 34) - 50_001, 0.5), (77, (1 << 64) - 1000, 0.9)):
+        y = torch.empty(n, device="cuda")
+        A.accept_dropout(A.DropoutParams(1, n, rate, seed=seed, rng_offset=first), torch.ones(n, device="cuda"), None, y)
+        numbers = torch.from_numpy(oracle.rng_words(seed, first, n).astype("int64") >> 8).cuda()
+        assert torch.equal(y > 0, numbers * 2.0 ** -24 >= plain.single(rate))
