@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kValueThreads) micro_dequantize_kernel(const M
       codes[i] = ldg_c(q + start / 8);
       byte[i] = next[i] = ldg_c(a.scale + scale_offset(row, start / 32, a.atoms));
       if (!WHOLE) {
-        const uint32_t end = min((uint32_t)(col[i] + 7), a.cols - 1);
+        const uint32_t end = min((uint32_t)col[i] + 7, a.cols - 1);
         uint32_t more = codes[i];
         if (end / 8 != start / 8) more = ldg_c(q + end / 8);
         if (end / 32 != start / 32) next[i] = ldg_c(a.scale + scale_offset(row, end / 32, a.atoms));
@@ -394,7 +394,7 @@ __global__ void __launch_bounds__(kValueThreads) micro_dequantize_kernel(const M
       const float s = micro_scale(byte[i]), s2 = WHOLE ? s : micro_scale(next[i]);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int lo = (col[i] + 2 * j) & 31, hi = (col[i] + 2 * j + 1) & 31;  // the second scale from the first boundary on
+        const int lo = ((uint32_t)col[i] + 2 * j) & 31, hi = ((uint32_t)col[i] + 2 * j + 1) & 31;  // the second scale from the first boundary on
         const bool second_lo = !WHOLE && col[i] >= 0 && lo < (col[i] & 31), second_hi = !WHOLE && col[i] >= 0 && hi < (col[i] & 31);
         v[j] = micro_value(codes[i], j, pair_of(second_lo ? s2 : s, second_hi ? s2 : s));
       }
@@ -405,8 +405,8 @@ __global__ void __launch_bounds__(kValueThreads) micro_dequantize_kernel(const M
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float2 f = split(v[j / 2]);
-          const int at = col[i] + j;
-          if (at >= 0 && (uint32_t)at < a.cols) st_c(x + at, from_float<T>(j % 2 ? f.y : f.x));
+          const uint32_t at = (uint32_t)col[i] + j;  // before the row: past every column
+          if (at < a.cols) st_c(x + at, from_float<T>(j % 2 ? f.y : f.x));
         }
       }
     }

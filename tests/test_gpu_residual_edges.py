@@ -126,3 +126,47 @@ def test_masks_are_the_codecs_own_numbers(A):
         A.accept_dropout(A.DropoutParams(1, n, rate, seed=seed, rng_offset=first), torch.ones(n, device="cuda"), None, y)
         numbers = torch.from_numpy(oracle.rng_words(seed, first, n).astype("int64") >> 8).cuda()
         assert torch.equal(y > 0, numbers * 2.0 ** -24 >= plain.single(rate))
+
+
+def test_operators_on_rows_that_lie_far_apart(A):
+    """Row strides of 2^31 values and more, all matrices in one buffer: the bits of the same calls on rows side by side."""
+    rows, cols, ld = 3, 300, (1 << 31) + 8
+    room = torch.empty(2 * ld + 9 * 512, dtype=BF16, device="cuda")
+    far = lambda k: torch.as_strided(room, (rows, cols), (ld, 1), 512 * k)  # noqa: E731
+    x, branch, dsum, dy = (random(k, rows, cols).to(BF16) for k in range(4))
+    gamma, results = 1 + 0.1 * random(5, cols), []
+    for apart in (False, True):
+        place = far if apart else lambda k: torch.empty(rows, cols, dtype=BF16, device="cuda")
+        step, names = ld if apart else cols, ("x", "branch", "dsum", "dy", "sum", "y", "dx", "dbranch", "out")
+        m = {name: place(k) for k, name in enumerate(names)}
+        for name, v in (("x", x), ("branch", branch), ("dsum", dsum), ("dy", dy)):
+            m[name].copy_(v)
+        p = A.RmsNormParams(rows, cols, 1e-5, A.DTYPE_BF16, A.DTYPE_BF16, A.DTYPE_F32, 0.2, 7, 11, ld_x=step, ld_y=step)
+        rstd, dgamma = torch.empty(rows, device="cuda"), torch.empty(cols, device="cuda")
+        A.accept_rms_norm_forward(p, m["x"], m["branch"], gamma, m["sum"], m["y"], None, None, rstd)
+        A.accept_rms_norm_backward(p, m["dy"], m["sum"], gamma, rstd, m["dsum"], m["dx"], m["dbranch"], dgamma, A.new_workspace(p))
+        A.accept_dropout(A.DropoutParams(rows, cols, 0.3, A.DTYPE_BF16, A.DTYPE_BF16, 5, 6, step, step), m["x"], m["branch"], m["out"])
+        found = [m[name].clone() for name in ("sum", "y", "dx", "dbranch", "out")] + [rstd, dgamma]
+        p = A.MicroParams(rows, cols, A.DTYPE_BF16, A.ROUND_STOCHASTIC, seed=3, rng_offset=4, ld=step)
+        codes = [torch.empty(size(p, side), dtype=torch.uint8, device="cuda") for side in (False, True) for size in (A.accept_micro_data_size, A.accept_micro_scale_size)]
+        A.accept_micro_quantize(p, m["x"], *codes, A.new_workspace(p))
+        A.accept_micro_dequantize(p, codes[0], codes[1], m["out"])
+        results.append(found + codes + [m["out"].clone()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_values_of_the_longest_row(A):
+    """2^31 - 1 values, off a 16-byte boundary: first, middle and last ones."""
+    cols, part = (1 << 31) - 1, 4096
+    p = A.MicroParams(1, cols, A.DTYPE_BF16)
+    q = torch.randint(0, 256, (A.accept_micro_data_size(p),), dtype=torch.uint8, device="cuda")
+    s = torch.randint(120, 130, (A.accept_micro_scale_size(p),), dtype=torch.uint8, device="cuda")
+    x = torch.full((cols + 18,), 7.0, dtype=BF16, device="cuda")
+    A.accept_micro_dequantize(p, q, s, x[9:9 + cols])
+    for c in (0, cols // 64 * 32, (cols - 1) // 32 * 32 - part):
+        n = min(2 * part, cols - c)
+        blocks = torch.arange(c // 32, -(-(c + n) // 32), device="cuda")
+        code = torch.stack([q[c // 2:c // 2 + part] & 15, q[c // 2:c // 2 + part] >> 4], 1).view(1, -1)[:, :n].long()
+        byte = s[plain.place(torch.zeros_like(blocks), blocks, 1)].long().view(1, -1)
+        assert torch.equal(x[9 + c:9 + c + n].double(), plain.values4(code, byte, n)[0]), c
+    assert bool((x[:9] == 7).all()) and bool((x[9 + cols:] == 7).all())
