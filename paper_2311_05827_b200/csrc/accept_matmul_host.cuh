@@ -112,7 +112,10 @@ PairPlan pair_plan(const accept_matmul_params* p, unsigned nt, uint64_t* cycles)
   s.parts = 1;
   s.whole = (uint32_t)s.tiles;
   // Measured at 16 to 128 blocks of k, one to four rounds: a block of k takes about 600 cycles with 256 columns and 480
-  // with 128 (whose operands' way into the SM binds it), a tile 2500 and 1500 more, the join of a cut tile 11000.
+  // with 128 (whose operands' way into the SM binds it), a tile 2500 and 1500 more, the join of a cut tile 11000.  That was 8-bit operands.
+  // With 4-bit ones, whose blocks are 256 values, every width, cut and the small kernel were timed on 24 products (k 171 to 40000): what these
+  // figures choose was the fastest or within 4 % of it, but for four that the other kernel does sooner: 700 x 1100 x 24000 (fp32 and bf16) 30 us
+  // here, 22 by small tiles; 500 x 700 x 40000 fp32 26 against 21; 512 x 512 x 4096 16 by small tiles, 11 here.
   const uint64_t block = nt == 256 ? 600 : 480, tile = nt == 256 ? 2500 : 1500, join = 11000;
   uint64_t last = left ? blocks * block + tile : 0;
   if (left != 0) {  // cut what is left so that all pairs share the last round, where the join costs less than that saves

@@ -137,8 +137,8 @@ enum class MicroRound { kNearest, kQuads, kAnywhere };
 // A tile is 8 or 16 warps of 32 rows by 64 or 32 columns, a thread has ROWS rows of eight neighbours.  A warp has whole blocks both ways,
 // so their largest values are found within it.  Eight rows; four for stochastic rounding of fp32, whose values and random numbers would
 // else not fit the registers (16384 x 4096 both ways 151 -> 138 us; no gain for bf16, 97 us).
-// Measured on 16384 x 4096 bf16: rows 28.5 us (0.91 of the copy rate), both ways 41 (0.77); stochastic rounding is bound by the logic
-// pipe (75 % busy): some 40 instructions a value both ways, 97 us.
+// Measured on 16384 x 4096 bf16: rows 28.5 us (0.91 of the copy rate), both ways 41 (0.77); stochastic rounding takes
+// 35 instructions a value both ways, 97 us: logic pipe 68 %, issue slots 67 % busy with a quarter of the warps that an SM could hold.
 template <typename T, MicroRound ROUND> constexpr int kMicroRows = ROUND != MicroRound::kNearest && sizeof(T) == 4 ? 4 : 8;
 template <typename T, MicroRound ROUND> constexpr int kMicroThreads = kTile * kTile / 8 / kMicroRows<T, ROUND>;
 template <typename T, MicroRound ROUND, bool WHOLE>

@@ -22,7 +22,8 @@ struct RmsShape { bool wide; int lanes; unsigned warps, groups, blocks; bool joi
 constexpr int kRmsRing = 147456, kRmsMostShared = kRmsRing + 64 * 16 * 3 * 4;
 // Rows ahead of the one in work, and it.  Up to three of less than 64 KB; of longer ones (for 8192 columns) that one alone, while
 // the block's other group computes: 16384 x 4096, fp32 both, forward 181 us with two, 166 with one; fp32 and bf16, backward 177 and
-// 168; fp32 and bf16 to codes, forward 123 with two, 113 with three or four.
+// 168.  fp32 and bf16, forward, with two, three and four (192 KB): dropped branch to codes 124, 125, 112, without dropout 132 each, without a
+// branch 61, 61, 63; to bf16 140, 140, 140, without a branch 63, 62, 65.
 constexpr int rms_stages_for(int bytes) {  // of a column in all tensors that a pass reads
   return 512 * kRmsOwn * bytes >= 65536 ? 1 : kRmsRing / (512 * kRmsOwn * bytes) < 4 ? kRmsRing / (512 * kRmsOwn * bytes) : 4;
 }
